@@ -53,6 +53,7 @@
 #define BOXCONV_H
 
 #include <stddef.h>
+#include <stdint.h>
 #include <hip/hip_runtime_api.h>
 
 #ifdef __cplusplus
@@ -70,7 +71,7 @@ typedef enum {
   BC_ERR_UNSUPPORTED = 7  /* valid request the library does not implement */
 } bc_status;
 
-typedef enum { BC_I32 = 0, BC_F32 = 1, BC_BF16 = 2 } bc_dtype;
+typedef enum { BC_I32 = 0, BC_F32 = 1, BC_BF16 = 2, BC_I8 = 3 } bc_dtype;
 
 typedef enum {
   BC_MIX_FWD = 0,         /* out[n] = w * in[n]                          */
@@ -406,6 +407,91 @@ bc_status box_conv_bwd_noalloc(const float* x, const float* boxes, const float* 
                                float* grad_x, float* grad_boxes, unsigned flags,
                                hipStream_t stream);
 size_t bc_noalloc_scratch_bytes(void);
+
+/* ========================================================================
+ * Recurrent layers: a gated linear recurrence along the sequence, one state a
+ * channel (the depthwise part, as the box filter is on maps), and 1x1 mixes
+ * across channels around it.  Two layouts, named by `layout`:
+ *   BC_TOKENS  [N][T][C], channels contiguous (rows are time steps);
+ *   BC_MAPS    [N][C][T], time contiguous (rows are channels), as pointwise_mix
+ *              reads and writes its maps.
+ * ---------------------------------------------------------------------- */
+typedef enum { BC_TOKENS = 0, BC_MAPS = 1 } bc_layout;
+typedef enum { BC_GATE_LOGIT = 0, BC_GATE_VALUE = 1 } bc_gate_form;
+
+/* ------------------------------------------------------------------------
+ * gated_scan_fwd -- for every sequence n and channel c, from h_{-1} = h0:
+ *   BC_GATE_LOGIT: a_t = sigmoid(gate_t), h_t = a_t h_{t-1} + (1 - a_t) x_t;
+ *   BC_GATE_VALUE: a_t = gate_t,          h_t = a_t h_{t-1} + x_t;
+ *   y_t = h_t, h_last = h_{T-1}.
+ * All arithmetic in fp32 (a and 1 - a each to fp32 accuracy; gate = -infinity
+ * is an exact reset); only y is rounded to its type.  Runs of steps are
+ * composed, so with BC_GATE_VALUE the products of consecutive coefficients
+ * have to stay inside fp32's range (|a| <= 1 always does).
+ *
+ * gate, x : device, dtype dt = BC_F32 or BC_BF16, in the layout's order with
+ *           batch_stride and row_stride elements between batches and rows
+ *           (>= the contiguous extent; both tensors share them), so that they
+ *           may be slices of one projection's output.
+ * h0      : device fp32 [N][C], or NULL: zero.
+ * lengths : device int32 [N], or NULL: all T.  Sequence n ends after
+ *           lengths[n] steps (clamped to [0, T]): gate and x are not read
+ *           past it, y is zero there and h_last is the state at it (h0 for an
+ *           empty sequence).
+ * y       : device, dense in the layout's order; y_dt = dt, or BC_BF16 for
+ *           BC_F32 inputs (the operand of a bf16 mix).
+ * h_last  : device fp32 [N][C], or NULL.  May be h0.
+ * states  : NULL, or device fp32, bc_gated_scan_states_bytes() bytes: the
+ *           states the backward starts from (its layout is the library's).
+ * ws      : >= bc_gated_scan_workspace_bytes(0, ...) bytes, NULL when that is 0.
+ * Non-finite values spread as the recurrence spreads them: forward in time in
+ * their own channel and sequence (also through a reset: 0 * infinity), nowhere
+ * else.
+ * Sizes: N, C <= 65536, N * C <= 2^25, T <= 2^30 (BC_ERR_SHAPE); strides
+ * smaller than a row or a batch are BC_ERR_SHAPE too.
+ *
+ * gated_scan_bwd -- gradients of L = <grad_y, y> + <grad_h_last, h_last>.
+ * With r_T = grad_h_last, delta_t = grad_y_t + r_{t+1}, r_t = a_t delta_t:
+ *   grad_x_t = delta_t (VALUE) or (1 - a_t) delta_t (LOGIT);
+ *   grad_gate_t = delta_t h_{t-1} (VALUE) or
+ *                 delta_t (h_{t-1} - x_t) a_t (1 - a_t) (LOGIT);
+ *   grad_h0 = r_0.
+ * The states h_{t-1} are computed again from `states` (the forward's, of the
+ * same gate, x, h0 and lengths), in fp32.  Past a sequence's end the gradients
+ * are zero and grad_y is not read.
+ * grad_y            : device, dtype dt, dense.
+ * grad_h_last       : device fp32 [N][C], or NULL: zero.
+ * grad_gate, grad_x : device, out_dt = dt, or BC_BF16 for BC_F32 inputs;
+ *                     grad_batch_stride and grad_row_stride as the inputs'.
+ *                     They share no memory with an input.
+ * grad_h0           : device fp32 [N][C], or NULL.  May be grad_h_last.
+ * ws                : >= bc_gated_scan_workspace_bytes(1, ...) bytes.
+ *
+ * gated_scan_step -- one step of N running sequences whose states are rows of
+ * a pool: with s = slots[n] (or n where slots is NULL),
+ *   y[n] = state_out[s] = a[n] state[s] + ... as above.
+ * gate, x : device [N][C], row_stride elements between rows; y: dense [N][C],
+ *           dtype dt.
+ * state   : device fp32 [S][C]; state_out: the same, or the same pointer (in
+ *           place).  Rows that no sequence names are not written.
+ * slots   : device int32 [N], or NULL (then N <= S).  A slot outside [0, S)
+ *           marks an idle row: y is zero, no state is read or written.  Two
+ *           rows may not name one slot.
+ * ---------------------------------------------------------------------- */
+bc_status gated_scan_fwd(const void* gate, const void* x, int dt, int64_t batch_stride, int64_t row_stride,
+                         const float* h0, const int* lengths, void* y, int y_dt, float* h_last, float* states,
+                         int N, int T, int C, int form, int layout, void* ws, size_t ws_bytes, hipStream_t stream);
+bc_status gated_scan_bwd(const void* gate, const void* x, int dt, int64_t batch_stride, int64_t row_stride,
+                         const float* states, const int* lengths, const void* grad_y, const float* grad_h_last,
+                         void* grad_gate, void* grad_x, int out_dt, int64_t grad_batch_stride,
+                         int64_t grad_row_stride, float* grad_h0, int N, int T, int C, int form, int layout,
+                         void* ws, size_t ws_bytes, hipStream_t stream);
+bc_status gated_scan_step(const void* gate, const void* x, int dt, int64_t row_stride, const float* state,
+                          float* state_out, const int* slots, void* y, int N, int C, int S, int form,
+                          hipStream_t stream);
+/* op: 0 = gated_scan_fwd, 1 = gated_scan_bwd; 0 for sizes the calls reject. */
+size_t bc_gated_scan_workspace_bytes(int op, int N, int T, int C, int dt, int layout);
+size_t bc_gated_scan_states_bytes(int N, int T, int C, int layout);
 
 /* Workspace sizes in bytes.  op: 0 = box_conv_fwd, 1 = box_conv_bwd (and
  * box_conv_bwd_relu_bf16); the _strided form for the strided entry points

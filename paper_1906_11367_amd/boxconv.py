@@ -9,8 +9,9 @@ Entry points (same names as the C ABI): box_prep, sat_build, box_conv_fwd,
 box_conv_bwd, box_conv_fwd_strided, box_conv_bwd_strided, pointwise_mix, the
 box-parameter reparameterisation (box_params_from_unit, box_params_unit_grad,
 box_params_clip), kernel splitting (box_conv_split_fwd, box_conv_split_bwd),
-the bf16 helpers (bc_cast_bf16, bc_relu_grad_bf16), plus the workspace-size
-queries.
+the bf16 helpers (bc_cast_bf16, bc_relu_grad_bf16), the gated scan of
+recurrent layers (gated_scan_fwd, gated_scan_bwd, gated_scan_step), plus the
+workspace-size queries.
 """
 from __future__ import annotations
 
@@ -22,16 +23,19 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libboxconv.so")
 
-BC_I32, BC_F32, BC_BF16 = 0, 1, 2
+BC_I32, BC_F32, BC_BF16, BC_I8 = 0, 1, 2, 3
 BC_MIX_FWD, BC_MIX_BWD_DATA, BC_MIX_BWD_WEIGHT = 0, 1, 2
 BC_FLAG_MEAN_OFFSET, BC_FLAG_FORCE_HBM, BC_FLAG_INTEGER_CORNERS = 1, 2, 4
 BC_SPLIT_2X, BC_SPLIT_2Y, BC_SPLIT_4 = 1, 2, 3
 BC_SPLIT_FORCE_HBM = 0x100
+BC_TOKENS, BC_MAPS = 0, 1
+BC_GATE_LOGIT, BC_GATE_VALUE = 0, 1
 STATUS = {0: "BC_OK", 1: "BC_ERR_NULL", 2: "BC_ERR_SHAPE", 3: "BC_ERR_DTYPE", 4: "BC_ERR_ALIGN",
           5: "BC_ERR_WORKSPACE", 6: "BC_ERR_HIP", 7: "BC_ERR_UNSUPPORTED"}
 
 # Exported symbols and their C signatures (kept in step with boxconv.h).
 _vp, _i, _u, _sz, _f = ctypes.c_void_p, ctypes.c_int, ctypes.c_uint, ctypes.c_size_t, ctypes.c_float
+_ll = ctypes.c_int64
 SIGNATURES = {
     "box_prep": (_i, [_vp, _i, _i, _u, _vp, _vp]),
     "sat_build": (_i, [_vp, _i, _vp, _vp, _i, _i, _i, _i, _vp]),
@@ -54,6 +58,12 @@ SIGNATURES = {
     "box_conv_bwd_relu_bf16": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _u, _vp, _sz, _vp]),
     "box_conv_bwd_noalloc": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp, _vp, _u, _vp]),
     "bc_noalloc_scratch_bytes": (_sz, []),
+    "gated_scan_fwd": (_i, [_vp, _vp, _i, _ll, _ll, _vp, _vp, _vp, _i, _vp, _vp, _i, _i, _i, _i, _i, _vp, _sz, _vp]),
+    "gated_scan_bwd": (_i, [_vp, _vp, _i, _ll, _ll, _vp, _vp, _vp, _vp, _vp, _vp, _i, _ll, _ll, _vp, _i, _i, _i, _i,
+                            _i, _vp, _sz, _vp]),
+    "gated_scan_step": (_i, [_vp, _vp, _i, _ll, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp]),
+    "bc_gated_scan_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
+    "bc_gated_scan_states_bytes": (_sz, [_i, _i, _i, _i]),
     "bc_status_string": (ctypes.c_char_p, [_i]),
     "bc_abi_version": (_i, []),
 }
@@ -153,6 +163,8 @@ def dtype_code(t: torch.Tensor) -> int:
         return BC_F32
     if t.dtype == torch.bfloat16:
         return BC_BF16
+    if t.dtype == torch.int8:
+        return BC_I8
     raise BoxConvError(f"unsupported dtype {t.dtype}")
 
 
@@ -419,3 +431,151 @@ def pointwise_mix(mode: int, a: torch.Tensor, b: torch.Tensor, out: torch.Tensor
                                         dtype_code(out), N, M, K, P, compute_dt, relu, _ptr(aux), accumulate,
                                         _ptr(ws), nbytes, _stream()), "pointwise_mix")
     return out
+
+
+# ---- recurrent layers ---------------------------------------------------------
+
+_FLOATS = (torch.float32, torch.bfloat16)
+
+
+def _rows(t: torch.Tensor, what: str, name: str):
+    """Pointer, batch stride and row stride of a 3-D tensor whose last dimension
+    is contiguous (a slice of a larger tensor, for one).  Strides of dimensions
+    of one element are the contiguous ones."""
+    if not isinstance(t, torch.Tensor):
+        raise BoxConvError(f"{what}: {name} must be a tensor")
+    if not t.is_cuda:
+        raise BoxConvError("tensors must be on the GPU")
+    n, r, c = t.shape
+    sn, sr, sc = t.stride()
+    if sc != 1 and c > 1:
+        raise BoxConvError(f"{what}: {name} must be contiguous in its last dimension")
+    if r == 1:
+        sr = c
+    return t.data_ptr(), (sn if n > 1 else sr * r), sr
+
+
+def _seq_sizes(x, layout, what):
+    """N, T, C of a sequence tensor in its layout."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 3:
+        raise BoxConvError(f"{what}: x must be a 3-D tensor")
+    if x.dtype not in _FLOATS:
+        raise BoxConvError(f"{what}: x has dtype {x.dtype}, expected one of {_FLOATS}")
+    if layout == BC_TOKENS:
+        return x.shape
+    if layout == BC_MAPS:
+        return x.shape[0], x.shape[2], x.shape[1]
+    raise BoxConvError(f"{what}: unknown layout {layout}")
+
+
+def _out_types(dtype):
+    return _FLOATS if dtype is torch.float32 else (dtype,)
+
+
+def gated_scan_workspace_bytes(op: int, N, T, C, dt: int, layout: int = BC_TOKENS) -> int:
+    """op: 0 = gated_scan_fwd, 1 = gated_scan_bwd; dt: dtype code of gate and x."""
+    return int(load_library().bc_gated_scan_workspace_bytes(op, N, T, C, dt, layout))
+
+
+def gated_scan_states(N, T, C, dtype=None, layout: int = BC_TOKENS, device="cuda") -> torch.Tensor:
+    """The buffer in which gated_scan_fwd keeps what gated_scan_bwd starts from
+    (its layout is the library's; fp32 whatever the tensors' dtype)."""
+    n = int(load_library().bc_gated_scan_states_bytes(N, T, C, layout))
+    if n == 0:
+        raise BoxConvError("gated_scan_states: BC_ERR_SHAPE")
+    return torch.empty(n // 4, dtype=torch.float32, device=device)
+
+
+def gated_scan_fwd(gate: torch.Tensor, x: torch.Tensor, y: torch.Tensor, h0: torch.Tensor | None = None,
+                   h_last: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                   states: torch.Tensor | None = None, form: int = BC_GATE_LOGIT, layout: int = BC_TOKENS,
+                   ws: torch.Tensor | None = None):
+    """gate, x [N, T, C] (BC_TOKENS) or [N, C, T] (BC_MAPS), contiguous in the
+    last dimension and of the same strides -> y, dense, of the same shape."""
+    what = "gated_scan_fwd"
+    N, T, C = _seq_sizes(x, layout, what)
+    _need(gate, x.shape, x.dtype, what, "gate")
+    _need(y, x.shape, _out_types(x.dtype), what, "y")
+    _need(h0, (N, C), _F32, what, "h0")
+    _need(h_last, (N, C), _F32, what, "h_last")
+    _need(lengths, (N,), torch.int32, what, "lengths")
+    lib = load_library()
+    if states is not None:
+        _need_numel(states, lib.bc_gated_scan_states_bytes(N, T, C, layout) // 4, _F32, what, "states")
+    gp, bs, rs = _rows(gate, what, "gate")
+    xp, xbs, xrs = _rows(x, what, "x")
+    if (bs, rs) != (xbs, xrs):
+        raise BoxConvError(f"{what}: gate and x must have the same strides")
+    dt = dtype_code(x)
+    if ws is None:
+        ws = _workspace(lib.bc_gated_scan_workspace_bytes(0, N, T, C, dt, layout), x.device)
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(lib.gated_scan_fwd(gp, xp, dt, bs, rs, _ptr(h0), _ptr(lengths), _ptr(y), dtype_code(y), _ptr(h_last),
+                              _ptr(states), N, T, C, form, layout, _ptr(ws), nbytes, _stream()), what)
+    return y
+
+
+def gated_scan_bwd(gate: torch.Tensor, x: torch.Tensor, states: torch.Tensor, grad_y: torch.Tensor,
+                   grad_gate: torch.Tensor, grad_x: torch.Tensor, grad_h_last: torch.Tensor | None = None,
+                   grad_h0: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                   form: int = BC_GATE_LOGIT, layout: int = BC_TOKENS, ws: torch.Tensor | None = None):
+    """The gradients of gated_scan_fwd; states: what that call kept.  grad_gate
+    and grad_x share their strides too (halves of one gradient, for one)."""
+    what = "gated_scan_bwd"
+    N, T, C = _seq_sizes(x, layout, what)
+    _need(gate, x.shape, x.dtype, what, "gate")
+    _need(grad_y, x.shape, x.dtype, what, "grad_y")
+    _need(grad_x, x.shape, _out_types(x.dtype), what, "grad_x")
+    _need(grad_gate, x.shape, grad_x.dtype, what, "grad_gate")
+    _need(grad_h_last, (N, C), _F32, what, "grad_h_last")
+    _need(grad_h0, (N, C), _F32, what, "grad_h0")
+    _need(lengths, (N,), torch.int32, what, "lengths")
+    if states is None or grad_y is None:
+        raise BoxConvError(f"{what}: states and grad_y must be tensors")
+    lib = load_library()
+    _need_numel(states, lib.bc_gated_scan_states_bytes(N, T, C, layout) // 4, _F32, what, "states")
+    gp, bs, rs = _rows(gate, what, "gate")
+    xp, xbs, xrs = _rows(x, what, "x")
+    ggp, gbs, grs = _rows(grad_gate, what, "grad_gate")
+    gxp, gxbs, gxrs = _rows(grad_x, what, "grad_x")
+    if (bs, rs) != (xbs, xrs) or (gbs, grs) != (gxbs, gxrs):
+        raise BoxConvError(f"{what}: gate and x, and grad_gate and grad_x, must have the same strides")
+    dt = dtype_code(x)
+    if ws is None:
+        ws = _workspace(lib.bc_gated_scan_workspace_bytes(1, N, T, C, dt, layout), x.device)
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(lib.gated_scan_bwd(gp, xp, dt, bs, rs, _ptr(states), _ptr(lengths), _ptr(grad_y), _ptr(grad_h_last), ggp,
+                              gxp, dtype_code(grad_x), gbs, grs, _ptr(grad_h0), N, T, C, form, layout, _ptr(ws),
+                              nbytes, _stream()), what)
+    return grad_gate, grad_x
+
+
+def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, y: torch.Tensor,
+                    slots: torch.Tensor | None = None, state_out: torch.Tensor | None = None,
+                    form: int = BC_GATE_LOGIT):
+    """One token of N sequences: gate, x [N, C] (rows of equal stride), state
+    [S, C] fp32 (the pool; state_out, default itself, takes the new states),
+    slots [N] int32 -> y [N, C]."""
+    what = "gated_scan_step"
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype not in _FLOATS:
+        raise BoxConvError(f"{what}: x must be a 2-D fp32 or bf16 tensor")
+    N, C = x.shape
+    if gate is None or state is None or y is None:
+        raise BoxConvError(f"{what}: gate, state and y must be tensors")
+    _need(gate, x.shape, x.dtype, what, "gate")
+    _need(y, x.shape, x.dtype, what, "y")
+    _need(state, (None, C), _F32, what, "state")
+    S = state.shape[0]
+    _need(state_out, (S, C), _F32, what, "state_out")
+    _need(slots, (N,), torch.int32, what, "slots")
+    if not gate.is_cuda or not x.is_cuda:
+        raise BoxConvError("tensors must be on the GPU")
+    gs, xs = gate.stride(), x.stride()
+    rs = xs[0] if N > 1 else C
+    if (N > 1 and gs[0] != rs) or (C > 1 and (gs[1] != 1 or xs[1] != 1)):
+        raise BoxConvError(f"{what}: gate and x must be contiguous in their last dimension and of the same strides")
+    sp = _ptr(state)
+    _check(load_library().gated_scan_step(gate.data_ptr(), x.data_ptr(), dtype_code(x), rs, sp,
+                                          sp if state_out is None else _ptr(state_out), _ptr(slots), _ptr(y), N, C, S,
+                                          form, _stream()), what)
+    return y

@@ -483,4 +483,101 @@ bc_status pointwise_mix(int mode, const void* a, int a_dt, const void* b, int b_
                                    ws_bytes, stream));
 }
 
+// ---- recurrent layers ------------------------------------------------------
+
+static bool scan_dims_ok(int N, int T, int C) {
+  if (N <= 0 || T <= 0 || C <= 0 || N > kMaxDim || C > kMaxDim || T > (1 << 30)) return false;
+  // a wave per row of maps: grids below 2^32 threads
+  return (long)N * C <= (1L << 25);
+}
+
+// Strides of a tensor of N batches of `rows` contiguous rows of `cols`.
+static bool strides_ok(int64_t bs, int64_t rs, int N, int rows, int cols) {
+  constexpr int64_t kMax = (int64_t)1 << 46;
+  if (rs < cols && rows > 1) return false;
+  if (bs < 0 || rs < 0 || bs > kMax || rs > kMax) return false;
+  const double batch = (double)rs * (rows - 1) + cols;
+  if (N > 1 && (double)bs < batch) return false;
+  return (double)bs * (N - 1) + batch < 4e18;
+}
+
+size_t bc_gated_scan_states_bytes(int N, int T, int C, int layout) {
+  if (!scan_dims_ok(N, T, C) || (layout != BC_TOKENS && layout != BC_MAPS)) return 0;
+  const int span = layout == BC_MAPS ? bc::kScanSpanMaps : bc::kScanSpan;
+  return (size_t)N * C * ((T + span - 1) / span) * 4;
+}
+
+size_t bc_gated_scan_workspace_bytes(int op, int N, int T, int C, int dt, int layout) {
+  if (!scan_dims_ok(N, T, C) || (layout != BC_TOKENS && layout != BC_MAPS) || (op != 0 && op != 1)) return 0;
+  if (dt != BC_F32 && dt != BC_BF16) return 0;
+  return bc::scan_workspace_bytes(op == 1, N, T, C, dt, layout == BC_MAPS);
+}
+
+static bc_status scan_checks(int N, int T, int C, int dt, int out_dt, int64_t bs, int64_t rs, int form, int layout) {
+  if (layout != BC_TOKENS && layout != BC_MAPS) return BC_ERR_UNSUPPORTED;
+  if (form != BC_GATE_LOGIT && form != BC_GATE_VALUE) return BC_ERR_UNSUPPORTED;
+  if (!scan_dims_ok(N, T, C)) return BC_ERR_SHAPE;
+  if (dt != BC_F32 && dt != BC_BF16) return BC_ERR_DTYPE;
+  if (out_dt != dt && !(dt == BC_F32 && out_dt == BC_BF16)) return BC_ERR_DTYPE;
+  const bool maps = layout == BC_MAPS;
+  return strides_ok(bs, rs, N, maps ? C : T, maps ? T : C) ? BC_OK : BC_ERR_SHAPE;
+}
+
+static bool aligned16_or_null(const void* p) { return !p || aligned16(p); }
+
+bc_status gated_scan_fwd(const void* gate, const void* x, int dt, int64_t batch_stride, int64_t row_stride,
+                         const float* h0, const int* lengths, void* y, int y_dt, float* h_last, float* states, int N,
+                         int T, int C, int form, int layout, void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (!gate || !x || !y) return BC_ERR_NULL;
+  const bc_status st = scan_checks(N, T, C, dt, y_dt, batch_stride, row_stride, form, layout);
+  if (st != BC_OK) return st;
+  if (!aligned16(gate) || !aligned16(x) || !aligned16(y) || !aligned16_or_null(h0) || !aligned16_or_null(lengths) ||
+      !aligned16_or_null(h_last) || !aligned16_or_null(states))
+    return BC_ERR_ALIGN;
+  const size_t need = bc::scan_workspace_bytes(false, N, T, C, dt, layout == BC_MAPS);
+  if (need > 0 && (!ws || ws_bytes < need)) return BC_ERR_WORKSPACE;
+  if (need > 0 && !aligned16(ws)) return BC_ERR_ALIGN;
+  return hip_status(bc::launch_scan_fwd({gate, x, (long)batch_stride, (long)row_stride, h0, lengths, y, h_last,
+                                         states, N, T, C, form, dt, y_dt, layout == BC_MAPS, ws},
+                                        stream));
+}
+
+bc_status gated_scan_bwd(const void* gate, const void* x, int dt, int64_t batch_stride, int64_t row_stride,
+                         const float* states, const int* lengths, const void* grad_y, const float* grad_h_last,
+                         void* grad_gate, void* grad_x, int out_dt, int64_t grad_batch_stride,
+                         int64_t grad_row_stride, float* grad_h0, int N, int T, int C, int form, int layout, void* ws,
+                         size_t ws_bytes, hipStream_t stream) {
+  if (!gate || !x || !states || !grad_y || !grad_gate || !grad_x) return BC_ERR_NULL;
+  const bc_status st = scan_checks(N, T, C, dt, out_dt, batch_stride, row_stride, form, layout);
+  if (st != BC_OK) return st;
+  const bool maps = layout == BC_MAPS;
+  if (!strides_ok(grad_batch_stride, grad_row_stride, N, maps ? C : T, maps ? T : C)) return BC_ERR_SHAPE;
+  if (!aligned16(gate) || !aligned16(x) || !aligned16(states) || !aligned16(grad_y) || !aligned16(grad_gate) ||
+      !aligned16(grad_x) || !aligned16_or_null(lengths) || !aligned16_or_null(grad_h_last) ||
+      !aligned16_or_null(grad_h0))
+    return BC_ERR_ALIGN;
+  const size_t need = bc::scan_workspace_bytes(true, N, T, C, dt, maps);
+  if (need > 0 && (!ws || ws_bytes < need)) return BC_ERR_WORKSPACE;
+  if (need > 0 && !aligned16(ws)) return BC_ERR_ALIGN;
+  return hip_status(bc::launch_scan_bwd({gate, x, (long)batch_stride, (long)row_stride, states, lengths, grad_y,
+                                         grad_h_last, grad_gate, grad_x, (long)grad_batch_stride,
+                                         (long)grad_row_stride, grad_h0, N, T, C, form, dt, out_dt, maps, ws},
+                                        stream));
+}
+
+bc_status gated_scan_step(const void* gate, const void* x, int dt, int64_t row_stride, const float* state,
+                          float* state_out, const int* slots, void* y, int N, int C, int S, int form,
+                          hipStream_t stream) {
+  if (!gate || !x || !state || !state_out || !y) return BC_ERR_NULL;
+  if (form != BC_GATE_LOGIT && form != BC_GATE_VALUE) return BC_ERR_UNSUPPORTED;
+  if (N <= 0 || C <= 0 || S <= 0 || N > (1 << 20) || C > kMaxDim || (!slots && N > S)) return BC_ERR_SHAPE;
+  if (!strides_ok(0, row_stride, 1, N, C)) return BC_ERR_SHAPE;
+  if (dt != BC_F32 && dt != BC_BF16) return BC_ERR_DTYPE;
+  if (!aligned16(gate) || !aligned16(x) || !aligned16(state) || !aligned16(state_out) || !aligned16(y) ||
+      !aligned16_or_null(slots))
+    return BC_ERR_ALIGN;
+  return hip_status(bc::launch_scan_step(gate, x, (long)row_stride, dt, state, state_out, slots, y, N, C, S, form,
+                                         stream));
+}
+
 }  // extern "C"

@@ -145,4 +145,64 @@ size_t mix_workspace_bytes(int mode, int N, int M, int K, int P, int compute_dt)
 hipError_t launch_cast_bf16(const float* src, void* dst, size_t n, hipStream_t s);
 hipError_t launch_relu_cast_bf16(const float* g, const float* aux, void* dst, size_t n, hipStream_t s);
 
+// Gated scan over token sequences [N][T][C] (bc_scan.hip) and over maps
+// [N][C][T] (bc_scan_maps.hip).  Strides in elements: bs between batches, rs
+// between rows (steps of tokens, channels of maps); rows are contiguous.
+constexpr int kScanSpan = 128;       // steps between kept states, tokens: [N][spans][C]
+constexpr int kScanSpanMaps = 512;   // maps: [N][C][spans]
+struct ScanFwd {
+  const void *gate, *x;
+  long bs, rs;
+  const float* h0;
+  const int* lengths;
+  void* y;
+  float *h_last, *states;
+  int N, T, C, form, in_dt, out_dt;
+  bool maps;
+  void* ws;
+};
+struct ScanBwd {
+  const void *gate, *x;
+  long bs, rs;
+  const float* states;
+  const int* lengths;
+  const void* gy;
+  const float* gh_last;
+  void *ggate, *gx;
+  long gbs, grs;
+  float* gh0;
+  int N, T, C, form, in_dt, out_dt;
+  bool maps;
+  void* ws;
+};
+hipError_t launch_scan_fwd(const ScanFwd& f, hipStream_t s);
+hipError_t launch_scan_bwd(const ScanBwd& f, hipStream_t s);
+namespace scan { struct FwdArgs; struct BwdArgs; }
+hipError_t launch_scan_fwd_maps(const scan::FwdArgs& p, int in_dt, int out_dt, int form, hipStream_t s);
+hipError_t launch_scan_bwd_maps(const scan::BwdArgs& p, int in_dt, int out_dt, int form, hipStream_t s);
+hipError_t launch_scan_step(const void* gate, const void* x, long rs, int dt, const float* state, float* state_out,
+                            const int* slots, void* y, int N, int C, int S, int form, hipStream_t s);
+size_t scan_workspace_bytes(bool bwd, int N, int T, int C, int in_dt, bool maps);
+
+// 1x1 mix of 8-bit codes (bc_mix_i8.hip).
+constexpr int kI8Pad = 128;   // rows of codes are padded with zeros to whole 128 bytes
+inline int i8_pitch(int K) { return (K + kI8Pad - 1) / kI8Pad * kI8Pad; }
+hipError_t launch_quantize_i8(const void* src, int dt, long bs, long rs, void* q, float* scale, int N, int K, int P,
+                              bool maps, hipStream_t s);
+struct MixI8 {
+  const void* wq;
+  const float* wscale;
+  const void* x;            // codes [rows][pitch] (dt BC_I8), or what they are made from
+  int dt;
+  long bs, rs;              // strides of x where it is not codes
+  const float* xscale;      // with codes
+  const float* bias;
+  void* out;
+  int out_dt, N, M, K, P, relu;
+  bool maps;
+  void* ws;
+};
+hipError_t launch_mix_i8(const MixI8& m, hipStream_t s);
+size_t mix_i8_workspace_bytes(int N, int M, int K, int P, int dt, bool maps);
+
 }  // namespace bc

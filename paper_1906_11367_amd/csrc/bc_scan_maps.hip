@@ -1,0 +1,226 @@
+// The gated scan on maps [N][C][T] (gfx950): every row is one sequence, time
+// contiguous, as the 1x1 mix writes its outputs (bc_scan.hpp has the algebra).
+//
+// A wave takes kSeg = 512 consecutive steps of a row at a time, 8 to a lane,
+// scans the lanes' pairs by lane moves and carries the state on.  W waves share
+// a row, kSeg steps each, where there are too few rows for a wave each.
+#include "bc_scan.hpp"
+
+namespace bc {
+namespace {
+
+using namespace scan;
+
+constexpr int kV = 8;
+constexpr int kSeg = 64 * kV;
+static_assert(kSeg == kScanSpanMaps, "a state is kept at each wave's segment");
+
+__device__ __forceinline__ void lanes_prefix(float& A, float& B, int lane, float& eA, float& eB) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const float pa = __shfl_up(A, d), pb = __shfl_up(B, d);
+    if (lane >= d) {
+      B = __fmaf_rn(A, pb, B);
+      A *= pa;
+    }
+  }
+  eA = __shfl_up(A, 1);
+  eB = __shfl_up(B, 1);
+  if (lane == 0) { eA = 1.f; eB = 0.f; }
+}
+
+__device__ __forceinline__ void lanes_suffix(float& A, float& B, int lane, float& eA, float& eB) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const float pa = __shfl_down(A, d), pb = __shfl_down(B, d);
+    if (lane + d < 64) {
+      B = __fmaf_rn(A, pb, B);
+      A *= pa;
+    }
+  }
+  eA = __shfl_down(A, 1);
+  eB = __shfl_down(B, 1);
+  if (lane == 63) { eA = 1.f; eB = 0.f; }
+}
+
+// W waves to a row; blocks of kRows rows.
+template <int W> constexpr int kRows = W >= 4 ? 1 : 4 / W;
+
+template <int IN, int OUT, int FORM, int W>
+__global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_fwd_maps(FwdArgs p) {
+  __shared__ float tot[2][W][2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % W;
+  const long row = (long)blockIdx.x * kRows<W> + wave / W;
+  if (row >= (long)p.N * p.C) return;   // W > 1: the whole block has one row
+  const int n = (int)(row / p.C), c = (int)(row % p.C);
+  const int len = seq_len(p.lengths, n, p.T);
+  const char* gate = p.gate + ((long)n * p.bs + (long)c * p.rs) * kBytes<IN>;
+  const char* xp = p.x + ((long)n * p.bs + (long)c * p.rs) * kBytes<IN>;
+  char* yp = p.y + row * p.T * kBytes<OUT>;
+  const int S = (p.T + kSeg - 1) / kSeg;
+  float carry = p.h0 ? p.h0[row] : 0.f;
+  int q = 0;
+  for (int s0 = 0; s0 < S; s0 += W, q ^= 1) {
+    const int t0 = (s0 + w) * kSeg + lane * kV;
+    const auto g = load_vec<IN, kV>(gate + (long)t0 * kBytes<IN>, len - t0);
+    const auto x = load_vec<IN, kV>(xp + (long)t0 * kBytes<IN>, len - t0);
+    float a[kV], b[kV], A = 1.f, B = 0.f, eA, eB;
+#pragma unroll
+    for (int k = 0; k < kV; ++k) {
+      float cx;
+      coefficients<IN, FORM>(elem<IN, kV>(g, k), a[k], cx);
+      b[k] = input_share<FORM>(cx, elem<IN, kV>(x, k));
+      if (t0 + k >= len) { a[k] = 1.f; b[k] = 0.f; }
+      A *= a[k];
+      B = __fmaf_rn(a[k], B, b[k]);
+    }
+    lanes_prefix(A, B, lane, eA, eB);
+    float hw = carry;   // the state before this wave's segment
+    if constexpr (W == 1) {
+      carry = __fmaf_rn(__shfl(A, 63), carry, __shfl(B, 63));
+    } else {
+      if (lane == 63) { tot[q][w][0] = A; tot[q][w][1] = B; }
+      __syncthreads();
+      for (int i = 0; i < W; ++i) {
+        if (i == w) hw = carry;
+        carry = __fmaf_rn(tot[q][i][0], carry, tot[q][i][1]);
+      }
+    }
+    if (p.states && lane == 0 && s0 + w < S) p.states[row * S + s0 + w] = hw;
+    float h = __fmaf_rn(eA, hw, eB), o[kV];
+#pragma unroll
+    for (int k = 0; k < kV; ++k) {
+      h = __fmaf_rn(a[k], h, b[k]);
+      o[k] = t0 + k < len ? h : 0.f;
+    }
+    store_vec<OUT, kV>(yp + (long)t0 * kBytes<OUT>, p.T - t0, o);
+  }
+  if (p.h_last && w == 0 && lane == 0) p.h_last[row] = carry;
+}
+
+template <int IN, int OUT, int FORM, int W>
+__global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_bwd_maps(BwdArgs p) {
+  __shared__ float tot[2][W][2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % W;
+  const long row = (long)blockIdx.x * kRows<W> + wave / W;
+  if (row >= (long)p.N * p.C) return;
+  const int n = (int)(row / p.C), c = (int)(row % p.C);
+  const int len = seq_len(p.lengths, n, p.T);
+  const char* gate = p.gate + ((long)n * p.bs + (long)c * p.rs) * kBytes<IN>;
+  const char* xp = p.x + ((long)n * p.bs + (long)c * p.rs) * kBytes<IN>;
+  const char* gy = p.gy + row * p.T * kBytes<IN>;
+  char* ggate = p.ggate + ((long)n * p.gbs + (long)c * p.grs) * kBytes<OUT>;
+  char* gx = p.gx + ((long)n * p.gbs + (long)c * p.grs) * kBytes<OUT>;
+  const int S = (p.T + kSeg - 1) / kSeg;
+  float carry = p.gh_last ? p.gh_last[row] : 0.f;
+  int q = 0;
+  for (int s0 = (S - 1) / W * W; s0 >= 0; s0 -= W, q ^= 1) {
+    const int t0 = (s0 + w) * kSeg + lane * kV;
+    const auto g = load_vec<IN, kV>(gate + (long)t0 * kBytes<IN>, len - t0);
+    const auto xr = load_vec<IN, kV>(xp + (long)t0 * kBytes<IN>, len - t0);
+    const auto dr = load_vec<IN, kV>(gy + (long)t0 * kBytes<IN>, len - t0);
+    const float st = s0 + w < S ? p.states[row * S + s0 + w] : 0.f;
+    float a[kV], cx[kV], h[kV], A = 1.f, B = 0.f, R = 0.f, eA, eB, sA, sB;
+#pragma unroll
+    for (int k = 0; k < kV; ++k) {
+      coefficients<IN, FORM>(elem<IN, kV>(g, k), a[k], cx[k]);
+      if (t0 + k >= len) { a[k] = 1.f; cx[k] = 0.f; }
+      A *= a[k];
+      B = __fmaf_rn(a[k], B, input_share<FORM>(cx[k], elem<IN, kV>(xr, k)));
+    }
+#pragma unroll
+    for (int k = kV - 1; k >= 0; --k) R = a[k] * (elem<IN, kV>(dr, k) + R);
+    float fA = A, fB = B;
+    lanes_prefix(fA, fB, lane, eA, eB);
+    lanes_suffix(A, R, lane, sA, sB);
+    float rw = carry;   // the gradient carried into this wave's segment from after it
+    if constexpr (W == 1) {
+      carry = __fmaf_rn(__shfl(A, 0), carry, __shfl(R, 0));
+    } else {
+      if (lane == 0) { tot[q][w][0] = A; tot[q][w][1] = R; }
+      __syncthreads();
+      for (int i = W - 1; i >= 0; --i) {
+        if (i == w) rw = carry;
+        carry = __fmaf_rn(tot[q][i][0], carry, tot[q][i][1]);
+      }
+    }
+    h[0] = __fmaf_rn(eA, st, eB);
+#pragma unroll
+    for (int k = 0; k + 1 < kV; ++k)
+      h[k + 1] = __fmaf_rn(a[k], h[k], input_share<FORM>(cx[k], elem<IN, kV>(xr, k)));
+    float r = __fmaf_rn(sA, rw, sB), og[kV], ox[kV];
+#pragma unroll
+    for (int k = kV - 1; k >= 0; --k) {
+      const float delta = elem<IN, kV>(dr, k) + r;
+      if constexpr (FORM == kValue) {
+        og[k] = delta * h[k];
+        ox[k] = delta;
+      } else {
+        ox[k] = delta * cx[k];
+        og[k] = ox[k] * a[k] * (h[k] - elem<IN, kV>(xr, k));
+      }
+      r = a[k] * delta;
+      if (t0 + k >= len) og[k] = ox[k] = 0.f;
+    }
+    store_vec<OUT, kV>(ggate + (long)t0 * kBytes<OUT>, p.T - t0, og);
+    store_vec<OUT, kV>(gx + (long)t0 * kBytes<OUT>, p.T - t0, ox);
+  }
+  if (p.gh0 && w == 0 && lane == 0) p.gh0[row] = carry;
+}
+
+// Waves to a row: as many as the row has segments for, until there are 4096
+// waves in all (four for each SIMD).
+int waves_per_row(int N, int C, int T) {
+  const long rows = (long)N * C;
+  const int segs = (T + kSeg - 1) / kSeg;
+  int w = 1;
+  while (w < 16 && w < segs && rows * w < 4096) w *= 4;
+  return w;
+}
+
+template <int W, class Args, class Kernel>
+hipError_t launch_rows(Kernel kernel, const Args& p, hipStream_t s) {
+  const long rows = (long)p.N * p.C;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + kRows<W> - 1) / kRows<W>)), dim3(64 * W * kRows<W>), 0, s, p);
+  return hipGetLastError();
+}
+
+template <int IN, int OUT, int FORM>
+hipError_t fwd_rows(const FwdArgs& p, hipStream_t s) {
+  switch (waves_per_row(p.N, p.C, p.T)) {
+    case 1: return launch_rows<1>(k_scan_fwd_maps<IN, OUT, FORM, 1>, p, s);
+    case 4: return launch_rows<4>(k_scan_fwd_maps<IN, OUT, FORM, 4>, p, s);
+    default: return launch_rows<16>(k_scan_fwd_maps<IN, OUT, FORM, 16>, p, s);
+  }
+}
+
+template <int IN, int OUT, int FORM>
+hipError_t bwd_rows(const BwdArgs& p, hipStream_t s) {
+  switch (waves_per_row(p.N, p.C, p.T)) {
+    case 1: return launch_rows<1>(k_scan_bwd_maps<IN, OUT, FORM, 1>, p, s);
+    case 4: return launch_rows<4>(k_scan_bwd_maps<IN, OUT, FORM, 4>, p, s);
+    default: return launch_rows<16>(k_scan_bwd_maps<IN, OUT, FORM, 16>, p, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_scan_fwd_maps(const scan::FwdArgs& p, int in_dt, int out_dt, int form, hipStream_t s) {
+  auto go = [&](auto f) {
+    constexpr int F = decltype(f)::value;
+    if (in_dt == kBF16) return fwd_rows<kBF16, kBF16, F>(p, s);
+    return out_dt == kBF16 ? fwd_rows<kF32, kBF16, F>(p, s) : fwd_rows<kF32, kF32, F>(p, s);
+  };
+  return form == kLogit ? go(std::integral_constant<int, kLogit>{}) : go(std::integral_constant<int, kValue>{});
+}
+
+hipError_t launch_scan_bwd_maps(const scan::BwdArgs& p, int in_dt, int out_dt, int form, hipStream_t s) {
+  auto go = [&](auto f) {
+    constexpr int F = decltype(f)::value;
+    if (in_dt == kBF16) return bwd_rows<kBF16, kBF16, F>(p, s);
+    return out_dt == kBF16 ? bwd_rows<kF32, kBF16, F>(p, s) : bwd_rows<kF32, kF32, F>(p, s);
+  };
+  return form == kLogit ? go(std::integral_constant<int, kLogit>{}) : go(std::integral_constant<int, kValue>{});
+}
+
+}  // namespace bc
