@@ -493,6 +493,49 @@ bc_status gated_scan_step(const void* gate, const void* x, int dt, int64_t row_s
 size_t bc_gated_scan_workspace_bytes(int op, int N, int T, int C, int dt, int layout);
 size_t bc_gated_scan_states_bytes(int N, int T, int C, int layout);
 
+/* ------------------------------------------------------------------------
+ * quantize_i8 -- 8-bit codes and scales of the rows a mix reduces over: for the
+ * K values v of a row, with m = max |v|, in fp32 arithmetic
+ *   scale = m / 127,  q = round to nearest even(v * (127 / m)),
+ * so that q * scale is v to within scale / 2.  m < 2^-100: codes and scale are
+ * zero.  A NaN or an infinity in a row: its codes are zero and its scale NaN.
+ *
+ * src    : device, dt = BC_F32 or BC_BF16: [N][P][K] (BC_TOKENS, rows of K) or
+ *          [N][K][P] (BC_MAPS, rows of P), contiguous rows, batch_stride and
+ *          row_stride elements between batches and rows.  Weights [M][K] are
+ *          BC_TOKENS with N = 1, P = M.
+ * q      : device int8 [N*P][bc_i8_pitch(K)], row r = n*P + p; codes K.. of a
+ *          row are zero (and have to be, in codes from elsewhere).
+ * scale  : device fp32 [N*P].
+ *
+ * pointwise_mix_i8 -- the 1x1 mix of 8-bit codes, for inference: with q_r the
+ * codes of token (pixel) r and w_m those of weight row m,
+ *   out(r, m) = (sum_k q_rk w_mk) * x_scale[r] * w_scale[m] + bias[m],
+ * then max(., 0) with relu.  The sum is exact (int32), the rest fp32, rounded
+ * once to out_dt.
+ *
+ * wq, w_scale : device int8 [M][bc_i8_pitch(K)] and fp32 [M] (quantize_i8 of
+ *               the weights, once).
+ * x           : x_dt = BC_F32 or BC_BF16: the tokens, laid out as src above;
+ *               their codes are made in the call.  x_dt = BC_I8: codes
+ *               [N*P][bc_i8_pitch(K)] with x_scale [N*P] (strides unused).
+ * x_scale     : with BC_I8 only; NULL otherwise (BC_ERR_UNSUPPORTED).
+ * bias        : device fp32 [M], or NULL.
+ * out         : device, dense, out_dt = BC_F32 or BC_BF16: [N][P][M]
+ *               (BC_TOKENS) or [N][M][P] (BC_MAPS).
+ * ws          : >= bc_mix_i8_workspace_bytes(...) bytes, NULL when that is 0.
+ * Sizes: N, M, K <= 65536, N * P <= 2^30, the output's tiles of 64 x 64 at
+ * most 2^24 (BC_ERR_SHAPE).
+ * ---------------------------------------------------------------------- */
+bc_status quantize_i8(const void* src, int dt, int64_t batch_stride, int64_t row_stride, void* q, float* scale,
+                      int N, int K, int P, int layout, hipStream_t stream);
+bc_status pointwise_mix_i8(const void* wq, const float* w_scale, const void* x, int x_dt, int64_t batch_stride,
+                           int64_t row_stride, const float* x_scale, const float* bias, void* out, int out_dt,
+                           int N, int M, int K, int P, int relu, int layout, void* ws, size_t ws_bytes,
+                           hipStream_t stream);
+int bc_i8_pitch(int K);   /* bytes between rows of K codes: K rounded up to 128; 0 for K outside 1..65536 */
+size_t bc_mix_i8_workspace_bytes(int N, int M, int K, int P, int x_dt, int layout);
+
 /* Workspace sizes in bytes.  op: 0 = box_conv_fwd, 1 = box_conv_bwd (and
  * box_conv_bwd_relu_bf16); the _strided form for the strided entry points
  * (stride 1 is the plain query).  0 for sizes the calls reject. */

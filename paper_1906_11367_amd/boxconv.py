@@ -10,8 +10,8 @@ box_conv_bwd, box_conv_fwd_strided, box_conv_bwd_strided, pointwise_mix, the
 box-parameter reparameterisation (box_params_from_unit, box_params_unit_grad,
 box_params_clip), kernel splitting (box_conv_split_fwd, box_conv_split_bwd),
 the bf16 helpers (bc_cast_bf16, bc_relu_grad_bf16), the gated scan of
-recurrent layers (gated_scan_fwd, gated_scan_bwd, gated_scan_step), plus the
-workspace-size queries.
+recurrent layers (gated_scan_fwd, gated_scan_bwd, gated_scan_step), the 8-bit
+mix (quantize_i8, pointwise_mix_i8), plus the workspace-size queries.
 """
 from __future__ import annotations
 
@@ -64,6 +64,10 @@ SIGNATURES = {
     "gated_scan_step": (_i, [_vp, _vp, _i, _ll, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp]),
     "bc_gated_scan_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
     "bc_gated_scan_states_bytes": (_sz, [_i, _i, _i, _i]),
+    "quantize_i8": (_i, [_vp, _i, _ll, _ll, _vp, _vp, _i, _i, _i, _i, _vp]),
+    "pointwise_mix_i8": (_i, [_vp, _vp, _vp, _i, _ll, _ll, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp, _sz, _vp]),
+    "bc_i8_pitch": (_i, [_i]),
+    "bc_mix_i8_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
     "bc_status_string": (ctypes.c_char_p, [_i]),
     "bc_abi_version": (_i, []),
 }
@@ -579,3 +583,97 @@ def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, y:
                                           sp if state_out is None else _ptr(state_out), _ptr(slots), _ptr(y), N, C, S,
                                           form, _stream()), what)
     return y
+
+
+def i8_pitch(K: int) -> int:
+    """Bytes between rows of K 8-bit codes."""
+    return int(load_library().bc_i8_pitch(K))
+
+
+def mix_i8_workspace_bytes(N, M, K, P, x_dt: int, layout: int = BC_TOKENS) -> int:
+    return int(load_library().bc_mix_i8_workspace_bytes(N, M, K, P, x_dt, layout))
+
+
+def _mix_input(x, layout, what, name):
+    """N, K, P, pointer and strides of a mix's input: tokens [T, K] or [N, P, K],
+    maps [N, K, P] or [N, K, H, W] (contiguous maps)."""
+    if not isinstance(x, torch.Tensor) or x.dtype not in _FLOATS:
+        raise BoxConvError(f"{what}: {name} must be an fp32 or bf16 tensor")
+    if layout == BC_TOKENS:
+        if x.dim() == 2:
+            x = x.unsqueeze(0)
+        if x.dim() != 3:
+            raise BoxConvError(f"{what}: {name} must be [T, K] or [N, P, K]")
+        N, P, K = x.shape
+    elif layout == BC_MAPS:
+        if x.dim() == 4:
+            if x.stride(2) != x.shape[3] * x.stride(3) and x.shape[2] > 1:
+                raise BoxConvError(f"{what}: {name}'s maps must be contiguous")
+            x = x.flatten(2)
+        if x.dim() != 3:
+            raise BoxConvError(f"{what}: {name} must be [N, K, P] or [N, K, H, W]")
+        N, K, P = x.shape
+    else:
+        raise BoxConvError(f"{what}: unknown layout {layout}")
+    return (N, K, P, *_rows(x, what, name))
+
+
+def quantize_i8(src: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, layout: int = BC_TOKENS):
+    """8-bit codes q [rows, i8_pitch(K)] int8 and scales [rows] fp32 of src:
+    tokens or weights [rows, K] ([N, P, K]), or maps [N, K, P] (rows = N * P)."""
+    what = "quantize_i8"
+    N, K, P, sp, bs, rs = _mix_input(src, layout, what, "src")
+    if q is None or scale is None:
+        raise BoxConvError(f"{what}: q and scale must be tensors")
+    lib = load_library()
+    _need(q, (N * P, lib.bc_i8_pitch(K)), torch.int8, what, "q")
+    _need(scale, (N * P,), _F32, what, "scale")
+    _check(lib.quantize_i8(sp, dtype_code(src), bs, rs, _ptr(q), _ptr(scale), N, K, P, layout, _stream()), what)
+    return q, scale
+
+
+def pointwise_mix_i8(wq: torch.Tensor, w_scale: torch.Tensor, x: torch.Tensor, out: torch.Tensor,
+                     layout: int = BC_TOKENS, x_scale: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                     relu: int = 0, ws: torch.Tensor | None = None):
+    """The 1x1 mix in 8-bit codes: wq [M, i8_pitch(K)], w_scale [M] (quantize_i8
+    of the weights); x: tokens [T, K] or [N, P, K] -> out [..., M], or maps
+    [N, K, P] -> out [N, M, P], fp32 or bf16 each; or x codes [rows, i8_pitch(K)]
+    with x_scale [rows]."""
+    what = "pointwise_mix_i8"
+    if wq is None or w_scale is None or not isinstance(out, torch.Tensor) or out.dtype not in _FLOATS:
+        raise BoxConvError(f"{what}: wq, w_scale and an fp32 or bf16 out must be given")
+    _need(wq, (None, None), torch.int8, what, "wq")
+    M, pitch = wq.shape
+    _need(w_scale, (M,), _F32, what, "w_scale")
+    _need(bias, (M,), _F32, what, "bias")
+    lib = load_library()
+    if isinstance(x, torch.Tensor) and x.dtype is torch.int8:
+        _need(x, (None, pitch), torch.int8, what, "x")
+        rows, K = x.shape[0], pitch
+        if x_scale is None:
+            raise BoxConvError(f"{what}: codes need x_scale")
+        _need(x_scale, (rows,), _F32, what, "x_scale")
+        if layout == BC_TOKENS:
+            N, P = 1, rows
+        else:
+            N = out.shape[0]
+            P = rows // max(N, 1)
+        if N * P != rows:
+            raise BoxConvError(f"{what}: {rows} rows of codes are not {N} maps")
+        xp, bs, rs = _ptr(x), 0, 0
+    else:
+        N, K, P, xp, bs, rs = _mix_input(x, layout, what, "x")
+    if lib.bc_i8_pitch(K) != pitch:
+        raise BoxConvError(f"{what}: wq has rows of {pitch} codes, expected i8_pitch({K}) = {lib.bc_i8_pitch(K)}")
+    if layout == BC_TOKENS:
+        if out.shape[-1] != M or out.numel() != N * P * M:
+            raise BoxConvError(f"{what}: out has shape {tuple(out.shape)}, expected {N * P} tokens of {M}")
+    elif out.dim() not in (3, 4) or out.shape[0] != N or out.shape[1] != M or out.numel() != N * M * P:
+        raise BoxConvError(f"{what}: out has shape {tuple(out.shape)}, expected {(N, M, P)}")
+    dt = dtype_code(x)
+    if ws is None:
+        ws = _workspace(lib.bc_mix_i8_workspace_bytes(N, M, K, P, dt, layout), x.device)
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(lib.pointwise_mix_i8(_ptr(wq), _ptr(w_scale), xp, dt, bs, rs, _ptr(x_scale), _ptr(bias), _ptr(out),
+                                dtype_code(out), N, M, K, P, relu, layout, _ptr(ws), nbytes, _stream()), what)
+    return out

@@ -580,4 +580,55 @@ bc_status gated_scan_step(const void* gate, const void* x, int dt, int64_t row_s
                                          stream));
 }
 
+static bool i8_dims_ok(int N, int M, int K, int P) {
+  if (N <= 0 || M <= 0 || K <= 0 || P <= 0 || N > kMaxDim || M > kMaxDim || K > kMaxDim) return false;
+  if ((long)N * P > (1L << 30)) return false;
+  return (((long)N * P + 63) / 64) * ((M + 63) / 64) <= (1L << 24);
+}
+
+int bc_i8_pitch(int K) { return K <= 0 || K > kMaxDim ? 0 : bc::i8_pitch(K); }
+
+size_t bc_mix_i8_workspace_bytes(int N, int M, int K, int P, int x_dt, int layout) {
+  if (!i8_dims_ok(N, M, K, P) || (layout != BC_TOKENS && layout != BC_MAPS)) return 0;
+  if (x_dt != BC_F32 && x_dt != BC_BF16 && x_dt != BC_I8) return 0;
+  return bc::mix_i8_workspace_bytes(N, M, K, P, x_dt, layout == BC_MAPS);
+}
+
+bc_status quantize_i8(const void* src, int dt, int64_t batch_stride, int64_t row_stride, void* q, float* scale, int N,
+                      int K, int P, int layout, hipStream_t stream) {
+  if (!src || !q || !scale) return BC_ERR_NULL;
+  if (layout != BC_TOKENS && layout != BC_MAPS) return BC_ERR_UNSUPPORTED;
+  if (!i8_dims_ok(N, 1, K, P)) return BC_ERR_SHAPE;
+  if (dt != BC_F32 && dt != BC_BF16) return BC_ERR_DTYPE;
+  const bool maps = layout == BC_MAPS;
+  if (!strides_ok(batch_stride, row_stride, N, maps ? K : P, maps ? P : K)) return BC_ERR_SHAPE;
+  if (!aligned16(src) || !aligned16(q) || !aligned16(scale)) return BC_ERR_ALIGN;
+  return hip_status(bc::launch_quantize_i8(src, dt, (long)batch_stride, (long)row_stride, q, scale, N, K, P, maps,
+                                           stream));
+}
+
+bc_status pointwise_mix_i8(const void* wq, const float* w_scale, const void* x, int x_dt, int64_t batch_stride,
+                           int64_t row_stride, const float* x_scale, const float* bias, void* out, int out_dt, int N,
+                           int M, int K, int P, int relu, int layout, void* ws, size_t ws_bytes,
+                           hipStream_t stream) {
+  if (!wq || !w_scale || !x || !out) return BC_ERR_NULL;
+  if (layout != BC_TOKENS && layout != BC_MAPS) return BC_ERR_UNSUPPORTED;
+  if (!i8_dims_ok(N, M, K, P)) return BC_ERR_SHAPE;
+  if (x_dt != BC_F32 && x_dt != BC_BF16 && x_dt != BC_I8) return BC_ERR_DTYPE;
+  if (out_dt != BC_F32 && out_dt != BC_BF16) return BC_ERR_DTYPE;
+  const bool codes = x_dt == BC_I8, maps = layout == BC_MAPS;
+  if (codes && !x_scale) return BC_ERR_NULL;
+  if (!codes && x_scale) return BC_ERR_UNSUPPORTED;
+  if (!codes && !strides_ok(batch_stride, row_stride, N, maps ? K : P, maps ? P : K)) return BC_ERR_SHAPE;
+  if (!aligned16(wq) || !aligned16(w_scale) || !aligned16(x) || !aligned16(out) || !aligned16_or_null(x_scale) ||
+      !aligned16_or_null(bias))
+    return BC_ERR_ALIGN;
+  const size_t need = bc::mix_i8_workspace_bytes(N, M, K, P, x_dt, maps);
+  if (need > 0 && (!ws || ws_bytes < need)) return BC_ERR_WORKSPACE;
+  if (need > 0 && !aligned16(ws)) return BC_ERR_ALIGN;
+  return hip_status(bc::launch_mix_i8({wq, w_scale, x, x_dt, (long)batch_stride, (long)row_stride, x_scale, bias, out,
+                                       out_dt, N, M, K, P, relu, maps, ws},
+                                      stream));
+}
+
 }  // extern "C"
