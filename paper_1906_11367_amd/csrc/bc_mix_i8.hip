@@ -35,35 +35,155 @@ __device__ __forceinline__ void store_out(const Args& p, int i, int j, int sum, 
   else reinterpret_cast<float*>(p.out)[at] = z;
 }
 
-// One wave per 32 x 32 outputs, operands straight from memory.
-template <int OUT, bool kMaps>
-__global__ __launch_bounds__(256) void k_mix_i8(Args p) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int nj = (p.J + 63) / 64;
-  const int i0 = (int)(blockIdx.x / nj) * 64 + (wave >> 1) * 32, j0 = (int)(blockIdx.x % nj) * 64 + (wave & 1) * 32;
-  const int8_t* a = p.a + (long)min(i0 + (lane & 31), p.I - 1) * p.pitch + 16 * (lane >> 5);
-  const int8_t* b = p.b + (long)min(j0 + (lane & 31), p.J - 1) * p.pitch + 16 * (lane >> 5);
-  i32x16_t acc;
+#define BC_LDS __attribute__((address_space(3)))
+
+constexpr int kBK = 64;   // codes of a row per stage
+
+__device__ __forceinline__ i32x4_t buf_desc(const void* p, uint32_t bytes) {
+  const uint64_t a = (uint64_t)p;
+  i32x4_t r;
+  r.x = __builtin_amdgcn_readfirstlane((int)a);
+  r.y = __builtin_amdgcn_readfirstlane((int)(a >> 32));
+  r.z = __builtin_amdgcn_readfirstlane((int)bytes);
+  r.w = 0x00020000;
+  return r;
+}
+
+// 16 bytes per lane from (desc, voff + soff) to LDS at lds + 16 * lane, waited
+// for by count (wait_loads).
+__device__ __forceinline__ void load_to_lds(const i32x4_t& rs, uint32_t voff, uint32_t soff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 1\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               ::"s"(lds), "v"(voff), "s"(rs), "s"(soff)
+               : "memory", "m0");
+}
+
+// Waits until at most kLeft of the wave's loads are pending, and for its LDS
+// reads (whose place the loads after the next barrier may take).
+template <int kLeft>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLeft) : "memory");
+}
+
+// Tiles through LDS: WI x WJ waves of FI x FJ blocks of 32 x 32 outputs.
+//
+// Both operands go from memory into a ring of LDS stages (kBK codes of every
+// row of the tile), kStages - 1 stages ahead, one barrier per stage.  The
+// 16-byte chunk c of row r sits at chunk c ^ ((r >> 2) & 3), so that the 16
+// lanes that read one chunk of 16 rows hit all banks; the loads write LDS in
+// lane order, so each lane fetches the chunk that belongs there.
+template <int OUT, bool kMaps, int WI, int WJ, int FI, int FJ, int kStages>
+__global__ __launch_bounds__(64 * WI * WJ) void k_mix_i8_tile(Args p, int ti, int tj, int per) {
+  constexpr int kWaves = WI * WJ, BI = WI * FI * 32, BJ = WJ * FJ * 32;
+  constexpr int kABytes = BI * kBK, kStage = (BI + BJ) * kBK;
+  constexpr int kALoads = kABytes / 1024, kLoads = kStage / 1024 / kWaves;   // kLoads: per wave
+  static_assert(kStage % (1024 * kWaves) == 0, "whole loads");
+  extern __shared__ __align__(16) unsigned char smem[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(BC_LDS unsigned char*)smem;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // consecutive tiles on one XCD; 8 tiles of i for each of j, so that the
+  // tiles running together share both operands in its L2
+  const int L = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if (L >= ti * tj) return;
+  const int grp = L / (8 * tj), in = L - grp * 8 * tj, gsz = min(8, ti - grp * 8);
+  const int i0 = (grp * 8 + in % gsz) * BI, j0 = in / gsz * BJ;
+  const int nk = p.pitch / kBK;
+  const i32x4_t ra = buf_desc(p.a + (long)i0 * p.pitch, (uint32_t)(min(BI, p.I - i0) * p.pitch));
+  const i32x4_t rb = buf_desc(p.b + (long)j0 * p.pitch, (uint32_t)(min(BJ, p.J - j0) * p.pitch));
+
+  uint32_t voff[kLoads];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = 0;
-  for (int k = 0; k < p.pitch; k += 32)
-    acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<const i32x4_t*>(a + k),
-                                                *reinterpret_cast<const i32x4_t*>(b + k), acc, 0, 0, 0);
-  const int j = j0 + (lane & 31);
-  if (j >= p.J) return;
-  const float sj = p.bscale[j], bj = p.bias && !kMaps ? p.bias[j] : 0.f;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int i = i0 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-    if (i < p.I) store_out<OUT, kMaps>(p, i, j, acc[r], p.ascale[i], sj, p.bias && kMaps ? p.bias[i] : 0.f, bj);
+  for (int l = 0; l < kLoads; ++l) {
+    const int ld = wave * kLoads + l;
+    const bool is_a = ld < kALoads;
+    const int row = (is_a ? ld : ld - kALoads) * 16 + (lane >> 2);
+    // rows past the operand read zeros (the descriptor ends there)
+    voff[l] = (uint32_t)row * (uint32_t)p.pitch + (uint32_t)(((lane & 3) ^ ((row >> 2) & 3)) * 16);
   }
+  int load_slot = 0, load_k = 0;
+  auto issue = [&]() {
+    const uint32_t base = lds0 + load_slot * kStage;
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) {
+      const int ld = wave * kLoads + l;
+      load_to_lds(ld < kALoads ? ra : rb, voff[l], (uint32_t)(load_k * kBK), base + ld * 1024);
+    }
+    load_slot = load_slot + 1 == kStages ? 0 : load_slot + 1;
+    ++load_k;
+  };
+
+  const int wi = wave / WJ, wj = wave % WJ;
+  // rows 32 apart swizzle alike
+  const int arow = wi * FI * 32 + (lane & 31), brow = wj * FJ * 32 + (lane & 31);
+  uint32_t aoff[2], boff[2];
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+    const int c = 2 * kk + (lane >> 5);
+    aoff[kk] = (uint32_t)(arow * kBK + ((c ^ ((arow >> 2) & 3)) << 4));
+    boff[kk] = (uint32_t)(kABytes + brow * kBK + ((c ^ ((brow >> 2) & 3)) << 4));
+  }
+  i32x16_t acc[FI][FJ];
+#pragma unroll
+  for (int x = 0; x < FI; ++x)
+#pragma unroll
+    for (int y = 0; y < FJ; ++y)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[x][y][r] = 0;
+
+  for (int s = 0; s < kStages - 1 && s < nk; ++s) issue();
+  int slot = 0;
+  for (int s = 0; s < nk; ++s) {
+    if (s + kStages - 2 < nk) wait_loads<kLoads * (kStages - 2)>();
+    else wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
+    if (load_k < nk) issue();
+    const uint32_t st = lds0 + slot * kStage;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      i32x4_t af[FI], bf[FJ];
+#pragma unroll
+      for (int x = 0; x < FI; ++x) af[x] = *(BC_LDS i32x4_t*)(uintptr_t)(st + aoff[kk] + x * 32 * kBK);
+#pragma unroll
+      for (int y = 0; y < FJ; ++y) bf[y] = *(BC_LDS i32x4_t*)(uintptr_t)(st + boff[kk] + y * 32 * kBK);
+#pragma unroll
+      for (int x = 0; x < FI; ++x)
+#pragma unroll
+        for (int y = 0; y < FJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_32x32x32_i8(af[x], bf[y], acc[x][y], 0, 0, 0);
+    }
+    slot = slot + 1 == kStages ? 0 : slot + 1;
+  }
+
+  const int ib = i0 + wi * FI * 32 + 4 * (lane >> 5), jb = j0 + wj * FJ * 32 + (lane & 31);
+#pragma unroll
+  for (int y = 0; y < FJ; ++y) {
+    const int j = jb + 32 * y;
+    if (j >= p.J) continue;
+    const float sj = p.bscale[j], bj = p.bias && !kMaps ? p.bias[j] : 0.f;
+#pragma unroll
+    for (int x = 0; x < FI; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i = ib + 32 * x + 8 * (r >> 2) + (r & 3);
+        if (i < p.I) store_out<OUT, kMaps>(p, i, j, acc[x][y][r], p.ascale[i], sj, p.bias && kMaps ? p.bias[i] : 0.f, bj);
+      }
+  }
+}
+
+template <int OUT, bool kMaps, int WI, int WJ, int FI, int FJ, int kStages>
+hipError_t launch_tile(const Args& p, hipStream_t s) {
+  constexpr int BI = WI * FI * 32, BJ = WJ * FJ * 32, kLds = kStages * (BI + BJ) * kBK;
+  const auto kernel = k_mix_i8_tile<OUT, kMaps, WI, WJ, FI, FJ, kStages>;
+  const int ti = (p.I + BI - 1) / BI, tj = (p.J + BJ - 1) / BJ, per = (ti * tj + 7) / 8;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(per * 8)), dim3(64 * WI * WJ), kLds, s, p, ti, tj, per);
+  return hipGetLastError();
 }
 
 template <int OUT, bool kMaps>
 hipError_t launch(const Args& p, hipStream_t s) {
-  const dim3 grid((unsigned)(((long)(p.I + 63) / 64) * ((p.J + 63) / 64)));
-  hipLaunchKernelGGL((k_mix_i8<OUT, kMaps>), grid, dim3(256), 0, s, p);
-  return hipGetLastError();
+  auto tiles = [&](int b) { return (long)((p.I + b - 1) / b) * ((p.J + b - 1) / b); };
+  if (tiles(256) >= 256) return launch_tile<OUT, kMaps, 2, 4, 4, 2, 4>(p, s);
+  if (tiles(128) >= 256) return launch_tile<OUT, kMaps, 2, 2, 2, 2, 4>(p, s);
+  return launch_tile<OUT, kMaps, 2, 2, 1, 1, 6>(p, s);
 }
 
 // Workspace: the tokens' codes, then their scales.
