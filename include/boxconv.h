@@ -447,8 +447,9 @@ typedef enum { BC_GATE_LOGIT = 0, BC_GATE_VALUE = 1 } bc_gate_form;
  * Non-finite values spread as the recurrence spreads them: forward in time in
  * their own channel and sequence (also through a reset: 0 * infinity), nowhere
  * else.
- * Sizes: N, C <= 65536, N * C <= 2^25, T <= 2^30 (BC_ERR_SHAPE); strides
- * smaller than a row or a batch are BC_ERR_SHAPE too.
+ * Sizes: N, C <= 65536, T <= 2^30; tokens: N * ceil(C/32) * ceil(T/64) < 2^31;
+ * maps: N * C <= 2^25 (BC_ERR_SHAPE).  Strides smaller than a row or a batch
+ * are BC_ERR_SHAPE too.
  *
  * gated_scan_bwd -- gradients of L = <grad_y, y> + <grad_h_last, h_last>.
  * With r_T = grad_h_last, delta_t = grad_y_t + r_{t+1}, r_t = a_t delta_t:

@@ -485,10 +485,12 @@ bc_status pointwise_mix(int mode, const void* a, int a_dt, const void* b, int b_
 
 // ---- recurrent layers ------------------------------------------------------
 
-static bool scan_dims_ok(int N, int T, int C) {
+static bool scan_dims_ok(int N, int T, int C, int layout) {
+  if (layout != BC_TOKENS && layout != BC_MAPS) return false;
   if (N <= 0 || T <= 0 || C <= 0 || N > kMaxDim || C > kMaxDim || T > (1 << 30)) return false;
-  // a wave per row of maps: grids below 2^32 threads
-  return (long)N * C <= (1L << 25);
+  // a block counts its tiles of at least 64 steps by 32 channels in 31 bits
+  if (layout == BC_TOKENS) return (double)N * ((C + 31) / 32) * ((T + 63) / 64) < 2147483648.0;
+  return (long)N * C <= (1L << 25);   // at least a wave per row: grids below 2^32 threads
 }
 
 // Strides of a tensor of N batches of `rows` contiguous rows of `cols`.
@@ -502,13 +504,13 @@ static bool strides_ok(int64_t bs, int64_t rs, int N, int rows, int cols) {
 }
 
 size_t bc_gated_scan_states_bytes(int N, int T, int C, int layout) {
-  if (!scan_dims_ok(N, T, C) || (layout != BC_TOKENS && layout != BC_MAPS)) return 0;
+  if (!scan_dims_ok(N, T, C, layout)) return 0;
   const int span = layout == BC_MAPS ? bc::kScanSpanMaps : bc::kScanSpan;
   return (size_t)N * C * ((T + span - 1) / span) * 4;
 }
 
 size_t bc_gated_scan_workspace_bytes(int op, int N, int T, int C, int dt, int layout) {
-  if (!scan_dims_ok(N, T, C) || (layout != BC_TOKENS && layout != BC_MAPS) || (op != 0 && op != 1)) return 0;
+  if (!scan_dims_ok(N, T, C, layout) || (op != 0 && op != 1)) return 0;
   if (dt != BC_F32 && dt != BC_BF16) return 0;
   return bc::scan_workspace_bytes(op == 1, N, T, C, dt, layout == BC_MAPS);
 }
@@ -516,7 +518,7 @@ size_t bc_gated_scan_workspace_bytes(int op, int N, int T, int C, int dt, int la
 static bc_status scan_checks(int N, int T, int C, int dt, int out_dt, int64_t bs, int64_t rs, int form, int layout) {
   if (layout != BC_TOKENS && layout != BC_MAPS) return BC_ERR_UNSUPPORTED;
   if (form != BC_GATE_LOGIT && form != BC_GATE_VALUE) return BC_ERR_UNSUPPORTED;
-  if (!scan_dims_ok(N, T, C)) return BC_ERR_SHAPE;
+  if (!scan_dims_ok(N, T, C, layout)) return BC_ERR_SHAPE;
   if (dt != BC_F32 && dt != BC_BF16) return BC_ERR_DTYPE;
   if (out_dt != dt && !(dt == BC_F32 && out_dt == BC_BF16)) return BC_ERR_DTYPE;
   const bool maps = layout == BC_MAPS;

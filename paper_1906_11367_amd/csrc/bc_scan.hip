@@ -8,25 +8,53 @@
 // consecutive steps in registers, so every element is read once.
 #include "bc_scan.hpp"
 
+#include <algorithm>
+
 namespace bc {
 namespace {
 
 using namespace scan;
 
-constexpr int kThreads = 256;
-constexpr int kGroups = 8;                    // lanes across a slab
-constexpr int kSlots = kThreads / kGroups;    // runs of steps in a tile
-constexpr int kWaves = kThreads / 64;
-template <int DT> constexpr int kV = 16 / kBytes<DT>;       // channels per lane
-template <int DT> constexpr int kSlab = kGroups * kV<DT>;   // channels per block
-constexpr int kFwdL = 8, kBwdL = 4;
-constexpr int kFwdTile = kSlots * kFwdL, kBwdTile = kSlots * kBwdL;
-// A state is kept every kScanSpan steps: where each backward tile starts.
-static_assert(kBwdTile == kScanSpan && kFwdTile % kScanSpan == 0, "states at the backward's tiles");
+// The division of a tile: lanes hold kV channels of kL consecutive steps;
+// kGroups lanes side by side make a slab (128 bytes: whole cache lines of every
+// row), kSlots runs of steps a tile.  W_: waves per SIMD to build for.
+template <int V_, int G_, int NT_, int L_, int W_>
+struct Cut {
+  static constexpr int kV = V_, kGroups = G_, kThreads = NT_, kL = L_, kWavesPerSimd = W_;
+  static constexpr int kSlab = kV * kGroups, kSlots = kThreads / kGroups, kTile = kSlots * kL, kWaves = kThreads / 64;
+};
+// Sequences of several tiles take the first cut; one tile takes the shortest
+// that holds it (a tile of 256 steps for a sequence of 4 would leave all but a
+// few lanes of the block idle).  Measured on 2^26 elements (bf16) and 2^25
+// (fp32) in chained tiles, us:
+//   forward, bf16: 4 channels x 8 steps a lane, 512 threads 100; 8 x 4 in 256
+//     threads 121; 2 x 16 99, 2 x 8 120, 8 x 8 150
+//   backward, bf16: 2 x 8 157-164; 4 x 4 178, 8 x 2 285, 2 x 16 186
+//   fp32: forward 4 x 4 in 512 threads 82-86 (256 threads 118, 4 x 8 87),
+//     backward 127-131 (256 threads 130, 2 x 8 129, 2 x 16 186)
+// Longer tiles cost registers (fewer waves), shorter ones more carries.
+template <int DT, int kSize> struct FwdCuts;
+template <> struct FwdCuts<kBF16, 0> { using type = Cut<4, 16, 512, 8, 4>; };   // 256 steps
+template <> struct FwdCuts<kBF16, 1> { using type = Cut<4, 16, 256, 8, 4>; };   // 128
+template <> struct FwdCuts<kBF16, 2> { using type = Cut<4, 16, 64, 8, 4>; };    // 32
+template <> struct FwdCuts<kF32, 0> { using type = Cut<4, 8, 512, 4, 4>; };     // 256
+template <> struct FwdCuts<kF32, 1> { using type = Cut<4, 8, 256, 4, 4>; };     // 128
+template <> struct FwdCuts<kF32, 2> { using type = Cut<4, 8, 64, 4, 4>; };      // 32
+template <int DT, int kSize> struct BwdCuts;
+template <> struct BwdCuts<kBF16, 0> { using type = Cut<2, 32, 512, 8, 4>; };   // 128
+template <> struct BwdCuts<kBF16, 1> { using type = Cut<2, 32, 256, 8, 4>; };   // 64
+template <> struct BwdCuts<kBF16, 2> { using type = Cut<2, 32, 64, 8, 4>; };    // 16
+template <> struct BwdCuts<kF32, 0> { using type = Cut<4, 8, 512, 4, 4>; };     // 256
+template <> struct BwdCuts<kF32, 1> { using type = Cut<4, 8, 256, 4, 4>; };     // 128
+template <> struct BwdCuts<kF32, 2> { using type = Cut<4, 8, 64, 4, 4>; };      // 32
+template <int DT, int kSize> using FwdCut = typename FwdCuts<DT, kSize>::type;
+template <int DT, int kSize> using BwdCut = typename BwdCuts<DT, kSize>::type;
+// States are kept every kScanSpan steps: at every tile of the chained backward.
+static_assert(BwdCut<kBF16, 0>::kTile % kScanSpan == 0 && BwdCut<kF32, 0>::kTile % kScanSpan == 0, "kept states");
 
 // (A, B) of the runs of lower slots of this wave (identity for the first), and
 // the inclusive pair.  Slots are kGroups lanes apart.
-template <int V>
+template <int V, int kGroups>
 __device__ __forceinline__ void wave_prefix(const float (&A)[V], const float (&B)[V], int lane, float (&iA)[V],
                                             float (&iB)[V], float (&eA)[V], float (&eB)[V]) {
 #pragma unroll
@@ -51,7 +79,7 @@ __device__ __forceinline__ void wave_prefix(const float (&A)[V], const float (&B
 }
 
 // The same from the other end: the runs of higher slots.
-template <int V>
+template <int V, int kGroups>
 __device__ __forceinline__ void wave_suffix(const float (&A)[V], const float (&B)[V], int lane, float (&iA)[V],
                                             float (&iB)[V], float (&eA)[V], float (&eB)[V]) {
 #pragma unroll
@@ -75,92 +103,232 @@ __device__ __forceinline__ void wave_suffix(const float (&A)[V], const float (&B
   }
 }
 
-template <int IN, int OUT, int FORM>
-__global__ __launch_bounds__(kThreads) void k_scan_fwd(FwdArgs p) {
-  constexpr int V = kV<IN>, L = kFwdL, CW = kSlab<IN>;
-  __shared__ float totA[2][kWaves][CW], totB[2][kWaves][CW], carry[2][CW];
+// Chained tiles.  Every tile has a block of its own, and the state before a
+// tile comes from the tiles before it in one launch: each publishes its pair
+// (A, B), and a block combines the pairs back to the start of its group of
+// kGroupTiles with the state published there (by the last block of the group
+// before).  A block waits only on lower tickets, drawn when a block starts,
+// whose owners are running and wait on still lower ones, so every wait ends;
+// which pairs are combined, and in which order, depends on the tile alone, so
+// results do not depend on the order in which blocks run.
+// A word carries its own validity: an 8-byte store is seen whole, and the
+// workspace is first filled with kEmpty, which no publisher writes.
+constexpr int kGroupTiles = 16;
+constexpr unsigned long long kEmpty = ~0ull;
+// A bound on the polls (about a second), in case the caller lets two calls
+// share a workspace: the outputs are then NaN rather than never.
+constexpr int kMaxPolls = 1 << 20;
+
+__device__ __forceinline__ void publish(unsigned long long* at, float lo, float hi) {
+  if (hi != hi) hi = __uint_as_float(0x7fc00000u);   // never kEmpty
+  const unsigned long long w = (unsigned long long)__float_as_uint(hi) << 32 | __float_as_uint(lo);
+  __hip_atomic_store(at, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ unsigned long long peek(const unsigned long long* at) {
+  return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ float word_lo(unsigned long long w) { return __uint_as_float((unsigned)w); }
+__device__ __forceinline__ float word_hi(unsigned long long w) { return __uint_as_float((unsigned)(w >> 32)); }
+
+// The words of a group that the lanes of one channel read: word 0 is the state
+// at the group's start, word 1 + i the pair of its tile i.  Each of the block's
+// kThreads / kSlab lanes of a channel takes a few consecutive ones and returns
+// their composition (A = 0 where the state itself is among them; the first
+// group's is in its tile 0's pair).
+template <class X>
+struct Lookback {
+  static constexpr int kParts = X::kThreads / X::kSlab, kPer = kGroupTiles / kParts;
+  static_assert(kParts * kPer == kGroupTiles, "whole words per lane");
+
+  // o: the tile's place in its chain; first: the chain's start; agg and pre:
+  // this channel's words of the chain
+  static __device__ __forceinline__ void read(int o, int part, float first, const unsigned long long* agg,
+                                              const unsigned long long* pre, float& A, float& B) {
+    const int base = o & ~(kGroupTiles - 1), n = o - base;
+    unsigned long long w[kPer];
+    A = 1.f;
+    B = 0.f;
+    for (int polls = 0;; ++polls) {
+      bool ready = true;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int k = part * kPer + i;
+        const unsigned long long* at = k == 0 ? pre + (long)(base / kGroupTiles) * X::kSlab
+                                              : agg + (long)(base + k - 1) * X::kSlab;
+        w[i] = (k == 0 ? base > 0 : k <= n) ? peek(at) : 0ull;
+        ready &= w[i] != kEmpty;
+      }
+      if (ready) break;
+      if (polls == kMaxPolls) {
+        A = B = __uint_as_float(0x7fc00000u);
+        return;
+      }
+      __builtin_amdgcn_s_sleep(1);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int k = part * kPer + i;
+      if (k == 0) {
+        A = 0.f;
+        B = base > 0 ? word_lo(w[i]) : first;   // first: 0 but in tile 0
+      } else if (k <= n) {
+        B = __fmaf_rn(word_hi(w[i]), B, word_lo(w[i]));
+        A *= word_hi(w[i]);
+      }
+    }
+  }
+};
+
+// Fills the words of a chained call (the ticket with them: it starts at -1).
+__global__ __launch_bounds__(256) void k_scan_clear(unsigned long long* ws, long words) {
+  const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 2;
+  if (i + 1 < words) *reinterpret_cast<ulonglong2*>(ws + i) = make_ulonglong2(kEmpty, kEmpty);
+  else if (i < words) ws[i] = kEmpty;
+}
+
+// This block's place in the chain: tickets count through the units (a slab of
+// a sequence) of tile 0, then of tile 1, and so on.
+__device__ __forceinline__ int draw_ticket(unsigned* ticket) {
+  __shared__ int t;
+  if (threadIdx.x == 0) t = (int)(atomicAdd(ticket, 1u) + 1u);
+  __syncthreads();
+  return t;
+}
+
+template <class X, int IN, int OUT, int FORM, bool kChain>
+__global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdArgs p) {
+  constexpr int V = X::kV, L = X::kL, CW = X::kSlab, kGroups = X::kGroups, kWaves = X::kWaves, kTile = X::kTile;
+  __shared__ float totA[kWaves][CW], totB[kWaves][CW], carry[CW], last[CW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int grp = tid % kGroups, slot = tid / kGroups;
-  const int n = blockIdx.x / p.slabs, slab = blockIdx.x % p.slabs;
+  constexpr int kParts = kChain ? X::kThreads / CW : 1;
+  __shared__ float lookA[kParts][CW], lookB[kParts][CW];
+  int unit = blockIdx.x, place = 0;
+  if constexpr (kChain) {
+    const int t = draw_ticket(p.ticket), units = p.N * p.slabs;
+    unit = t % units;
+    place = t / units;
+    if (place >= p.tiles) return;   // the grid's last row
+  }
+  const int n = unit / p.slabs, slab = unit % p.slabs;
   const int c0 = slab * CW + grp * V, avail = p.C - c0;   // <= 0: no channel here
   const int len = seq_len(p.lengths, n, p.T);
   const char* gate = p.gate + ((long)n * p.bs + c0) * kBytes<IN>;
   const char* xp = p.x + ((long)n * p.bs + c0) * kBytes<IN>;
   char* yp = p.y + ((long)n * p.T * p.C + c0) * kBytes<OUT>;
   const int S = (p.T + kScanSpan - 1) / kScanSpan;
+  float first = 0.f;
   if (tid < CW) {
     const int c = slab * CW + tid;
-    carry[0][tid] = p.h0 && c < p.C ? p.h0[(size_t)n * p.C + c] : 0.f;
+    if (place == 0) first = p.h0 && c < p.C ? p.h0[(size_t)n * p.C + c] : 0.f;
+    if (!kChain) carry[tid] = first;
   }
-  int q = 0;
-  for (int tile = 0; tile < p.tiles; ++tile, q ^= 1) {
-    const int t0 = tile * kFwdTile + slot * L;
-    Raw<kWords<IN, V>> g[L], x[L];
+  const int tile = place;
+  const int t0 = tile * kTile + slot * L;
+  Raw<kWords<IN, V>> g[L], x[L];
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const int have = t0 + i < len ? avail : 0;
-      g[i] = load_vec<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>, have);
-      x[i] = load_vec<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>, have);
-    }
-    float a[L][V], b[L][V], A[V], B[V];
+  for (int i = 0; i < L; ++i) {
+    const int have = t0 + i < len ? avail : 0;
+    g[i] = t0 + i < len ? load_vec<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>, avail) : hold_gate<IN, FORM, V>();
+    x[i] = load_vec<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>, have);
+  }
+  float a[L][V], b[L][V], A[V], B[V];
 #pragma unroll
-    for (int k = 0; k < V; ++k) { A[k] = 1.f; B[k] = 0.f; }
+  for (int k = 0; k < V; ++k) { A[k] = 1.f; B[k] = 0.f; }
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        float c;
-        coefficients<IN, FORM>(elem<IN, V>(g[i], k), a[i][k], c);
-        b[i][k] = input_share<FORM>(c, elem<IN, V>(x[i], k));
-        if (t0 + i >= len) { a[i][k] = 1.f; b[i][k] = 0.f; }
-        A[k] *= a[i][k];
-        B[k] = __fmaf_rn(a[i][k], B[k], b[i][k]);
-      }
-    float iA[V], iB[V], eA[V], eB[V];
-    wave_prefix<V>(A, B, lane, iA, iB, eA, eB);
-    if (lane >= 64 - kGroups) {
-#pragma unroll
-      for (int k = 0; k < V; ++k) { totA[q][wave][grp * V + k] = iA[k]; totB[q][wave][grp * V + k] = iB[k]; }
-    }
-    __syncthreads();
-    if (tid < CW) {
-      float h = carry[q][tid];
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) h = __fmaf_rn(totA[q][w][tid], h, totB[q][w][tid]);
-      carry[q ^ 1][tid] = h;
-    }
-    float h[V];
+  for (int i = 0; i < L; ++i)
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      h[k] = carry[q][grp * V + k];
-      for (int w = 0; w < wave; ++w) h[k] = __fmaf_rn(totA[q][w][grp * V + k], h[k], totB[q][w][grp * V + k]);
-      h[k] = __fmaf_rn(eA[k], h[k], eB[k]);
+      float c;
+      coefficients<IN, FORM>(elem<IN, V>(g[i], k), a[i][k], c);
+      b[i][k] = input_share<FORM>(c, elem<IN, V>(x[i], k));
+      A[k] *= a[i][k];
+      B[k] = __fmaf_rn(a[i][k], B[k], b[i][k]);
     }
-    if (p.states && t0 % kScanSpan == 0 && t0 < p.T && avail > 0)
-      store_vec<kF32, V>(reinterpret_cast<char*>(p.states + ((size_t)n * S + t0 / kScanSpan) * p.C + c0), avail, h);
+  float iA[V], iB[V], eA[V], eB[V];
+  wave_prefix<V, kGroups>(A, B, lane, iA, iB, eA, eB);
+  if (lane >= 64 - kGroups) {
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      if (t0 + i >= p.T) break;
-      float o[V];
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        h[k] = __fmaf_rn(a[i][k], h[k], b[i][k]);
-        o[k] = t0 + i < len ? h[k] : 0.f;
-      }
-      store_vec<OUT, V>(yp + (long)(t0 + i) * p.C * kBytes<OUT>, avail, o);
-    }
+    for (int k = 0; k < V; ++k) { totA[wave][grp * V + k] = iA[k]; totB[wave][grp * V + k] = iB[k]; }
   }
   __syncthreads();
-  if (p.h_last && tid < CW && slab * CW + tid < p.C) p.h_last[(size_t)n * p.C + slab * CW + tid] = carry[q][tid];
+  if constexpr (kChain) {
+    using Look = Lookback<X>;
+    const int ch = tid % CW, part = tid / CW;
+    const long chain = (long)unit * p.tiles * CW + ch, groups = (long)unit * p.groups * CW + ch;
+    float ta = 1.f, tz = 0.f, A, B;
+    if (tid < CW) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        tz = __fmaf_rn(totA[w][ch], tz, totB[w][ch]);
+        ta *= totA[w][ch];
+      }
+      // tile 0 publishes a state (A = 0): only it reads the chain's start, whose
+      // memory the chain's end may be
+      if (place == 0) publish(p.agg + chain, __fmaf_rn(ta, first, tz), 0.f);
+      else publish(p.agg + chain + (long)tile * CW, tz, ta);
+    }
+    Look::read(tile, part, first, p.agg + chain, p.pre + groups, A, B);
+    lookA[part][ch] = A;
+    lookB[part][ch] = B;
+    __syncthreads();
+    if (tid < CW) {
+      float v = B;   // part 0 starts from the state itself
+#pragma unroll
+      for (int i = 1; i < kParts; ++i) v = __fmaf_rn(lookA[i][ch], v, lookB[i][ch]);
+      carry[ch] = v;
+      v = __fmaf_rn(ta, v, tz);
+      last[ch] = v;
+      if (tile % kGroupTiles == kGroupTiles - 1 && tile + 1 < p.tiles)
+        publish(p.pre + groups + (long)(tile / kGroupTiles + 1) * CW, v, 0.f);
+    }
+    __syncthreads();
+  } else if (tid < CW) {
+    float h = first;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) h = __fmaf_rn(totA[w][tid], h, totB[w][tid]);
+    last[tid] = h;
+  }
+  float h[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    h[k] = carry[grp * V + k];
+    for (int w = 0; w < wave; ++w) h[k] = __fmaf_rn(totA[w][grp * V + k], h[k], totB[w][grp * V + k]);
+    h[k] = __fmaf_rn(eA[k], h[k], eB[k]);
+  }
+  if (p.states && t0 % kScanSpan == 0 && t0 < p.T && avail > 0)
+    store_vec<kF32, V>(reinterpret_cast<char*>(p.states + ((size_t)n * S + t0 / kScanSpan) * p.C + c0), avail, h);
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) h[k] = __fmaf_rn(a[i][k], h[k], b[i][k]);
+    char* at = yp + (long)(t0 + i) * p.C * kBytes<OUT>;
+    if (t0 + i < len) store_vec<OUT, V>(at, avail, h);
+    else if (t0 + i < p.T) store_zero<OUT, V>(at, avail);
+  }
+  if (kChain && place + 1 < p.tiles) return;
+  __syncthreads();
+  if (p.h_last && tid < CW && slab * CW + tid < p.C) p.h_last[(size_t)n * p.C + slab * CW + tid] = last[tid];
 }
 
-template <int IN, int OUT, int FORM>
-__global__ __launch_bounds__(kThreads) void k_scan_bwd(BwdArgs p) {
-  constexpr int V = kV<IN>, L = kBwdL, CW = kSlab<IN>;
-  __shared__ float totA[2][kWaves][CW], totB[2][kWaves][CW], totR[2][kWaves][CW], carry[2][CW];
+template <class X, int IN, int OUT, int FORM, bool kChain>
+__global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_bwd(BwdArgs p) {
+  constexpr int V = X::kV, L = X::kL, CW = X::kSlab, kGroups = X::kGroups, kWaves = X::kWaves, kTile = X::kTile;
+  __shared__ float totA[kWaves][CW], totB[kWaves][CW], totR[kWaves][CW], carry[CW], last[CW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int grp = tid % kGroups, slot = tid / kGroups;
-  const int n = blockIdx.x / p.slabs, slab = blockIdx.x % p.slabs;
+  constexpr int kParts = kChain ? X::kThreads / CW : 1;
+  __shared__ float lookA[kParts][CW], lookB[kParts][CW];
+  int unit = blockIdx.x, place = 0;
+  if constexpr (kChain) {
+    const int t = draw_ticket(p.ticket), units = p.N * p.slabs;
+    unit = t % units;
+    place = t / units;
+    if (place >= p.tiles) return;   // the grid's last row
+  }
+  const int n = unit / p.slabs, slab = unit % p.slabs;
   const int c0 = slab * CW + grp * V, avail = p.C - c0;
   const int len = seq_len(p.lengths, n, p.T);
   const char* gate = p.gate + ((long)n * p.bs + c0) * kBytes<IN>;
@@ -168,98 +336,133 @@ __global__ __launch_bounds__(kThreads) void k_scan_bwd(BwdArgs p) {
   const char* gy = p.gy + ((long)n * p.T * p.C + c0) * kBytes<IN>;
   char* ggate = p.ggate + ((long)n * p.gbs + c0) * kBytes<OUT>;
   char* gx = p.gx + ((long)n * p.gbs + c0) * kBytes<OUT>;
+  const int S = (p.T + kScanSpan - 1) / kScanSpan;
+  float first = 0.f;
   if (tid < CW) {
     const int c = slab * CW + tid;
-    carry[0][tid] = p.gh_last && c < p.C ? p.gh_last[(size_t)n * p.C + c] : 0.f;
+    if (place == 0) first = p.gh_last && c < p.C ? p.gh_last[(size_t)n * p.C + c] : 0.f;
+    if (!kChain) carry[tid] = first;
   }
-  int q = 0;
-  for (int tile = p.tiles - 1; tile >= 0; --tile, q ^= 1) {
-    const int t0 = tile * kBwdTile + slot * L;
-    Raw<kWords<IN, V>> g[L], x[L], d[L];
+  const int o = place, tile = p.tiles - 1 - o;   // the chain runs backwards in time
+  const int t0 = tile * kTile + slot * L;
+  Raw<kWords<IN, V>> g[L], x[L], d[L];
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const int have = t0 + i < len ? avail : 0;
-      g[i] = load_vec<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>, have);
-      x[i] = load_vec<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>, have);
-      d[i] = load_vec<IN, V>(gy + (long)(t0 + i) * p.C * kBytes<IN>, have);
-    }
-    // the state before the tile, kept by the forward
-    const Raw<V> st = load_vec<kF32, V>(
-        reinterpret_cast<const char*>(p.states + ((size_t)n * p.tiles + tile) * p.C + c0), avail);
-    float a[L][V], c[L][V], A[V], B[V], R[V];
+  for (int i = 0; i < L; ++i) {
+    const int have = t0 + i < len ? avail : 0;
+    g[i] = t0 + i < len ? load_vec<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>, avail) : hold_gate<IN, FORM, V>();
+    x[i] = load_vec<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>, have);
+    d[i] = load_vec<IN, V>(gy + (long)(t0 + i) * p.C * kBytes<IN>, have);
+  }
+  // the state before the tile, kept by the forward
+  const Raw<V> st = load_vec<kF32, V>(
+      reinterpret_cast<const char*>(p.states + ((size_t)n * S + tile * kTile / kScanSpan) * p.C + c0), avail);
+  float a[L][V], c[L][V], A[V], B[V], R[V];
 #pragma unroll
-    for (int k = 0; k < V; ++k) { A[k] = 1.f; B[k] = 0.f; R[k] = 0.f; }
+  for (int k = 0; k < V; ++k) { A[k] = 1.f; B[k] = 0.f; R[k] = 0.f; }
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        coefficients<IN, FORM>(elem<IN, V>(g[i], k), a[i][k], c[i][k]);
-        if (t0 + i >= len) { a[i][k] = 1.f; c[i][k] = 0.f; }   // x and grad_y read as zero there
-        A[k] *= a[i][k];
-        B[k] = __fmaf_rn(a[i][k], B[k], input_share<FORM>(c[i][k], elem<IN, V>(x[i], k)));
-      }
-#pragma unroll
-    for (int i = L - 1; i >= 0; --i)
-#pragma unroll
-      for (int k = 0; k < V; ++k) R[k] = a[i][k] * (elem<IN, V>(d[i], k) + R[k]);
-    float iA[V], iB[V], fA[V], fB[V], sA[V], sB[V];
-    wave_prefix<V>(A, B, lane, iA, iB, fA, fB);   // f: runs before this one
-    if (lane >= 64 - kGroups) {
-#pragma unroll
-      for (int k = 0; k < V; ++k) { totA[q][wave][grp * V + k] = iA[k]; totB[q][wave][grp * V + k] = iB[k]; }
-    }
-    wave_suffix<V>(A, R, lane, iA, iB, sA, sB);   // s: runs after it
-    if (lane < kGroups) {
-#pragma unroll
-      for (int k = 0; k < V; ++k) totR[q][wave][grp * V + k] = iB[k];
-    }
-    __syncthreads();
-    if (tid < CW) {
-      float r = carry[q][tid];
-#pragma unroll
-      for (int w = kWaves - 1; w >= 0; --w) r = __fmaf_rn(totA[q][w][tid], r, totR[q][w][tid]);
-      carry[q ^ 1][tid] = r;
-    }
-    float h[L][V], r[V];
+  for (int i = 0; i < L; ++i)
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const int ch = grp * V + k;
-      float hk = elem<kF32, V>(st, k);
-      for (int w = 0; w < wave; ++w) hk = __fmaf_rn(totA[q][w][ch], hk, totB[q][w][ch]);
-      h[0][k] = __fmaf_rn(fA[k], hk, fB[k]);
-      float rk = carry[q][ch];
-      for (int w = kWaves - 1; w > wave; --w) rk = __fmaf_rn(totA[q][w][ch], rk, totR[q][w][ch]);
-      r[k] = __fmaf_rn(sA[k], rk, sB[k]);
+      coefficients<IN, FORM>(elem<IN, V>(g[i], k), a[i][k], c[i][k]);
+      A[k] *= a[i][k];
+      B[k] = __fmaf_rn(a[i][k], B[k], input_share<FORM>(c[i][k], elem<IN, V>(x[i], k)));
     }
 #pragma unroll
-    for (int i = 0; i + 1 < L; ++i)
+  for (int i = L - 1; i >= 0; --i)
 #pragma unroll
-      for (int k = 0; k < V; ++k)
-        h[i + 1][k] = __fmaf_rn(a[i][k], h[i][k], input_share<FORM>(c[i][k], elem<IN, V>(x[i], k)));
+    for (int k = 0; k < V; ++k) R[k] = a[i][k] * (elem<IN, V>(d[i], k) + R[k]);
+  float iA[V], iB[V], fA[V], fB[V], sA[V], sB[V];
+  wave_prefix<V, kGroups>(A, B, lane, iA, iB, fA, fB);   // f: runs before this one
+  if (lane >= 64 - kGroups) {
 #pragma unroll
-    for (int i = L - 1; i >= 0; --i) {
-      float og[V], ox[V];
+    for (int k = 0; k < V; ++k) { totA[wave][grp * V + k] = iA[k]; totB[wave][grp * V + k] = iB[k]; }
+  }
+  wave_suffix<V, kGroups>(A, R, lane, iA, iB, sA, sB);   // s: runs after it
+  if (lane < kGroups) {
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const float delta = elem<IN, V>(d[i], k) + r[k];
-        if constexpr (FORM == kValue) {
-          og[k] = delta * h[i][k];
-          ox[k] = delta;
-        } else {
-          ox[k] = delta * c[i][k];
-          og[k] = ox[k] * a[i][k] * (h[i][k] - elem<IN, V>(x[i], k));
-        }
-        r[k] = a[i][k] * delta;
-        if (t0 + i >= len) og[k] = ox[k] = 0.f;
-      }
-      if (t0 + i < p.T) {
-        store_vec<OUT, V>(ggate + (long)(t0 + i) * p.grs * kBytes<OUT>, avail, og);
-        store_vec<OUT, V>(gx + (long)(t0 + i) * p.grs * kBytes<OUT>, avail, ox);
-      }
-    }
+    for (int k = 0; k < V; ++k) totR[wave][grp * V + k] = iB[k];
   }
   __syncthreads();
-  if (p.gh0 && tid < CW && slab * CW + tid < p.C) p.gh0[(size_t)n * p.C + slab * CW + tid] = carry[q][tid];
+  if constexpr (kChain) {
+    using Look = Lookback<X>;
+    const int ch = tid % CW, part = tid / CW;
+    const long chain = (long)unit * p.tiles * CW + ch, groups = (long)unit * p.groups * CW + ch;
+    float ta = 1.f, tz = 0.f, A, B;
+    if (tid < CW) {
+#pragma unroll
+      for (int w = kWaves - 1; w >= 0; --w) {
+        tz = __fmaf_rn(totA[w][ch], tz, totR[w][ch]);
+        ta *= totA[w][ch];
+      }
+      // tile 0 publishes a state (A = 0): only it reads the chain's start, whose
+      // memory the chain's end may be
+      if (place == 0) publish(p.agg + chain, __fmaf_rn(ta, first, tz), 0.f);
+      else publish(p.agg + chain + (long)o * CW, tz, ta);
+    }
+    Look::read(o, part, first, p.agg + chain, p.pre + groups, A, B);
+    lookA[part][ch] = A;
+    lookB[part][ch] = B;
+    __syncthreads();
+    if (tid < CW) {
+      float v = B;   // part 0 starts from the state itself
+#pragma unroll
+      for (int i = 1; i < kParts; ++i) v = __fmaf_rn(lookA[i][ch], v, lookB[i][ch]);
+      carry[ch] = v;
+      v = __fmaf_rn(ta, v, tz);
+      last[ch] = v;
+      if (o % kGroupTiles == kGroupTiles - 1 && o + 1 < p.tiles)
+        publish(p.pre + groups + (long)(o / kGroupTiles + 1) * CW, v, 0.f);
+    }
+    __syncthreads();
+  } else if (tid < CW) {
+    float r = first;
+#pragma unroll
+    for (int w = kWaves - 1; w >= 0; --w) r = __fmaf_rn(totA[w][tid], r, totR[w][tid]);
+    last[tid] = r;
+  }
+  float h[L][V], r[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    const int ch = grp * V + k;
+    float hk = elem<kF32, V>(st, k);
+    for (int w = 0; w < wave; ++w) hk = __fmaf_rn(totA[w][ch], hk, totB[w][ch]);
+    h[0][k] = __fmaf_rn(fA[k], hk, fB[k]);
+    float rk = carry[ch];
+    for (int w = kWaves - 1; w > wave; --w) rk = __fmaf_rn(totA[w][ch], rk, totR[w][ch]);
+    r[k] = __fmaf_rn(sA[k], rk, sB[k]);
+  }
+#pragma unroll
+  for (int i = 0; i + 1 < L; ++i)
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      h[i + 1][k] = __fmaf_rn(a[i][k], h[i][k], input_share<FORM>(c[i][k], elem<IN, V>(x[i], k)));
+#pragma unroll
+  for (int i = L - 1; i >= 0; --i) {
+    float og[V], ox[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const float delta = elem<IN, V>(d[i], k) + r[k];
+      if constexpr (FORM == kValue) {
+        og[k] = delta * h[i][k];
+        ox[k] = delta;
+      } else {
+        ox[k] = delta * c[i][k];
+        og[k] = ox[k] * a[i][k] * (h[i][k] - elem<IN, V>(x[i], k));
+      }
+      r[k] = a[i][k] * delta;
+    }
+    char *gat = ggate + (long)(t0 + i) * p.grs * kBytes<OUT>, *xat = gx + (long)(t0 + i) * p.grs * kBytes<OUT>;
+    if (t0 + i < len) {
+      store_vec<OUT, V>(gat, avail, og);
+      store_vec<OUT, V>(xat, avail, ox);
+    } else if (t0 + i < p.T) {
+      store_zero<OUT, V>(gat, avail);
+      store_zero<OUT, V>(xat, avail);
+    }
+  }
+  if (kChain && place + 1 < p.tiles) return;
+  __syncthreads();
+  if (p.gh0 && tid < CW && slab * CW + tid < p.C) p.gh0[(size_t)n * p.C + slab * CW + tid] = last[tid];
 }
 
 // One token for N sequences: state rows from one pool to another (or in place).
@@ -268,7 +471,7 @@ template <int IN, int FORM>
 __global__ __launch_bounds__(256) void k_scan_step(const char* gate, const char* x, long rs, const float* state,
                                                    float* state_out, const int* slots, char* y, int N, int C, int S,
                                                    int groups) {
-  constexpr int V = kV<IN>;
+  constexpr int V = 16 / kBytes<IN>;
   const long i = (long)blockIdx.x * 256 + threadIdx.x;
   const int n = (int)(i / groups), c0 = (int)(i % groups) * V;
   if (n >= N) return;
@@ -293,29 +496,107 @@ __global__ __launch_bounds__(256) void k_scan_step(const char* gate, const char*
   store_vec<IN, V>(y + ((long)n * C + c0) * kBytes<IN>, avail, h);
 }
 
-template <int IN, int OUT>
-hipError_t fwd_tokens(FwdArgs& p, int form, hipStream_t s) {
-  p.slabs = (p.C + kSlab<IN> - 1) / kSlab<IN>;
-  p.tiles = (p.T + kFwdTile - 1) / kFwdTile;
-  const dim3 grid((unsigned)(p.N * p.slabs));
-  if (form == kLogit) hipLaunchKernelGGL((k_scan_fwd<IN, OUT, kLogit>), grid, dim3(kThreads), 0, s, p);
-  else hipLaunchKernelGGL((k_scan_fwd<IN, OUT, kValue>), grid, dim3(kThreads), 0, s, p);
+// How a call on token sequences is divided, and its workspace: the ticket (in
+// 256 bytes of its own), a word per channel and tile, and one per channel and
+// group.
+struct Plan { int size, slab, slabs, tiles, groups; long words; };   // words > 0: chained
+constexpr long kTicketWords = 32;
+
+template <template <int, int> class Cuts>
+struct Tiles {
+  // the cut of a call, and the steps of its tile
+  static int size(int in_dt, int T) {
+    const bool b = in_dt == kBF16;
+    if (T <= (b ? Cuts<kBF16, 2>::type::kTile : Cuts<kF32, 2>::type::kTile)) return 2;
+    return T <= (b ? Cuts<kBF16, 1>::type::kTile : Cuts<kF32, 1>::type::kTile) ? 1 : 0;
+  }
+  static int steps(int in_dt) { return in_dt == kBF16 ? Cuts<kBF16, 0>::type::kTile : Cuts<kF32, 0>::type::kTile; }
+};
+
+Plan make_plan(bool bwd, int N, int T, int C, int in_dt) {
+  const int tile = bwd ? Tiles<BwdCuts>::steps(in_dt) : Tiles<FwdCuts>::steps(in_dt);
+  Plan q{};
+  q.size = bwd ? Tiles<BwdCuts>::size(in_dt, T) : Tiles<FwdCuts>::size(in_dt, T);
+  q.slab = 128 / (in_dt == kBF16 ? 2 : 4);   // all cuts alike
+  q.slabs = (C + q.slab - 1) / q.slab;
+  q.tiles = (T + tile - 1) / tile;
+  q.groups = (q.tiles + kGroupTiles - 1) / kGroupTiles;
+  q.words = q.tiles > 1 ? kTicketWords + (long)N * q.slabs * q.slab * ((long)q.tiles + q.groups) : 0;
+  return q;
+}
+
+// Grids of at most 2^32 threads along x; a chained block past the end has no
+// ticket to serve.  (One tile: at most 2^21 blocks, one row.)
+dim3 blocks(long n) {
+  const long x = std::min(n, 1L << 22);
+  return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
+}
+
+template <class Args>
+hipError_t start(Args& p, const Plan& q, void* ws, hipStream_t s) {
+  p.slabs = q.slabs;
+  p.tiles = q.tiles;
+  p.groups = q.groups;
+  if (q.words == 0) return hipSuccess;
+  unsigned long long* w = static_cast<unsigned long long*>(ws);
+  p.ticket = reinterpret_cast<unsigned*>(w);
+  p.agg = w + kTicketWords;
+  p.pre = p.agg + (long)p.N * p.slabs * q.tiles * q.slab;
+  hipLaunchKernelGGL(k_scan_clear, dim3((unsigned)((q.words / 2 + 256) / 256)), dim3(256), 0, s, w, q.words);
+  return hipGetLastError();
+}
+
+template <int IN, int OUT, int FORM>
+hipError_t fwd_form(FwdArgs& p, void* ws, hipStream_t s) {
+  const Plan q = make_plan(false, p.N, p.T, p.C, IN);
+  const hipError_t e = start(p, q, ws, s);
+  if (e != hipSuccess) return e;
+  auto go = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, blocks((long)p.N * p.slabs * p.tiles), dim3(threads), 0, s, p);
+  };
+  using X0 = FwdCut<IN, 0>;
+  using X1 = FwdCut<IN, 1>;
+  using X2 = FwdCut<IN, 2>;
+  if (q.words > 0) go(k_scan_fwd<X0, IN, OUT, FORM, true>, X0::kThreads);
+  else if (q.size == 0) go(k_scan_fwd<X0, IN, OUT, FORM, false>, X0::kThreads);
+  else if (q.size == 1) go(k_scan_fwd<X1, IN, OUT, FORM, false>, X1::kThreads);
+  else go(k_scan_fwd<X2, IN, OUT, FORM, false>, X2::kThreads);
   return hipGetLastError();
 }
 
 template <int IN, int OUT>
-hipError_t bwd_tokens(BwdArgs& p, int form, hipStream_t s) {
-  p.slabs = (p.C + kSlab<IN> - 1) / kSlab<IN>;
-  p.tiles = (p.T + kBwdTile - 1) / kBwdTile;
-  const dim3 grid((unsigned)(p.N * p.slabs));
-  if (form == kLogit) hipLaunchKernelGGL((k_scan_bwd<IN, OUT, kLogit>), grid, dim3(kThreads), 0, s, p);
-  else hipLaunchKernelGGL((k_scan_bwd<IN, OUT, kValue>), grid, dim3(kThreads), 0, s, p);
+hipError_t fwd_tokens(FwdArgs& p, int form, void* ws, hipStream_t s) {
+  return form == kLogit ? fwd_form<IN, OUT, kLogit>(p, ws, s) : fwd_form<IN, OUT, kValue>(p, ws, s);
+}
+
+template <int IN, int OUT, int FORM>
+hipError_t bwd_form(BwdArgs& p, void* ws, hipStream_t s) {
+  const Plan q = make_plan(true, p.N, p.T, p.C, IN);
+  const hipError_t e = start(p, q, ws, s);
+  if (e != hipSuccess) return e;
+  auto go = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, blocks((long)p.N * p.slabs * p.tiles), dim3(threads), 0, s, p);
+  };
+  using X0 = BwdCut<IN, 0>;
+  using X1 = BwdCut<IN, 1>;
+  using X2 = BwdCut<IN, 2>;
+  if (q.words > 0) go(k_scan_bwd<X0, IN, OUT, FORM, true>, X0::kThreads);
+  else if (q.size == 0) go(k_scan_bwd<X0, IN, OUT, FORM, false>, X0::kThreads);
+  else if (q.size == 1) go(k_scan_bwd<X1, IN, OUT, FORM, false>, X1::kThreads);
+  else go(k_scan_bwd<X2, IN, OUT, FORM, false>, X2::kThreads);
   return hipGetLastError();
+}
+
+template <int IN, int OUT>
+hipError_t bwd_tokens(BwdArgs& p, int form, void* ws, hipStream_t s) {
+  return form == kLogit ? bwd_form<IN, OUT, kLogit>(p, ws, s) : bwd_form<IN, OUT, kValue>(p, ws, s);
 }
 
 }  // namespace
 
-size_t scan_workspace_bytes(bool, int, int, int, int, bool) { return 0; }
+size_t scan_workspace_bytes(bool bwd, int N, int T, int C, int in_dt, bool maps) {
+  return maps ? 0 : (size_t)make_plan(bwd, N, T, C, in_dt).words * 8;
+}
 
 hipError_t launch_scan_fwd(const ScanFwd& f, hipStream_t s) {
   FwdArgs p{};
@@ -332,8 +613,8 @@ hipError_t launch_scan_fwd(const ScanFwd& f, hipStream_t s) {
   p.T = f.T;
   p.C = f.C;
   if (f.maps) return launch_scan_fwd_maps(p, f.in_dt, f.out_dt, f.form, s);
-  if (f.in_dt == kBF16) return fwd_tokens<kBF16, kBF16>(p, f.form, s);
-  return f.out_dt == kBF16 ? fwd_tokens<kF32, kBF16>(p, f.form, s) : fwd_tokens<kF32, kF32>(p, f.form, s);
+  if (f.in_dt == kBF16) return fwd_tokens<kBF16, kBF16>(p, f.form, f.ws, s);
+  return f.out_dt == kBF16 ? fwd_tokens<kF32, kBF16>(p, f.form, f.ws, s) : fwd_tokens<kF32, kF32>(p, f.form, f.ws, s);
 }
 
 hipError_t launch_scan_bwd(const ScanBwd& f, hipStream_t s) {
@@ -355,13 +636,13 @@ hipError_t launch_scan_bwd(const ScanBwd& f, hipStream_t s) {
   p.T = f.T;
   p.C = f.C;
   if (f.maps) return launch_scan_bwd_maps(p, f.in_dt, f.out_dt, f.form, s);
-  if (f.in_dt == kBF16) return bwd_tokens<kBF16, kBF16>(p, f.form, s);
-  return f.out_dt == kBF16 ? bwd_tokens<kF32, kBF16>(p, f.form, s) : bwd_tokens<kF32, kF32>(p, f.form, s);
+  if (f.in_dt == kBF16) return bwd_tokens<kBF16, kBF16>(p, f.form, f.ws, s);
+  return f.out_dt == kBF16 ? bwd_tokens<kF32, kBF16>(p, f.form, f.ws, s) : bwd_tokens<kF32, kF32>(p, f.form, f.ws, s);
 }
 
 hipError_t launch_scan_step(const void* gate, const void* x, long rs, int dt, const float* state, float* state_out,
                             const int* slots, void* y, int N, int C, int S, int form, hipStream_t s) {
-  const int V = dt == kBF16 ? kV<kBF16> : kV<kF32>, groups = (C + V - 1) / V;
+  const int V = dt == kBF16 ? 8 : 4, groups = (C + V - 1) / V;
   const dim3 grid((unsigned)(((long)N * groups + 255) / 256));
   const char *g = static_cast<const char*>(gate), *xp = static_cast<const char*>(x);
   char* yp = static_cast<char*>(y);

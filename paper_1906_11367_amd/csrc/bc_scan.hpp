@@ -90,6 +90,23 @@ __device__ __forceinline__ void store_vec(char* p, int avail, const float (&v)[V
   }
 }
 
+template <int DT, int V>
+__device__ __forceinline__ void store_zero(char* p, int avail) {
+  const float z[V] = {};
+  store_vec<DT, V>(p, avail, z);
+}
+
+// Gates of steps past a sequence's end: a = 1 exactly (and c = 0 in the logit
+// form; the input reads as zero there), so that the state stays as it is.
+template <int DT, int FORM, int V>
+__device__ __forceinline__ Raw<kWords<DT, V>> hold_gate() {
+  constexpr uint32_t bits = FORM == kValue ? 0x3f800000u : 0x7f800000u;   // 1, or infinity
+  Raw<kWords<DT, V>> r;
+#pragma unroll
+  for (int k = 0; k < kWords<DT, V>; ++k) r[k] = DT == kBF16 ? bits | bits >> 16 : bits;
+  return r;
+}
+
 // exp(-v), v >= 0.  fp32 storage: the rounding of v / ln 2, which would grow
 // with v, is put back to first order.
 template <int DT>
@@ -113,8 +130,7 @@ __device__ __forceinline__ void coefficients(float gate, float& a, float& c) {
     const float e = exp_neg<DT>(fabsf(gate));
     const float r = __builtin_amdgcn_rcpf(1.f + e), er = e * r;
     a = gate >= 0.f ? r : er;
-    c = gate >= 0.f ? er : r;
-    if (gate != gate) a = c = gate;
+    c = gate >= 0.f ? er : r;   // a NaN is in r and er already
   }
 }
 
@@ -131,7 +147,7 @@ struct FwdArgs {
   float* h_last;            // [N][C] or null
   float* states;            // or null
   int N, T, C;
-  int slabs, tiles;         // tokens: channel slabs, tiles of time steps
+  int slabs, tiles, groups;   // tokens: channel slabs, tiles of time steps, groups of tiles
   unsigned* ticket;         // chained: see bc_scan.hip
   unsigned long long *agg, *pre;
 };
@@ -147,7 +163,7 @@ struct BwdArgs {
   long gbs, grs;            // strides of ggate and gx
   float* gh0;               // [N][C] or null
   int N, T, C;
-  int slabs, tiles;
+  int slabs, tiles, groups;
   unsigned* ticket;
   unsigned long long *agg, *pre;
 };

@@ -36,7 +36,8 @@ MIX = dict(wq=P16, ws=P16, x=P16, x_dt=bc.BC_F32, bs=40, rs=8, x_scale=None, bia
 
 COMMON = [(dict(gate=None), NULL), (dict(x=None), NULL), (dict(N=0), SHAPE), (dict(T=0), SHAPE), (dict(C=0), SHAPE),
           (dict(N=-1), SHAPE), (dict(T=(1 << 30) + 1), SHAPE), (dict(C=65537, rs=65537, bs=1 << 40), SHAPE),
-          (dict(N=65536, C=1024, rs=1024, bs=1 << 30), SHAPE), (dict(rs=7), SHAPE), (dict(bs=39), SHAPE),
+          (dict(N=65536, C=1024, rs=1024, bs=1 << 30, layout=1), SHAPE),
+          (dict(N=65536, T=1 << 24, C=64, rs=64, bs=1 << 40), SHAPE), (dict(rs=7), SHAPE), (dict(bs=39), SHAPE),
           (dict(rs=-8), SHAPE), (dict(bs=-40), SHAPE), (dict(bs=1 << 62), SHAPE), (dict(rs=1 << 62), SHAPE),
           (dict(dt=bc.BC_I32), DTYPE), (dict(dt=bc.BC_I8), DTYPE), (dict(dt=9), DTYPE), (dict(form=2), UNSUPPORTED),
           (dict(form=-1), UNSUPPORTED), (dict(layout=2), UNSUPPORTED), (dict(gate=P4), ALIGN), (dict(x=P4), ALIGN),
