@@ -1,11 +1,15 @@
 // The 1x1 mix of 8-bit codes (gfx950): out = (codes of a token . codes of a
 // weight row) * token scale * weight scale + bias, the product exact in int32.
 // Both operands are rows contiguous along the reduction, padded with zeros to
-// whole 128 bytes; rows i of one and rows j of the other give out(i, j), with
-// the index that is contiguous in the output as j: tokens [T][M] take i =
-// token, j = weight row, maps [N][M][P] the reverse.
+// whole 128 bytes; rows i of one and rows j of the other give out(i, j), i the
+// index that is contiguous in the output: tokens [T][M] take i = weight row,
+// j = token, maps [N][M][P] the reverse.
 #include "bc_internal.hpp"
 #include "bc_scan.hpp"
+
+#include <math.h>
+
+#include <algorithm>
 
 namespace bc {
 namespace {
@@ -21,18 +25,20 @@ struct Args {
   const float* bias;          // of the weight rows, or null
   char* out;
   int I, J;                   // rows of a and of b
-  int pitch, M, P, relu;
+  int pitch, M, P;
+  float floor;                // 0 with relu, else -infinity
 };
 
-// out(i, j) of a 32-bit sum.
-template <int OUT, bool kMaps>
-__device__ __forceinline__ void store_out(const Args& p, int i, int j, int sum, float si, float sj, float bi, float bj) {
-  float z = kMaps ? (float)sum * sj * si : (float)sum * si * sj;   // token scale first
-  if (p.bias) z += kMaps ? bi : bj;
-  if (p.relu) z = z > 0.f || z != z ? z : 0.f;
-  const long at = kMaps ? ((long)(j / p.P) * p.M + i) * p.P + j % p.P : (long)i * p.M + j;
-  if constexpr (OUT == kBF16) reinterpret_cast<uint16_t*>(p.out)[at] = (uint16_t)pair_bf16(z, 0.f);
-  else reinterpret_cast<float*>(p.out)[at] = z;
+// Where out(i, j) stands, in elements.
+template <bool kMaps>
+__device__ __forceinline__ long out_at(const Args& p, int i, int j) {
+  if constexpr (kMaps) return ((long)(i / p.P) * p.M + j) * p.P + i % p.P;
+  else return (long)j * p.M + i;
+}
+
+__device__ __forceinline__ float finish(int sum, float token, float weight, float bias, float floor) {
+  const float z = __fmaf_rn((float)sum * token, weight, bias);
+  return z < floor ? floor : z;   // a NaN stays
 }
 
 #define BC_LDS __attribute__((address_space(3)))
@@ -130,48 +136,124 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_mix_i8_tile(Args p, int ti, in
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[x][y][r] = 0;
 
-  for (int s = 0; s < kStages - 1 && s < nk; ++s) issue();
-  int slot = 0;
-  for (int s = 0; s < nk; ++s) {
-    if (s + kStages - 2 < nk) wait_loads<kLoads * (kStages - 2)>();
-    else wait_loads<0>();
-    __builtin_amdgcn_s_barrier();
-    if (load_k < nk) issue();
-    const uint32_t st = lds0 + slot * kStage;
+  // A stage is two halves of 32 codes.  The operands of a half are read from
+  // LDS during the half before, across the barrier too, which stands between
+  // the halves: no wave then starts a stage by waiting for its reads.
+  i32x4_t fa[2][FI], fb[2][FJ];
+  auto read = [&](int half, uint32_t st) {
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      i32x4_t af[FI], bf[FJ];
+    for (int x = 0; x < FI; ++x) fa[half][x] = *(BC_LDS i32x4_t*)(uintptr_t)(st + aoff[half] + x * 32 * kBK);
 #pragma unroll
-      for (int x = 0; x < FI; ++x) af[x] = *(BC_LDS i32x4_t*)(uintptr_t)(st + aoff[kk] + x * 32 * kBK);
-#pragma unroll
-      for (int y = 0; y < FJ; ++y) bf[y] = *(BC_LDS i32x4_t*)(uintptr_t)(st + boff[kk] + y * 32 * kBK);
-#pragma unroll
-      for (int x = 0; x < FI; ++x)
-#pragma unroll
-        for (int y = 0; y < FJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_32x32x32_i8(af[x], bf[y], acc[x][y], 0, 0, 0);
-    }
-    slot = slot + 1 == kStages ? 0 : slot + 1;
-  }
-
-  const int ib = i0 + wi * FI * 32 + 4 * (lane >> 5), jb = j0 + wj * FJ * 32 + (lane & 31);
-#pragma unroll
-  for (int y = 0; y < FJ; ++y) {
-    const int j = jb + 32 * y;
-    if (j >= p.J) continue;
-    const float sj = p.bscale[j], bj = p.bias && !kMaps ? p.bias[j] : 0.f;
+    for (int y = 0; y < FJ; ++y) fb[half][y] = *(BC_LDS i32x4_t*)(uintptr_t)(st + boff[half] + y * 32 * kBK);
+  };
+  auto multiply = [&](int half) {
 #pragma unroll
     for (int x = 0; x < FI; ++x)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int i = ib + 32 * x + 8 * (r >> 2) + (r & 3);
-        if (i < p.I) store_out<OUT, kMaps>(p, i, j, acc[x][y][r], p.ascale[i], sj, p.bias && kMaps ? p.bias[i] : 0.f, bj);
+      for (int y = 0; y < FJ; ++y)
+        acc[x][y] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[half][x], fb[half][y], acc[x][y], 0, 0, 0);
+  };
+  // the reads spread over the matrix instructions
+  auto interleave = [&]() {
+#pragma unroll
+    for (int k = 0; k < (FI * FJ > FI + FJ ? FI * FJ : FI + FJ); ++k) {
+      if (k < FI * FJ) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (k < FI + FJ) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+  };
+  for (int s = 0; s < kStages - 1 && s < nk; ++s) issue();
+  if (nk >= kStages - 1) wait_loads<kLoads * (kStages - 2)>();
+  else wait_loads<0>();
+  __builtin_amdgcn_s_barrier();
+  read(0, lds0);
+  int slot = 0;
+  for (int s = 0; s < nk; ++s) {
+    const uint32_t st = lds0 + slot * kStage;
+    __builtin_amdgcn_sched_barrier(0);
+    read(1, st);
+    multiply(0);
+    interleave();
+    __builtin_amdgcn_sched_barrier(0);
+    // the next stage's loads are done when at most the later ones' are pending
+    if (s + kStages - 2 < nk) wait_loads<kLoads * (kStages - 3)>();
+    else wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    if (load_k < nk) issue();
+    slot = slot + 1 == kStages ? 0 : slot + 1;
+    read(0, lds0 + slot * kStage);   // past the last stage: never used
+    multiply(1);
+    interleave();
+  }
+  __builtin_amdgcn_sched_barrier(0);
+
+  // Outputs.  A lane holds, of column j = lane % 32 of a block, rows 8 (r / 4) +
+  // 4 (lane / 32) + r % 4: four consecutive i at a time.  They go through the
+  // wave's own part of LDS, 32 columns j at a time, to be stored 16 bytes a lane
+  // along i.
+  constexpr int kE = kBytes<OUT>, kWide = 16 / kE, kRow = FI * 32 * kE + 16;   // + 16: lanes hit distinct banks
+  const int ib = i0 + wi * FI * 32, jb = j0 + wj * FJ * 32;
+  const uint32_t mine = lds0 + wave * 32 * kRow;
+  float* iscale = reinterpret_cast<float*>(smem + kWaves * 32 * kRow);   // and the biases after the scales
+  __syncthreads();   // the stages are read
+  for (int i = threadIdx.x; i < BI; i += 64 * kWaves) {
+    const int at = min(i0 + i, p.I - 1);
+    iscale[i] = p.ascale[at];
+    iscale[BI + i] = !kMaps && p.bias ? p.bias[at] : 0.f;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int y = 0; y < FJ; ++y) {
+    const int j = min(jb + 32 * y + (lane & 31), p.J - 1);
+    const float sj = p.bscale[j], bj = kMaps && p.bias ? p.bias[j] : 0.f;
+#pragma unroll
+    for (int x = 0; x < FI; ++x)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float* si = iscale + wi * FI * 32 + 32 * x + 8 * g + 4 * (lane >> 5);
+        float z[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          z[k] = kMaps ? finish(acc[x][y][4 * g + k], si[k], sj, bj, p.floor)
+                       : finish(acc[x][y][4 * g + k], sj, si[k], si[BI + k], p.floor);
+        const uint32_t at = mine + (lane & 31) * kRow + (32 * x + 8 * g + 4 * (lane >> 5)) * kE;
+        if constexpr (OUT == kBF16) {
+          const Raw<2> w = {pair_bf16(z[0], z[1]), pair_bf16(z[2], z[3])};
+          *(BC_LDS Raw<2>*)(uintptr_t)at = w;
+        } else {
+          const Raw<4> w = {__float_as_uint(z[0]), __float_as_uint(z[1]), __float_as_uint(z[2]), __float_as_uint(z[3])};
+          *(BC_LDS Raw<4>*)(uintptr_t)at = w;
+        }
       }
+    constexpr int kChunks = FI * 32 / kWide;   // 16-byte chunks of a column j
+    static_assert(32 * kChunks % 64 == 0, "whole waves of chunks");
+#pragma unroll
+    for (int c0 = 0; c0 < 32 * kChunks; c0 += 64) {
+      const int c = c0 + lane, jj = c / kChunks, ii = c % kChunks * kWide;
+      const Raw<4> w = *(BC_LDS Raw<4>*)(uintptr_t)(mine + jj * kRow + ii * kE);
+      const int i = ib + ii, jo = jb + 32 * y + jj;
+      if (i >= p.I || jo >= p.J) continue;
+      char* o = p.out + out_at<kMaps>(p, i, jo) * kE;
+      const int left = kMaps ? min(p.I - i, p.P - i % p.P) : p.I - i;   // elements contiguous from here
+      if (left >= kWide) {
+        *reinterpret_cast<Loose<4, kE>*>(o) = __builtin_bit_cast(Loose<4, kE>, w);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kWide; ++k) {
+          if (i + k >= p.I) break;
+          char* e = p.out + out_at<kMaps>(p, i + k, jo) * kE;
+          if constexpr (OUT == kBF16) *reinterpret_cast<uint16_t*>(e) = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
+          else *reinterpret_cast<uint32_t*>(e) = w[k];
+        }
+      }
+    }
   }
 }
 
 template <int OUT, bool kMaps, int WI, int WJ, int FI, int FJ, int kStages>
 hipError_t launch_tile(const Args& p, hipStream_t s) {
-  constexpr int BI = WI * FI * 32, BJ = WJ * FJ * 32, kLds = kStages * (BI + BJ) * kBK;
+  constexpr int BI = WI * FI * 32, BJ = WJ * FJ * 32;
+  constexpr int kLds = std::max(kStages * (BI + BJ) * kBK, WI * WJ * 32 * (FI * 32 * kBytes<OUT> + 16) + BI * 8);
   const auto kernel = k_mix_i8_tile<OUT, kMaps, WI, WJ, FI, FJ, kStages>;
   const int ti = (p.I + BI - 1) / BI, tj = (p.J + BJ - 1) / BJ, per = (ti * tj + 7) / 8;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(per * 8)), dim3(64 * WI * WJ), kLds, s, p, ti, tj, per);
@@ -216,14 +298,14 @@ hipError_t launch_mix_i8(const MixI8& m, hipStream_t s) {
   p.pitch = i8_pitch(m.K);
   p.M = m.M;
   p.P = m.P;
-  p.relu = m.relu;
+  p.floor = m.relu ? 0.f : -INFINITY;
   if (m.maps) {
-    p.a = w; p.ascale = m.wscale; p.I = m.M;
-    p.b = x; p.bscale = xscale; p.J = (int)rows;
+    p.a = x; p.ascale = xscale; p.I = (int)rows;
+    p.b = w; p.bscale = m.wscale; p.J = m.M;
     return m.out_dt == kBF16 ? launch<kBF16, true>(p, s) : launch<kF32, true>(p, s);
   }
-  p.a = x; p.ascale = xscale; p.I = (int)rows;
-  p.b = w; p.bscale = m.wscale; p.J = m.M;
+  p.a = w; p.ascale = m.wscale; p.I = m.M;
+  p.b = x; p.bscale = xscale; p.J = (int)rows;
   return m.out_dt == kBF16 ? launch<kBF16, false>(p, s) : launch<kF32, false>(p, s);
 }
 
