@@ -1,0 +1,151 @@
+// Shared device code of the 8-bit codes (gfx950): for K values x of one token
+// (or of one weight row), with m = max |x|,
+//   scale = m / 127,  q = round to nearest even(x * (127 / m)),
+// in fp32, all zero where m < 2^-100 (127 / m would leave fp32's range); a row
+// with a NaN or an infinity gets zero codes and a NaN scale, so that every
+// output made from it is NaN.
+#pragma once
+#include "bc_internal.hpp"
+#include "bc_scan.hpp"   // load_vec, elem
+
+namespace bc {
+namespace i8 {
+
+using namespace scan;
+
+#define BC_LDS __attribute__((address_space(3)))
+
+struct RowScale { float inv, scale; };
+
+// top: the largest |x| of the row as bits (a NaN's are above infinity's).
+__device__ __forceinline__ RowScale row_scale(uint32_t top) {
+  const float m = __uint_as_float(top);
+  if (top >= 0x7f800000u) return {0.f, __uint_as_float(0x7fc00000u)};
+  if (m < 0x1p-100f) return {0.f, 0.f};
+  return {127.f / m, m / 127.f};
+}
+
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Four codes in a word.  Adding 1.5 * 2^23 to the rounded product rounds it to
+// the nearest even integer and leaves that in the low byte; inv = 0 (a row
+// without codes, whatever it holds) gives zeros.
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
+#pragma clang fp contract(off)   // the product is rounded before the sum
+  constexpr float kMagic = 12582912.f;
+  const uint32_t qa = __float_as_uint(a * inv + kMagic), qb = __float_as_uint(b * inv + kMagic);
+  const uint32_t qc = __float_as_uint(c * inv + kMagic), qd = __float_as_uint(d * inv + kMagic);
+  const uint32_t lo = __builtin_amdgcn_perm(qb, qa, 0x0c0c0400u), hi = __builtin_amdgcn_perm(qd, qc, 0x04000c0cu);
+  return inv == 0.f ? 0u : lo | hi;
+}
+
+// A tile of maps [K][P]: 64 pixels by all K channels, by a block of 512
+// threads.  A lane has 8 pixels (pg = lane % 8) of 4 consecutive channels
+// (group kg, 64 groups in the block) at a time: loads are whole 128-byte lines
+// (bf16), and four codes of a pixel make a word.
+constexpr int kTileP = 64, kTileThreads = 512, kStepK = 256;
+
+// The codes of pixel p stand in LDS as a row of `pitch` bytes (a multiple of
+// 256), its 16-byte chunk c at c ^ chunk_swap(p): 16 pixels' reads of one
+// chunk, and a wave's writes, then hit all banks.
+__device__ __forceinline__ int chunk_swap(int p) { return (((p ^ (p >> 3)) & 7) << 1) | ((p >> 3) & 1); }
+
+// The lane's 8 pixels of channel k.  kFull: all 8 exist.
+template <int DT, bool kFull>
+__device__ __forceinline__ Raw<kWords<DT, 8>> tile_load(const char* base, long rs, int avail, int k, int K) {
+  const char* p = base + (long)k * rs * kBytes<DT>;
+  if constexpr (kFull) {
+    Raw<kWords<DT, 8>> r = {};
+    if (k < K) r = __builtin_bit_cast(Raw<kWords<DT, 8>>, *reinterpret_cast<const Loose<kWords<DT, 8>, kBytes<DT>>*>(p));
+    return r;
+  } else {
+    return load_vec<DT, 8>(p, k < K ? avail : 0);
+  }
+}
+
+// Row scales of the tile.  base: the lane's pixels at channel 0 (`avail` of the
+// 8 exist), rs elements between channels.  The first kHold steps of 256
+// channels stay in registers (x); later ones are read again for their codes.
+// tops: 8 x 64 words of LDS, rows: 64 RowScales of LDS, whole after the call.
+template <int DT, int kHold, bool kFull>
+__device__ __forceinline__ void tile_scales(const char* base, long rs, int avail, int K,
+                                            Raw<kWords<DT, 8>> (&x)[kHold + 1][4], uint32_t* tops, RowScale* rows) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kg = tid >> 3;
+#pragma unroll
+  for (int s = 0; s < kHold; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[s][i] = tile_load<DT, kFull>(base, rs, avail, s * kStepK + kg * 4 + i, K);
+  uint32_t top[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top[j] = 0;
+#pragma unroll
+  for (int s = 0; s < kHold; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top[j] = max(top[j], abs_bits(elem<DT, 8>(x[s][i], j)));
+  for (int s = kHold; s * kStepK < K; ++s) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[kHold][i] = tile_load<DT, kFull>(base, rs, avail, s * kStepK + kg * 4 + i, K);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top[j] = max(top[j], abs_bits(elem<DT, 8>(x[kHold][i], j)));
+  }
+#pragma unroll
+  for (int d = 8; d < 64; d *= 2)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], d));
+  if (lane < 8) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) tops[wave * kTileP + lane * 8 + j] = top[j];
+  }
+  __syncthreads();
+  if (tid < kTileP) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int w = 0; w < kTileThreads / 64; ++w) m = max(m, tops[w * kTileP + tid]);
+    rows[tid] = row_scale(m);
+  }
+  __syncthreads();
+}
+
+// Codes of channels [s0 * 256, s1 * 256) into LDS at `lds` (channel s0 * 256
+// first), for the rows scaled above.
+template <int DT, int kHold, bool kFull>
+__device__ __forceinline__ void tile_codes(const char* base, long rs, int avail, int K,
+                                           Raw<kWords<DT, 8>> (&x)[kHold + 1][4], const RowScale* rows, uint32_t lds,
+                                           int pitch, int s0, int s1) {
+  const int lane = threadIdx.x & 63, kg = threadIdx.x >> 3, p0 = (lane & 7) * 8;
+  float inv[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) inv[j] = rows[p0 + j].inv;
+  auto put = [&](int s, const Raw<kWords<DT, 8>> (&y)[4]) {
+    const int k = (s - s0) * kStepK + kg * 4;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t w = codes4(elem<DT, 8>(y[0], j), elem<DT, 8>(y[1], j), elem<DT, 8>(y[2], j), elem<DT, 8>(y[3], j), inv[j]);
+      const int p = p0 + j;
+      *(BC_LDS uint32_t*)(uintptr_t)(lds + p * pitch + (((k >> 4) ^ chunk_swap(p)) << 4) + (k & 15)) = w;
+    }
+  };
+  // the words stay as loaded: unpacked values are not kept from the scales on
+#pragma unroll
+  for (int s = 0; s < kHold; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm("" : "+v"(x[s][i]));
+#pragma unroll
+  for (int s = 0; s < kHold; ++s)
+    if (s >= s0 && s < s1) put(s, x[s]);
+  for (int s = max(s0, kHold); s < s1; ++s) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[kHold][i] = tile_load<DT, kFull>(base, rs, avail, s * kStepK + kg * 4 + i, K);
+    put(s, x[kHold]);
+  }
+}
+
+// Steps held in registers: 16 words of x a step in bf16, 32 in fp32.
+template <int DT> constexpr int kHeld = DT == kBF16 ? 4 : 2;
+
+}  // namespace i8
+}  // namespace bc

@@ -203,6 +203,11 @@ struct MixI8 {
   void* ws;
 };
 hipError_t launch_mix_i8(const MixI8& m, hipStream_t s);
+// Maps that are not codes yet, in one pass (bc_mix_i8_maps.hip): whether it
+// takes the request, its workspace, and the launch.
+bool mix_i8_maps_takes(int K);
+size_t mix_i8_maps_workspace_bytes(int N, int M, int K, int P);
+hipError_t launch_mix_i8_maps(const MixI8& m, hipStream_t s);
 size_t mix_i8_workspace_bytes(int N, int M, int K, int P, int dt, bool maps);
 
 }  // namespace bc

@@ -1,0 +1,167 @@
+// The 1x1 mix in 8-bit codes on maps [N][K][P], codes and product in one pass
+// (gfx950; bc_i8.hpp has the codes' definition).
+//
+// Bound by memory: maps in, maps out, and little arithmetic for them (M is a
+// few hundred).  A block takes 64 pixels of one image by all K channels: it
+// reads them once, keeping them in registers until the pixels' scales are
+// known, turns the codes through LDS into the rows that the matrix
+// instructions read, and multiplies them with all M weight rows, which come
+// from the XCD's L2.  The codes never go to memory.
+#include "bc_i8.hpp"
+
+#include <math.h>
+
+namespace bc {
+namespace {
+
+using namespace i8;
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x16_t __attribute__((ext_vector_type(16)));
+
+struct Args {
+  const char* x;
+  long bs, rs;
+  const int8_t* w;
+  const float *wscale, *bias;
+  char* out;
+  int M, K, P, pitch, strips, steps, packed;
+  float floor;
+};
+
+template <int DT, int OUT, int kHold, bool kFull>
+__device__ __forceinline__ void mix_tile(const Args& p, int n, int pt, uint32_t lds, uint32_t* tops, RowScale* rows) {
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int p0 = pt + (tid & 7) * 8, lp = p.steps * kStepK;
+  const char* base = p.x + ((long)n * p.bs + p0) * kBytes<DT>;
+  {
+    Raw<kWords<DT, 8>> x[kHold + 1][4];
+    tile_scales<DT, kHold, kFull>(base, p.rs, p.P - p0, p.K, x, tops, rows);
+    tile_codes<DT, kHold, kFull>(base, p.rs, p.P - p0, p.K, x, rows, lds, lp, 0, p.steps);
+  }
+  __syncthreads();
+  // a wave: 32 weight rows by the 64 pixels.  Lane l of matrix instruction t of
+  // a block of 128 codes has chunk 2 t + l / 32 of row l % 32.
+  const int pa = lane & 31, swap[2] = {chunk_swap(pa), chunk_swap(pa + 32)}, blocks = p.pitch / 128;
+  for (int m0 = wave * 32; m0 < p.M; m0 += kTileThreads / 64 * 32) {
+    const int8_t* w = p.packed ? p.w + (long)m0 * p.pitch + lane * 16
+                               : p.w + (long)min(m0 + pa, p.M - 1) * p.pitch + half * 16;
+    const int wt = p.packed ? 1024 : 32, wk = 4 * wt;   // bytes from one t to the next, from a block to the next
+    i32x16_t acc[2];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[0][r] = acc[1][r] = 0;
+    i32x4_t b[4], next[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) b[t] = *reinterpret_cast<const i32x4_t*>(w + t * wt);
+    for (int k = 0; k < blocks; ++k) {
+      if (k + 1 < blocks) w += wk;   // the last block again: never used
+#pragma unroll
+      for (int t = 0; t < 4; ++t) next[t] = *reinterpret_cast<const i32x4_t*>(w + t * wt);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int c = k * 8 + 2 * t + half;
+          const i32x4_t a = *(BC_LDS i32x4_t*)(uintptr_t)(lds + (pa + 32 * x) * lp + ((c ^ swap[x]) << 4));
+          acc[x] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[t], a, acc[x], 0, 0, 0);
+        }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) b[t] = next[t];
+    }
+    // element r of a lane: weight row 8 (r / 4) + 4 half + r % 4, pixel lane %
+    // 32 of its block: a store writes a row's 32 pixels in one run
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int mr = m0 + 8 * (r >> 2) + 4 * half + (r & 3);
+      if (mr >= p.M) continue;
+      const float sw = p.wscale[mr], bias = p.bias ? p.bias[mr] : 0.f;
+      char* o = p.out + (((long)n * p.M + mr) * p.P + pt + pa) * kBytes<OUT>;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const float v = __fmaf_rn((float)acc[x][r] * rows[pa + 32 * x].scale, sw, bias);
+        const float z = v < p.floor ? p.floor : v;   // a NaN stays
+        if (!kFull && pt + pa + 32 * x >= p.P) continue;
+        if constexpr (OUT == kBF16) __builtin_nontemporal_store((uint16_t)pair_bf16(z, 0.f), reinterpret_cast<uint16_t*>(o) + 32 * x);
+        else __builtin_nontemporal_store(z, reinterpret_cast<float*>(o) + 32 * x);
+      }
+    }
+  }
+}
+
+template <int DT, int OUT>
+__global__ __launch_bounds__(kTileThreads, 4) void k_mix_i8_maps(Args p) {
+  extern __shared__ __align__(16) unsigned char smem[];   // codes of 64 pixels
+  __shared__ uint32_t tops[kTileThreads / 64 * kTileP];
+  __shared__ RowScale rows[kTileP];
+  const int n = blockIdx.x / p.strips, pt = (blockIdx.x % p.strips) * kTileP;
+  const uint32_t lds = (uint32_t)(uintptr_t)(BC_LDS unsigned char*)smem;
+  if (p.P - pt >= kTileP) mix_tile<DT, OUT, kHeld<DT>, true>(p, n, pt, lds, tops, rows);
+  else mix_tile<DT, OUT, kHeld<DT>, false>(p, n, pt, lds, tops, rows);
+}
+
+// Weight rows in the order in which the waves read them: 32 rows by 128 codes at
+// a time, 4 matrix instructions, 64 lanes, 16 bytes.  A wave's load is then 1
+// KiB in one piece, where rows as they are cost it 32 cache lines.
+__global__ __launch_bounds__(256) void k_pack_rows(const int8_t* w, i32x4_t* out, int M, int pitch, long chunks) {
+  const long i = (long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= chunks) return;
+  const int lane = (int)(i & 63), t = (int)(i >> 6) & 3;
+  const long block = i >> 8;   // of 32 x 128 codes
+  const int per = pitch / 128, m = min((int)(block / per) * 32 + (lane & 31), M - 1);
+  const int k = (int)(block % per) * 128 + (2 * t + (lane >> 5)) * 16;
+  out[i] = *reinterpret_cast<const i32x4_t*>(w + (long)m * pitch + k);
+}
+
+// Blocks from which the packing's launch pays (32 images of 1024 x 64 x 64 to
+// 256 maps: 124 us without, 95 + 5 with; 64 blocks 33 and 32).
+constexpr long kPackBlocks = 32;
+long strips_of(int N, int P) { return (long)N * ((P + kTileP - 1) / kTileP); }
+
+constexpr size_t kLdsBytes = 128 * 1024;   // of codes: K up to 2048
+
+}  // namespace
+
+bool mix_i8_maps_takes(int K) {
+  return (size_t)kTileP * ((i8_pitch(K) + kStepK - 1) / kStepK * kStepK) <= kLdsBytes;
+}
+
+size_t mix_i8_maps_workspace_bytes(int N, int M, int K, int P) {
+  return strips_of(N, P) < kPackBlocks ? 0 : (size_t)(M + 31) / 32 * 32 * i8_pitch(K);
+}
+
+hipError_t launch_mix_i8_maps(const MixI8& m, hipStream_t s) {
+  Args p{};
+  p.x = static_cast<const char*>(m.x);
+  p.bs = m.bs;
+  p.rs = m.rs;
+  p.w = static_cast<const int8_t*>(m.wq);
+  p.wscale = m.wscale;
+  p.bias = m.bias;
+  p.out = static_cast<char*>(m.out);
+  p.M = m.M;
+  p.K = m.K;
+  p.P = m.P;
+  p.pitch = i8_pitch(m.K);
+  p.strips = (m.P + kTileP - 1) / kTileP;
+  p.steps = (p.pitch + kStepK - 1) / kStepK;
+  p.floor = m.relu ? 0.f : -INFINITY;
+  const size_t packed = mix_i8_maps_workspace_bytes(m.N, m.M, m.K, m.P);
+  if (packed > 0) {
+    const long chunks = (long)packed / 16;
+    hipLaunchKernelGGL(k_pack_rows, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, p.w,
+                       static_cast<i32x4_t*>(m.ws), p.M, p.pitch, chunks);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    p.w = static_cast<const int8_t*>(m.ws);
+    p.packed = 1;
+  }
+  const dim3 grid((unsigned)((long)m.N * p.strips));
+  const size_t lds = (size_t)kTileP * p.steps * kStepK;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kTileThreads), lds, s, p); };
+  if (m.dt == kBF16) m.out_dt == kBF16 ? go(k_mix_i8_maps<kBF16, kBF16>) : go(k_mix_i8_maps<kBF16, kF32>);
+  else m.out_dt == kBF16 ? go(k_mix_i8_maps<kF32, kBF16>) : go(k_mix_i8_maps<kF32, kF32>);
+  return hipGetLastError();
+}
+
+}  // namespace bc

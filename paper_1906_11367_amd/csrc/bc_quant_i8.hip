@@ -1,43 +1,15 @@
-// 8-bit codes of the rows a mix reduces over (gfx950): for K values x of one
-// token (or of one weight row), with m = max |x|,
-//   scale = m / 127,  q = round to nearest even(x * (127 / m)),
-// in fp32, all zero where m < 2^-100 (127 / m would leave fp32's range); a row
-// with a NaN or an infinity gets a NaN scale, so that every output made from
-// it is NaN.  Rows of codes are padded with zeros to whole 128 bytes, which
-// leaves the products no tail along the reduction.
-// Bound by memory: one read of x (the second comes from cache) and a byte out
-// for each value.
-#include "bc_internal.hpp"
-#include "bc_scan.hpp"   // load_vec, elem
+// 8-bit codes and scales of the rows a mix reduces over (gfx950; bc_i8.hpp has
+// the definition).  Rows of codes are padded with zeros to whole 128 bytes,
+// which leaves the products no tail along the reduction.
+// Bound by memory: one read of x and a byte out for each value.
+#include "bc_i8.hpp"
+
+#include <algorithm>
 
 namespace bc {
 namespace {
 
-using namespace scan;
-
-constexpr uint32_t kInfBits = 0x7f800000u;
-
-struct RowScale { float inv, scale; };
-
-// top: the largest |x| of the row as bits (a NaN's are above infinity's).
-__device__ __forceinline__ RowScale row_scale(uint32_t top) {
-  const float m = __uint_as_float(top);
-  if (top >= kInfBits) return {0.f, __uint_as_float(0x7fc00000u)};
-  if (m < 0x1p-100f) return {0.f, 0.f};
-  return {127.f / m, m / 127.f};
-}
-
-// inv = 0: a row of zeros whatever it holds (NaN * 0 converts to 0).
-__device__ __forceinline__ uint32_t code(float v, float inv) {
-  return (uint32_t)(int)rintf(inv == 0.f ? 0.f : v * inv) & 0xffu;
-}
-
-template <int V>
-__device__ __forceinline__ uint32_t top_bits(uint32_t top, const float (&v)[V]) {
-#pragma unroll
-  for (int k = 0; k < V; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
-  return top;
-}
+using namespace i8;
 
 // Rows of tokens: a wave per row, 16 values a lane at a time.
 template <int DT>
@@ -50,10 +22,8 @@ __global__ __launch_bounds__(256) void k_quant_rows(const char* src, long bs, lo
   uint32_t top = 0;
   for (int k0 = lane * 16; k0 < K; k0 += 1024) {
     const auto r = load_vec<DT, 16>(p + (long)k0 * kBytes<DT>, K - k0);
-    float v[16];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) v[k] = elem<DT, 16>(r, k);
-    top = top_bits(top, v);
+    for (int k = 0; k < 16; ++k) top = max(top, abs_bits(elem<DT, 16>(r, k)));
   }
 #pragma unroll
   for (int d = 32; d > 0; d /= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
@@ -62,45 +32,55 @@ __global__ __launch_bounds__(256) void k_quant_rows(const char* src, long bs, lo
     const auto r = load_vec<DT, 16>(p + (long)k0 * kBytes<DT>, K - k0);
     Raw<4> out;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      out[w] = 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) out[w] |= code(elem<DT, 16>(r, 4 * w + k), s.inv) << (8 * k);
-    }
+    for (int w = 0; w < 4; ++w)
+      out[w] = codes4(elem<DT, 16>(r, 4 * w), elem<DT, 16>(r, 4 * w + 1), elem<DT, 16>(r, 4 * w + 2),
+                      elem<DT, 16>(r, 4 * w + 3), s.inv);
     *reinterpret_cast<Raw<4>*>(q + row * pitch + k0) = out;
   }
   if (lane == 0) scale[row] = s.scale;
 }
 
-// Maps [N][K][P] to rows of tokens: a block takes 64 pixels of one image, a
-// lane one pixel; its four waves share the channels.
-template <int DT>
-__global__ __launch_bounds__(256) void k_quant_maps(const char* src, long bs, long rs, int8_t* q, float* scale, int P,
-                                                    int K, int pitch, int strips) {
-  __shared__ uint32_t tops[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int n = blockIdx.x / strips, p = (blockIdx.x % strips) * 64 + lane;
-  const bool on = p < P;
-  const char* base = src + ((long)n * bs + p) * kBytes<DT>;
-  auto at = [&](int k) { return elem<DT, 2>(load_vec<DT, 2>(base + (long)k * rs * kBytes<DT>, on && k < K ? 1 : 0), 0); };
-  uint32_t top = 0;
-  for (int k = wave; k < K; k += 4) top = max(top, __float_as_uint(at(k)) & 0x7fffffffu);
-  tops[wave][lane] = top;
-  __syncthreads();
-  top = max(max(tops[0][lane], tops[1][lane]), max(tops[2][lane], tops[3][lane]));
-  const RowScale s = row_scale(top);
-  const long row = (long)n * P + p;
-  for (int k0 = wave * 16; k0 < pitch; k0 += 64) {
-    Raw<4> out;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      out[w] = 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) out[w] |= code(at(k0 + 4 * w + k), s.inv) << (8 * k);
+// Maps [N][K][P] to rows of tokens: a block takes 64 pixels of one image, and
+// turns them through LDS, up to kPart steps of 256 channels at a time.
+constexpr int kPart = 4;
+
+template <int DT, int kHold, bool kFull>
+__device__ __forceinline__ void quant_tile(const char* base, long rs, int avail, int8_t* q, int left, int K, int pitch,
+                                           int steps, uint32_t lds, uint32_t* tops, RowScale* rows) {
+  const int tid = threadIdx.x, lp = min(steps, kPart) * kStepK;
+  Raw<kWords<DT, 8>> x[kHold + 1][4];
+  tile_scales<DT, kHold, kFull>(base, rs, avail, K, x, tops, rows);
+  for (int s0 = 0; s0 < steps; s0 += kPart) {
+    const int s1 = min(steps, s0 + kPart);
+    if (s0 > 0) __syncthreads();
+    tile_codes<DT, kHold, kFull>(base, rs, avail, K, x, rows, lds, lp, s0, s1);
+    __syncthreads();
+    // whole rows out, 16 bytes a lane
+    const int chunks = min(pitch - s0 * kStepK, (s1 - s0) * kStepK) >> 4;
+    for (int c = tid; c < kTileP * chunks; c += kTileThreads) {
+      const int p = c / chunks, ch = c % chunks;
+      if (p >= left) break;
+      const Raw<4> w = *(BC_LDS Raw<4>*)(uintptr_t)(lds + p * lp + ((ch ^ chunk_swap(p)) << 4));
+      *reinterpret_cast<Raw<4>*>(q + (long)p * pitch + s0 * kStepK + ch * 16) = w;
     }
-    if (on) *reinterpret_cast<Raw<4>*>(q + row * pitch + k0) = out;
   }
-  if (on && wave == 0) scale[row] = s.scale;
+}
+
+template <int DT>
+__global__ __launch_bounds__(kTileThreads, 4) void k_quant_maps(const char* src, long bs, long rs, int8_t* q,
+                                                                float* scale, int P, int K, int pitch, int strips,
+                                                                int steps) {
+  extern __shared__ __align__(16) unsigned char smem[];   // codes of 64 pixels
+  __shared__ uint32_t tops[kTileThreads / 64 * kTileP];
+  __shared__ RowScale rows[kTileP];
+  const int tid = threadIdx.x, n = blockIdx.x / strips, pt = (blockIdx.x % strips) * kTileP, left = P - pt;
+  const int p0 = pt + (tid & 7) * 8;
+  const uint32_t lds = (uint32_t)(uintptr_t)(BC_LDS unsigned char*)smem;
+  const char* base = src + ((long)n * bs + p0) * kBytes<DT>;
+  int8_t* out = q + ((long)n * P + pt) * pitch;
+  if (left >= kTileP) quant_tile<DT, kHeld<DT>, true>(base, rs, P - p0, out, left, K, pitch, steps, lds, tops, rows);
+  else quant_tile<DT, kHeld<DT>, false>(base, rs, P - p0, out, left, K, pitch, steps, lds, tops, rows);
+  if (tid < kTileP && tid < left) scale[(long)n * P + pt + tid] = rows[tid].scale;
 }
 
 }  // namespace
@@ -111,10 +91,13 @@ hipError_t launch_quantize_i8(const void* src, int dt, long bs, long rs, void* q
   int8_t* out = static_cast<int8_t*>(q);
   const int pitch = i8_pitch(K);
   if (maps) {
-    const int strips = (P + 63) / 64;
+    const int strips = (P + kTileP - 1) / kTileP, steps = (pitch + kStepK - 1) / kStepK;
     const dim3 grid((unsigned)((long)N * strips));
-    if (dt == kBF16) hipLaunchKernelGGL((k_quant_maps<kBF16>), grid, dim3(256), 0, s, x, bs, rs, out, scale, P, K, pitch, strips);
-    else hipLaunchKernelGGL((k_quant_maps<kF32>), grid, dim3(256), 0, s, x, bs, rs, out, scale, P, K, pitch, strips);
+    const size_t lds = (size_t)kTileP * std::min(steps, kPart) * kStepK;
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid, dim3(kTileThreads), lds, s, x, bs, rs, out, scale, P, K, pitch, strips, steps);
+    };
+    dt == kBF16 ? go(k_quant_maps<kBF16>) : go(k_quant_maps<kF32>);
   } else {
     const long rows = (long)N * P;
     const dim3 grid((unsigned)((rows + 3) / 4));
