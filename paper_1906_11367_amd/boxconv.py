@@ -157,7 +157,9 @@ def _maps_and_boxes(x, boxes, what):
 
 
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    # the current device's current stream, without building a Stream object (a
+    # microsecond of a small call)
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def dtype_code(t: torch.Tensor) -> int:
@@ -459,6 +461,9 @@ def _rows(t: torch.Tensor, what: str, name: str):
     return t.data_ptr(), (sn if n > 1 else sr * r), sr
 
 
+_CODES = {torch.int32: BC_I32, torch.float32: BC_F32, torch.bfloat16: BC_BF16, torch.int8: BC_I8}
+
+
 def _seq_sizes(x, layout, what):
     """N, T, C of a sequence tensor in its layout."""
     if not isinstance(x, torch.Tensor) or x.dim() != 3:
@@ -510,7 +515,7 @@ def gated_scan_fwd(gate: torch.Tensor, x: torch.Tensor, y: torch.Tensor, h0: tor
     xp, xbs, xrs = _rows(x, what, "x")
     if (bs, rs) != (xbs, xrs):
         raise BoxConvError(f"{what}: gate and x must have the same strides")
-    dt = dtype_code(x)
+    dt = _CODES[x.dtype]
     if ws is None:
         ws = _workspace(lib.bc_gated_scan_workspace_bytes(0, N, T, C, dt, layout), x.device)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
@@ -544,7 +549,7 @@ def gated_scan_bwd(gate: torch.Tensor, x: torch.Tensor, states: torch.Tensor, gr
     gxp, gxbs, gxrs = _rows(grad_x, what, "grad_x")
     if (bs, rs) != (xbs, xrs) or (gbs, grs) != (gxbs, gxrs):
         raise BoxConvError(f"{what}: gate and x, and grad_gate and grad_x, must have the same strides")
-    dt = dtype_code(x)
+    dt = _CODES[x.dtype]
     if ws is None:
         ws = _workspace(lib.bc_gated_scan_workspace_bytes(1, N, T, C, dt, layout), x.device)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
@@ -568,8 +573,8 @@ def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, y:
         raise BoxConvError(f"{what}: gate, state and y must be tensors")
     _need(gate, x.shape, x.dtype, what, "gate")
     _need(y, x.shape, x.dtype, what, "y")
-    _need(state, (None, C), _F32, what, "state")
-    S = state.shape[0]
+    S = state.shape[0] if isinstance(state, torch.Tensor) and state.dim() == 2 else None
+    _need(state, (S, C), _F32, what, "state")
     _need(state_out, (S, C), _F32, what, "state_out")
     _need(slots, (N,), torch.int32, what, "slots")
     if not gate.is_cuda or not x.is_cuda:
@@ -579,7 +584,7 @@ def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, y:
     if (N > 1 and gs[0] != rs) or (C > 1 and (gs[1] != 1 or xs[1] != 1)):
         raise BoxConvError(f"{what}: gate and x must be contiguous in their last dimension and of the same strides")
     sp = _ptr(state)
-    _check(load_library().gated_scan_step(gate.data_ptr(), x.data_ptr(), dtype_code(x), rs, sp,
+    _check(load_library().gated_scan_step(gate.data_ptr(), x.data_ptr(), _CODES[x.dtype], rs, sp,
                                           sp if state_out is None else _ptr(state_out), _ptr(slots), _ptr(y), N, C, S,
                                           form, _stream()), what)
     return y
@@ -601,7 +606,15 @@ def _mix_input(x, layout, what, name):
         raise BoxConvError(f"{what}: {name} must be an fp32 or bf16 tensor")
     if layout == BC_TOKENS:
         if x.dim() == 2:
-            x = x.unsqueeze(0)
+            P, K = x.shape
+            sr, sc = x.stride()
+            if not x.is_cuda:
+                raise BoxConvError("tensors must be on the GPU")
+            if sc != 1 and K > 1:
+                raise BoxConvError(f"{what}: {name} must be contiguous in its last dimension")
+            if P == 1:
+                sr = K
+            return 1, K, P, x.data_ptr(), sr * P, sr
         if x.dim() != 3:
             raise BoxConvError(f"{what}: {name} must be [T, K] or [N, P, K]")
         N, P, K = x.shape
@@ -640,13 +653,13 @@ def pointwise_mix_i8(wq: torch.Tensor, w_scale: torch.Tensor, x: torch.Tensor, o
     [N, K, P] -> out [N, M, P], fp32 or bf16 each; or x codes [rows, i8_pitch(K)]
     with x_scale [rows]."""
     what = "pointwise_mix_i8"
-    if wq is None or w_scale is None or not isinstance(out, torch.Tensor) or out.dtype not in _FLOATS:
-        raise BoxConvError(f"{what}: wq, w_scale and an fp32 or bf16 out must be given")
-    _need(wq, (None, None), torch.int8, what, "wq")
+    if not isinstance(out, torch.Tensor) or out.dtype not in _FLOATS:
+        raise BoxConvError(f"{what}: out must be an fp32 or bf16 tensor")
+    if not isinstance(wq, torch.Tensor) or wq.dtype is not torch.int8 or wq.dim() != 2 or w_scale is None:
+        raise BoxConvError(f"{what}: wq must be a 2-D int8 tensor, with w_scale")
     M, pitch = wq.shape
     _need(w_scale, (M,), _F32, what, "w_scale")
     _need(bias, (M,), _F32, what, "bias")
-    lib = load_library()
     if isinstance(x, torch.Tensor) and x.dtype is torch.int8:
         _need(x, (None, pitch), torch.int8, what, "x")
         rows, K = x.shape[0], pitch
@@ -663,17 +676,19 @@ def pointwise_mix_i8(wq: torch.Tensor, w_scale: torch.Tensor, x: torch.Tensor, o
         xp, bs, rs = _ptr(x), 0, 0
     else:
         N, K, P, xp, bs, rs = _mix_input(x, layout, what, "x")
-    if lib.bc_i8_pitch(K) != pitch:
-        raise BoxConvError(f"{what}: wq has rows of {pitch} codes, expected i8_pitch({K}) = {lib.bc_i8_pitch(K)}")
+    if (K + 127) // 128 * 128 != pitch:   # i8_pitch(K)
+        raise BoxConvError(f"{what}: wq has rows of {pitch} codes, expected i8_pitch({K})")
+    shape = out.shape
     if layout == BC_TOKENS:
-        if out.shape[-1] != M or out.numel() != N * P * M:
-            raise BoxConvError(f"{what}: out has shape {tuple(out.shape)}, expected {N * P} tokens of {M}")
-    elif out.dim() not in (3, 4) or out.shape[0] != N or out.shape[1] != M or out.numel() != N * M * P:
-        raise BoxConvError(f"{what}: out has shape {tuple(out.shape)}, expected {(N, M, P)}")
-    dt = dtype_code(x)
+        if shape[-1] != M or out.numel() != N * P * M:
+            raise BoxConvError(f"{what}: out has shape {tuple(shape)}, expected {N * P} tokens of {M}")
+    elif len(shape) not in (3, 4) or shape[0] != N or shape[1] != M or out.numel() != N * M * P:
+        raise BoxConvError(f"{what}: out has shape {tuple(shape)}, expected {(N, M, P)}")
+    lib = load_library()
+    dt = _CODES[x.dtype]
     if ws is None:
         ws = _workspace(lib.bc_mix_i8_workspace_bytes(N, M, K, P, dt, layout), x.device)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check(lib.pointwise_mix_i8(_ptr(wq), _ptr(w_scale), xp, dt, bs, rs, _ptr(x_scale), _ptr(bias), _ptr(out),
-                                dtype_code(out), N, M, K, P, relu, layout, _ptr(ws), nbytes, _stream()), what)
+                                _CODES[out.dtype], N, M, K, P, relu, layout, _ptr(ws), nbytes, _stream()), what)
     return out

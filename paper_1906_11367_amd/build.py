@@ -21,8 +21,8 @@ BUILD = os.path.join(PKG, "_build")
 ARCH = "gfx950"
 
 SOURCES = ["bc_api.cpp", "bc_box.hip", "bc_box_lds.hip", "bc_box_split.hip", "bc_mix.hip", "bc_mix_direct.hip",
-           "bc_mix_i8.hip", "bc_mix_i8_maps.hip", "bc_mix_pipe.hip", "bc_noalloc.hip", "bc_quant_i8.hip", "bc_scan.hip",
-           "bc_scan_maps.hip", "bc_stream.hip"]
+           "bc_mix_i8.hip", "bc_mix_i8_few.hip", "bc_mix_i8_maps.hip", "bc_mix_pipe.hip", "bc_noalloc.hip", "bc_quant_i8.hip",
+           "bc_scan.hip", "bc_scan_maps.hip", "bc_stream.hip"]
 
 
 def hipcc() -> str:

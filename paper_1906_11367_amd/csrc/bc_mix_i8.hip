@@ -277,14 +277,17 @@ size_t mix_i8_workspace_bytes(int N, int M, int K, int P, int dt, bool maps) {
   if (dt == 3) return 0;   // codes already
   if (maps && mix_i8_maps_takes(K)) return mix_i8_maps_workspace_bytes(N, M, K, P);
   const long rows = (long)N * P;
+  if (!maps && mix_i8_few_makes_codes(rows, K)) return 0;
   return codes_bytes(rows, K) + (size_t)rows * 4;
 }
 
 hipError_t launch_mix_i8(const MixI8& m, hipStream_t s) {
   if (m.maps && m.dt != 3 && mix_i8_maps_takes(m.K)) return launch_mix_i8_maps(m, s);
   const long rows = (long)m.N * m.P;
+  const bool few = !m.maps && mix_i8_few_takes(rows, m.K);
   const int8_t* x = static_cast<const int8_t*>(m.x);
   const float* xscale = m.xscale;
+  if (few && (m.dt == 3 || mix_i8_few_makes_codes(rows, m.K))) return launch_mix_i8_few(m, s);
   if (m.dt != 3) {
     char* ws = static_cast<char*>(m.ws);
     float* scale = reinterpret_cast<float*>(ws + codes_bytes(rows, m.K));
@@ -292,6 +295,15 @@ hipError_t launch_mix_i8(const MixI8& m, hipStream_t s) {
     if (e != hipSuccess) return e;
     x = reinterpret_cast<const int8_t*>(ws);
     xscale = scale;
+  }
+  if (few) {
+    MixI8 c = m;
+    c.x = x;
+    c.xscale = xscale;
+    c.dt = 3;
+    c.N = 1;
+    c.P = (int)rows;
+    return launch_mix_i8_few(c, s);
   }
   const int8_t* w = static_cast<const int8_t*>(m.wq);
   Args p{};

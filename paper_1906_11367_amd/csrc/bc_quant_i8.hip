@@ -11,33 +11,52 @@ namespace {
 
 using namespace i8;
 
-// Rows of tokens: a wave per row, 16 values a lane at a time.
-template <int DT>
+// Rows of tokens: W waves to a row, 16 values a lane at a time.  The first two
+// pieces of a row (2048 W values) stay in registers; the rest is read again.
+constexpr int kHeldPieces = 2;
+
+template <int DT, int W>
 __global__ __launch_bounds__(256) void k_quant_rows(const char* src, long bs, long rs, int8_t* q, float* scale,
                                                     long rows, int P, int K, int pitch) {
-  const int lane = threadIdx.x & 63;
-  const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
+  constexpr int kPiece = W * 1024;
+  __shared__ uint32_t tops[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k1 = (threadIdx.x & (64 * W - 1)) * 16;
+  const long row = W == 4 ? blockIdx.x : (long)blockIdx.x * 4 + wave;
+  if (row >= rows) return;   // W = 4: never
   const char* p = src + ((row / P) * bs + (row % P) * rs) * kBytes<DT>;
+  auto load = [&](int k) { return load_vec<DT, 16>(p + (long)k * kBytes<DT>, K - k); };
+  Raw<kWords<DT, 16>> x[kHeldPieces];
+#pragma unroll
+  for (int i = 0; i < kHeldPieces; ++i) x[i] = load(k1 + i * kPiece);
   uint32_t top = 0;
-  for (int k0 = lane * 16; k0 < K; k0 += 1024) {
-    const auto r = load_vec<DT, 16>(p + (long)k0 * kBytes<DT>, K - k0);
+  auto note = [&](const Raw<kWords<DT, 16>>& r) {
 #pragma unroll
     for (int k = 0; k < 16; ++k) top = max(top, abs_bits(elem<DT, 16>(r, k)));
-  }
+  };
+#pragma unroll
+  for (int i = 0; i < kHeldPieces; ++i) note(x[i]);
+  for (int k = k1 + kHeldPieces * kPiece; k < K; k += kPiece) note(load(k));
 #pragma unroll
   for (int d = 32; d > 0; d /= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+  if constexpr (W == 4) {
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+    top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+  }
   const RowScale s = row_scale(top);
-  for (int k0 = lane * 16; k0 < pitch; k0 += 1024) {
-    const auto r = load_vec<DT, 16>(p + (long)k0 * kBytes<DT>, K - k0);
+  auto put = [&](int k, const Raw<kWords<DT, 16>>& r) {
+    if (k >= pitch) return;
     Raw<4> out;
 #pragma unroll
     for (int w = 0; w < 4; ++w)
       out[w] = codes4(elem<DT, 16>(r, 4 * w), elem<DT, 16>(r, 4 * w + 1), elem<DT, 16>(r, 4 * w + 2),
                       elem<DT, 16>(r, 4 * w + 3), s.inv);
-    *reinterpret_cast<Raw<4>*>(q + row * pitch + k0) = out;
-  }
-  if (lane == 0) scale[row] = s.scale;
+    *reinterpret_cast<Raw<4>*>(q + row * pitch + k) = out;
+  };
+#pragma unroll
+  for (int i = 0; i < kHeldPieces; ++i) put(k1 + i * kPiece, x[i]);
+  for (int k = k1 + kHeldPieces * kPiece; k < pitch; k += kPiece) put(k, load(k));
+  if (k1 == 0) scale[row] = s.scale;
 }
 
 // Maps [N][K][P] to rows of tokens: a block takes 64 pixels of one image, and
@@ -100,9 +119,11 @@ hipError_t launch_quantize_i8(const void* src, int dt, long bs, long rs, void* q
     dt == kBF16 ? go(k_quant_maps<kBF16>) : go(k_quant_maps<kF32>);
   } else {
     const long rows = (long)N * P;
-    const dim3 grid((unsigned)((rows + 3) / 4));
-    if (dt == kBF16) hipLaunchKernelGGL((k_quant_rows<kBF16>), grid, dim3(256), 0, s, x, bs, rs, out, scale, rows, P, K, pitch);
-    else hipLaunchKernelGGL((k_quant_rows<kF32>), grid, dim3(256), 0, s, x, bs, rs, out, scale, rows, P, K, pitch);
+    const bool block = K > 2 * 1024 || rows < 1024;   // a block to a row
+    const dim3 grid((unsigned)(block ? rows : (rows + 3) / 4));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, x, bs, rs, out, scale, rows, P, K, pitch); };
+    if (dt == kBF16) block ? go(k_quant_rows<kBF16, 4>) : go(k_quant_rows<kBF16, 1>);
+    else block ? go(k_quant_rows<kF32, 4>) : go(k_quant_rows<kF32, 1>);
   }
   return hipGetLastError();
 }
