@@ -27,6 +27,7 @@ struct Args {
   int I, J;                   // rows of a and of b
   int pitch, M, P;
   float floor;                // 0 with relu, else -infinity
+  bool stream;                // out past the caches (bc_scan.hpp: streams)
 };
 
 // Where out(i, j) stands, in elements.
@@ -235,7 +236,12 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_mix_i8_tile(Args p, int ti, in
       if (i >= p.I || jo >= p.J) continue;
       char* o = p.out + out_at<kMaps>(p, i, jo) * kE;
       const int left = kMaps ? min(p.I - i, p.P - i % p.P) : p.I - i;   // elements contiguous from here
-      if (left >= kWide) {
+      if (left >= kWide && p.stream) {
+        typedef Raw<kWide * kE / 4> Any __attribute__((aligned(kE)));
+        asm volatile("");   // keeps the compiler from merging the two stores into a plain one
+        __builtin_nontemporal_store(w, reinterpret_cast<Any*>(o));
+        asm volatile("");
+      } else if (left >= kWide) {
         *reinterpret_cast<Loose<4, kE>*>(o) = __builtin_bit_cast(Loose<4, kE>, w);
       } else {
 #pragma unroll
@@ -313,6 +319,7 @@ hipError_t launch_mix_i8(const MixI8& m, hipStream_t s) {
   p.M = m.M;
   p.P = m.P;
   p.floor = m.relu ? 0.f : -INFINITY;
+  p.stream = streams((double)rows * m.M, m.maps ? m.P : m.M, m.out_dt, m.out, m.out);
   if (m.maps) {
     p.a = x; p.ascale = xscale; p.I = (int)rows;
     p.b = w; p.bscale = m.wscale; p.J = m.M;

@@ -305,7 +305,7 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdA
 #pragma unroll
     for (int k = 0; k < V; ++k) h[k] = __fmaf_rn(a[i][k], h[k], b[i][k]);
     char* at = yp + (long)(t0 + i) * p.C * kBytes<OUT>;
-    if (t0 + i < len) store_vec<OUT, V>(at, avail, h);
+    if (t0 + i < len) store_vec<OUT, V>(at, avail, h, p.stream);
     else if (t0 + i < p.T) store_zero<OUT, V>(at, avail);
   }
   if (kChain && place + 1 < p.tiles) return;
@@ -453,8 +453,8 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_bwd(BwdA
     }
     char *gat = ggate + (long)(t0 + i) * p.grs * kBytes<OUT>, *xat = gx + (long)(t0 + i) * p.grs * kBytes<OUT>;
     if (t0 + i < len) {
-      store_vec<OUT, V>(gat, avail, og);
-      store_vec<OUT, V>(xat, avail, ox);
+      store_vec<OUT, V>(gat, avail, og, p.stream);
+      store_vec<OUT, V>(xat, avail, ox, p.stream);
     } else if (t0 + i < p.T) {
       store_zero<OUT, V>(gat, avail);
       store_zero<OUT, V>(xat, avail);
@@ -612,6 +612,7 @@ hipError_t launch_scan_fwd(const ScanFwd& f, hipStream_t s) {
   p.N = f.N;
   p.T = f.T;
   p.C = f.C;
+  p.stream = streams((double)f.N * f.T * f.C, f.maps ? f.T : f.C, f.out_dt, f.y, f.y);
   if (f.maps) return launch_scan_fwd_maps(p, f.in_dt, f.out_dt, f.form, s);
   if (f.in_dt == kBF16) return fwd_tokens<kBF16, kBF16>(p, f.form, f.ws, s);
   return f.out_dt == kBF16 ? fwd_tokens<kF32, kBF16>(p, f.form, f.ws, s) : fwd_tokens<kF32, kF32>(p, f.form, f.ws, s);
@@ -635,6 +636,7 @@ hipError_t launch_scan_bwd(const ScanBwd& f, hipStream_t s) {
   p.N = f.N;
   p.T = f.T;
   p.C = f.C;
+  p.stream = streams((double)f.N * f.T * f.C, f.grs, f.out_dt, f.ggate, f.gx) && f.gbs % 64 == 0;
   if (f.maps) return launch_scan_bwd_maps(p, f.in_dt, f.out_dt, f.form, s);
   if (f.in_dt == kBF16) return bwd_tokens<kBF16, kBF16>(p, f.form, f.ws, s);
   return f.out_dt == kBF16 ? bwd_tokens<kF32, kBF16>(p, f.form, f.ws, s) : bwd_tokens<kF32, kF32>(p, f.form, f.ws, s);

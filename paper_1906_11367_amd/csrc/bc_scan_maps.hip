@@ -1,9 +1,10 @@
 // The gated scan on maps [N][C][T] (gfx950): every row is one sequence, time
 // contiguous, as the 1x1 mix writes its outputs (bc_scan.hpp has the algebra).
 //
-// A wave takes kSeg = 512 consecutive steps of a row at a time, 8 to a lane,
-// scans the lanes' pairs by lane moves and carries the state on.  W waves share
-// a row, kSeg steps each, where there are too few rows for a wave each.
+// A wave takes 512 (bf16) or 256 (fp32) consecutive steps of a row at a time,
+// 16 bytes to a lane, scans the lanes' pairs by lane moves and carries the
+// state on.  W waves share a row, a segment each, where there are too few rows
+// for a wave each.
 #include "bc_scan.hpp"
 
 namespace bc {
@@ -11,9 +12,11 @@ namespace {
 
 using namespace scan;
 
-constexpr int kV = 8;
-constexpr int kSeg = 64 * kV;
-static_assert(kSeg == kScanSpanMaps, "a state is kept at each wave's segment");
+// Steps a lane (16 bytes: a wave's access is 1 KiB in one piece), and a wave's
+// segment, at each of which a state is kept.
+template <int DT> constexpr int kV = DT == kBF16 ? 8 : 4;
+template <int DT> constexpr int kSeg = 64 * kV<DT>;
+static_assert(kSeg<kBF16> % kScanSpanMaps == 0 && kSeg<kF32> % kScanSpanMaps == 0, "room for the states");
 
 __device__ __forceinline__ void lanes_prefix(float& A, float& B, int lane, float& eA, float& eB) {
 #pragma unroll
@@ -48,6 +51,7 @@ template <int W> constexpr int kRows = W >= 4 ? 1 : 4 / W;
 
 template <int IN, int OUT, int FORM, int W>
 __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_fwd_maps(FwdArgs p) {
+  constexpr int V = kV<IN>, Seg = kSeg<IN>;
   __shared__ float tot[2][W][2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % W;
   const long row = (long)blockIdx.x * kRows<W> + wave / W;
@@ -57,19 +61,19 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_fwd_maps(FwdArgs p) 
   const char* gate = p.gate + ((long)n * p.bs + (long)c * p.rs) * kBytes<IN>;
   const char* xp = p.x + ((long)n * p.bs + (long)c * p.rs) * kBytes<IN>;
   char* yp = p.y + row * p.T * kBytes<OUT>;
-  const int S = (p.T + kSeg - 1) / kSeg;
+  const int S = (p.T + Seg - 1) / Seg;
   float carry = p.h0 ? p.h0[row] : 0.f;
   int q = 0;
   for (int s0 = 0; s0 < S; s0 += W, q ^= 1) {
-    const int t0 = (s0 + w) * kSeg + lane * kV;
-    const auto g = load_vec<IN, kV>(gate + (long)t0 * kBytes<IN>, len - t0);
-    const auto x = load_vec<IN, kV>(xp + (long)t0 * kBytes<IN>, len - t0);
-    float a[kV], b[kV], A = 1.f, B = 0.f, eA, eB;
+    const int t0 = (s0 + w) * Seg + lane * V;
+    const auto g = load_vec<IN, V>(gate + (long)t0 * kBytes<IN>, len - t0);
+    const auto x = load_vec<IN, V>(xp + (long)t0 * kBytes<IN>, len - t0);
+    float a[V], b[V], A = 1.f, B = 0.f, eA, eB;
 #pragma unroll
-    for (int k = 0; k < kV; ++k) {
+    for (int k = 0; k < V; ++k) {
       float cx;
-      coefficients<IN, FORM>(elem<IN, kV>(g, k), a[k], cx);
-      b[k] = input_share<FORM>(cx, elem<IN, kV>(x, k));
+      coefficients<IN, FORM>(elem<IN, V>(g, k), a[k], cx);
+      b[k] = input_share<FORM>(cx, elem<IN, V>(x, k));
       if (t0 + k >= len) { a[k] = 1.f; b[k] = 0.f; }
       A *= a[k];
       B = __fmaf_rn(a[k], B, b[k]);
@@ -87,19 +91,20 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_fwd_maps(FwdArgs p) 
       }
     }
     if (p.states && lane == 0 && s0 + w < S) p.states[row * S + s0 + w] = hw;
-    float h = __fmaf_rn(eA, hw, eB), o[kV];
+    float h = __fmaf_rn(eA, hw, eB), o[V];
 #pragma unroll
-    for (int k = 0; k < kV; ++k) {
+    for (int k = 0; k < V; ++k) {
       h = __fmaf_rn(a[k], h, b[k]);
       o[k] = t0 + k < len ? h : 0.f;
     }
-    store_vec<OUT, kV>(yp + (long)t0 * kBytes<OUT>, p.T - t0, o);
+    store_vec<OUT, V>(yp + (long)t0 * kBytes<OUT>, p.T - t0, o, p.stream);
   }
   if (p.h_last && w == 0 && lane == 0) p.h_last[row] = carry;
 }
 
 template <int IN, int OUT, int FORM, int W>
 __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_bwd_maps(BwdArgs p) {
+  constexpr int V = kV<IN>, Seg = kSeg<IN>;
   __shared__ float tot[2][W][2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % W;
   const long row = (long)blockIdx.x * kRows<W> + wave / W;
@@ -111,25 +116,25 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_bwd_maps(BwdArgs p) 
   const char* gy = p.gy + row * p.T * kBytes<IN>;
   char* ggate = p.ggate + ((long)n * p.gbs + (long)c * p.grs) * kBytes<OUT>;
   char* gx = p.gx + ((long)n * p.gbs + (long)c * p.grs) * kBytes<OUT>;
-  const int S = (p.T + kSeg - 1) / kSeg;
+  const int S = (p.T + Seg - 1) / Seg;
   float carry = p.gh_last ? p.gh_last[row] : 0.f;
   int q = 0;
   for (int s0 = (S - 1) / W * W; s0 >= 0; s0 -= W, q ^= 1) {
-    const int t0 = (s0 + w) * kSeg + lane * kV;
-    const auto g = load_vec<IN, kV>(gate + (long)t0 * kBytes<IN>, len - t0);
-    const auto xr = load_vec<IN, kV>(xp + (long)t0 * kBytes<IN>, len - t0);
-    const auto dr = load_vec<IN, kV>(gy + (long)t0 * kBytes<IN>, len - t0);
+    const int t0 = (s0 + w) * Seg + lane * V;
+    const auto g = load_vec<IN, V>(gate + (long)t0 * kBytes<IN>, len - t0);
+    const auto xr = load_vec<IN, V>(xp + (long)t0 * kBytes<IN>, len - t0);
+    const auto dr = load_vec<IN, V>(gy + (long)t0 * kBytes<IN>, len - t0);
     const float st = s0 + w < S ? p.states[row * S + s0 + w] : 0.f;
-    float a[kV], cx[kV], h[kV], A = 1.f, B = 0.f, R = 0.f, eA, eB, sA, sB;
+    float a[V], cx[V], h[V], A = 1.f, B = 0.f, R = 0.f, eA, eB, sA, sB;
 #pragma unroll
-    for (int k = 0; k < kV; ++k) {
-      coefficients<IN, FORM>(elem<IN, kV>(g, k), a[k], cx[k]);
+    for (int k = 0; k < V; ++k) {
+      coefficients<IN, FORM>(elem<IN, V>(g, k), a[k], cx[k]);
       if (t0 + k >= len) { a[k] = 1.f; cx[k] = 0.f; }
       A *= a[k];
-      B = __fmaf_rn(a[k], B, input_share<FORM>(cx[k], elem<IN, kV>(xr, k)));
+      B = __fmaf_rn(a[k], B, input_share<FORM>(cx[k], elem<IN, V>(xr, k)));
     }
 #pragma unroll
-    for (int k = kV - 1; k >= 0; --k) R = a[k] * (elem<IN, kV>(dr, k) + R);
+    for (int k = V - 1; k >= 0; --k) R = a[k] * (elem<IN, V>(dr, k) + R);
     float fA = A, fB = B;
     lanes_prefix(fA, fB, lane, eA, eB);
     lanes_suffix(A, R, lane, sA, sB);
@@ -146,33 +151,33 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_bwd_maps(BwdArgs p) 
     }
     h[0] = __fmaf_rn(eA, st, eB);
 #pragma unroll
-    for (int k = 0; k + 1 < kV; ++k)
-      h[k + 1] = __fmaf_rn(a[k], h[k], input_share<FORM>(cx[k], elem<IN, kV>(xr, k)));
-    float r = __fmaf_rn(sA, rw, sB), og[kV], ox[kV];
+    for (int k = 0; k + 1 < V; ++k)
+      h[k + 1] = __fmaf_rn(a[k], h[k], input_share<FORM>(cx[k], elem<IN, V>(xr, k)));
+    float r = __fmaf_rn(sA, rw, sB), og[V], ox[V];
 #pragma unroll
-    for (int k = kV - 1; k >= 0; --k) {
-      const float delta = elem<IN, kV>(dr, k) + r;
+    for (int k = V - 1; k >= 0; --k) {
+      const float delta = elem<IN, V>(dr, k) + r;
       if constexpr (FORM == kValue) {
         og[k] = delta * h[k];
         ox[k] = delta;
       } else {
         ox[k] = delta * cx[k];
-        og[k] = ox[k] * a[k] * (h[k] - elem<IN, kV>(xr, k));
+        og[k] = ox[k] * a[k] * (h[k] - elem<IN, V>(xr, k));
       }
       r = a[k] * delta;
       if (t0 + k >= len) og[k] = ox[k] = 0.f;
     }
-    store_vec<OUT, kV>(ggate + (long)t0 * kBytes<OUT>, p.T - t0, og);
-    store_vec<OUT, kV>(gx + (long)t0 * kBytes<OUT>, p.T - t0, ox);
+    store_vec<OUT, V>(ggate + (long)t0 * kBytes<OUT>, p.T - t0, og, p.stream);
+    store_vec<OUT, V>(gx + (long)t0 * kBytes<OUT>, p.T - t0, ox, p.stream);
   }
   if (p.gh0 && w == 0 && lane == 0) p.gh0[row] = carry;
 }
 
 // Waves to a row: as many as the row has segments for, until there are 4096
 // waves in all (four for each SIMD).
-int waves_per_row(int N, int C, int T) {
+int waves_per_row(int N, int C, int T, int seg) {
   const long rows = (long)N * C;
-  const int segs = (T + kSeg - 1) / kSeg;
+  const int segs = (T + seg - 1) / seg;
   int w = 1;
   while (w < 16 && w < segs && rows * w < 4096) w *= 4;
   return w;
@@ -187,7 +192,7 @@ hipError_t launch_rows(Kernel kernel, const Args& p, hipStream_t s) {
 
 template <int IN, int OUT, int FORM>
 hipError_t fwd_rows(const FwdArgs& p, hipStream_t s) {
-  switch (waves_per_row(p.N, p.C, p.T)) {
+  switch (waves_per_row(p.N, p.C, p.T, kSeg<IN>)) {
     case 1: return launch_rows<1>(k_scan_fwd_maps<IN, OUT, FORM, 1>, p, s);
     case 4: return launch_rows<4>(k_scan_fwd_maps<IN, OUT, FORM, 4>, p, s);
     default: return launch_rows<16>(k_scan_fwd_maps<IN, OUT, FORM, 16>, p, s);
@@ -196,7 +201,7 @@ hipError_t fwd_rows(const FwdArgs& p, hipStream_t s) {
 
 template <int IN, int OUT, int FORM>
 hipError_t bwd_rows(const BwdArgs& p, hipStream_t s) {
-  switch (waves_per_row(p.N, p.C, p.T)) {
+  switch (waves_per_row(p.N, p.C, p.T, kSeg<IN>)) {
     case 1: return launch_rows<1>(k_scan_bwd_maps<IN, OUT, FORM, 1>, p, s);
     case 4: return launch_rows<4>(k_scan_bwd_maps<IN, OUT, FORM, 4>, p, s);
     default: return launch_rows<16>(k_scan_bwd_maps<IN, OUT, FORM, 16>, p, s);
