@@ -44,8 +44,6 @@ __device__ __forceinline__ float finish(int sum, float token, float weight, floa
 
 #define BC_LDS __attribute__((address_space(3)))
 
-constexpr int kBK = 64;   // codes of a row per stage
-
 __device__ __forceinline__ i32x4_t buf_desc(const void* p, uint32_t bytes) {
   const uint64_t a = (uint64_t)p;
   i32x4_t r;
@@ -73,12 +71,15 @@ __device__ __forceinline__ void wait_loads() {
 
 // Tiles through LDS: WI x WJ waves of FI x FJ blocks of 32 x 32 outputs.
 //
-// Both operands go from memory into a ring of LDS stages (kBK codes of every
-// row of the tile), kStages - 1 stages ahead, one barrier per stage.  The
-// 16-byte chunk c of row r sits at chunk c ^ ((r >> 2) & 3), so that the 16
+// Both operands go from memory into a ring of LDS stages (kBK codes, 64 or 128,
+// of every row of the tile), kStages - 1 stages ahead, one barrier per stage.
+// The 16-byte chunk c of row r sits at chunk c ^ chunk_of(r), so that the 16
 // lanes that read one chunk of 16 rows hit all banks; the loads write LDS in
 // lane order, so each lane fetches the chunk that belongs there.
-template <int OUT, bool kMaps, int WI, int WJ, int FI, int FJ, int kStages>
+template <int kBK>
+__device__ __forceinline__ int chunk_of(int r) { return kBK == 64 ? (r >> 2) & 3 : (r >> 1) & 7; }
+
+template <int OUT, bool kMaps, int WI, int WJ, int FI, int FJ, int kBK, int kStages>
 __global__ __launch_bounds__(64 * WI * WJ) void k_mix_i8_tile(Args p, int ti, int tj, int per) {
   constexpr int kWaves = WI * WJ, BI = WI * FI * 32, BJ = WJ * FJ * 32;
   constexpr int kABytes = BI * kBK, kStage = (BI + BJ) * kBK;
@@ -103,9 +104,10 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_mix_i8_tile(Args p, int ti, in
   for (int l = 0; l < kLoads; ++l) {
     const int ld = wave * kLoads + l;
     const bool is_a = ld < kALoads;
-    const int row = (is_a ? ld : ld - kALoads) * 16 + (lane >> 2);
+    constexpr int kLanes = kBK / 16, kLoadRows = 64 / kLanes;   // lanes on a row, rows of a load
+    const int row = (is_a ? ld : ld - kALoads) * kLoadRows + lane / kLanes;
     // rows past the operand read zeros (the descriptor ends there)
-    voff[l] = (uint32_t)row * (uint32_t)p.pitch + (uint32_t)(((lane & 3) ^ ((row >> 2) & 3)) * 16);
+    voff[l] = (uint32_t)row * (uint32_t)p.pitch + (uint32_t)(((lane & (kLanes - 1)) ^ chunk_of<kBK>(row)) * 16);
   }
   int load_slot = 0, load_k = 0;
   auto issue = [&]() {
@@ -122,12 +124,13 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_mix_i8_tile(Args p, int ti, in
   const int wi = wave / WJ, wj = wave % WJ;
   // rows 32 apart swizzle alike
   const int arow = wi * FI * 32 + (lane & 31), brow = wj * FJ * 32 + (lane & 31);
-  uint32_t aoff[2], boff[2];
+  constexpr int kSteps = kBK / 32;   // matrix instructions deep
+  uint32_t aoff[kSteps], boff[kSteps];
 #pragma unroll
-  for (int kk = 0; kk < 2; ++kk) {
+  for (int kk = 0; kk < kSteps; ++kk) {
     const int c = 2 * kk + (lane >> 5);
-    aoff[kk] = (uint32_t)(arow * kBK + ((c ^ ((arow >> 2) & 3)) << 4));
-    boff[kk] = (uint32_t)(kABytes + brow * kBK + ((c ^ ((brow >> 2) & 3)) << 4));
+    aoff[kk] = (uint32_t)(arow * kBK + ((c ^ chunk_of<kBK>(arow)) << 4));
+    boff[kk] = (uint32_t)(kABytes + brow * kBK + ((c ^ chunk_of<kBK>(brow)) << 4));
   }
   i32x16_t acc[FI][FJ];
 #pragma unroll
@@ -137,17 +140,19 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_mix_i8_tile(Args p, int ti, in
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[x][y][r] = 0;
 
-  // A stage is two halves of 32 codes.  The operands of a half are read from
-  // LDS during the half before, across the barrier too, which stands between
-  // the halves: no wave then starts a stage by waiting for its reads.
+  // A stage is kSteps steps of 32 codes.  The operands of a step are read from
+  // LDS during the step before, across the barrier too, which stands before a
+  // stage's last step: no wave then starts a stage by waiting for its reads.
   i32x4_t fa[2][FI], fb[2][FJ];
-  auto read = [&](int half, uint32_t st) {
+  auto read = [&](int step, uint32_t st) {
+    const int half = step & 1;
 #pragma unroll
-    for (int x = 0; x < FI; ++x) fa[half][x] = *(BC_LDS i32x4_t*)(uintptr_t)(st + aoff[half] + x * 32 * kBK);
+    for (int x = 0; x < FI; ++x) fa[half][x] = *(BC_LDS i32x4_t*)(uintptr_t)(st + aoff[step] + x * 32 * kBK);
 #pragma unroll
-    for (int y = 0; y < FJ; ++y) fb[half][y] = *(BC_LDS i32x4_t*)(uintptr_t)(st + boff[half] + y * 32 * kBK);
+    for (int y = 0; y < FJ; ++y) fb[half][y] = *(BC_LDS i32x4_t*)(uintptr_t)(st + boff[step] + y * 32 * kBK);
   };
-  auto multiply = [&](int half) {
+  auto multiply = [&](int step) {
+    const int half = step & 1;
 #pragma unroll
     for (int x = 0; x < FI; ++x)
 #pragma unroll
@@ -170,10 +175,13 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_mix_i8_tile(Args p, int ti, in
   int slot = 0;
   for (int s = 0; s < nk; ++s) {
     const uint32_t st = lds0 + slot * kStage;
-    __builtin_amdgcn_sched_barrier(0);
-    read(1, st);
-    multiply(0);
-    interleave();
+#pragma unroll
+    for (int step = 0; step + 1 < kSteps; ++step) {
+      __builtin_amdgcn_sched_barrier(0);
+      read(step + 1, st);
+      multiply(step);
+      interleave();
+    }
     __builtin_amdgcn_sched_barrier(0);
     // the next stage's loads are done when at most the later ones' are pending
     if (s + kStages - 2 < nk) wait_loads<kLoads * (kStages - 3)>();
@@ -183,7 +191,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_mix_i8_tile(Args p, int ti, in
     if (load_k < nk) issue();
     slot = slot + 1 == kStages ? 0 : slot + 1;
     read(0, lds0 + slot * kStage);   // past the last stage: never used
-    multiply(1);
+    multiply(kSteps - 1);
     interleave();
   }
   __builtin_amdgcn_sched_barrier(0);
@@ -256,22 +264,34 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_mix_i8_tile(Args p, int ti, in
   }
 }
 
-template <int OUT, bool kMaps, int WI, int WJ, int FI, int FJ, int kStages>
+template <int OUT, bool kMaps, int WI, int WJ, int FI, int FJ, int kBK, int kStages>
 hipError_t launch_tile(const Args& p, hipStream_t s) {
   constexpr int BI = WI * FI * 32, BJ = WJ * FJ * 32;
   constexpr int kLds = std::max(kStages * (BI + BJ) * kBK, WI * WJ * 32 * (FI * 32 * kBytes<OUT> + 16) + BI * 8);
-  const auto kernel = k_mix_i8_tile<OUT, kMaps, WI, WJ, FI, FJ, kStages>;
+  const auto kernel = k_mix_i8_tile<OUT, kMaps, WI, WJ, FI, FJ, kBK, kStages>;
   const int ti = (p.I + BI - 1) / BI, tj = (p.J + BJ - 1) / BJ, per = (ti * tj + 7) / 8;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(per * 8)), dim3(64 * WI * WJ), kLds, s, p, ti, tj, per);
   return hipGetLastError();
 }
 
+// The largest tile of which there are at least as many as CUs: an operand's
+// traffic falls with the tile's side, a half-empty chip costs more.  Stages of
+// 128 codes halve the barriers where LDS has room for them: one block to a CU
+// (256 x 128, and 128 x 128 where there is one each) or small tiles.  Kernel us
+// of 256 x 256, 256 x 128, 128 x 128 (128 and 64 deep), 64 x 64:
+//   2048 x 8192 -> 8192  121,  144,  169,         286
+//   2048 x 4096 -> 4096  53.6, 38.1, 46.2 (47.8), 58.1
+//   1024 x 4096 -> 4096  48.8, 31.0, 24.7 (27.2), 30.4
+//   1500 x 2000 -> 3000  29.0, 21.0, 27.1 (20.5), 24.6
+//   512 x 4096 -> 4096   46.6, 30.4, 22.0 (24.6), 18.4
 template <int OUT, bool kMaps>
 hipError_t launch(const Args& p, hipStream_t s) {
-  auto tiles = [&](int b) { return (long)((p.I + b - 1) / b) * ((p.J + b - 1) / b); };
-  if (tiles(256) >= 256) return launch_tile<OUT, kMaps, 2, 4, 4, 2, 4>(p, s);
-  if (tiles(128) >= 256) return launch_tile<OUT, kMaps, 2, 2, 2, 2, 4>(p, s);
-  return launch_tile<OUT, kMaps, 2, 2, 1, 1, 6>(p, s);
+  auto tiles = [&](int i, int j) { return (long)((p.I + i - 1) / i) * ((p.J + j - 1) / j); };
+  if (tiles(256, 256) >= 256) return launch_tile<OUT, kMaps, 2, 4, 4, 2, 64, 4>(p, s);
+  if (tiles(256, 128) >= 256) return launch_tile<OUT, kMaps, 4, 2, 2, 2, 128, 3>(p, s);
+  if (tiles(128, 128) > 256) return launch_tile<OUT, kMaps, 2, 2, 2, 2, 64, 4>(p, s);
+  if (tiles(128, 128) == 256) return launch_tile<OUT, kMaps, 2, 2, 2, 2, 128, 4>(p, s);
+  return launch_tile<OUT, kMaps, 2, 2, 1, 1, 128, 4>(p, s);
 }
 
 // Workspace: the tokens' codes, then their scales.

@@ -120,7 +120,8 @@ def test_tokens(T, K, M):
 
 # sizes that take the large tiles, ragged on every side
 @pytest.mark.parametrize("T,K,M", [(700, 1000, 1537), (1030, 4096, 2049), (4100, 300, 520), (2048, 640, 4096),
-                                   (40, 8192, 3000), (3, 8000, 4100), (1, 4096, 8192), (256, 256, 256)])
+                                   (40, 8192, 3000), (3, 8000, 4100), (1, 4096, 8192), (256, 256, 256),
+                                   (4090, 130, 4000), (2047, 500, 4090), (2040, 200, 2048), (1500, 260, 3000)])
 def test_tokens_large(T, K, M):
     say("mix tokens", T, K, M)
     wq, ws = weights(M, M, K)
