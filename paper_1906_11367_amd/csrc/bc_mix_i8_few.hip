@@ -70,7 +70,13 @@ __global__ __launch_bounds__(kThreads) void k_mix_i8_few(Args p) {
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       const int it = wave + i * kWaves, t = it / per, k = (it % per) * 512 + lane * 8;
-      x[i] = load_vec<DT, 8>(p.x + ((long)(t / p.P) * p.bs + (long)(t % p.P) * p.rs + k) * kBytes<DT>, it < items ? p.K - k : 0);
+      const char* at = p.x + ((long)(t / p.P) * p.bs + (long)(t % p.P) * p.rs + k) * kBytes<DT>;
+      x[i] = Raw<kWords<DT, 8>>{};
+      if (p.K % 512 == 0) {   // whole pieces
+        if (it < items) x[i] = load_wide<DT, 8>(at);
+      } else {
+        x[i] = load_vec<DT, 8>(at, it < items ? p.K - k : 0);
+      }
     }
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {

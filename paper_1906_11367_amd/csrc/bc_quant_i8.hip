@@ -26,8 +26,16 @@ __global__ __launch_bounds__(256) void k_quant_rows(const char* src, long bs, lo
   const char* p = src + ((row / P) * bs + (row % P) * rs) * kBytes<DT>;
   auto load = [&](int k) { return load_vec<DT, 16>(p + (long)k * kBytes<DT>, K - k); };
   Raw<kWords<DT, 16>> x[kHeldPieces];
+  if (K >= kHeldPieces * kPiece) {   // all there, for every lane
 #pragma unroll
-  for (int i = 0; i < kHeldPieces; ++i) x[i] = load(k1 + i * kPiece);
+    for (int i = 0; i < kHeldPieces; ++i) x[i] = load_wide<DT, 16>(p + (long)(k1 + i * kPiece) * kBytes<DT>);
+  } else if (K == kPiece) {
+    x[0] = load_wide<DT, 16>(p + (long)k1 * kBytes<DT>);
+    x[1] = Raw<kWords<DT, 16>>{};
+  } else {
+#pragma unroll
+    for (int i = 0; i < kHeldPieces; ++i) x[i] = load(k1 + i * kPiece);
+  }
   uint32_t top = 0;
   auto note = [&](const Raw<kWords<DT, 16>>& r) {
 #pragma unroll

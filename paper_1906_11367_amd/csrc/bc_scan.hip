@@ -23,29 +23,30 @@ struct Cut {
   static constexpr int kV = V_, kGroups = G_, kThreads = NT_, kL = L_, kWavesPerSimd = W_;
   static constexpr int kSlab = kV * kGroups, kSlots = kThreads / kGroups, kTile = kSlots * kL, kWaves = kThreads / 64;
 };
-// Sequences of several tiles take the first cut; one tile takes the shortest
-// that holds it (a tile of 256 steps for a sequence of 4 would leave all but a
-// few lanes of the block idle).  Measured on 2^26 elements (bf16) and 2^25
-// (fp32) in chained tiles, us:
-//   forward, bf16: 4 channels x 8 steps a lane, 512 threads 100; 8 x 4 in 256
-//     threads 121; 2 x 16 99, 2 x 8 120, 8 x 8 150
-//   backward, bf16: 2 x 8 157-164; 4 x 4 178, 8 x 2 285, 2 x 16 186
-//   fp32: forward 4 x 4 in 512 threads 82-86 (256 threads 118, 4 x 8 87),
-//     backward 127-131 (256 threads 130, 2 x 8 129, 2 x 16 186)
+// Cut 0 is the chained tiles'.  A sequence of one tile takes the shortest cut
+// that holds it (a tile of 128 steps for a sequence of 4 would leave all but a
+// few lanes of the block idle): cut 2, cut 0, or the longer cut 1.
+// Measured on 2^26 elements (bf16) and 2^25 (fp32) in chained tiles, us, for 256
+// and for 16 chains:
+//   forward, bf16: 4 channels x 8 steps a lane in 256 threads 81, 94; in 512
+//     threads 90, 93; 8 x 4 in 512 107, 105
+//   backward, bf16: 2 x 8 in 512 threads 143, 159; in 256 140, 178; 4 x 4 in 512
+//     171, 180; 2 x 4 in 512 160, 193
+//   fp32: forward 4 x 4 in 512 threads 76, backward 127
 // Longer tiles cost registers (fewer waves), shorter ones more carries.
 template <int DT, int kSize> struct FwdCuts;
-template <> struct FwdCuts<kBF16, 0> { using type = Cut<4, 16, 512, 8, 4>; };   // 256 steps
-template <> struct FwdCuts<kBF16, 1> { using type = Cut<4, 16, 256, 8, 4>; };   // 128
+template <> struct FwdCuts<kBF16, 0> { using type = Cut<4, 16, 256, 8, 4>; };   // 128 steps
+template <> struct FwdCuts<kBF16, 1> { using type = Cut<4, 16, 512, 8, 4>; };   // 256
 template <> struct FwdCuts<kBF16, 2> { using type = Cut<4, 16, 64, 8, 4>; };    // 32
 template <> struct FwdCuts<kF32, 0> { using type = Cut<4, 8, 512, 4, 4>; };     // 256
-template <> struct FwdCuts<kF32, 1> { using type = Cut<4, 8, 256, 4, 4>; };     // 128
+template <> struct FwdCuts<kF32, 1> { using type = Cut<4, 8, 512, 4, 4>; };     // 256
 template <> struct FwdCuts<kF32, 2> { using type = Cut<4, 8, 64, 4, 4>; };      // 32
 template <int DT, int kSize> struct BwdCuts;
 template <> struct BwdCuts<kBF16, 0> { using type = Cut<2, 32, 512, 8, 4>; };   // 128
-template <> struct BwdCuts<kBF16, 1> { using type = Cut<2, 32, 256, 8, 4>; };   // 64
+template <> struct BwdCuts<kBF16, 1> { using type = Cut<2, 32, 512, 8, 4>; };   // 128
 template <> struct BwdCuts<kBF16, 2> { using type = Cut<2, 32, 64, 8, 4>; };    // 16
 template <> struct BwdCuts<kF32, 0> { using type = Cut<4, 8, 512, 4, 4>; };     // 256
-template <> struct BwdCuts<kF32, 1> { using type = Cut<4, 8, 256, 4, 4>; };     // 128
+template <> struct BwdCuts<kF32, 1> { using type = Cut<4, 8, 512, 4, 4>; };     // 256
 template <> struct BwdCuts<kF32, 2> { using type = Cut<4, 8, 64, 4, 4>; };      // 32
 template <int DT, int kSize> using FwdCut = typename FwdCuts<DT, kSize>::type;
 template <int DT, int kSize> using BwdCut = typename BwdCuts<DT, kSize>::type;
@@ -107,14 +108,15 @@ __device__ __forceinline__ void wave_suffix(const float (&A)[V], const float (&B
 // tile comes from the tiles before it in one launch: each publishes its pair
 // (A, B), and a block combines the pairs back to the start of its group of
 // kGroupTiles with the state published there (by the last block of the group
-// before).  A block waits only on lower tickets, drawn when a block starts,
-// whose owners are running and wait on still lower ones, so every wait ends;
+// before).  A block waits only on lower places of its chain, drawn as blocks
+// start, whose owners are running and wait on still lower ones: every wait ends;
 // which pairs are combined, and in which order, depends on the tile alone, so
 // results do not depend on the order in which blocks run.
 // A word carries its own validity: an 8-byte store is seen whole, and the
 // workspace is first filled with kEmpty, which no publisher writes.
 constexpr int kGroupTiles = 16;
 constexpr unsigned long long kEmpty = ~0ull;
+constexpr long kTicketWords = 16;   // a cache line for each counter
 // A bound on the polls (about a second), in case the caller lets two calls
 // share a workspace: the outputs are then NaN rather than never.
 constexpr int kMaxPolls = 1 << 20;
@@ -139,8 +141,7 @@ __device__ __forceinline__ float word_hi(unsigned long long w) { return __uint_a
 // group's is in its tile 0's pair).
 template <class X>
 struct Lookback {
-  static constexpr int kParts = X::kThreads / X::kSlab, kPer = kGroupTiles / kParts;
-  static_assert(kParts * kPer == kGroupTiles, "whole words per lane");
+  static constexpr int kParts = X::kThreads / X::kSlab, kPer = (kGroupTiles + kParts - 1) / kParts;
 
   // o: the tile's place in its chain; first: the chain's start; agg and pre:
   // this channel's words of the chain
@@ -181,20 +182,29 @@ struct Lookback {
   }
 };
 
-// Fills the words of a chained call (the ticket with them: it starts at -1).
+// Fills the words of a chained call (the counters with them: they start at -1).
 __global__ __launch_bounds__(256) void k_scan_clear(unsigned long long* ws, long words) {
   const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 2;
   if (i + 1 < words) *reinterpret_cast<ulonglong2*>(ws + i) = make_ulonglong2(kEmpty, kEmpty);
   else if (i < words) ws[i] = kEmpty;
 }
 
-// This block's place in the chain: tickets count through the units (a slab of
-// a sequence) of tile 0, then of tile 1, and so on.
-__device__ __forceinline__ int draw_ticket(unsigned* ticket) {
+// This block's unit (a slab of a sequence) and its place in the unit's chain, a
+// ticket drawn from the unit's own counter: one counter for all serialised the
+// blocks (about 15 ns a draw; with 8192 tiles 115 us instead of 90).  false: a
+// block past the end (the grid's last row).
+__device__ __forceinline__ bool draw_ticket(unsigned long long* tickets, int units, int tiles, int& unit, int& place) {
   __shared__ int t;
-  if (threadIdx.x == 0) t = (int)(atomicAdd(ticket, 1u) + 1u);
+  const long b = (long)blockIdx.y * gridDim.x + blockIdx.x;
+  unit = (int)(b % units);
+  // blocks go to the XCDs in turn: neighbouring slabs to one XCD
+  const int eighth = units >> 3;
+  if (unit < eighth * 8) unit = (unit & 7) * eighth + (unit >> 3);
+  if (b >= (long)units * tiles) return false;
+  if (threadIdx.x == 0) t = (int)(atomicAdd(reinterpret_cast<unsigned*>(tickets + (long)unit * kTicketWords), 1u) + 1u);
   __syncthreads();
-  return t;
+  place = t;
+  return true;
 }
 
 template <class X, int IN, int OUT, int FORM, bool kChain>
@@ -207,10 +217,7 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdA
   __shared__ float lookA[kParts][CW], lookB[kParts][CW];
   int unit = blockIdx.x, place = 0;
   if constexpr (kChain) {
-    const int t = draw_ticket(p.ticket), units = p.N * p.slabs;
-    unit = t % units;
-    place = t / units;
-    if (place >= p.tiles) return;   // the grid's last row
+    if (!draw_ticket(p.tickets, p.N * p.slabs, p.tiles, unit, place)) return;
   }
   const int n = unit / p.slabs, slab = unit % p.slabs;
   const int c0 = slab * CW + grp * V, avail = p.C - c0;   // <= 0: no channel here
@@ -227,12 +234,23 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdA
   }
   const int tile = place;
   const int t0 = tile * kTile + slot * L;
+  // every lane has all of its elements (else: past a sequence's end, or the
+  // last slab)
+  const bool whole = (tile + 1) * kTile <= len && (slab + 1) * CW <= p.C;
   Raw<kWords<IN, V>> g[L], x[L];
+  if (whole) {
 #pragma unroll
-  for (int i = 0; i < L; ++i) {
-    const int have = t0 + i < len ? avail : 0;
-    g[i] = t0 + i < len ? load_vec<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>, avail) : hold_gate<IN, FORM, V>();
-    x[i] = load_vec<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>, have);
+    for (int i = 0; i < L; ++i) {
+      g[i] = load_wide<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>);
+      x[i] = load_wide<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const bool on = t0 + i < len;
+      g[i] = on ? load_vec<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>, avail) : hold_gate<IN, FORM, V>();
+      x[i] = load_vec<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>, on ? avail : 0);
+    }
   }
   float a[L][V], b[L][V], A[V], B[V];
 #pragma unroll
@@ -305,7 +323,8 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdA
 #pragma unroll
     for (int k = 0; k < V; ++k) h[k] = __fmaf_rn(a[i][k], h[k], b[i][k]);
     char* at = yp + (long)(t0 + i) * p.C * kBytes<OUT>;
-    if (t0 + i < len) store_vec<OUT, V>(at, avail, h, p.stream);
+    if (whole) store_wide<OUT, V>(at, h, p.stream);
+    else if (t0 + i < len) store_vec<OUT, V>(at, avail, h);
     else if (t0 + i < p.T) store_zero<OUT, V>(at, avail);
   }
   if (kChain && place + 1 < p.tiles) return;
@@ -323,10 +342,7 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_bwd(BwdA
   __shared__ float lookA[kParts][CW], lookB[kParts][CW];
   int unit = blockIdx.x, place = 0;
   if constexpr (kChain) {
-    const int t = draw_ticket(p.ticket), units = p.N * p.slabs;
-    unit = t % units;
-    place = t / units;
-    if (place >= p.tiles) return;   // the grid's last row
+    if (!draw_ticket(p.tickets, p.N * p.slabs, p.tiles, unit, place)) return;
   }
   const int n = unit / p.slabs, slab = unit % p.slabs;
   const int c0 = slab * CW + grp * V, avail = p.C - c0;
@@ -345,17 +361,28 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_bwd(BwdA
   }
   const int o = place, tile = p.tiles - 1 - o;   // the chain runs backwards in time
   const int t0 = tile * kTile + slot * L;
+  const bool whole = (tile + 1) * kTile <= len && (slab + 1) * CW <= p.C;
   Raw<kWords<IN, V>> g[L], x[L], d[L];
+  Raw<V> st;   // the state before the tile, kept by the forward
+  const char* sp = reinterpret_cast<const char*>(p.states + ((size_t)n * S + tile * kTile / kScanSpan) * p.C + c0);
+  if (whole) {
 #pragma unroll
-  for (int i = 0; i < L; ++i) {
-    const int have = t0 + i < len ? avail : 0;
-    g[i] = t0 + i < len ? load_vec<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>, avail) : hold_gate<IN, FORM, V>();
-    x[i] = load_vec<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>, have);
-    d[i] = load_vec<IN, V>(gy + (long)(t0 + i) * p.C * kBytes<IN>, have);
+    for (int i = 0; i < L; ++i) {
+      g[i] = load_wide<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>);
+      x[i] = load_wide<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>);
+      d[i] = load_wide<IN, V>(gy + (long)(t0 + i) * p.C * kBytes<IN>);
+    }
+    st = load_wide<kF32, V>(sp);
+  } else {
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const bool on = t0 + i < len;
+      g[i] = on ? load_vec<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>, avail) : hold_gate<IN, FORM, V>();
+      x[i] = load_vec<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>, on ? avail : 0);
+      d[i] = load_vec<IN, V>(gy + (long)(t0 + i) * p.C * kBytes<IN>, on ? avail : 0);
+    }
+    st = load_vec<kF32, V>(sp, avail);
   }
-  // the state before the tile, kept by the forward
-  const Raw<V> st = load_vec<kF32, V>(
-      reinterpret_cast<const char*>(p.states + ((size_t)n * S + tile * kTile / kScanSpan) * p.C + c0), avail);
   float a[L][V], c[L][V], A[V], B[V], R[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) { A[k] = 1.f; B[k] = 0.f; R[k] = 0.f; }
@@ -452,9 +479,12 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_bwd(BwdA
       r[k] = a[i][k] * delta;
     }
     char *gat = ggate + (long)(t0 + i) * p.grs * kBytes<OUT>, *xat = gx + (long)(t0 + i) * p.grs * kBytes<OUT>;
-    if (t0 + i < len) {
-      store_vec<OUT, V>(gat, avail, og, p.stream);
-      store_vec<OUT, V>(xat, avail, ox, p.stream);
+    if (whole) {
+      store_wide<OUT, V>(gat, og, p.stream);
+      store_wide<OUT, V>(xat, ox, p.stream);
+    } else if (t0 + i < len) {
+      store_vec<OUT, V>(gat, avail, og);
+      store_vec<OUT, V>(xat, avail, ox);
     } else if (t0 + i < p.T) {
       store_zero<OUT, V>(gat, avail);
       store_zero<OUT, V>(xat, avail);
@@ -482,9 +512,19 @@ __global__ __launch_bounds__(256) void k_scan_step(const char* gate, const char*
 #pragma unroll
   for (int k = 0; k < V; ++k) h[k] = 0.f;
   if (live) {
-    const auto g = load_vec<IN, V>(gate + ((long)n * rs + c0) * kBytes<IN>, avail);
-    const auto xv = load_vec<IN, V>(x + ((long)n * rs + c0) * kBytes<IN>, avail);
-    const auto st = load_vec<kF32, V>(reinterpret_cast<const char*>(state + (size_t)s * C + c0), avail);
+    const char *gp = gate + ((long)n * rs + c0) * kBytes<IN>, *xp = x + ((long)n * rs + c0) * kBytes<IN>;
+    const char* sp = reinterpret_cast<const char*>(state + (size_t)s * C + c0);
+    Raw<kWords<IN, V>> g, xv;
+    Raw<V> st;
+    if (C % V == 0) {
+      g = load_wide<IN, V>(gp);
+      xv = load_wide<IN, V>(xp);
+      st = load_wide<kF32, V>(sp);
+    } else {
+      g = load_vec<IN, V>(gp, avail);
+      xv = load_vec<IN, V>(xp, avail);
+      st = load_vec<kF32, V>(sp, avail);
+    }
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       float a, c;
@@ -496,32 +536,29 @@ __global__ __launch_bounds__(256) void k_scan_step(const char* gate, const char*
   store_vec<IN, V>(y + ((long)n * C + c0) * kBytes<IN>, avail, h);
 }
 
-// How a call on token sequences is divided, and its workspace: the ticket (in
-// 256 bytes of its own), a word per channel and tile, and one per channel and
-// group.
+// How a call on token sequences is divided, and its workspace: the units'
+// counters, a word per channel and tile, and one per channel and group.
 struct Plan { int size, slab, slabs, tiles, groups; long words; };   // words > 0: chained
-constexpr long kTicketWords = 32;
 
-template <template <int, int> class Cuts>
-struct Tiles {
-  // the cut of a call, and the steps of its tile
-  static int size(int in_dt, int T) {
-    const bool b = in_dt == kBF16;
-    if (T <= (b ? Cuts<kBF16, 2>::type::kTile : Cuts<kF32, 2>::type::kTile)) return 2;
-    return T <= (b ? Cuts<kBF16, 1>::type::kTile : Cuts<kF32, 1>::type::kTile) ? 1 : 0;
-  }
-  static int steps(int in_dt) { return in_dt == kBF16 ? Cuts<kBF16, 0>::type::kTile : Cuts<kF32, 0>::type::kTile; }
-};
+// The cut of a call: the smallest whose tile holds the sequence.
+template <template <int, int> class Cuts, int DT>
+Plan cut_of(int T) {
+  using X0 = typename Cuts<DT, 0>::type;
+  using X1 = typename Cuts<DT, 1>::type;
+  using X2 = typename Cuts<DT, 2>::type;
+  Plan q{};
+  q.size = T <= X2::kTile ? 2 : T > X0::kTile && T <= X1::kTile ? 1 : 0;
+  q.slab = q.size == 2 ? X2::kSlab : q.size == 1 ? X1::kSlab : X0::kSlab;
+  q.tiles = q.size > 0 ? 1 : (T + X0::kTile - 1) / X0::kTile;   // more than one: chained
+  return q;
+}
 
 Plan make_plan(bool bwd, int N, int T, int C, int in_dt) {
-  const int tile = bwd ? Tiles<BwdCuts>::steps(in_dt) : Tiles<FwdCuts>::steps(in_dt);
-  Plan q{};
-  q.size = bwd ? Tiles<BwdCuts>::size(in_dt, T) : Tiles<FwdCuts>::size(in_dt, T);
-  q.slab = 128 / (in_dt == kBF16 ? 2 : 4);   // all cuts alike
+  Plan q = in_dt == kBF16 ? (bwd ? cut_of<BwdCuts, kBF16>(T) : cut_of<FwdCuts, kBF16>(T))
+                          : (bwd ? cut_of<BwdCuts, kF32>(T) : cut_of<FwdCuts, kF32>(T));
   q.slabs = (C + q.slab - 1) / q.slab;
-  q.tiles = (T + tile - 1) / tile;
   q.groups = (q.tiles + kGroupTiles - 1) / kGroupTiles;
-  q.words = q.tiles > 1 ? kTicketWords + (long)N * q.slabs * q.slab * ((long)q.tiles + q.groups) : 0;
+  q.words = q.tiles > 1 ? (long)N * q.slabs * (kTicketWords + q.slab * ((long)q.tiles + q.groups)) : 0;
   return q;
 }
 
@@ -539,9 +576,10 @@ hipError_t start(Args& p, const Plan& q, void* ws, hipStream_t s) {
   p.groups = q.groups;
   if (q.words == 0) return hipSuccess;
   unsigned long long* w = static_cast<unsigned long long*>(ws);
-  p.ticket = reinterpret_cast<unsigned*>(w);
-  p.agg = w + kTicketWords;
-  p.pre = p.agg + (long)p.N * p.slabs * q.tiles * q.slab;
+  const long units = (long)p.N * p.slabs;
+  p.tickets = w;
+  p.agg = w + units * kTicketWords;
+  p.pre = p.agg + units * q.tiles * q.slab;
   hipLaunchKernelGGL(k_scan_clear, dim3((unsigned)((q.words / 2 + 256) / 256)), dim3(256), 0, s, w, q.words);
   return hipGetLastError();
 }

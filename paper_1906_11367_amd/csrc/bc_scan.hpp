@@ -35,13 +35,22 @@ template <int DT, int V> constexpr int kWords = V * kBytes<DT> / 4;
 // one wide access at that alignment, which global memory allows here.
 template <int N, int kAlign> struct __attribute__((packed, aligned(kAlign))) Loose { uint32_t w[N]; };
 
+// V elements from p.
+template <int DT, int V>
+__device__ __forceinline__ Raw<kWords<DT, V>> load_wide(const char* p) {
+  return __builtin_bit_cast(Raw<kWords<DT, V>>, *reinterpret_cast<const Loose<kWords<DT, V>, kBytes<DT>>*>(p));
+}
+
 // V elements from p, of which the first `avail` exist (the rest read as zero).
+// Loads that are to be in flight together do not come through here: the short
+// form writes the registers of the wide one, which first has to arrive.  They
+// are load_wide in a branch that all lanes of the block take.
 template <int DT, int V>
 __device__ __forceinline__ Raw<kWords<DT, V>> load_vec(const char* p, int avail) {
   constexpr int W = kWords<DT, V>;
   Raw<W> r;
   if (avail >= V) {
-    r = __builtin_bit_cast(Raw<W>, *reinterpret_cast<const Loose<W, kBytes<DT>>*>(p));
+    r = load_wide<DT, V>(p);
   } else {
 #pragma unroll
     for (int k = 0; k < W; ++k) {
@@ -69,22 +78,37 @@ __device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
   return (uint32_t)__builtin_bit_cast(uint16_t, a) | ((uint32_t)__builtin_bit_cast(uint16_t, b) << 16);
 }
 
-// stream: past the caches (whole cache lines of large tensors; see streams()).
 template <int DT, int V>
-__device__ __forceinline__ void store_vec(char* p, int avail, const float (&v)[V], bool stream = false) {
-  constexpr int W = kWords<DT, V>;
-  Raw<W> r;
+__device__ __forceinline__ Raw<kWords<DT, V>> rounded(const float (&v)[V]) {
+  Raw<kWords<DT, V>> r;
 #pragma unroll
-  for (int k = 0; k < W; ++k) {
+  for (int k = 0; k < kWords<DT, V>; ++k) {
     if constexpr (DT == kBF16) r[k] = pair_bf16(v[2 * k], v[2 * k + 1]);
     else r[k] = __float_as_uint(v[k]);
   }
-  if (avail >= V && stream) {
+  return r;
+}
+
+// stream: past the caches (see streams()).
+template <int DT, int V>
+__device__ __forceinline__ void store_wide(char* p, const float (&v)[V], bool stream) {
+  constexpr int W = kWords<DT, V>;
+  const Raw<W> r = rounded<DT, V>(v);
+  if (stream) {
     typedef Raw<W> Any __attribute__((aligned(kBytes<DT>)));
     asm volatile("");   // keeps the compiler from merging the two stores into a plain one
     __builtin_nontemporal_store(r, reinterpret_cast<Any*>(p));
     asm volatile("");
-  } else if (avail >= V) {
+  } else {
+    *reinterpret_cast<Loose<W, kBytes<DT>>*>(p) = __builtin_bit_cast(Loose<W, kBytes<DT>>, r);
+  }
+}
+
+template <int DT, int V>
+__device__ __forceinline__ void store_vec(char* p, int avail, const float (&v)[V]) {
+  constexpr int W = kWords<DT, V>;
+  const Raw<W> r = rounded<DT, V>(v);
+  if (avail >= V) {
     *reinterpret_cast<Loose<W, kBytes<DT>>*>(p) = __builtin_bit_cast(Loose<W, kBytes<DT>>, r);
   } else {
 #pragma unroll
@@ -155,8 +179,7 @@ struct FwdArgs {
   int N, T, C;
   int slabs, tiles, groups;   // tokens: channel slabs, tiles of time steps, groups of tiles
   bool stream;              // y past the caches
-  unsigned* ticket;         // chained: see bc_scan.hip
-  unsigned long long *agg, *pre;
+  unsigned long long *tickets, *agg, *pre;   // chained: see bc_scan.hip
 };
 
 struct BwdArgs {
@@ -172,8 +195,7 @@ struct BwdArgs {
   int N, T, C;
   int slabs, tiles, groups;
   bool stream;              // ggate and gx past the caches
-  unsigned* ticket;
-  unsigned long long *agg, *pre;
+  unsigned long long *tickets, *agg, *pre;
 };
 
 __device__ __forceinline__ int seq_len(const int* lengths, int n, int T) {

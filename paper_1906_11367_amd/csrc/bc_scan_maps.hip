@@ -66,8 +66,15 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_fwd_maps(FwdArgs p) 
   int q = 0;
   for (int s0 = 0; s0 < S; s0 += W, q ^= 1) {
     const int t0 = (s0 + w) * Seg + lane * V;
-    const auto g = load_vec<IN, V>(gate + (long)t0 * kBytes<IN>, len - t0);
-    const auto x = load_vec<IN, V>(xp + (long)t0 * kBytes<IN>, len - t0);
+    const bool whole = (s0 + w + 1) * Seg <= len;   // for every lane
+    Raw<kWords<IN, V>> g, x;
+    if (whole) {
+      g = load_wide<IN, V>(gate + (long)t0 * kBytes<IN>);
+      x = load_wide<IN, V>(xp + (long)t0 * kBytes<IN>);
+    } else {
+      g = load_vec<IN, V>(gate + (long)t0 * kBytes<IN>, len - t0);
+      x = load_vec<IN, V>(xp + (long)t0 * kBytes<IN>, len - t0);
+    }
     float a[V], b[V], A = 1.f, B = 0.f, eA, eB;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
@@ -97,7 +104,8 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_fwd_maps(FwdArgs p) 
       h = __fmaf_rn(a[k], h, b[k]);
       o[k] = t0 + k < len ? h : 0.f;
     }
-    store_vec<OUT, V>(yp + (long)t0 * kBytes<OUT>, p.T - t0, o, p.stream);
+    if (whole) store_wide<OUT, V>(yp + (long)t0 * kBytes<OUT>, o, p.stream);
+    else store_vec<OUT, V>(yp + (long)t0 * kBytes<OUT>, p.T - t0, o);
   }
   if (p.h_last && w == 0 && lane == 0) p.h_last[row] = carry;
 }
@@ -121,9 +129,17 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_bwd_maps(BwdArgs p) 
   int q = 0;
   for (int s0 = (S - 1) / W * W; s0 >= 0; s0 -= W, q ^= 1) {
     const int t0 = (s0 + w) * Seg + lane * V;
-    const auto g = load_vec<IN, V>(gate + (long)t0 * kBytes<IN>, len - t0);
-    const auto xr = load_vec<IN, V>(xp + (long)t0 * kBytes<IN>, len - t0);
-    const auto dr = load_vec<IN, V>(gy + (long)t0 * kBytes<IN>, len - t0);
+    const bool whole = (s0 + w + 1) * Seg <= len;
+    Raw<kWords<IN, V>> g, xr, dr;
+    if (whole) {
+      g = load_wide<IN, V>(gate + (long)t0 * kBytes<IN>);
+      xr = load_wide<IN, V>(xp + (long)t0 * kBytes<IN>);
+      dr = load_wide<IN, V>(gy + (long)t0 * kBytes<IN>);
+    } else {
+      g = load_vec<IN, V>(gate + (long)t0 * kBytes<IN>, len - t0);
+      xr = load_vec<IN, V>(xp + (long)t0 * kBytes<IN>, len - t0);
+      dr = load_vec<IN, V>(gy + (long)t0 * kBytes<IN>, len - t0);
+    }
     const float st = s0 + w < S ? p.states[row * S + s0 + w] : 0.f;
     float a[V], cx[V], h[V], A = 1.f, B = 0.f, R = 0.f, eA, eB, sA, sB;
 #pragma unroll
@@ -167,8 +183,13 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_bwd_maps(BwdArgs p) 
       r = a[k] * delta;
       if (t0 + k >= len) og[k] = ox[k] = 0.f;
     }
-    store_vec<OUT, V>(ggate + (long)t0 * kBytes<OUT>, p.T - t0, og, p.stream);
-    store_vec<OUT, V>(gx + (long)t0 * kBytes<OUT>, p.T - t0, ox, p.stream);
+    if (whole) {
+      store_wide<OUT, V>(ggate + (long)t0 * kBytes<OUT>, og, p.stream);
+      store_wide<OUT, V>(gx + (long)t0 * kBytes<OUT>, ox, p.stream);
+    } else {
+      store_vec<OUT, V>(ggate + (long)t0 * kBytes<OUT>, p.T - t0, og);
+      store_vec<OUT, V>(gx + (long)t0 * kBytes<OUT>, p.T - t0, ox);
+    }
   }
   if (p.gh0 && w == 0 && lane == 0) p.gh0[row] = carry;
 }
