@@ -568,11 +568,12 @@ def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, y:
     what = "gated_scan_step"
     if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype not in _FLOATS:
         raise BoxConvError(f"{what}: x must be a 2-D fp32 or bf16 tensor")
-    N, C = x.shape
     if gate is None or state is None or y is None:
         raise BoxConvError(f"{what}: gate, state and y must be tensors")
-    _need(gate, x.shape, x.dtype, what, "gate")
-    _need(y, x.shape, x.dtype, what, "y")
+    shape, dtype = x.shape, x.dtype
+    N, C = shape
+    _need(gate, shape, dtype, what, "gate")
+    _need(y, shape, dtype, what, "y")
     S = state.shape[0] if isinstance(state, torch.Tensor) and state.dim() == 2 else None
     _need(state, (S, C), _F32, what, "state")
     _need(state_out, (S, C), _F32, what, "state_out")
@@ -580,13 +581,15 @@ def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, y:
     if not gate.is_cuda or not x.is_cuda:
         raise BoxConvError("tensors must be on the GPU")
     gs, xs = gate.stride(), x.stride()
-    rs = xs[0] if N > 1 else C
-    if (N > 1 and gs[0] != rs) or (C > 1 and (gs[1] != 1 or xs[1] != 1)):
+    if N > 1 and gs[0] != xs[0] or C > 1 and (gs[1] != 1 or xs[1] != 1):
         raise BoxConvError(f"{what}: gate and x must be contiguous in their last dimension and of the same strides")
     sp = _ptr(state)
-    _check(load_library().gated_scan_step(gate.data_ptr(), x.data_ptr(), _CODES[x.dtype], rs, sp,
-                                          sp if state_out is None else _ptr(state_out), _ptr(slots), _ptr(y), N, C, S,
-                                          form, _stream()), what)
+    lib = _lib or load_library()
+    st = lib.gated_scan_step(gate.data_ptr(), x.data_ptr(), _CODES[dtype], xs[0] if N > 1 else C, sp,
+                              sp if state_out is None else _ptr(state_out), _ptr(slots), _ptr(y), N, C, S, form,
+                              _stream())
+    if st:
+        _check(st, what)
     return y
 
 
@@ -684,11 +687,13 @@ def pointwise_mix_i8(wq: torch.Tensor, w_scale: torch.Tensor, x: torch.Tensor, o
             raise BoxConvError(f"{what}: out has shape {tuple(shape)}, expected {N * P} tokens of {M}")
     elif len(shape) not in (3, 4) or shape[0] != N or shape[1] != M or out.numel() != N * M * P:
         raise BoxConvError(f"{what}: out has shape {tuple(shape)}, expected {(N, M, P)}")
-    lib = load_library()
+    lib = _lib or load_library()
     dt = _CODES[x.dtype]
     if ws is None:
         ws = _workspace(lib.bc_mix_i8_workspace_bytes(N, M, K, P, dt, layout), x.device)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check(lib.pointwise_mix_i8(_ptr(wq), _ptr(w_scale), xp, dt, bs, rs, _ptr(x_scale), _ptr(bias), _ptr(out),
-                                _CODES[out.dtype], N, M, K, P, relu, layout, _ptr(ws), nbytes, _stream()), what)
+    st = lib.pointwise_mix_i8(_ptr(wq), _ptr(w_scale), xp, dt, bs, rs, _ptr(x_scale), _ptr(bias), _ptr(out),
+                              _CODES[out.dtype], N, M, K, P, relu, layout, _ptr(ws), nbytes, _stream())
+    if st:
+        _check(st, what)
     return out
