@@ -24,8 +24,8 @@ struct Cut {
   static constexpr int kSlab = kV * kGroups, kSlots = kThreads / kGroups, kTile = kSlots * kL, kWaves = kThreads / 64;
 };
 // Cut 0 is the chained tiles'.  A sequence of one tile takes the shortest cut
-// that holds it (a tile of 128 steps for a sequence of 4 would leave all but a
-// few lanes of the block idle): cut 2, cut 0, or the longer cut 1.
+// that holds it: a tile of 128 steps for a sequence of 4 would leave all but a
+// few lanes of the block idle (256 x 8 x 4096 bf16 forward: 31 us instead of 8).
 // Measured on 2^26 elements (bf16) and 2^25 (fp32) in chained tiles, us, for 256
 // and for 16 chains:
 //   forward, bf16: 4 channels x 8 steps a lane in 256 threads 81, 94; in 512
@@ -34,24 +34,32 @@ struct Cut {
 //     171, 180; 2 x 4 in 512 160, 193
 //   fp32: forward 4 x 4 in 512 threads 76, backward 127
 // Longer tiles cost registers (fewer waves), shorter ones more carries.
-template <int DT, int kSize> struct FwdCuts;
-template <> struct FwdCuts<kBF16, 0> { using type = Cut<4, 16, 256, 8, 4>; };   // 128 steps
-template <> struct FwdCuts<kBF16, 1> { using type = Cut<4, 16, 512, 8, 4>; };   // 256
-template <> struct FwdCuts<kBF16, 2> { using type = Cut<4, 16, 64, 8, 4>; };    // 32
-template <> struct FwdCuts<kF32, 0> { using type = Cut<4, 8, 512, 4, 4>; };     // 256
-template <> struct FwdCuts<kF32, 1> { using type = Cut<4, 8, 512, 4, 4>; };     // 256
-template <> struct FwdCuts<kF32, 2> { using type = Cut<4, 8, 64, 4, 4>; };      // 32
-template <int DT, int kSize> struct BwdCuts;
-template <> struct BwdCuts<kBF16, 0> { using type = Cut<2, 32, 512, 8, 4>; };   // 128
-template <> struct BwdCuts<kBF16, 1> { using type = Cut<2, 32, 512, 8, 4>; };   // 128
-template <> struct BwdCuts<kBF16, 2> { using type = Cut<2, 32, 64, 8, 4>; };    // 16
-template <> struct BwdCuts<kF32, 0> { using type = Cut<4, 8, 512, 4, 4>; };     // 256
-template <> struct BwdCuts<kF32, 1> { using type = Cut<4, 8, 512, 4, 4>; };     // 256
-template <> struct BwdCuts<kF32, 2> { using type = Cut<4, 8, 64, 4, 4>; };      // 32
-template <int DT, int kSize> using FwdCut = typename FwdCuts<DT, kSize>::type;
-template <int DT, int kSize> using BwdCut = typename BwdCuts<DT, kSize>::type;
+template <class... Xs> struct CutList {};
+template <int DT> struct FwdCuts;   // the chained cut, then the others' tiles in rising order
+template <> struct FwdCuts<kBF16> {
+  using chained = Cut<4, 16, 256, 8, 4>;   // 128 steps
+  using list = CutList<Cut<4, 64, 64, 8, 4>, Cut<4, 16, 64, 8, 4>, Cut<4, 16, 128, 8, 4>, chained,
+                       Cut<4, 16, 512, 8, 4>>;   // 8, 32, 64, 128, 256
+};
+template <> struct FwdCuts<kF32> {
+  using chained = Cut<4, 8, 512, 4, 4>;   // 256
+  using list = CutList<Cut<4, 64, 64, 8, 4>, Cut<4, 8, 64, 4, 4>, Cut<4, 8, 128, 4, 4>, Cut<4, 8, 256, 4, 4>,
+                       chained>;   // 8, 32, 64, 128, 256
+};
+template <int DT> struct BwdCuts;
+template <> struct BwdCuts<kBF16> {
+  using chained = Cut<2, 32, 512, 8, 4>;   // 128
+  using list = CutList<Cut<2, 64, 64, 8, 4>, Cut<2, 32, 64, 8, 4>, Cut<2, 32, 128, 8, 4>, Cut<2, 32, 256, 8, 4>,
+                       chained>;   // 8, 16, 32, 64, 128
+};
+template <> struct BwdCuts<kF32> {
+  using chained = Cut<4, 8, 512, 4, 4>;   // 256
+  using list = CutList<Cut<4, 64, 64, 4, 4>, Cut<4, 8, 64, 4, 4>, Cut<4, 8, 128, 4, 4>, Cut<4, 8, 256, 4, 4>,
+                       chained>;   // 4, 32, 64, 128, 256
+};
 // States are kept every kScanSpan steps: at every tile of the chained backward.
-static_assert(BwdCut<kBF16, 0>::kTile % kScanSpan == 0 && BwdCut<kF32, 0>::kTile % kScanSpan == 0, "kept states");
+static_assert(BwdCuts<kBF16>::chained::kTile % kScanSpan == 0 && BwdCuts<kF32>::chained::kTile % kScanSpan == 0,
+              "kept states");
 
 // (A, B) of the runs of lower slots of this wave (identity for the first), and
 // the inclusive pair.  Slots are kGroups lanes apart.
@@ -234,9 +242,10 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdA
   }
   const int tile = place;
   const int t0 = tile * kTile + slot * L;
-  // every lane has all of its elements (else: past a sequence's end, or the
-  // last slab)
+  // every lane has all of its elements, or none of a step's (past a sequence's
+  // end, past the channels), or a part of them (the last channels)
   const bool whole = (tile + 1) * kTile <= len && (slab + 1) * CW <= p.C;
+  const bool vectors = p.C % V == 0 || (slab + 1) * CW <= p.C;
   Raw<kWords<IN, V>> g[L], x[L];
   if (whole) {
 #pragma unroll
@@ -244,6 +253,18 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdA
       g[i] = load_wide<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>);
       x[i] = load_wide<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>);
     }
+  } else if (vectors) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      g[i] = hold_gate<IN, FORM, V>();
+      x[i] = Raw<kWords<IN, V>>{};
+    }
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (t0 + i < len && avail > 0) {
+        g[i] = load_wide<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>);
+        x[i] = load_wide<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>);
+      }
   } else {
 #pragma unroll
     for (int i = 0; i < L; ++i) {
@@ -324,7 +345,7 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdA
     for (int k = 0; k < V; ++k) h[k] = __fmaf_rn(a[i][k], h[k], b[i][k]);
     char* at = yp + (long)(t0 + i) * p.C * kBytes<OUT>;
     if (whole) store_wide<OUT, V>(at, h, p.stream);
-    else if (t0 + i < len) store_vec<OUT, V>(at, avail, h);
+    else if (t0 + i < len) store_vec<OUT, V>(at, avail, h);   // avail <= 0: nothing
     else if (t0 + i < p.T) store_zero<OUT, V>(at, avail);
   }
   if (kChain && place + 1 < p.tiles) return;
@@ -362,6 +383,7 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_bwd(BwdA
   const int o = place, tile = p.tiles - 1 - o;   // the chain runs backwards in time
   const int t0 = tile * kTile + slot * L;
   const bool whole = (tile + 1) * kTile <= len && (slab + 1) * CW <= p.C;
+  const bool vectors = p.C % V == 0 || (slab + 1) * CW <= p.C;
   Raw<kWords<IN, V>> g[L], x[L], d[L];
   Raw<V> st;   // the state before the tile, kept by the forward
   const char* sp = reinterpret_cast<const char*>(p.states + ((size_t)n * S + tile * kTile / kScanSpan) * p.C + c0);
@@ -373,6 +395,21 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_bwd(BwdA
       d[i] = load_wide<IN, V>(gy + (long)(t0 + i) * p.C * kBytes<IN>);
     }
     st = load_wide<kF32, V>(sp);
+  } else if (vectors) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      g[i] = hold_gate<IN, FORM, V>();
+      x[i] = d[i] = Raw<kWords<IN, V>>{};
+    }
+    st = Raw<V>{};
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (t0 + i < len && avail > 0) {
+        g[i] = load_wide<IN, V>(gate + (long)(t0 + i) * p.rs * kBytes<IN>);
+        x[i] = load_wide<IN, V>(xp + (long)(t0 + i) * p.rs * kBytes<IN>);
+        d[i] = load_wide<IN, V>(gy + (long)(t0 + i) * p.C * kBytes<IN>);
+      }
+    if (avail > 0) st = load_wide<kF32, V>(sp);
   } else {
 #pragma unroll
     for (int i = 0; i < L; ++i) {
@@ -536,93 +573,82 @@ __global__ __launch_bounds__(256) void k_scan_step(const char* gate, const char*
   store_vec<IN, V>(y + ((long)n * C + c0) * kBytes<IN>, avail, h);
 }
 
-// How a call on token sequences is divided, and its workspace: the units'
+// How a call on token sequences is divided, and its workspace: the chains'
 // counters, a word per channel and tile, and one per channel and group.
-struct Plan { int size, slab, slabs, tiles, groups; long words; };   // words > 0: chained
+struct Plan { int slab, tiles; long units, words; };   // words > 0: chained
 
-// The cut of a call: the smallest whose tile holds the sequence.
-template <template <int, int> class Cuts, int DT>
-Plan cut_of(int T) {
-  using X0 = typename Cuts<DT, 0>::type;
-  using X1 = typename Cuts<DT, 1>::type;
-  using X2 = typename Cuts<DT, 2>::type;
+template <class X>
+Plan plan_of(int N, int T, int C) {
   Plan q{};
-  q.size = T <= X2::kTile ? 2 : T > X0::kTile && T <= X1::kTile ? 1 : 0;
-  q.slab = q.size == 2 ? X2::kSlab : q.size == 1 ? X1::kSlab : X0::kSlab;
-  q.tiles = q.size > 0 ? 1 : (T + X0::kTile - 1) / X0::kTile;   // more than one: chained
+  q.slab = X::kSlab;
+  q.tiles = (T + X::kTile - 1) / X::kTile;
+  q.units = (long)N * ((C + X::kSlab - 1) / X::kSlab);
+  const int groups = (q.tiles + kGroupTiles - 1) / kGroupTiles;
+  if (q.tiles > 1) q.words = q.units * (kTicketWords + q.slab * ((long)q.tiles + groups));
   return q;
 }
 
-Plan make_plan(bool bwd, int N, int T, int C, int in_dt) {
-  Plan q = in_dt == kBF16 ? (bwd ? cut_of<BwdCuts, kBF16>(T) : cut_of<FwdCuts, kBF16>(T))
-                          : (bwd ? cut_of<BwdCuts, kF32>(T) : cut_of<FwdCuts, kF32>(T));
-  q.slabs = (C + q.slab - 1) / q.slab;
-  q.groups = (q.tiles + kGroupTiles - 1) / kGroupTiles;
-  q.words = q.tiles > 1 ? (long)N * q.slabs * (kTicketWords + q.slab * ((long)q.tiles + q.groups)) : 0;
-  return q;
+// Calls f with the cut of a sequence of T steps: the first of the list that
+// holds it, or the chained one.
+template <class Chained, class F, class X, class... Xs>
+auto with_cut(int T, F f, CutList<X, Xs...>) {
+  if (T <= X::kTile) return f(X{});
+  if constexpr (sizeof...(Xs) > 0) return with_cut<Chained>(T, f, CutList<Xs...>{});
+  else return f(Chained{});
+}
+template <class Cuts, class F>
+auto with_cut(int T, F f) { return with_cut<typename Cuts::chained>(T, f, typename Cuts::list{}); }
+
+template <class Cuts>
+size_t words_of(int N, int T, int C) {
+  return (size_t)with_cut<Cuts>(T, [&](auto x) { return plan_of<decltype(x)>(N, T, C).words; });
 }
 
-// Grids of at most 2^32 threads along x; a chained block past the end has no
-// ticket to serve.  (One tile: at most 2^21 blocks, one row.)
-dim3 blocks(long n) {
-  const long x = std::min(n, 1L << 22);
-  return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
-}
-
-template <class Args>
-hipError_t start(Args& p, const Plan& q, void* ws, hipStream_t s) {
-  p.slabs = q.slabs;
+// Launches the kernel of a cut; chained ones after a fill of their words.  A
+// grid has at most 2^32 threads along x; chained blocks past the end return.
+template <class X, class Args, class Chained, class Single>
+hipError_t launch_cut(Args& p, Chained chained, Single single, void* ws, hipStream_t s) {
+  const Plan q = plan_of<X>(p.N, p.T, p.C);
+  p.slabs = (int)(q.units / p.N);
   p.tiles = q.tiles;
-  p.groups = q.groups;
-  if (q.words == 0) return hipSuccess;
+  p.groups = (q.tiles + kGroupTiles - 1) / kGroupTiles;
+  if (q.words == 0) {
+    hipLaunchKernelGGL(single, dim3((unsigned)q.units), dim3(X::kThreads), 0, s, p);
+    return hipGetLastError();
+  }
   unsigned long long* w = static_cast<unsigned long long*>(ws);
-  const long units = (long)p.N * p.slabs;
   p.tickets = w;
-  p.agg = w + units * kTicketWords;
-  p.pre = p.agg + units * q.tiles * q.slab;
+  p.agg = w + q.units * kTicketWords;
+  p.pre = p.agg + q.units * q.tiles * q.slab;
   hipLaunchKernelGGL(k_scan_clear, dim3((unsigned)((q.words / 2 + 256) / 256)), dim3(256), 0, s, w, q.words);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const long blocks = q.units * q.tiles, x = std::min(blocks, 1L << 22);
+  hipLaunchKernelGGL(chained, dim3((unsigned)x, (unsigned)((blocks + x - 1) / x)), dim3(X::kThreads), 0, s, p);
   return hipGetLastError();
 }
 
 template <int IN, int OUT, int FORM>
 hipError_t fwd_form(FwdArgs& p, void* ws, hipStream_t s) {
-  const Plan q = make_plan(false, p.N, p.T, p.C, IN);
-  const hipError_t e = start(p, q, ws, s);
-  if (e != hipSuccess) return e;
-  auto go = [&](auto kernel, int threads) {
-    hipLaunchKernelGGL(kernel, blocks((long)p.N * p.slabs * p.tiles), dim3(threads), 0, s, p);
-  };
-  using X0 = FwdCut<IN, 0>;
-  using X1 = FwdCut<IN, 1>;
-  using X2 = FwdCut<IN, 2>;
-  if (q.words > 0) go(k_scan_fwd<X0, IN, OUT, FORM, true>, X0::kThreads);
-  else if (q.size == 0) go(k_scan_fwd<X0, IN, OUT, FORM, false>, X0::kThreads);
-  else if (q.size == 1) go(k_scan_fwd<X1, IN, OUT, FORM, false>, X1::kThreads);
-  else go(k_scan_fwd<X2, IN, OUT, FORM, false>, X2::kThreads);
-  return hipGetLastError();
+  using Chained = typename FwdCuts<IN>::chained;
+  return with_cut<FwdCuts<IN>>(p.T, [&](auto x) {
+    using X = decltype(x);
+    return launch_cut<X>(p, k_scan_fwd<Chained, IN, OUT, FORM, true>, k_scan_fwd<X, IN, OUT, FORM, false>, ws, s);
+  });
+}
+
+template <int IN, int OUT, int FORM>
+hipError_t bwd_form(BwdArgs& p, void* ws, hipStream_t s) {
+  using Chained = typename BwdCuts<IN>::chained;
+  return with_cut<BwdCuts<IN>>(p.T, [&](auto x) {
+    using X = decltype(x);
+    return launch_cut<X>(p, k_scan_bwd<Chained, IN, OUT, FORM, true>, k_scan_bwd<X, IN, OUT, FORM, false>, ws, s);
+  });
 }
 
 template <int IN, int OUT>
 hipError_t fwd_tokens(FwdArgs& p, int form, void* ws, hipStream_t s) {
   return form == kLogit ? fwd_form<IN, OUT, kLogit>(p, ws, s) : fwd_form<IN, OUT, kValue>(p, ws, s);
-}
-
-template <int IN, int OUT, int FORM>
-hipError_t bwd_form(BwdArgs& p, void* ws, hipStream_t s) {
-  const Plan q = make_plan(true, p.N, p.T, p.C, IN);
-  const hipError_t e = start(p, q, ws, s);
-  if (e != hipSuccess) return e;
-  auto go = [&](auto kernel, int threads) {
-    hipLaunchKernelGGL(kernel, blocks((long)p.N * p.slabs * p.tiles), dim3(threads), 0, s, p);
-  };
-  using X0 = BwdCut<IN, 0>;
-  using X1 = BwdCut<IN, 1>;
-  using X2 = BwdCut<IN, 2>;
-  if (q.words > 0) go(k_scan_bwd<X0, IN, OUT, FORM, true>, X0::kThreads);
-  else if (q.size == 0) go(k_scan_bwd<X0, IN, OUT, FORM, false>, X0::kThreads);
-  else if (q.size == 1) go(k_scan_bwd<X1, IN, OUT, FORM, false>, X1::kThreads);
-  else go(k_scan_bwd<X2, IN, OUT, FORM, false>, X2::kThreads);
-  return hipGetLastError();
 }
 
 template <int IN, int OUT>
@@ -633,7 +659,9 @@ hipError_t bwd_tokens(BwdArgs& p, int form, void* ws, hipStream_t s) {
 }  // namespace
 
 size_t scan_workspace_bytes(bool bwd, int N, int T, int C, int in_dt, bool maps) {
-  return maps ? 0 : (size_t)make_plan(bwd, N, T, C, in_dt).words * 8;
+  if (maps) return 0;
+  if (in_dt == kBF16) return 8 * (bwd ? words_of<BwdCuts<kBF16>>(N, T, C) : words_of<FwdCuts<kBF16>>(N, T, C));
+  return 8 * (bwd ? words_of<BwdCuts<kF32>>(N, T, C) : words_of<FwdCuts<kF32>>(N, T, C));
 }
 
 hipError_t launch_scan_fwd(const ScanFwd& f, hipStream_t s) {

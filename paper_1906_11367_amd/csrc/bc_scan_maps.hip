@@ -18,9 +18,11 @@ template <int DT> constexpr int kV = DT == kBF16 ? 8 : 4;
 template <int DT> constexpr int kSeg = 64 * kV<DT>;
 static_assert(kSeg<kBF16> % kScanSpanMaps == 0 && kSeg<kF32> % kScanSpanMaps == 0, "room for the states");
 
+// Runs of lower lanes of a group of G lanes (lane: within the group).
+template <int G>
 __device__ __forceinline__ void lanes_prefix(float& A, float& B, int lane, float& eA, float& eB) {
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
+  for (int d = 1; d < G; d *= 2) {
     const float pa = __shfl_up(A, d), pb = __shfl_up(B, d);
     if (lane >= d) {
       B = __fmaf_rn(A, pb, B);
@@ -32,18 +34,20 @@ __device__ __forceinline__ void lanes_prefix(float& A, float& B, int lane, float
   if (lane == 0) { eA = 1.f; eB = 0.f; }
 }
 
+// Runs of higher lanes.
+template <int G>
 __device__ __forceinline__ void lanes_suffix(float& A, float& B, int lane, float& eA, float& eB) {
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
+  for (int d = 1; d < G; d *= 2) {
     const float pa = __shfl_down(A, d), pb = __shfl_down(B, d);
-    if (lane + d < 64) {
+    if (lane + d < G) {
       B = __fmaf_rn(A, pb, B);
       A *= pa;
     }
   }
   eA = __shfl_down(A, 1);
   eB = __shfl_down(B, 1);
-  if (lane == 63) { eA = 1.f; eB = 0.f; }
+  if (lane == G - 1) { eA = 1.f; eB = 0.f; }
 }
 
 // W waves to a row; blocks of kRows rows.
@@ -64,17 +68,21 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_fwd_maps(FwdArgs p) 
   const int S = (p.T + Seg - 1) / Seg;
   float carry = p.h0 ? p.h0[row] : 0.f;
   int q = 0;
+  Raw<kWords<IN, V>> g, x;
+  auto load = [&](int seg) {
+    const int t = seg * Seg + lane * V;
+    if ((seg + 1) * Seg <= len) {   // for every lane
+      g = load_wide<IN, V>(gate + (long)t * kBytes<IN>);
+      x = load_wide<IN, V>(xp + (long)t * kBytes<IN>);
+    } else {
+      g = load_vec<IN, V>(gate + (long)t * kBytes<IN>, len - t);
+      x = load_vec<IN, V>(xp + (long)t * kBytes<IN>, len - t);
+    }
+  };
+  load(w);
   for (int s0 = 0; s0 < S; s0 += W, q ^= 1) {
     const int t0 = (s0 + w) * Seg + lane * V;
-    const bool whole = (s0 + w + 1) * Seg <= len;   // for every lane
-    Raw<kWords<IN, V>> g, x;
-    if (whole) {
-      g = load_wide<IN, V>(gate + (long)t0 * kBytes<IN>);
-      x = load_wide<IN, V>(xp + (long)t0 * kBytes<IN>);
-    } else {
-      g = load_vec<IN, V>(gate + (long)t0 * kBytes<IN>, len - t0);
-      x = load_vec<IN, V>(xp + (long)t0 * kBytes<IN>, len - t0);
-    }
+    const bool whole = (s0 + w + 1) * Seg <= len;
     float a[V], b[V], A = 1.f, B = 0.f, eA, eB;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
@@ -85,7 +93,8 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_fwd_maps(FwdArgs p) 
       A *= a[k];
       B = __fmaf_rn(a[k], B, b[k]);
     }
-    lanes_prefix(A, B, lane, eA, eB);
+    if (s0 + W < S) load(s0 + W + w);   // on its way meanwhile
+    lanes_prefix<64>(A, B, lane, eA, eB);
     float hw = carry;   // the state before this wave's segment
     if constexpr (W == 1) {
       carry = __fmaf_rn(__shfl(A, 63), carry, __shfl(B, 63));
@@ -127,20 +136,34 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_bwd_maps(BwdArgs p) 
   const int S = (p.T + Seg - 1) / Seg;
   float carry = p.gh_last ? p.gh_last[row] : 0.f;
   int q = 0;
-  for (int s0 = (S - 1) / W * W; s0 >= 0; s0 -= W, q ^= 1) {
+  struct Piece {
+    Raw<kWords<IN, V>> g, x, d;
+    float st;   // the state before the segment
+  };
+  auto load = [&](int seg) {
+    const int t = seg * Seg + lane * V;
+    Piece r;
+    if ((seg + 1) * Seg <= len) {   // for every lane
+      r.g = load_wide<IN, V>(gate + (long)t * kBytes<IN>);
+      r.x = load_wide<IN, V>(xp + (long)t * kBytes<IN>);
+      r.d = load_wide<IN, V>(gy + (long)t * kBytes<IN>);
+    } else {
+      r.g = load_vec<IN, V>(gate + (long)t * kBytes<IN>, len - t);
+      r.x = load_vec<IN, V>(xp + (long)t * kBytes<IN>, len - t);
+      r.d = load_vec<IN, V>(gy + (long)t * kBytes<IN>, len - t);
+    }
+    r.st = seg < S ? p.states[row * S + seg] : 0.f;
+    return r;
+  };
+  const int top = (S - 1) / W * W;
+  Piece next = load(top + w);
+  for (int s0 = top; s0 >= 0; s0 -= W, q ^= 1) {
     const int t0 = (s0 + w) * Seg + lane * V;
     const bool whole = (s0 + w + 1) * Seg <= len;
-    Raw<kWords<IN, V>> g, xr, dr;
-    if (whole) {
-      g = load_wide<IN, V>(gate + (long)t0 * kBytes<IN>);
-      xr = load_wide<IN, V>(xp + (long)t0 * kBytes<IN>);
-      dr = load_wide<IN, V>(gy + (long)t0 * kBytes<IN>);
-    } else {
-      g = load_vec<IN, V>(gate + (long)t0 * kBytes<IN>, len - t0);
-      xr = load_vec<IN, V>(xp + (long)t0 * kBytes<IN>, len - t0);
-      dr = load_vec<IN, V>(gy + (long)t0 * kBytes<IN>, len - t0);
-    }
-    const float st = s0 + w < S ? p.states[row * S + s0 + w] : 0.f;
+    const Piece now = next;
+    if (s0 > 0) next = load(s0 - W + w);   // on its way meanwhile
+    const auto &g = now.g, &xr = now.x, &dr = now.d;
+    const float st = now.st;
     float a[V], cx[V], h[V], A = 1.f, B = 0.f, R = 0.f, eA, eB, sA, sB;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
@@ -152,8 +175,8 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_bwd_maps(BwdArgs p) 
 #pragma unroll
     for (int k = V - 1; k >= 0; --k) R = a[k] * (elem<IN, V>(dr, k) + R);
     float fA = A, fB = B;
-    lanes_prefix(fA, fB, lane, eA, eB);
-    lanes_suffix(A, R, lane, sA, sB);
+    lanes_prefix<64>(fA, fB, lane, eA, eB);
+    lanes_suffix<64>(A, R, lane, sA, sB);
     float rw = carry;   // the gradient carried into this wave's segment from after it
     if constexpr (W == 1) {
       carry = __fmaf_rn(__shfl(A, 0), carry, __shfl(R, 0));
@@ -194,6 +217,107 @@ __global__ __launch_bounds__(64 * W * kRows<W>) void k_scan_bwd_maps(BwdArgs p) 
   if (p.gh0 && w == 0 && lane == 0) p.gh0[row] = carry;
 }
 
+// Short rows: G lanes to a row, 64 / G rows to a wave, T <= G * V.
+template <int IN, int OUT, int FORM, int G>
+__global__ __launch_bounds__(256) void k_scan_fwd_short(FwdArgs p) {
+  constexpr int V = kV<IN>;
+  const int sub = threadIdx.x & (G - 1);
+  const long row = (long)blockIdx.x * (256 / G) + threadIdx.x / G;
+  const bool on = row < (long)p.N * p.C;   // all lanes of the wave take part in the lane moves
+  const int n = on ? (int)(row / p.C) : 0, c = on ? (int)(row % p.C) : 0;
+  const int len = on ? seq_len(p.lengths, n, p.T) : 0, t0 = sub * V;
+  const char* gate = p.gate + ((long)n * p.bs + (long)c * p.rs + t0) * kBytes<IN>;
+  const char* xp = p.x + ((long)n * p.bs + (long)c * p.rs + t0) * kBytes<IN>;
+  Raw<kWords<IN, V>> g = {}, x = {};
+  if (__any(t0 < len && t0 + V > len)) {
+    g = load_vec<IN, V>(gate, len - t0);
+    x = load_vec<IN, V>(xp, len - t0);
+  } else if (t0 < len) {
+    g = load_wide<IN, V>(gate);
+    x = load_wide<IN, V>(xp);
+  }
+  float a[V], b[V], A = 1.f, B = 0.f, eA, eB, o[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    float cx;
+    coefficients<IN, FORM>(elem<IN, V>(g, k), a[k], cx);
+    b[k] = input_share<FORM>(cx, elem<IN, V>(x, k));
+    if (t0 + k >= len) { a[k] = 1.f; b[k] = 0.f; }
+    A *= a[k];
+    B = __fmaf_rn(a[k], B, b[k]);
+  }
+  lanes_prefix<G>(A, B, sub, eA, eB);
+  const float first = on && p.h0 ? p.h0[row] : 0.f;
+  float h = __fmaf_rn(eA, first, eB);
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    h = __fmaf_rn(a[k], h, b[k]);
+    o[k] = t0 + k < len ? h : 0.f;
+  }
+  if (!on) return;
+  if (p.states && sub == 0) p.states[row] = first;
+  store_vec<OUT, V>(p.y + (row * p.T + t0) * kBytes<OUT>, p.T - t0, o);
+  if (p.h_last && sub == G - 1) p.h_last[row] = h;
+}
+
+template <int IN, int OUT, int FORM, int G>
+__global__ __launch_bounds__(256) void k_scan_bwd_short(BwdArgs p) {
+  constexpr int V = kV<IN>;
+  const int sub = threadIdx.x & (G - 1);
+  const long row = (long)blockIdx.x * (256 / G) + threadIdx.x / G;
+  const bool on = row < (long)p.N * p.C;
+  const int n = on ? (int)(row / p.C) : 0, c = on ? (int)(row % p.C) : 0;
+  const int len = on ? seq_len(p.lengths, n, p.T) : 0, t0 = sub * V;
+  const char* gate = p.gate + ((long)n * p.bs + (long)c * p.rs + t0) * kBytes<IN>;
+  const char* xp = p.x + ((long)n * p.bs + (long)c * p.rs + t0) * kBytes<IN>;
+  const char* gy = p.gy + ((on ? row : 0) * p.T + t0) * kBytes<IN>;
+  Raw<kWords<IN, V>> g = {}, x = {}, d = {};
+  if (__any(t0 < len && t0 + V > len)) {
+    g = load_vec<IN, V>(gate, len - t0);
+    x = load_vec<IN, V>(xp, len - t0);
+    d = load_vec<IN, V>(gy, len - t0);
+  } else if (t0 < len) {
+    g = load_wide<IN, V>(gate);
+    x = load_wide<IN, V>(xp);
+    d = load_wide<IN, V>(gy);
+  }
+  float a[V], cx[V], h[V], A = 1.f, B = 0.f, R = 0.f, eA, eB, sA, sB, og[V], ox[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    coefficients<IN, FORM>(elem<IN, V>(g, k), a[k], cx[k]);
+    if (t0 + k >= len) { a[k] = 1.f; cx[k] = 0.f; }
+    A *= a[k];
+    B = __fmaf_rn(a[k], B, input_share<FORM>(cx[k], elem<IN, V>(x, k)));
+  }
+#pragma unroll
+  for (int k = V - 1; k >= 0; --k) R = a[k] * (elem<IN, V>(d, k) + R);
+  float fA = A, fB = B;
+  lanes_prefix<G>(fA, fB, sub, eA, eB);
+  lanes_suffix<G>(A, R, sub, sA, sB);
+  const float last = on && p.gh_last ? p.gh_last[row] : 0.f;
+  h[0] = __fmaf_rn(eA, on ? p.states[row] : 0.f, eB);
+#pragma unroll
+  for (int k = 0; k + 1 < V; ++k) h[k + 1] = __fmaf_rn(a[k], h[k], input_share<FORM>(cx[k], elem<IN, V>(x, k)));
+  float r = __fmaf_rn(sA, last, sB);
+#pragma unroll
+  for (int k = V - 1; k >= 0; --k) {
+    const float delta = elem<IN, V>(d, k) + r;
+    if constexpr (FORM == kValue) {
+      og[k] = delta * h[k];
+      ox[k] = delta;
+    } else {
+      ox[k] = delta * cx[k];
+      og[k] = ox[k] * a[k] * (h[k] - elem<IN, V>(x, k));
+    }
+    r = a[k] * delta;
+    if (t0 + k >= len) og[k] = ox[k] = 0.f;
+  }
+  if (!on) return;
+  store_vec<OUT, V>(p.ggate + ((long)n * p.gbs + (long)c * p.grs + t0) * kBytes<OUT>, p.T - t0, og);
+  store_vec<OUT, V>(p.gx + ((long)n * p.gbs + (long)c * p.grs + t0) * kBytes<OUT>, p.T - t0, ox);
+  if (p.gh0 && sub == 0) p.gh0[row] = r;
+}
+
 // Waves to a row: as many as the row has segments for, until there are 4096
 // waves in all (four for each SIMD).
 int waves_per_row(int N, int C, int T, int seg) {
@@ -211,8 +335,20 @@ hipError_t launch_rows(Kernel kernel, const Args& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int G, class Args, class Kernel>
+hipError_t launch_short(Kernel kernel, const Args& p, hipStream_t s) {
+  const long rows = (long)p.N * p.C;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + 256 / G - 1) / (256 / G))), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
 template <int IN, int OUT, int FORM>
 hipError_t fwd_rows(const FwdArgs& p, hipStream_t s) {
+  constexpr int V = kV<IN>;
+  if (p.T <= V) return launch_short<1>(k_scan_fwd_short<IN, OUT, FORM, 1>, p, s);
+  if (p.T <= 4 * V) return launch_short<4>(k_scan_fwd_short<IN, OUT, FORM, 4>, p, s);
+  if (p.T <= 16 * V) return launch_short<16>(k_scan_fwd_short<IN, OUT, FORM, 16>, p, s);
+  if (p.T <= 32 * V) return launch_short<32>(k_scan_fwd_short<IN, OUT, FORM, 32>, p, s);
   switch (waves_per_row(p.N, p.C, p.T, kSeg<IN>)) {
     case 1: return launch_rows<1>(k_scan_fwd_maps<IN, OUT, FORM, 1>, p, s);
     case 4: return launch_rows<4>(k_scan_fwd_maps<IN, OUT, FORM, 4>, p, s);
@@ -222,6 +358,11 @@ hipError_t fwd_rows(const FwdArgs& p, hipStream_t s) {
 
 template <int IN, int OUT, int FORM>
 hipError_t bwd_rows(const BwdArgs& p, hipStream_t s) {
+  constexpr int V = kV<IN>;
+  if (p.T <= V) return launch_short<1>(k_scan_bwd_short<IN, OUT, FORM, 1>, p, s);
+  if (p.T <= 4 * V) return launch_short<4>(k_scan_bwd_short<IN, OUT, FORM, 4>, p, s);
+  if (p.T <= 16 * V) return launch_short<16>(k_scan_bwd_short<IN, OUT, FORM, 16>, p, s);
+  if (p.T <= 32 * V) return launch_short<32>(k_scan_bwd_short<IN, OUT, FORM, 32>, p, s);
   switch (waves_per_row(p.N, p.C, p.T, kSeg<IN>)) {
     case 1: return launch_rows<1>(k_scan_bwd_maps<IN, OUT, FORM, 1>, p, s);
     case 4: return launch_rows<4>(k_scan_bwd_maps<IN, OUT, FORM, 4>, p, s);

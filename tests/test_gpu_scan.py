@@ -109,7 +109,8 @@ def run_both(d, N, T, C, dt, layout, form, lengths=None, start=True, out_dt=None
 @pytest.mark.parametrize("form", ["logit", "value"])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("N,T,C", [(1, 1, 1), (3, 2, 7), (2, 5, 8), (1, 127, 33), (2, 128, 64), (2, 129, 65),
-                                   (1, 255, 130), (1, 257, 9), (5, 31, 100), (1, 1000, 72), (2, 513, 31)])
+                                   (1, 255, 130), (1, 257, 9), (5, 31, 100), (1, 1000, 72), (2, 513, 31), (3, 9, 300),
+                                   (2, 17, 257), (2, 33, 70), (1, 64, 40), (2, 65, 66), (1, 256, 33)])
 def test_tokens(N, T, C, dt, form):
     say("scan tokens", N, T, C, dt, form)
     run_both(inputs(11, N, T, C, dt, "tokens", form), N, T, C, dt, "tokens", form)
@@ -120,7 +121,9 @@ def test_tokens(N, T, C, dt, form):
 @pytest.mark.parametrize("form", ["logit", "value"])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("N,T,C", [(1, 1, 1), (2, 7, 3), (3, 8, 5), (1, 511, 6), (2, 512, 4), (1, 513, 7),
-                                   (2, 2049, 3), (1, 9000, 2), (9, 600, 130), (2, 520, 2100)])
+                                   (2, 2049, 3), (1, 9000, 2), (9, 600, 130), (2, 520, 2100), (3, 4, 50),
+                                   (2, 9, 70), (5, 32, 33), (2, 33, 17), (3, 64, 5), (2, 65, 9), (2, 128, 7), (2, 129, 3),
+                                   (1, 256, 5), (3, 257, 3), (2, 17000, 3)])
 def test_maps(N, T, C, dt, form):
     say("scan maps", N, T, C, dt, form)
     run_both(inputs(12, N, T, C, dt, "maps", form), N, T, C, dt, "maps", form)
@@ -129,7 +132,7 @@ def test_maps(N, T, C, dt, form):
 @pytest.mark.parametrize("layout", ["tokens", "maps"])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("T,lengths", [(300, [300, 0, 1, 299, 128, 129]), (700, [0, 700, 513, 512, 511, 8]),
-                                       (5, [0, 0, 5, 4, 1, 3]), (300, [-4, 900, 256, 257, 255, 2])])
+                                       (5, [0, 0, 5, 4, 1, 3]), (30, [30, 0, 7, 8, 9, 29]), (100, [64, 0, 100, 65, 1, 99]), (300, [-4, 900, 256, 257, 255, 2])])
 def test_ragged(T, lengths, dt, layout):
     """Sequences of their own lengths (out-of-range ones are clamped); what
     stands past them, NaN here, reaches nothing."""
