@@ -39,16 +39,23 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, f
   return inv == 0.f ? 0u : lo | hi;
 }
 
-// A tile of maps [K][P]: 64 pixels by all K channels, by a block of 512
-// threads.  A lane has 8 pixels (pg = lane % 8) of 4 consecutive channels
-// (group kg, 64 groups in the block) at a time: loads are whole 128-byte lines
-// (bf16), and four codes of a pixel make a word.
-constexpr int kTileP = 64, kTileThreads = 512, kStepK = 256;
+// A tile of maps [K][P]: PX pixels (64, 32 or 16) by all K channels, by a block
+// of 512 threads.  A lane has 8 pixels (pg = tid % (PX / 8)) of 4 consecutive
+// channels (group kg = tid / (PX / 8)) at a time, kStepK channels in the block:
+// loads are runs of PX pixels, and four codes of a pixel make a word.
+constexpr int kTileThreads = 512;
+template <int PX> constexpr int kStepK = kTileThreads / (PX / 8) * 4;
 
-// The codes of pixel p stand in LDS as a row of `pitch` bytes (a multiple of
-// 256), its 16-byte chunk c at c ^ chunk_swap(p): 16 pixels' reads of one
-// chunk, and a wave's writes, then hit all banks.
-__device__ __forceinline__ int chunk_swap(int p) { return (((p ^ (p >> 3)) & 7) << 1) | ((p >> 3) & 1); }
+// The codes of pixel p stand in LDS as a row of whole steps (a multiple of 256
+// bytes), its 16-byte chunk c at c ^ chunk_swap(p).  The reads of one chunk of
+// 16 consecutive pixels, and the words that a wave writes (a pixel in 8, and
+// 16 * 8 / PX consecutive chunks), then hit all banks.
+template <int PX>
+__device__ __forceinline__ int chunk_swap(int p) {
+  if constexpr (PX == 64) return (((p ^ (p >> 3)) & 7) << 1) | ((p >> 3) & 1);
+  else if constexpr (PX == 32) return ((p >> 1) & 3) | (((p ^ (p >> 4)) & 1) << 2) | (p & 8);
+  else return p & 15;
+}
 
 // The lane's 8 pixels of channel k.  kFull: all 8 exist.
 template <int DT, bool kFull>
@@ -64,17 +71,18 @@ __device__ __forceinline__ Raw<kWords<DT, 8>> tile_load(const char* base, long r
 }
 
 // Row scales of the tile.  base: the lane's pixels at channel 0 (`avail` of the
-// 8 exist), rs elements between channels.  The first kHold steps of 256
-// channels stay in registers (x); later ones are read again for their codes.
-// tops: 8 x 64 words of LDS, rows: 64 RowScales of LDS, whole after the call.
-template <int DT, int kHold, bool kFull>
+// 8 exist), rs elements between channels.  The first kHold steps of channels
+// stay in registers (x); later ones are read again for their codes.
+// tops: 8 x PX words of LDS, rows: PX RowScales of LDS, whole after the call.
+template <int DT, int PX, int kHold, bool kFull>
 __device__ __forceinline__ void tile_scales(const char* base, long rs, int avail, int K,
                                             Raw<kWords<DT, 8>> (&x)[kHold + 1][4], uint32_t* tops, RowScale* rows) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kg = tid >> 3;
+  constexpr int PL = PX / 8, Step = kStepK<PX>;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kg = tid / PL;
 #pragma unroll
   for (int s = 0; s < kHold; ++s)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[s][i] = tile_load<DT, kFull>(base, rs, avail, s * kStepK + kg * 4 + i, K);
+    for (int i = 0; i < 4; ++i) x[s][i] = tile_load<DT, kFull>(base, rs, avail, s * Step + kg * 4 + i, K);
   uint32_t top[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) top[j] = 0;
@@ -84,49 +92,50 @@ __device__ __forceinline__ void tile_scales(const char* base, long rs, int avail
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) top[j] = max(top[j], abs_bits(elem<DT, 8>(x[s][i], j)));
-  for (int s = kHold; s * kStepK < K; ++s) {
+  for (int s = kHold; s * Step < K; ++s) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[kHold][i] = tile_load<DT, kFull>(base, rs, avail, s * kStepK + kg * 4 + i, K);
+    for (int i = 0; i < 4; ++i) x[kHold][i] = tile_load<DT, kFull>(base, rs, avail, s * Step + kg * 4 + i, K);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) top[j] = max(top[j], abs_bits(elem<DT, 8>(x[kHold][i], j)));
   }
 #pragma unroll
-  for (int d = 8; d < 64; d *= 2)
+  for (int d = PL; d < 64; d *= 2)
 #pragma unroll
     for (int j = 0; j < 8; ++j) top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], d));
-  if (lane < 8) {
+  if (lane < PL) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) tops[wave * kTileP + lane * 8 + j] = top[j];
+    for (int j = 0; j < 8; ++j) tops[wave * PX + lane * 8 + j] = top[j];
   }
   __syncthreads();
-  if (tid < kTileP) {
+  if (tid < PX) {
     uint32_t m = 0;
 #pragma unroll
-    for (int w = 0; w < kTileThreads / 64; ++w) m = max(m, tops[w * kTileP + tid]);
+    for (int w = 0; w < kTileThreads / 64; ++w) m = max(m, tops[w * PX + tid]);
     rows[tid] = row_scale(m);
   }
   __syncthreads();
 }
 
-// Codes of channels [s0 * 256, s1 * 256) into LDS at `lds` (channel s0 * 256
-// first), for the rows scaled above.
-template <int DT, int kHold, bool kFull>
+// Codes of the channels of steps [s0, s1) into LDS at `lds`, for the rows scaled
+// above.
+template <int DT, int PX, int kHold, bool kFull>
 __device__ __forceinline__ void tile_codes(const char* base, long rs, int avail, int K,
                                            Raw<kWords<DT, 8>> (&x)[kHold + 1][4], const RowScale* rows, uint32_t lds,
                                            int pitch, int s0, int s1) {
-  const int lane = threadIdx.x & 63, kg = threadIdx.x >> 3, p0 = (lane & 7) * 8;
+  constexpr int PL = PX / 8, Step = kStepK<PX>;
+  const int kg = threadIdx.x / PL, p0 = (threadIdx.x % PL) * 8;
   float inv[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) inv[j] = rows[p0 + j].inv;
   auto put = [&](int s, const Raw<kWords<DT, 8>> (&y)[4]) {
-    const int k = (s - s0) * kStepK + kg * 4;
+    const int k = (s - s0) * Step + kg * 4;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint32_t w = codes4(elem<DT, 8>(y[0], j), elem<DT, 8>(y[1], j), elem<DT, 8>(y[2], j), elem<DT, 8>(y[3], j), inv[j]);
       const int p = p0 + j;
-      *(BC_LDS uint32_t*)(uintptr_t)(lds + p * pitch + (((k >> 4) ^ chunk_swap(p)) << 4) + (k & 15)) = w;
+      *(BC_LDS uint32_t*)(uintptr_t)(lds + p * pitch + (((k >> 4) ^ chunk_swap<PX>(p)) << 4) + (k & 15)) = w;
     }
   };
   // the words stay as loaded: unpacked values are not kept from the scales on
@@ -139,7 +148,7 @@ __device__ __forceinline__ void tile_codes(const char* base, long rs, int avail,
     if (s >= s0 && s < s1) put(s, x[s]);
   for (int s = max(s0, kHold); s < s1; ++s) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[kHold][i] = tile_load<DT, kFull>(base, rs, avail, s * kStepK + kg * 4 + i, K);
+    for (int i = 0; i < 4; ++i) x[kHold][i] = tile_load<DT, kFull>(base, rs, avail, s * Step + kg * 4 + i, K);
     put(s, x[kHold]);
   }
 }

@@ -205,7 +205,7 @@ struct MixI8 {
 hipError_t launch_mix_i8(const MixI8& m, hipStream_t s);
 // Maps that are not codes yet, in one pass (bc_mix_i8_maps.hip): whether it
 // takes the request, its workspace, and the launch.
-bool mix_i8_maps_takes(int K);
+bool mix_i8_maps_takes(int N, int M, int K, int P);
 size_t mix_i8_maps_workspace_bytes(int N, int M, int K, int P);
 hipError_t launch_mix_i8_maps(const MixI8& m, hipStream_t s);
 // Few tokens, layout tokens (bc_mix_i8_few.hip): whether it takes so many, and

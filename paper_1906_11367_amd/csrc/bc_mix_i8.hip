@@ -301,14 +301,14 @@ size_t codes_bytes(long rows, int K) { return ((size_t)rows * i8_pitch(K) + 255)
 
 size_t mix_i8_workspace_bytes(int N, int M, int K, int P, int dt, bool maps) {
   if (dt == 3) return 0;   // codes already
-  if (maps && mix_i8_maps_takes(K)) return mix_i8_maps_workspace_bytes(N, M, K, P);
+  if (maps && mix_i8_maps_takes(N, M, K, P)) return mix_i8_maps_workspace_bytes(N, M, K, P);
   const long rows = (long)N * P;
   if (!maps && mix_i8_few_makes_codes(rows, K)) return 0;
   return codes_bytes(rows, K) + (size_t)rows * 4;
 }
 
 hipError_t launch_mix_i8(const MixI8& m, hipStream_t s) {
-  if (m.maps && m.dt != 3 && mix_i8_maps_takes(m.K)) return launch_mix_i8_maps(m, s);
+  if (m.maps && m.dt != 3 && mix_i8_maps_takes(m.N, m.M, m.K, m.P)) return launch_mix_i8_maps(m, s);
   const long rows = (long)m.N * m.P;
   const bool few = !m.maps && mix_i8_few_takes(rows, m.K);
   const int8_t* x = static_cast<const int8_t*>(m.x);

@@ -2,11 +2,13 @@
 // (gfx950; bc_i8.hpp has the codes' definition).
 //
 // Bound by memory: maps in, maps out, and little arithmetic for them (M is a
-// few hundred).  A block takes 64 pixels of one image by all K channels: it
-// reads them once, keeping them in registers until the pixels' scales are
-// known, turns the codes through LDS into the rows that the matrix
-// instructions read, and multiplies them with all M weight rows, which come
-// from the XCD's L2.  The codes never go to memory.
+// few hundred).  A block takes 64 (or 32) pixels of one image by all K channels:
+// it reads them once, keeping them in registers until the pixels' scales are
+// known (as many as fit; the rest is read again), turns the codes through LDS
+// into the rows that the matrix instructions read, and multiplies them with all
+// M weight rows, which come from the XCD's L2.  The codes never go to memory.
+// 32 images of 1024 x 64 x 64 bf16 to 256 fp32 maps: 95 us, 403 MB at 4.2 TB/s;
+// the products take 20 us of it, in which the block's loads stand still.
 #include "bc_i8.hpp"
 
 #include <math.h>
@@ -29,28 +31,31 @@ struct Args {
   float floor;
 };
 
-template <int DT, int OUT, int kHold, bool kFull>
+template <int DT, int OUT, int PX, int kHold, bool kFull>
 __device__ __forceinline__ void mix_tile(const Args& p, int n, int pt, uint32_t lds, uint32_t* tops, RowScale* rows) {
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int p0 = pt + (tid & 7) * 8, lp = p.steps * kStepK;
+  constexpr int XB = PX / 32;   // blocks of 32 pixels
+  const int p0 = pt + (tid % (PX / 8)) * 8, lp = p.steps * kStepK<PX>;
   const char* base = p.x + ((long)n * p.bs + p0) * kBytes<DT>;
   {
     Raw<kWords<DT, 8>> x[kHold + 1][4];
-    tile_scales<DT, kHold, kFull>(base, p.rs, p.P - p0, p.K, x, tops, rows);
-    tile_codes<DT, kHold, kFull>(base, p.rs, p.P - p0, p.K, x, rows, lds, lp, 0, p.steps);
+    tile_scales<DT, PX, kHold, kFull>(base, p.rs, p.P - p0, p.K, x, tops, rows);
+    tile_codes<DT, PX, kHold, kFull>(base, p.rs, p.P - p0, p.K, x, rows, lds, lp, 0, p.steps);
   }
   __syncthreads();
   // a wave: 32 weight rows by the 64 pixels.  Lane l of matrix instruction t of
   // a block of 128 codes has chunk 2 t + l / 32 of row l % 32.
-  const int pa = lane & 31, swap[2] = {chunk_swap(pa), chunk_swap(pa + 32)}, blocks = p.pitch / 128;
+  const int pa = lane & 31, swap[2] = {chunk_swap<PX>(pa), chunk_swap<PX>(pa + 32)}, blocks = p.pitch / 128;
   for (int m0 = wave * 32; m0 < p.M; m0 += kTileThreads / 64 * 32) {
     const int8_t* w = p.packed ? p.w + (long)m0 * p.pitch + lane * 16
                                : p.w + (long)min(m0 + pa, p.M - 1) * p.pitch + half * 16;
     const int wt = p.packed ? 1024 : 32, wk = 4 * wt;   // bytes from one t to the next, from a block to the next
-    i32x16_t acc[2];
+    i32x16_t acc[XB];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[0][r] = acc[1][r] = 0;
+    for (int x = 0; x < XB; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[x][r] = 0;
     i32x4_t b[4], next[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) b[t] = *reinterpret_cast<const i32x4_t*>(w + t * wt);
@@ -61,7 +66,7 @@ __device__ __forceinline__ void mix_tile(const Args& p, int n, int pt, uint32_t 
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < XB; ++x) {
           const int c = k * 8 + 2 * t + half;
           const i32x4_t a = *(BC_LDS i32x4_t*)(uintptr_t)(lds + (pa + 32 * x) * lp + ((c ^ swap[x]) << 4));
           acc[x] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[t], a, acc[x], 0, 0, 0);
@@ -78,7 +83,7 @@ __device__ __forceinline__ void mix_tile(const Args& p, int n, int pt, uint32_t 
       const float sw = p.wscale[mr], bias = p.bias ? p.bias[mr] : 0.f;
       char* o = p.out + (((long)n * p.M + mr) * p.P + pt + pa) * kBytes<OUT>;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < XB; ++x) {
         const float v = __fmaf_rn((float)acc[x][r] * rows[pa + 32 * x].scale, sw, bias);
         const float z = v < p.floor ? p.floor : v;   // a NaN stays
         if (!kFull && pt + pa + 32 * x >= p.P) continue;
@@ -89,15 +94,15 @@ __device__ __forceinline__ void mix_tile(const Args& p, int n, int pt, uint32_t 
   }
 }
 
-template <int DT, int OUT>
+template <int DT, int OUT, int PX>
 __global__ __launch_bounds__(kTileThreads, 4) void k_mix_i8_maps(Args p) {
-  extern __shared__ __align__(16) unsigned char smem[];   // codes of 64 pixels
-  __shared__ uint32_t tops[kTileThreads / 64 * kTileP];
-  __shared__ RowScale rows[kTileP];
-  const int n = blockIdx.x / p.strips, pt = (blockIdx.x % p.strips) * kTileP;
+  extern __shared__ __align__(16) unsigned char smem[];   // codes of the pixels
+  __shared__ uint32_t tops[kTileThreads / 64 * PX];
+  __shared__ RowScale rows[PX];
+  const int n = blockIdx.x / p.strips, pt = (blockIdx.x % p.strips) * PX;
   const uint32_t lds = (uint32_t)(uintptr_t)(BC_LDS unsigned char*)smem;
-  if (p.P - pt >= kTileP) mix_tile<DT, OUT, kHeld<DT>, true>(p, n, pt, lds, tops, rows);
-  else mix_tile<DT, OUT, kHeld<DT>, false>(p, n, pt, lds, tops, rows);
+  if (p.P - pt >= PX) mix_tile<DT, OUT, PX, kHeld<DT>, true>(p, n, pt, lds, tops, rows);
+  else mix_tile<DT, OUT, PX, kHeld<DT>, false>(p, n, pt, lds, tops, rows);
 }
 
 // Weight rows in the order in which the waves read them: 32 rows by 128 codes at
@@ -113,21 +118,47 @@ __global__ __launch_bounds__(256) void k_pack_rows(const int8_t* w, i32x4_t* out
   out[i] = *reinterpret_cast<const i32x4_t*>(w + (long)m * pitch + k);
 }
 
+long strips_of(int N, int P, int px) { return (long)N * ((P + px - 1) / px); }
+
+// Pixels of a block.  64 read the weights half as often as 32 (32 images of 1024
+// x 64 x 64 to 256 maps: 95 and 147 us); 32 make twice the blocks where there
+// are few (1 x 1024 x 64 x 64 to 256: 14.4 and 12.6), and leave room for two on a
+// CU where a pixel's codes are many and the weight rows few (16 x 2048 x 1000 to
+// 200: 48 and 43; 2 x 2048 x 8000 to 1024: 67 and 74).
+bool wide_blocks(int N, int M, int K, int P) {
+  return strips_of(N, P, 64) >= 256 && (K <= 1024 || M > 512);
+}
+
 // Blocks from which the packing's launch pays (32 images of 1024 x 64 x 64 to
 // 256 maps: 124 us without, 95 + 5 with; 64 blocks 33 and 32).
 constexpr long kPackBlocks = 32;
-long strips_of(int N, int P) { return (long)N * ((P + kTileP - 1) / kTileP); }
 
-constexpr size_t kLdsBytes = 128 * 1024;   // of codes: K up to 2048
+template <int DT, int OUT, int PX>
+hipError_t launch(Args& p, int N, hipStream_t s) {
+  p.strips = (p.P + PX - 1) / PX;
+  p.steps = (p.pitch + kStepK<PX> - 1) / kStepK<PX>;
+  const size_t lds = (size_t)PX * p.steps * kStepK<PX>;
+  hipLaunchKernelGGL((k_mix_i8_maps<DT, OUT, PX>), dim3((unsigned)((long)N * p.strips)), dim3(kTileThreads), lds, s, p);
+  return hipGetLastError();
+}
+
+template <int DT, int OUT>
+hipError_t launch(Args& p, int N, hipStream_t s) {
+  return wide_blocks(N, p.M, p.K, p.P) ? launch<DT, OUT, 64>(p, N, s) : launch<DT, OUT, 32>(p, N, s);
+}
 
 }  // namespace
 
-bool mix_i8_maps_takes(int K) {
-  return (size_t)kTileP * ((i8_pitch(K) + kStepK - 1) / kStepK * kStepK) <= kLdsBytes;
+// Not the calls whose few pixels meet many weight rows: the tiles of
+// bc_mix_i8.hip divide those over the chip (kernel us here and there: 1 x 2000 x
+// 500 to 1000 79 and 20, 4 x 2048 x 1000 to 1024 51 and 38; 1 x 1024 x 64 x 64 to
+// 256 15 and 19).
+bool mix_i8_maps_takes(int N, int M, int K, int P) {
+  return K <= 2048 && (M <= 256 || strips_of(N, P, 64) >= 128);
 }
 
 size_t mix_i8_maps_workspace_bytes(int N, int M, int K, int P) {
-  return strips_of(N, P) < kPackBlocks ? 0 : (size_t)(M + 31) / 32 * 32 * i8_pitch(K);
+  return strips_of(N, P, 64) < kPackBlocks ? 0 : (size_t)(M + 31) / 32 * 32 * i8_pitch(K);
 }
 
 hipError_t launch_mix_i8_maps(const MixI8& m, hipStream_t s) {
@@ -143,8 +174,6 @@ hipError_t launch_mix_i8_maps(const MixI8& m, hipStream_t s) {
   p.K = m.K;
   p.P = m.P;
   p.pitch = i8_pitch(m.K);
-  p.strips = (m.P + kTileP - 1) / kTileP;
-  p.steps = (p.pitch + kStepK - 1) / kStepK;
   p.floor = m.relu ? 0.f : -INFINITY;
   const size_t packed = mix_i8_maps_workspace_bytes(m.N, m.M, m.K, m.P);
   if (packed > 0) {
@@ -156,12 +185,8 @@ hipError_t launch_mix_i8_maps(const MixI8& m, hipStream_t s) {
     p.w = static_cast<const int8_t*>(m.ws);
     p.packed = 1;
   }
-  const dim3 grid((unsigned)((long)m.N * p.strips));
-  const size_t lds = (size_t)kTileP * p.steps * kStepK;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kTileThreads), lds, s, p); };
-  if (m.dt == kBF16) m.out_dt == kBF16 ? go(k_mix_i8_maps<kBF16, kBF16>) : go(k_mix_i8_maps<kBF16, kF32>);
-  else m.out_dt == kBF16 ? go(k_mix_i8_maps<kF32, kBF16>) : go(k_mix_i8_maps<kF32, kF32>);
-  return hipGetLastError();
+  if (m.dt == kBF16) return m.out_dt == kBF16 ? launch<kBF16, kBF16>(p, m.N, s) : launch<kBF16, kF32>(p, m.N, s);
+  return m.out_dt == kBF16 ? launch<kF32, kBF16>(p, m.N, s) : launch<kF32, kF32>(p, m.N, s);
 }
 
 }  // namespace bc

@@ -67,47 +67,58 @@ __global__ __launch_bounds__(256) void k_quant_rows(const char* src, long bs, lo
   if (k1 == 0) scale[row] = s.scale;
 }
 
-// Maps [N][K][P] to rows of tokens: a block takes 64 pixels of one image, and
-// turns them through LDS, up to kPart steps of 256 channels at a time.
-constexpr int kPart = 4;
+// Maps [N][K][P] to rows of tokens: a block takes PX pixels of one image, and
+// turns them through LDS, up to kPart steps of channels at a time.
+template <int PX> constexpr int kPart = PX == 64 ? 4 : 2;
 
-template <int DT, int kHold, bool kFull>
+template <int DT, int PX, int kHold, bool kFull>
 __device__ __forceinline__ void quant_tile(const char* base, long rs, int avail, int8_t* q, int left, int K, int pitch,
                                            int steps, uint32_t lds, uint32_t* tops, RowScale* rows) {
-  const int tid = threadIdx.x, lp = min(steps, kPart) * kStepK;
+  constexpr int Step = kStepK<PX>;
+  const int tid = threadIdx.x, lp = min(steps, kPart<PX>) * Step;
   Raw<kWords<DT, 8>> x[kHold + 1][4];
-  tile_scales<DT, kHold, kFull>(base, rs, avail, K, x, tops, rows);
-  for (int s0 = 0; s0 < steps; s0 += kPart) {
-    const int s1 = min(steps, s0 + kPart);
+  tile_scales<DT, PX, kHold, kFull>(base, rs, avail, K, x, tops, rows);
+  for (int s0 = 0; s0 < steps; s0 += kPart<PX>) {
+    const int s1 = min(steps, s0 + kPart<PX>);
     if (s0 > 0) __syncthreads();
-    tile_codes<DT, kHold, kFull>(base, rs, avail, K, x, rows, lds, lp, s0, s1);
+    tile_codes<DT, PX, kHold, kFull>(base, rs, avail, K, x, rows, lds, lp, s0, s1);
     __syncthreads();
     // whole rows out, 16 bytes a lane
-    const int chunks = min(pitch - s0 * kStepK, (s1 - s0) * kStepK) >> 4;
-    for (int c = tid; c < kTileP * chunks; c += kTileThreads) {
+    const int chunks = min(pitch - s0 * Step, (s1 - s0) * Step) >> 4;
+    for (int c = tid; c < PX * chunks; c += kTileThreads) {
       const int p = c / chunks, ch = c % chunks;
       if (p >= left) break;
-      const Raw<4> w = *(BC_LDS Raw<4>*)(uintptr_t)(lds + p * lp + ((ch ^ chunk_swap(p)) << 4));
-      *reinterpret_cast<Raw<4>*>(q + (long)p * pitch + s0 * kStepK + ch * 16) = w;
+      const Raw<4> w = *(BC_LDS Raw<4>*)(uintptr_t)(lds + p * lp + ((ch ^ chunk_swap<PX>(p)) << 4));
+      *reinterpret_cast<Raw<4>*>(q + (long)p * pitch + s0 * Step + ch * 16) = w;
     }
   }
 }
 
-template <int DT>
+template <int DT, int PX>
 __global__ __launch_bounds__(kTileThreads, 4) void k_quant_maps(const char* src, long bs, long rs, int8_t* q,
                                                                 float* scale, int P, int K, int pitch, int strips,
                                                                 int steps) {
-  extern __shared__ __align__(16) unsigned char smem[];   // codes of 64 pixels
-  __shared__ uint32_t tops[kTileThreads / 64 * kTileP];
-  __shared__ RowScale rows[kTileP];
-  const int tid = threadIdx.x, n = blockIdx.x / strips, pt = (blockIdx.x % strips) * kTileP, left = P - pt;
-  const int p0 = pt + (tid & 7) * 8;
+  extern __shared__ __align__(16) unsigned char smem[];   // codes of the pixels
+  __shared__ uint32_t tops[kTileThreads / 64 * PX];
+  __shared__ RowScale rows[PX];
+  const int tid = threadIdx.x, n = blockIdx.x / strips, pt = (blockIdx.x % strips) * PX, left = P - pt;
+  const int p0 = pt + (tid % (PX / 8)) * 8;
   const uint32_t lds = (uint32_t)(uintptr_t)(BC_LDS unsigned char*)smem;
   const char* base = src + ((long)n * bs + p0) * kBytes<DT>;
   int8_t* out = q + ((long)n * P + pt) * pitch;
-  if (left >= kTileP) quant_tile<DT, kHeld<DT>, true>(base, rs, P - p0, out, left, K, pitch, steps, lds, tops, rows);
-  else quant_tile<DT, kHeld<DT>, false>(base, rs, P - p0, out, left, K, pitch, steps, lds, tops, rows);
-  if (tid < kTileP && tid < left) scale[(long)n * P + pt + tid] = rows[tid].scale;
+  if (left >= PX) quant_tile<DT, PX, kHeld<DT>, true>(base, rs, P - p0, out, left, K, pitch, steps, lds, tops, rows);
+  else quant_tile<DT, PX, kHeld<DT>, false>(base, rs, P - p0, out, left, K, pitch, steps, lds, tops, rows);
+  if (tid < PX && tid < left) scale[(long)n * P + pt + tid] = rows[tid].scale;
+}
+
+template <int DT, int PX>
+hipError_t launch_maps(const char* x, long bs, long rs, int8_t* q, float* scale, int N, int P, int K, int pitch,
+                       hipStream_t s) {
+  const int strips = (P + PX - 1) / PX, steps = (pitch + kStepK<PX> - 1) / kStepK<PX>;
+  const size_t lds = (size_t)PX * std::min(steps, kPart<PX>) * kStepK<PX>;
+  hipLaunchKernelGGL((k_quant_maps<DT, PX>), dim3((unsigned)((long)N * strips)), dim3(kTileThreads), lds, s, x, bs, rs,
+                     q, scale, P, K, pitch, strips, steps);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -118,13 +129,13 @@ hipError_t launch_quantize_i8(const void* src, int dt, long bs, long rs, void* q
   int8_t* out = static_cast<int8_t*>(q);
   const int pitch = i8_pitch(K);
   if (maps) {
-    const int strips = (P + kTileP - 1) / kTileP, steps = (pitch + kStepK - 1) / kStepK;
-    const dim3 grid((unsigned)((long)N * strips));
-    const size_t lds = (size_t)kTileP * std::min(steps, kPart) * kStepK;
-    auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, grid, dim3(kTileThreads), lds, s, x, bs, rs, out, scale, P, K, pitch, strips, steps);
-    };
-    dt == kBF16 ? go(k_quant_maps<kBF16>) : go(k_quant_maps<kF32>);
+    // narrow strips where wide ones leave the chip empty
+    const bool narrow = (long)N * ((P + 63) / 64) < 256;
+    if (dt == kBF16)
+      return narrow ? launch_maps<kBF16, 16>(x, bs, rs, out, scale, N, P, K, pitch, s)
+                    : launch_maps<kBF16, 64>(x, bs, rs, out, scale, N, P, K, pitch, s);
+    return narrow ? launch_maps<kF32, 16>(x, bs, rs, out, scale, N, P, K, pitch, s)
+                  : launch_maps<kF32, 64>(x, bs, rs, out, scale, N, P, K, pitch, s);
   } else {
     const long rows = (long)N * P;
     const bool block = K > 2 * 1024 || rows < 1024;   // a block to a row

@@ -136,7 +136,8 @@ def test_tokens_large(T, K, M):
 @pytest.mark.parametrize("N,K,P,M", [(1, 72, 1, 5), (3, 100, 7, 33), (2, 128, 64, 64), (1, 513, 65, 130),
                                      (4, 64, 300, 257), (2, 1024, 640, 256), (3, 300, 1023, 96), (2, 1024, 96, 70),
                                      (5, 2048, 130, 300), (1, 1100, 513, 512), (9, 200, 1900, 70),
-                                     (1, 2100, 200, 90), (2, 4000, 70, 40)])
+                                     (1, 2100, 200, 90), (2, 4000, 70, 40), (1, 600, 500, 400), (4, 1500, 1100, 60),
+                                     (2, 1200, 8256, 530), (16, 128, 1030, 40)])
 def test_maps(N, K, P, M):
     say("mix maps", N, K, P, M)
     wq, ws = weights(M, M, K)
