@@ -478,6 +478,7 @@ typedef enum { BC_GATE_LOGIT = 0, BC_GATE_VALUE = 1 } bc_gate_form;
  * slots   : device int32 [N], or NULL (then N <= S).  A slot outside [0, S)
  *           marks an idle row: y is zero, no state is read or written.  Two
  *           rows may not name one slot.
+ * Sizes: N <= 2^20, C <= 65536, N * C <= 2^31 (BC_ERR_SHAPE).
  * ---------------------------------------------------------------------- */
 bc_status gated_scan_fwd(const void* gate, const void* x, int dt, int64_t batch_stride, int64_t row_stride,
                          const float* h0, const int* lengths, void* y, int y_dt, float* h_last, float* states,
@@ -525,8 +526,8 @@ size_t bc_gated_scan_states_bytes(int N, int T, int C, int layout);
  * out         : device, dense, out_dt = BC_F32 or BC_BF16: [N][P][M]
  *               (BC_TOKENS) or [N][M][P] (BC_MAPS).
  * ws          : >= bc_mix_i8_workspace_bytes(...) bytes, NULL when that is 0.
- * Sizes: N, M, K <= 65536, N * P <= 2^30, the output's tiles of 64 x 64 at
- * most 2^24 (BC_ERR_SHAPE).
+ * Sizes: N, M, K <= 65536, N * P <= 2^28, the output's tiles of 64 x 64 at
+ * most 2^23 (BC_ERR_SHAPE).
  * ---------------------------------------------------------------------- */
 bc_status quantize_i8(const void* src, int dt, int64_t batch_stride, int64_t row_stride, void* q, float* scale,
                       int N, int K, int P, int layout, hipStream_t stream);

@@ -572,7 +572,8 @@ bc_status gated_scan_step(const void* gate, const void* x, int dt, int64_t row_s
                           hipStream_t stream) {
   if (!gate || !x || !state || !state_out || !y) return BC_ERR_NULL;
   if (form != BC_GATE_LOGIT && form != BC_GATE_VALUE) return BC_ERR_UNSUPPORTED;
-  if (N <= 0 || C <= 0 || S <= 0 || N > (1 << 20) || C > kMaxDim || (!slots && N > S)) return BC_ERR_SHAPE;
+  if (N <= 0 || C <= 0 || S <= 0 || N > (1 << 20) || C > kMaxDim || (long)N * C > (1L << 31)) return BC_ERR_SHAPE;
+  if (!slots && N > S) return BC_ERR_SHAPE;
   if (!strides_ok(0, row_stride, 1, N, C)) return BC_ERR_SHAPE;
   if (dt != BC_F32 && dt != BC_BF16) return BC_ERR_DTYPE;
   if (!aligned16(gate) || !aligned16(x) || !aligned16(state) || !aligned16(state_out) || !aligned16(y) ||
@@ -582,10 +583,12 @@ bc_status gated_scan_step(const void* gate, const void* x, int dt, int64_t row_s
                                          stream));
 }
 
+// Grids below 2^32 threads: tiles of 64 x 64 outputs by 256 threads, strips of
+// maps by 512.
 static bool i8_dims_ok(int N, int M, int K, int P) {
   if (N <= 0 || M <= 0 || K <= 0 || P <= 0 || N > kMaxDim || M > kMaxDim || K > kMaxDim) return false;
-  if ((long)N * P > (1L << 30)) return false;
-  return (((long)N * P + 63) / 64) * ((M + 63) / 64) <= (1L << 24);
+  if ((long)N * P > (1L << 28)) return false;
+  return (((long)N * P + 63) / 64) * ((M + 63) / 64) <= (1L << 23);
 }
 
 int bc_i8_pitch(int K) { return K <= 0 || K > kMaxDim ? 0 : bc::i8_pitch(K); }

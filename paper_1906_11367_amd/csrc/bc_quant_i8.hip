@@ -21,8 +21,8 @@ __global__ __launch_bounds__(256) void k_quant_rows(const char* src, long bs, lo
   constexpr int kPiece = W * 1024;
   __shared__ uint32_t tops[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k1 = (threadIdx.x & (64 * W - 1)) * 16;
-  const long row = W == 4 ? blockIdx.x : (long)blockIdx.x * 4 + wave;
-  if (row >= rows) return;   // W = 4: never
+  const long b = (long)blockIdx.y * gridDim.x + blockIdx.x, row = W == 4 ? b : b * 4 + wave;
+  if (row >= rows) return;   // W = 4: the whole block
   const char* p = src + ((row / P) * bs + (row % P) * rs) * kBytes<DT>;
   auto load = [&](int k) { return load_vec<DT, 16>(p + (long)k * kBytes<DT>, K - k); };
   Raw<kWords<DT, 16>> x[kHeldPieces];
@@ -139,7 +139,8 @@ hipError_t launch_quantize_i8(const void* src, int dt, long bs, long rs, void* q
   } else {
     const long rows = (long)N * P;
     const bool block = K > 2 * 1024 || rows < 1024;   // a block to a row
-    const dim3 grid((unsigned)(block ? rows : (rows + 3) / 4));
+    const long blocks = block ? rows : (rows + 3) / 4, across = std::min(blocks, 1L << 22);
+    const dim3 grid((unsigned)across, (unsigned)((blocks + across - 1) / across));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, x, bs, rs, out, scale, rows, P, K, pitch); };
     if (dt == kBF16) block ? go(k_quant_rows<kBF16, 4>) : go(k_quant_rows<kBF16, 1>);
     else block ? go(k_quant_rows<kF32, 4>) : go(k_quant_rows<kF32, 1>);

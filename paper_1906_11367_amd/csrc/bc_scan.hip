@@ -223,9 +223,13 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdA
   const int grp = tid % kGroups, slot = tid / kGroups;
   constexpr int kParts = kChain ? X::kThreads / CW : 1;
   __shared__ float lookA[kParts][CW], lookB[kParts][CW];
-  int unit = blockIdx.x, place = 0;
+  int unit, place = 0;
   if constexpr (kChain) {
     if (!draw_ticket(p.tickets, p.N * p.slabs, p.tiles, unit, place)) return;
+  } else {
+    const long b = (long)blockIdx.y * gridDim.x + blockIdx.x;
+    if (b >= (long)p.N * p.slabs) return;
+    unit = (int)b;
   }
   const int n = unit / p.slabs, slab = unit % p.slabs;
   const int c0 = slab * CW + grp * V, avail = p.C - c0;   // <= 0: no channel here
@@ -361,9 +365,13 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_bwd(BwdA
   const int grp = tid % kGroups, slot = tid / kGroups;
   constexpr int kParts = kChain ? X::kThreads / CW : 1;
   __shared__ float lookA[kParts][CW], lookB[kParts][CW];
-  int unit = blockIdx.x, place = 0;
+  int unit, place = 0;
   if constexpr (kChain) {
     if (!draw_ticket(p.tickets, p.N * p.slabs, p.tiles, unit, place)) return;
+  } else {
+    const long b = (long)blockIdx.y * gridDim.x + blockIdx.x;
+    if (b >= (long)p.N * p.slabs) return;
+    unit = (int)b;
   }
   const int n = unit / p.slabs, slab = unit % p.slabs;
   const int c0 = slab * CW + grp * V, avail = p.C - c0;
@@ -605,15 +613,17 @@ size_t words_of(int N, int T, int C) {
 }
 
 // Launches the kernel of a cut; chained ones after a fill of their words.  A
-// grid has at most 2^32 threads along x; chained blocks past the end return.
+// grid has less than 2^32 threads along x; blocks past the end return.
 template <class X, class Args, class Chained, class Single>
 hipError_t launch_cut(Args& p, Chained chained, Single single, void* ws, hipStream_t s) {
   const Plan q = plan_of<X>(p.N, p.T, p.C);
   p.slabs = (int)(q.units / p.N);
   p.tiles = q.tiles;
   p.groups = (q.tiles + kGroupTiles - 1) / kGroupTiles;
+  const long blocks = q.units * q.tiles, x = std::min(blocks, 1L << 22);
+  const dim3 grid((unsigned)x, (unsigned)((blocks + x - 1) / x));
   if (q.words == 0) {
-    hipLaunchKernelGGL(single, dim3((unsigned)q.units), dim3(X::kThreads), 0, s, p);
+    hipLaunchKernelGGL(single, grid, dim3(X::kThreads), 0, s, p);
     return hipGetLastError();
   }
   unsigned long long* w = static_cast<unsigned long long*>(ws);
@@ -623,8 +633,7 @@ hipError_t launch_cut(Args& p, Chained chained, Single single, void* ws, hipStre
   hipLaunchKernelGGL(k_scan_clear, dim3((unsigned)((q.words / 2 + 256) / 256)), dim3(256), 0, s, w, q.words);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const long blocks = q.units * q.tiles, x = std::min(blocks, 1L << 22);
-  hipLaunchKernelGGL(chained, dim3((unsigned)x, (unsigned)((blocks + x - 1) / x)), dim3(X::kThreads), 0, s, p);
+  hipLaunchKernelGGL(chained, grid, dim3(X::kThreads), 0, s, p);
   return hipGetLastError();
 }
 

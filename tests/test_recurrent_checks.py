@@ -63,7 +63,7 @@ def test_scan_bwd_refuses(bad, status):
 @pytest.mark.parametrize("bad,status", [
     (dict(gate=None), NULL), (dict(x=None), NULL), (dict(state=None), NULL), (dict(state_out=None), NULL),
     (dict(y=None), NULL), (dict(N=0), SHAPE), (dict(C=0), SHAPE), (dict(S=0), SHAPE), (dict(C=65537, rs=65537), SHAPE),
-    (dict(N=(1 << 20) + 1), SHAPE), (dict(slots=None, N=5), SHAPE), (dict(rs=7), SHAPE), (dict(dt=bc.BC_I32), DTYPE),
+    (dict(N=(1 << 20) + 1), SHAPE), (dict(N=65536, C=65536, rs=65536), SHAPE), (dict(slots=None, N=5), SHAPE), (dict(rs=7), SHAPE), (dict(dt=bc.BC_I32), DTYPE),
     (dict(form=5), UNSUPPORTED), (dict(gate=P4), ALIGN), (dict(state=P4), ALIGN), (dict(state_out=P4), ALIGN),
     (dict(slots=P4), ALIGN), (dict(y=P4), ALIGN)])
 def test_scan_step_refuses(bad, status):
