@@ -38,27 +38,49 @@ __device__ __forceinline__ void mix_tile(const Args& p, int n, int pt, uint32_t 
   constexpr int XB = PX / 32;   // blocks of 32 pixels
   const int p0 = pt + (tid % (PX / 8)) * 8, lp = p.steps * kStepK<PX>;
   const char* base = p.x + ((long)n * p.bs + p0) * kBytes<DT>;
+  // a wave: 32 weight rows by the pixels.  Lane l of matrix instruction t of a
+  // block of 128 codes has chunk 2 t + l / 32 of row l % 32.
+  const int pa = lane & 31, blocks = p.pitch / 128;
+  const int wt = p.packed ? 1024 : 32, wk = 4 * wt;   // bytes from one t to the next, from a block to the next
+  auto weights = [&](int m0) {
+    return p.packed ? p.w + (long)m0 * p.pitch + lane * 16
+                    : p.w + (long)min(m0 + pa, p.M - 1) * p.pitch + half * 16;
+  };
+  i32x4_t b[4], next[4];
+  auto first = [&](int m0) {
+    const int8_t* w = weights(m0);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) b[t] = *reinterpret_cast<const i32x4_t*>(w + t * wt);
+  };
   {
     Raw<kWords<DT, 8>> x[kHold + 1][4];
     tile_scales<DT, PX, kHold, kFull>(base, p.rs, p.P - p0, p.K, x, tops, rows);
+    if (wave * 32 < p.M) first(wave * 32);   // on its way while the codes are made
     tile_codes<DT, PX, kHold, kFull>(base, p.rs, p.P - p0, p.K, x, rows, lds, lp, 0, p.steps);
   }
   __syncthreads();
-  // a wave: 32 weight rows by the 64 pixels.  Lane l of matrix instruction t of
-  // a block of 128 codes has chunk 2 t + l / 32 of row l % 32.
-  const int pa = lane & 31, swap[2] = {chunk_swap<PX>(pa), chunk_swap<PX>(pa + 32)}, blocks = p.pitch / 128;
+  const int swap[2] = {chunk_swap<PX>(pa), chunk_swap<PX>(pa + 32)};
   for (int m0 = wave * 32; m0 < p.M; m0 += kTileThreads / 64 * 32) {
-    const int8_t* w = p.packed ? p.w + (long)m0 * p.pitch + lane * 16
-                               : p.w + (long)min(m0 + pa, p.M - 1) * p.pitch + half * 16;
-    const int wt = p.packed ? 1024 : 32, wk = 4 * wt;   // bytes from one t to the next, from a block to the next
+    if (m0 > wave * 32) first(m0);
+    const int8_t* w = weights(m0);
+    // scales and biases of the lane's rows: element r of a lane is weight row
+    // 8 (r / 4) + 4 half + r % 4.  Ahead of the products where registers are left.
+    constexpr bool kEarly = XB == 1;
+    float sw[16], bias[16];
+    auto row_factors = [&]() {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int mr = min(m0 + 8 * (r >> 2) + 4 * half + (r & 3), p.M - 1);
+        sw[r] = p.wscale[mr];
+        bias[r] = p.bias ? p.bias[mr] : 0.f;
+      }
+    };
+    if (kEarly) row_factors();
     i32x16_t acc[XB];
 #pragma unroll
     for (int x = 0; x < XB; ++x)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[x][r] = 0;
-    i32x4_t b[4], next[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) b[t] = *reinterpret_cast<const i32x4_t*>(w + t * wt);
     for (int k = 0; k < blocks; ++k) {
       if (k + 1 < blocks) w += wk;   // the last block again: never used
 #pragma unroll
@@ -74,17 +96,16 @@ __device__ __forceinline__ void mix_tile(const Args& p, int n, int pt, uint32_t 
 #pragma unroll
       for (int t = 0; t < 4; ++t) b[t] = next[t];
     }
-    // element r of a lane: weight row 8 (r / 4) + 4 half + r % 4, pixel lane %
-    // 32 of its block: a store writes a row's 32 pixels in one run
+    if (!kEarly) row_factors();
+    // a store writes 32 pixels of a row in one run
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int mr = m0 + 8 * (r >> 2) + 4 * half + (r & 3);
       if (mr >= p.M) continue;
-      const float sw = p.wscale[mr], bias = p.bias ? p.bias[mr] : 0.f;
       char* o = p.out + (((long)n * p.M + mr) * p.P + pt + pa) * kBytes<OUT>;
 #pragma unroll
       for (int x = 0; x < XB; ++x) {
-        const float v = __fmaf_rn((float)acc[x][r] * rows[pa + 32 * x].scale, sw, bias);
+        const float v = __fmaf_rn((float)acc[x][r] * rows[pa + 32 * x].scale, sw[r], bias[r]);
         const float z = v < p.floor ? p.floor : v;   // a NaN stays
         if (!kFull && pt + pa + 32 * x >= p.P) continue;
         if constexpr (OUT == kBF16) __builtin_nontemporal_store((uint16_t)pair_bf16(z, 0.f), reinterpret_cast<uint16_t*>(o) + 32 * x);
