@@ -25,7 +25,32 @@ __device__ __forceinline__ RowScale row_scale(uint32_t top) {
   return {127.f / m, m / 127.f};
 }
 
-__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// The largest |x| of elements that stand in one place of several vectors, as
+// bits: bf16 two at a time, as they are stored.
+template <int DT, int V>
+struct Largest {
+  Raw<kWords<DT, V>> m = {};
+  __device__ __forceinline__ void take(const Raw<kWords<DT, V>>& x) {
+    typedef unsigned short U16 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int w = 0; w < kWords<DT, V>; ++w) {
+      const uint32_t a = m[w], b = x[w];   // words of their own: a bit cast of a vector's element takes the vector's first
+      if constexpr (DT == kBF16)
+        m[w] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(U16, a),
+                                                                      __builtin_bit_cast(U16, b & 0x7fff7fffu)));
+      else
+        m[w] = max(a, b & 0x7fffffffu);
+    }
+  }
+  // of element k; of all of them
+  __device__ __forceinline__ uint32_t at(int k) const { return __float_as_uint(elem<DT, V>(m, k)); }
+  __device__ __forceinline__ uint32_t all() const {
+    uint32_t t = 0;
+#pragma unroll
+    for (int k = 0; k < V; ++k) t = max(t, at(k));
+    return t;
+  }
+};
 
 // Four codes in a word.  Adding 1.5 * 2^23 to the rounded product rounds it to
 // the nearest even integer and leaves that in the low byte; inv = 0 (a row
@@ -83,23 +108,20 @@ __device__ __forceinline__ void tile_scales(const char* base, long rs, int avail
   for (int s = 0; s < kHold; ++s)
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[s][i] = tile_load<DT, kFull>(base, rs, avail, s * Step + kg * 4 + i, K);
-  uint32_t top[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) top[j] = 0;
+  Largest<DT, 8> largest;
 #pragma unroll
   for (int s = 0; s < kHold; ++s)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top[j] = max(top[j], abs_bits(elem<DT, 8>(x[s][i], j)));
+    for (int i = 0; i < 4; ++i) largest.take(x[s][i]);
   for (int s = kHold; s * Step < K; ++s) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[kHold][i] = tile_load<DT, kFull>(base, rs, avail, s * Step + kg * 4 + i, K);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top[j] = max(top[j], abs_bits(elem<DT, 8>(x[kHold][i], j)));
+    for (int i = 0; i < 4; ++i) largest.take(x[kHold][i]);
   }
+  uint32_t top[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top[j] = largest.at(j);
 #pragma unroll
   for (int d = PL; d < 64; d *= 2)
 #pragma unroll

@@ -82,9 +82,9 @@ __global__ __launch_bounds__(kThreads) void k_mix_i8_few(Args p) {
     for (int i = 0; i < kItems; ++i) {
       const int it = wave + i * kWaves;
       if (it >= items) break;
-      uint32_t top = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = max(top, abs_bits(elem<DT, 8>(x[i], j)));
+      Largest<DT, 8> largest;
+      largest.take(x[i]);
+      uint32_t top = largest.all();
 #pragma unroll
       for (int d = 32; d > 0; d /= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
       if (lane == 0) atomicMax(&tops[it / per], top);   // the largest: in any order

@@ -36,14 +36,11 @@ __global__ __launch_bounds__(256) void k_quant_rows(const char* src, long bs, lo
 #pragma unroll
     for (int i = 0; i < kHeldPieces; ++i) x[i] = load(k1 + i * kPiece);
   }
-  uint32_t top = 0;
-  auto note = [&](const Raw<kWords<DT, 16>>& r) {
+  Largest<DT, 16> largest;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) top = max(top, abs_bits(elem<DT, 16>(r, k)));
-  };
-#pragma unroll
-  for (int i = 0; i < kHeldPieces; ++i) note(x[i]);
-  for (int k = k1 + kHeldPieces * kPiece; k < K; k += kPiece) note(load(k));
+  for (int i = 0; i < kHeldPieces; ++i) largest.take(x[i]);
+  for (int k = k1 + kHeldPieces * kPiece; k < K; k += kPiece) largest.take(load(k));
+  uint32_t top = largest.all();
 #pragma unroll
   for (int d = 32; d > 0; d /= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
   if constexpr (W == 4) {

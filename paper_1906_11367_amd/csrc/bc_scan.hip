@@ -3,9 +3,12 @@
 //
 // Bound by memory: the forward reads two tensors and writes one, the backward
 // reads three and writes two, with 10 to 40 operations per element.  A block
-// takes a slab of 128 bytes of channels (whole cache lines of every row) and
-// walks tiles of kSlots * L steps: a lane holds 16 bytes of channels for L
-// consecutive steps in registers, so every element is read once.
+// takes a slab of channels (whole cache lines of every row) by a tile of steps: a
+// lane holds a few channels of a few consecutive steps in registers, so every
+// element is read once.
+// 8 x 4096 x 2048 bf16: forward 90 us (4.5 TB/s), backward 146 (4.6 TB/s); 1 x
+// 65536 x 1024 bf16 forward 105 (3.8); 64 x 512 x 1024 fp32 82 and 122 (4.9, 5.5):
+// a copy of 1 GiB reaches 5.2 here.
 #include "bc_scan.hpp"
 
 #include <algorithm>
@@ -16,8 +19,8 @@ namespace {
 using namespace scan;
 
 // The division of a tile: lanes hold kV channels of kL consecutive steps;
-// kGroups lanes side by side make a slab (128 bytes: whole cache lines of every
-// row), kSlots runs of steps a tile.  W_: waves per SIMD to build for.
+// kGroups lanes side by side make a slab (128 bytes or more: whole cache lines of
+// every row), kSlots runs of steps a tile.  W_: waves per SIMD to build for.
 template <int V_, int G_, int NT_, int L_, int W_>
 struct Cut {
   static constexpr int kV = V_, kGroups = G_, kThreads = NT_, kL = L_, kWavesPerSimd = W_;
@@ -25,14 +28,15 @@ struct Cut {
 };
 // Cut 0 is the chained tiles'.  A sequence of one tile takes the shortest cut
 // that holds it: a tile of 128 steps for a sequence of 4 would leave all but a
-// few lanes of the block idle (256 x 8 x 4096 bf16 forward: 31 us instead of 8).
-// Measured on 2^26 elements (bf16) and 2^25 (fp32) in chained tiles, us, for 256
-// and for 16 chains:
-//   forward, bf16: 4 channels x 8 steps a lane in 256 threads 81, 94; in 512
-//     threads 90, 93; 8 x 4 in 512 107, 105
-//   backward, bf16: 2 x 8 in 512 threads 143, 159; in 256 140, 178; 4 x 4 in 512
-//     171, 180; 2 x 4 in 512 160, 193
-//   fp32: forward 4 x 4 in 512 threads 76, backward 127
+// few lanes of the block idle (256 x 4 x 4096 bf16 forward: 31 us instead of 11).
+// Measured on 2^26 elements (bf16) and 2^25 (fp32) in chained tiles, us, other
+// tensors from call to call, for 256 and for 16 chains:
+//   forward, bf16: 4 channels x 8 steps a lane in 256 threads 90, 105; in 512
+//     threads 99, 100; 8 x 8 in 512 132, 125; 2 x 8 in 512 91, 110
+//   backward, bf16: 2 x 8 in 512 threads 146, 160; in 256 142, 178; 4 x 4 in 512
+//     175, 180; 2 x 4 in 512 163, 193
+//   fp32, 4 x 4 in 512 threads on 64 channels: forward 82, 85, backward 121, 123;
+//     on 32 channels 93, 86 and 130, 126; in 256 threads on 32 82, 88 and 118, 127
 // Longer tiles cost registers (fewer waves), shorter ones more carries.
 template <class... Xs> struct CutList {};
 template <int DT> struct FwdCuts;   // the chained cut, then the others' tiles in rising order
@@ -42,9 +46,9 @@ template <> struct FwdCuts<kBF16> {
                        Cut<4, 16, 512, 8, 4>>;   // 8, 32, 64, 128, 256
 };
 template <> struct FwdCuts<kF32> {
-  using chained = Cut<4, 8, 512, 4, 4>;   // 256
-  using list = CutList<Cut<4, 64, 64, 8, 4>, Cut<4, 8, 64, 4, 4>, Cut<4, 8, 128, 4, 4>, Cut<4, 8, 256, 4, 4>,
-                       chained>;   // 8, 32, 64, 128, 256
+  using chained = Cut<4, 16, 512, 4, 4>;   // 128
+  using list = CutList<Cut<4, 64, 64, 8, 4>, Cut<4, 8, 64, 4, 4>, Cut<4, 8, 128, 4, 4>, chained,
+                       Cut<4, 8, 512, 4, 4>>;   // 8, 32, 64, 128, 256
 };
 template <int DT> struct BwdCuts;
 template <> struct BwdCuts<kBF16> {
@@ -53,9 +57,9 @@ template <> struct BwdCuts<kBF16> {
                        chained>;   // 8, 16, 32, 64, 128
 };
 template <> struct BwdCuts<kF32> {
-  using chained = Cut<4, 8, 512, 4, 4>;   // 256
-  using list = CutList<Cut<4, 64, 64, 4, 4>, Cut<4, 8, 64, 4, 4>, Cut<4, 8, 128, 4, 4>, Cut<4, 8, 256, 4, 4>,
-                       chained>;   // 4, 32, 64, 128, 256
+  using chained = Cut<4, 16, 512, 4, 4>;   // 128
+  using list = CutList<Cut<4, 64, 64, 4, 4>, Cut<4, 8, 64, 4, 4>, Cut<4, 8, 128, 4, 4>, chained,
+                       Cut<4, 8, 512, 4, 4>>;   // 4, 32, 64, 128, 256
 };
 // States are kept every kScanSpan steps: at every tile of the chained backward.
 static_assert(BwdCuts<kBF16>::chained::kTile % kScanSpan == 0 && BwdCuts<kF32>::chained::kTile % kScanSpan == 0,
