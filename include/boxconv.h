@@ -439,11 +439,13 @@ typedef enum { BC_GATE_LOGIT = 0, BC_GATE_VALUE = 1 } bc_gate_form;
  *           past it, y is zero there and h_last is the state at it (h0 for an
  *           empty sequence).
  * y       : device, dense in the layout's order; y_dt = dt, or BC_BF16 for
- *           BC_F32 inputs (the operand of a bf16 mix).
+ *           BC_F32 inputs (the operand of a bf16 mix).  It shares no memory
+ *           with an input.
  * h_last  : device fp32 [N][C], or NULL.  May be h0.
  * states  : NULL, or device fp32, bc_gated_scan_states_bytes() bytes: the
  *           states the backward starts from (its layout is the library's).
  * ws      : >= bc_gated_scan_workspace_bytes(0, ...) bytes, NULL when that is 0.
+ *           A workspace for more steps (T) serves fewer.
  * Non-finite values spread as the recurrence spreads them: forward in time in
  * their own channel and sequence (also through a reset: 0 * infinity), nowhere
  * else.
@@ -524,7 +526,7 @@ size_t bc_gated_scan_states_bytes(int N, int T, int C, int layout);
  * x_scale     : with BC_I8 only; NULL otherwise (BC_ERR_UNSUPPORTED).
  * bias        : device fp32 [M], or NULL.
  * out         : device, dense, out_dt = BC_F32 or BC_BF16: [N][P][M]
- *               (BC_TOKENS) or [N][M][P] (BC_MAPS).
+ *               (BC_TOKENS) or [N][M][P] (BC_MAPS); it shares no memory with an input.
  * ws          : >= bc_mix_i8_workspace_bytes(...) bytes, NULL when that is 0.
  * Sizes: N, M, K <= 65536, N * P <= 2^28, the output's tiles of 64 x 64 at
  * most 2^23 (BC_ERR_SHAPE).

@@ -38,26 +38,35 @@ struct Cut {
 //   fp32, 4 x 4 in 512 threads on 64 channels: forward 82, 85, backward 121, 123;
 //     on 32 channels 93, 86 and 130, 126; in 256 threads on 32 82, 88 and 118, 127
 // Longer tiles cost registers (fewer waves), shorter ones more carries.
+// A few long chains wait for their carries, one after the other: the forward cuts
+// them into half as many tiles (`far`), us at 4, 8 and 16 chains of 2048, 1024 and
+// 512 tiles: bf16 112 for 158, 109 for 118, 100 for 105; fp32, 4 chains of 1024,
+// 85 for 104.  At 32 chains of 256 tiles both take 98, and 2 of 32 tiles take 9.1
+// for 7.7; the backward with such tiles takes 182 for 161 (16 chains).
 template <class... Xs> struct CutList {};
-template <int DT> struct FwdCuts;   // the chained cut, then the others' tiles in rising order
+template <int DT> struct FwdCuts;   // the chained cuts, then the others' tiles in rising order
 template <> struct FwdCuts<kBF16> {
   using chained = Cut<4, 16, 256, 8, 4>;   // 128 steps
+  using far = Cut<4, 16, 512, 8, 4>;       // 256
   using list = CutList<Cut<4, 64, 64, 8, 4>, Cut<4, 16, 64, 8, 4>, Cut<4, 16, 128, 8, 4>, chained,
-                       Cut<4, 16, 512, 8, 4>>;   // 8, 32, 64, 128, 256
+                       far>;   // 8, 32, 64, 128, 256
 };
 template <> struct FwdCuts<kF32> {
   using chained = Cut<4, 16, 512, 4, 4>;   // 128
+  using far = Cut<4, 16, 512, 8, 4>;       // 256
   using list = CutList<Cut<4, 64, 64, 8, 4>, Cut<4, 8, 64, 4, 4>, Cut<4, 8, 128, 4, 4>, chained,
                        Cut<4, 8, 512, 4, 4>>;   // 8, 32, 64, 128, 256
 };
 template <int DT> struct BwdCuts;
 template <> struct BwdCuts<kBF16> {
   using chained = Cut<2, 32, 512, 8, 4>;   // 128
+  using far = chained;
   using list = CutList<Cut<2, 64, 64, 8, 4>, Cut<2, 32, 64, 8, 4>, Cut<2, 32, 128, 8, 4>, Cut<2, 32, 256, 8, 4>,
                        chained>;   // 8, 16, 32, 64, 128
 };
 template <> struct BwdCuts<kF32> {
   using chained = Cut<4, 16, 512, 4, 4>;   // 128
+  using far = chained;
   using list = CutList<Cut<4, 64, 64, 4, 4>, Cut<4, 8, 64, 4, 4>, Cut<4, 8, 128, 4, 4>, chained,
                        Cut<4, 8, 512, 4, 4>>;   // 4, 32, 64, 128, 256
 };
@@ -600,20 +609,32 @@ Plan plan_of(int N, int T, int C) {
   return q;
 }
 
-// Calls f with the cut of a sequence of T steps: the first of the list that
-// holds it, or the chained one.
-template <class Chained, class F, class X, class... Xs>
-auto with_cut(int T, F f, CutList<X, Xs...>) {
-  if (T <= X::kTile) return f(X{});
-  if constexpr (sizeof...(Xs) > 0) return with_cut<Chained>(T, f, CutList<Xs...>{});
-  else return f(Chained{});
+// Calls f with the cut of N x C sequences of T steps and that of its chained
+// kernel: the first of the list that holds the steps, or one of the chained.
+template <class Cuts, class F, class X, class... Xs>
+auto with_cut(int N, int T, int C, F f, CutList<X, Xs...>) {
+  using Chained = typename Cuts::chained;
+  using Far = typename Cuts::far;
+  if (T <= X::kTile) return f(X{}, Chained{});
+  if constexpr (sizeof...(Xs) > 0) {
+    return with_cut<Cuts>(N, T, C, f, CutList<Xs...>{});
+  } else {
+    const Plan q = plan_of<Chained>(N, T, C);
+    if (q.tiles >= 128 && q.tiles >= 16 * q.units) return f(Far{}, Far{});
+    return f(Chained{}, Chained{});
+  }
 }
 template <class Cuts, class F>
-auto with_cut(int T, F f) { return with_cut<typename Cuts::chained>(T, f, typename Cuts::list{}); }
+auto with_cut(int N, int T, int C, F f) { return with_cut<Cuts>(N, T, C, f, typename Cuts::list{}); }
 
+// The workspace's words: the chained cut's where the far one, with half of them,
+// is taken too, so that a workspace for longer sequences serves shorter ones.
 template <class Cuts>
 size_t words_of(int N, int T, int C) {
-  return (size_t)with_cut<Cuts>(T, [&](auto x) { return plan_of<decltype(x)>(N, T, C).words; });
+  return (size_t)with_cut<Cuts>(N, T, C, [&](auto x, auto) {
+    using X = decltype(x);
+    return X::kTile < T ? plan_of<typename Cuts::chained>(N, T, C).words : 0;
+  });
 }
 
 // Launches the kernel of a cut; chained ones after a fill of their words.  A
@@ -643,19 +664,17 @@ hipError_t launch_cut(Args& p, Chained chained, Single single, void* ws, hipStre
 
 template <int IN, int OUT, int FORM>
 hipError_t fwd_form(FwdArgs& p, void* ws, hipStream_t s) {
-  using Chained = typename FwdCuts<IN>::chained;
-  return with_cut<FwdCuts<IN>>(p.T, [&](auto x) {
+  return with_cut<FwdCuts<IN>>(p.N, p.T, p.C, [&](auto x, auto chained) {
     using X = decltype(x);
-    return launch_cut<X>(p, k_scan_fwd<Chained, IN, OUT, FORM, true>, k_scan_fwd<X, IN, OUT, FORM, false>, ws, s);
+    return launch_cut<X>(p, k_scan_fwd<decltype(chained), IN, OUT, FORM, true>, k_scan_fwd<X, IN, OUT, FORM, false>, ws, s);
   });
 }
 
 template <int IN, int OUT, int FORM>
 hipError_t bwd_form(BwdArgs& p, void* ws, hipStream_t s) {
-  using Chained = typename BwdCuts<IN>::chained;
-  return with_cut<BwdCuts<IN>>(p.T, [&](auto x) {
+  return with_cut<BwdCuts<IN>>(p.N, p.T, p.C, [&](auto x, auto chained) {
     using X = decltype(x);
-    return launch_cut<X>(p, k_scan_bwd<Chained, IN, OUT, FORM, true>, k_scan_bwd<X, IN, OUT, FORM, false>, ws, s);
+    return launch_cut<X>(p, k_scan_bwd<decltype(chained), IN, OUT, FORM, true>, k_scan_bwd<X, IN, OUT, FORM, false>, ws, s);
   });
 }
 

@@ -116,6 +116,15 @@ def test_tokens(N, T, C, dt, form):
     run_both(inputs(11, N, T, C, dt, "tokens", form), N, T, C, dt, "tokens", form)
 
 
+# few chains, long enough that the forward cuts them into longer tiles (256 steps)
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("N,T,C,lengths", [(1, 16385, 9, None), (1, 16640, 64, [16639]), (2, 17001, 70, [17001, 4353]),
+                                           (3, 16500, 3, [0, 1, 16257])])
+def test_few_long_chains(N, T, C, lengths, dt):
+    say("scan few long chains", N, T, C, lengths, dt)
+    run_both(inputs(21, N, T, C, dt, "tokens", "logit"), N, T, C, dt, "tokens", "logit", lengths)
+
+
 # lengths around a lane's run (8), a wave's segment (512) and several of them;
 # rows that take one wave, four and sixteen
 @pytest.mark.parametrize("form", ["logit", "value"])

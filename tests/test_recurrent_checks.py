@@ -107,6 +107,15 @@ def test_sizes():
     assert lib.bc_mix_i8_workspace_bytes(1, 300, 500, 2000, bc.BC_F32, 0) >= 2000 * (512 + 4)
 
 
+def test_a_longer_scans_workspace_serves_shorter_ones():
+    lib = bc.load_library()
+    for op in (0, 1):
+        for dt in (bc.BC_F32, bc.BC_BF16):
+            sizes = [lib.bc_gated_scan_workspace_bytes(op, 1, T, 200, dt, bc.BC_TOKENS)
+                     for T in (1, 128, 129, 257, 300, 2048, 16256, 16257, 16384, 16385, 40000, 300000)]
+            assert sizes == sorted(sizes) and sizes[0] == 0 and sizes[-1] > 0
+
+
 def t(*shape, dtype=torch.float32):
     return torch.zeros(shape, dtype=dtype)
 
