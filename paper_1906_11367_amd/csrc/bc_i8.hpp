@@ -82,32 +82,43 @@ __device__ __forceinline__ int chunk_swap(int p) {
   else return p & 15;
 }
 
-// The lane's 8 pixels of channel k.  kFull: all 8 exist.
+// The 8 pixels of a lane, from the tile's pixel `first` on.  In a row's last tile
+// the lanes that pass its end take the 8 before the end again (the same values in
+// the same places; pixels before the tile are left out), so that every load is a
+// wide one; a row of less than 8 pixels is read piece by piece (short).
+struct Pixels {
+  int first, avail;
+  bool short_row;
+  __device__ __forceinline__ Pixels(int lane_first, int left, int P)
+      : first(P < 8 ? lane_first : min(lane_first, left - 8)), avail(left - first), short_row(P < 8) {}
+};
+
+// The lane's 8 pixels of channel k.  kFull: a tile of whole rows.
 template <int DT, bool kFull>
-__device__ __forceinline__ Raw<kWords<DT, 8>> tile_load(const char* base, long rs, int avail, int k, int K) {
+__device__ __forceinline__ Raw<kWords<DT, 8>> tile_load(const char* base, long rs, const Pixels& at, int k, int K) {
   const char* p = base + (long)k * rs * kBytes<DT>;
-  if constexpr (kFull) {
+  if (kFull || !at.short_row) {   // for all lanes of the block
     Raw<kWords<DT, 8>> r = {};
     if (k < K) r = __builtin_bit_cast(Raw<kWords<DT, 8>>, *reinterpret_cast<const Loose<kWords<DT, 8>, kBytes<DT>>*>(p));
     return r;
   } else {
-    return load_vec<DT, 8>(p, k < K ? avail : 0);
+    return load_vec<DT, 8>(p, k < K ? at.avail : 0);
   }
 }
 
-// Row scales of the tile.  base: the lane's pixels at channel 0 (`avail` of the
-// 8 exist), rs elements between channels.  The first kHold steps of channels
-// stay in registers (x); later ones are read again for their codes.
+// Row scales of the tile.  base: the lane's pixels at channel 0, rs elements
+// between channels.  The first kHold steps of channels stay in registers (x);
+// later ones are read again for their codes.
 // tops: 8 x PX words of LDS, rows: PX RowScales of LDS, whole after the call.
 template <int DT, int PX, int kHold, bool kFull>
-__device__ __forceinline__ void tile_scales(const char* base, long rs, int avail, int K,
+__device__ __forceinline__ void tile_scales(const char* base, long rs, const Pixels& at, int K,
                                             Raw<kWords<DT, 8>> (&x)[kHold + 1][4], uint32_t* tops, RowScale* rows) {
   constexpr int PL = PX / 8, Step = kStepK<PX>;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kg = tid / PL;
 #pragma unroll
   for (int s = 0; s < kHold; ++s)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[s][i] = tile_load<DT, kFull>(base, rs, avail, s * Step + kg * 4 + i, K);
+    for (int i = 0; i < 4; ++i) x[s][i] = tile_load<DT, kFull>(base, rs, at, s * Step + kg * 4 + i, K);
   Largest<DT, 8> largest;
 #pragma unroll
   for (int s = 0; s < kHold; ++s)
@@ -115,7 +126,7 @@ __device__ __forceinline__ void tile_scales(const char* base, long rs, int avail
     for (int i = 0; i < 4; ++i) largest.take(x[s][i]);
   for (int s = kHold; s * Step < K; ++s) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[kHold][i] = tile_load<DT, kFull>(base, rs, avail, s * Step + kg * 4 + i, K);
+    for (int i = 0; i < 4; ++i) x[kHold][i] = tile_load<DT, kFull>(base, rs, at, s * Step + kg * 4 + i, K);
 #pragma unroll
     for (int i = 0; i < 4; ++i) largest.take(x[kHold][i]);
   }
@@ -128,7 +139,8 @@ __device__ __forceinline__ void tile_scales(const char* base, long rs, int avail
     for (int j = 0; j < 8; ++j) top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], d));
   if (lane < PL) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) tops[wave * PX + lane * 8 + j] = top[j];
+    for (int j = 0; j < 8; ++j)
+      if (kFull || at.first + j >= 0) tops[wave * PX + at.first + j] = top[j];
   }
   __syncthreads();
   if (tid < PX) {
@@ -143,21 +155,21 @@ __device__ __forceinline__ void tile_scales(const char* base, long rs, int avail
 // Codes of the channels of steps [s0, s1) into LDS at `lds`, for the rows scaled
 // above.
 template <int DT, int PX, int kHold, bool kFull>
-__device__ __forceinline__ void tile_codes(const char* base, long rs, int avail, int K,
+__device__ __forceinline__ void tile_codes(const char* base, long rs, const Pixels& at, int K,
                                            Raw<kWords<DT, 8>> (&x)[kHold + 1][4], const RowScale* rows, uint32_t lds,
                                            int pitch, int s0, int s1) {
   constexpr int PL = PX / 8, Step = kStepK<PX>;
-  const int kg = threadIdx.x / PL, p0 = (threadIdx.x % PL) * 8;
+  const int kg = threadIdx.x / PL, p0 = at.first;
   float inv[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) inv[j] = rows[p0 + j].inv;
+  for (int j = 0; j < 8; ++j) inv[j] = rows[kFull ? p0 + j : max(p0 + j, 0)].inv;
   auto put = [&](int s, const Raw<kWords<DT, 8>> (&y)[4]) {
     const int k = (s - s0) * Step + kg * 4;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint32_t w = codes4(elem<DT, 8>(y[0], j), elem<DT, 8>(y[1], j), elem<DT, 8>(y[2], j), elem<DT, 8>(y[3], j), inv[j]);
       const int p = p0 + j;
-      *(BC_LDS uint32_t*)(uintptr_t)(lds + p * pitch + (((k >> 4) ^ chunk_swap<PX>(p)) << 4) + (k & 15)) = w;
+      if (kFull || p >= 0) *(BC_LDS uint32_t*)(uintptr_t)(lds + p * pitch + (((k >> 4) ^ chunk_swap<PX>(p)) << 4) + (k & 15)) = w;
     }
   };
   // the words stay as loaded: unpacked values are not kept from the scales on
@@ -170,7 +182,7 @@ __device__ __forceinline__ void tile_codes(const char* base, long rs, int avail,
     if (s >= s0 && s < s1) put(s, x[s]);
   for (int s = max(s0, kHold); s < s1; ++s) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[kHold][i] = tile_load<DT, kFull>(base, rs, avail, s * Step + kg * 4 + i, K);
+    for (int i = 0; i < 4; ++i) x[kHold][i] = tile_load<DT, kFull>(base, rs, at, s * Step + kg * 4 + i, K);
     put(s, x[kHold]);
   }
 }

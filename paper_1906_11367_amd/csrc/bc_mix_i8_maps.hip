@@ -13,6 +13,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace bc {
 namespace {
 
@@ -27,17 +29,29 @@ struct Args {
   const int8_t* w;
   const float *wscale, *bias;
   char* out;
-  int M, K, P, pitch, strips, steps, packed;
+  int M, K, P, pitch, strips, steps, packed, near;
   float floor;
 };
 
-template <int DT, int OUT, int PX, int kHold, bool kFull>
+// kLined: past the caches.
+template <int OUT, bool kLined>
+__device__ __forceinline__ void store_one(char* o, float z) {
+  typedef typename std::conditional<OUT == kBF16, uint16_t, float>::type T;
+  T v;
+  if constexpr (OUT == kBF16) v = (uint16_t)pair_bf16(z, 0.f);
+  else v = z;
+  if constexpr (kLined) __builtin_nontemporal_store(v, reinterpret_cast<T*>(o));
+  else *reinterpret_cast<T*>(o) = v;
+}
+
+template <int DT, int OUT, int PX, bool kLined, int kHold, bool kFull>
 __device__ __forceinline__ void mix_tile(const Args& p, int n, int pt, uint32_t lds, uint32_t* tops, RowScale* rows) {
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   constexpr int XB = PX / 32;   // blocks of 32 pixels
-  const int p0 = pt + (tid % (PX / 8)) * 8, lp = p.steps * kStepK<PX>;
-  const char* base = p.x + ((long)n * p.bs + p0) * kBytes<DT>;
+  const Pixels at(tid % (PX / 8) * 8, p.P - pt, p.P);
+  const int lp = p.steps * kStepK<PX>;
+  const char* base = p.x + ((long)n * p.bs + pt + at.first) * kBytes<DT>;
   // a wave: 32 weight rows by the pixels.  Lane l of matrix instruction t of a
   // block of 128 codes has chunk 2 t + l / 32 of row l % 32.
   const int pa = lane & 31, blocks = p.pitch / 128;
@@ -54,9 +68,9 @@ __device__ __forceinline__ void mix_tile(const Args& p, int n, int pt, uint32_t 
   };
   {
     Raw<kWords<DT, 8>> x[kHold + 1][4];
-    tile_scales<DT, PX, kHold, kFull>(base, p.rs, p.P - p0, p.K, x, tops, rows);
+    tile_scales<DT, PX, kHold, kFull>(base, p.rs, at, p.K, x, tops, rows);
     if (wave * 32 < p.M) first(wave * 32);   // on its way while the codes are made
-    tile_codes<DT, PX, kHold, kFull>(base, p.rs, p.P - p0, p.K, x, rows, lds, lp, 0, p.steps);
+    tile_codes<DT, PX, kHold, kFull>(base, p.rs, at, p.K, x, rows, lds, lp, 0, p.steps);
   }
   __syncthreads();
   const int swap[2] = {chunk_swap<PX>(pa), chunk_swap<PX>(pa + 32)};
@@ -108,22 +122,31 @@ __device__ __forceinline__ void mix_tile(const Args& p, int n, int pt, uint32_t 
         const float v = __fmaf_rn((float)acc[x][r] * rows[pa + 32 * x].scale, sw[r], bias[r]);
         const float z = v < p.floor ? p.floor : v;   // a NaN stays
         if (!kFull && pt + pa + 32 * x >= p.P) continue;
-        if constexpr (OUT == kBF16) __builtin_nontemporal_store((uint16_t)pair_bf16(z, 0.f), reinterpret_cast<uint16_t*>(o) + 32 * x);
-        else __builtin_nontemporal_store(z, reinterpret_cast<float*>(o) + 32 * x);
+        store_one<OUT, kLined>(o + 32 * x * kBytes<OUT>, z);
       }
     }
   }
 }
 
-template <int DT, int OUT, int PX>
+// kLined: outputs go past the caches, where their rows are whole runs of 16 bytes;
+// others' shared pieces are put together in an L2.  Where rows are not whole 64
+// bytes, neighbouring strips go to one XCD (18 images of 160 x 7469 to 383 fp32
+// maps: 119 us past the caches in order, 105 through them, 89 with neighbours;
+// rows of 7464 bf16 past the caches 75 and 68; rows of 7472 fp32 67 and 77).
+template <int DT, int OUT, int PX, bool kLined>
 __global__ __launch_bounds__(kTileThreads, 4) void k_mix_i8_maps(Args p) {
   extern __shared__ __align__(16) unsigned char smem[];   // codes of the pixels
   __shared__ uint32_t tops[kTileThreads / 64 * PX];
   __shared__ RowScale rows[PX];
-  const int n = blockIdx.x / p.strips, pt = (blockIdx.x % p.strips) * PX;
+  int b = blockIdx.x;
+  if (p.near) {   // blocks go to the XCDs in turn
+    const int eighth = gridDim.x >> 3;
+    if (b < eighth * 8) b = (b & 7) * eighth + (b >> 3);
+  }
+  const int n = b / p.strips, pt = (b % p.strips) * PX;
   const uint32_t lds = (uint32_t)(uintptr_t)(BC_LDS unsigned char*)smem;
-  if (p.P - pt >= PX) mix_tile<DT, OUT, PX, kHeld<DT>, true>(p, n, pt, lds, tops, rows);
-  else mix_tile<DT, OUT, PX, kHeld<DT>, false>(p, n, pt, lds, tops, rows);
+  if (p.P - pt >= PX) mix_tile<DT, OUT, PX, kLined, kHeld<DT>, true>(p, n, pt, lds, tops, rows);
+  else mix_tile<DT, OUT, PX, kLined, kHeld<DT>, false>(p, n, pt, lds, tops, rows);
 }
 
 // Weight rows in the order in which the waves read them: 32 rows by 128 codes at
@@ -154,18 +177,20 @@ bool wide_blocks(int N, int M, int K, int P) {
 // 256 maps: 124 us without, 95 + 5 with; 64 blocks 33 and 32).
 constexpr long kPackBlocks = 32;
 
-template <int DT, int OUT, int PX>
+template <int DT, int OUT, int PX, bool kLined>
 hipError_t launch(Args& p, int N, hipStream_t s) {
   p.strips = (p.P + PX - 1) / PX;
   p.steps = (p.pitch + kStepK<PX> - 1) / kStepK<PX>;
   const size_t lds = (size_t)PX * p.steps * kStepK<PX>;
-  hipLaunchKernelGGL((k_mix_i8_maps<DT, OUT, PX>), dim3((unsigned)((long)N * p.strips)), dim3(kTileThreads), lds, s, p);
+  hipLaunchKernelGGL((k_mix_i8_maps<DT, OUT, PX, kLined>), dim3((unsigned)((long)N * p.strips)), dim3(kTileThreads), lds, s, p);
   return hipGetLastError();
 }
 
 template <int DT, int OUT>
 hipError_t launch(Args& p, int N, hipStream_t s) {
-  return wide_blocks(N, p.M, p.K, p.P) ? launch<DT, OUT, 64>(p, N, s) : launch<DT, OUT, 32>(p, N, s);
+  const bool lined = (long)p.P * kBytes<OUT> % 16 == 0 && (uintptr_t)p.out % 16 == 0;
+  if (wide_blocks(N, p.M, p.K, p.P)) return lined ? launch<DT, OUT, 64, true>(p, N, s) : launch<DT, OUT, 64, false>(p, N, s);
+  return lined ? launch<DT, OUT, 32, true>(p, N, s) : launch<DT, OUT, 32, false>(p, N, s);
 }
 
 }  // namespace
@@ -196,6 +221,7 @@ hipError_t launch_mix_i8_maps(const MixI8& m, hipStream_t s) {
   p.P = m.P;
   p.pitch = i8_pitch(m.K);
   p.floor = m.relu ? 0.f : -INFINITY;
+  p.near = (long)m.P * (m.out_dt == kBF16 ? 2 : 4) % 64 != 0;
   const size_t packed = mix_i8_maps_workspace_bytes(m.N, m.M, m.K, m.P);
   if (packed > 0) {
     const long chunks = (long)packed / 16;

@@ -69,16 +69,16 @@ __global__ __launch_bounds__(256) void k_quant_rows(const char* src, long bs, lo
 template <int PX> constexpr int kPart = PX == 64 ? 4 : 2;
 
 template <int DT, int PX, int kHold, bool kFull>
-__device__ __forceinline__ void quant_tile(const char* base, long rs, int avail, int8_t* q, int left, int K, int pitch,
+__device__ __forceinline__ void quant_tile(const char* base, long rs, const Pixels& at, int8_t* q, int left, int K, int pitch,
                                            int steps, uint32_t lds, uint32_t* tops, RowScale* rows) {
   constexpr int Step = kStepK<PX>;
   const int tid = threadIdx.x, lp = min(steps, kPart<PX>) * Step;
   Raw<kWords<DT, 8>> x[kHold + 1][4];
-  tile_scales<DT, PX, kHold, kFull>(base, rs, avail, K, x, tops, rows);
+  tile_scales<DT, PX, kHold, kFull>(base, rs, at, K, x, tops, rows);
   for (int s0 = 0; s0 < steps; s0 += kPart<PX>) {
     const int s1 = min(steps, s0 + kPart<PX>);
     if (s0 > 0) __syncthreads();
-    tile_codes<DT, PX, kHold, kFull>(base, rs, avail, K, x, rows, lds, lp, s0, s1);
+    tile_codes<DT, PX, kHold, kFull>(base, rs, at, K, x, rows, lds, lp, s0, s1);
     __syncthreads();
     // whole rows out, 16 bytes a lane
     const int chunks = min(pitch - s0 * Step, (s1 - s0) * Step) >> 4;
@@ -99,12 +99,12 @@ __global__ __launch_bounds__(kTileThreads, 4) void k_quant_maps(const char* src,
   __shared__ uint32_t tops[kTileThreads / 64 * PX];
   __shared__ RowScale rows[PX];
   const int tid = threadIdx.x, n = blockIdx.x / strips, pt = (blockIdx.x % strips) * PX, left = P - pt;
-  const int p0 = pt + (tid % (PX / 8)) * 8;
+  const Pixels at(tid % (PX / 8) * 8, left, P);
   const uint32_t lds = (uint32_t)(uintptr_t)(BC_LDS unsigned char*)smem;
-  const char* base = src + ((long)n * bs + p0) * kBytes<DT>;
+  const char* base = src + ((long)n * bs + pt + at.first) * kBytes<DT>;
   int8_t* out = q + ((long)n * P + pt) * pitch;
-  if (left >= PX) quant_tile<DT, PX, kHeld<DT>, true>(base, rs, P - p0, out, left, K, pitch, steps, lds, tops, rows);
-  else quant_tile<DT, PX, kHeld<DT>, false>(base, rs, P - p0, out, left, K, pitch, steps, lds, tops, rows);
+  if (left >= PX) quant_tile<DT, PX, kHeld<DT>, true>(base, rs, at, out, left, K, pitch, steps, lds, tops, rows);
+  else quant_tile<DT, PX, kHeld<DT>, false>(base, rs, at, out, left, K, pitch, steps, lds, tops, rows);
   if (tid < PX && tid < left) scale[(long)n * P + pt + tid] = rows[tid].scale;
 }
 

@@ -153,6 +153,25 @@ def test_maps(N, K, P, M):
         close(out, back(z), back(b), out_dt)
 
 
+# a row's last strip of 1 to 63 pixels, in strips of 64, 32 and 16, and rows of
+# outputs that are whole runs of 64 or 16 bytes, or none
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("N,K,P,M", [(2, 90, 8, 33), (2, 300, 9, 40), (1, 520, 15, 70), (70, 40, 71, 20),
+                                     (90, 140, 143, 300), (4, 1239, 138, 251), (3, 1909, 143, 704), (100, 33, 184, 17),
+                                     (300, 50, 12, 9), (2, 70, 4104, 30)])
+def test_last_strips(N, K, P, M, dt):
+    say("mix last strips", N, K, P, M, dt)
+    x = rand(N + K + P, N, K, P).to(DT[dt]).cuda()
+    rows = np.ascontiguousarray(x.float().cpu().numpy().transpose(0, 2, 1).reshape(N * P, K))
+    check_codes(rows, *quantize(x, bc.BC_MAPS))
+    wq, ws = weights(M, M, K)
+    out = torch.full((N, M, P), float("nan"), dtype=DT[dt], device="cuda")
+    bc.pointwise_mix_i8(wq, ws, x, out, layout=bc.BC_MAPS)
+    z, b = R.mix_codes(*R.codes(rows), wq[:, :K].cpu().numpy(), ws.cpu().numpy(), None, 0)
+    back = lambda v: v.reshape(N, P, M).transpose(0, 2, 1)
+    close(out, back(z), back(b), dt)
+
+
 def test_extreme_codes():
     """Codes at both ends of the type (also -128, which quantize_i8 never makes)
     over a long reduction: the largest sums, exact."""
