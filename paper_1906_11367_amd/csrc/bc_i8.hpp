@@ -82,6 +82,13 @@ __device__ __forceinline__ int chunk_swap(int p) {
   else return p & 15;
 }
 
+// The tile of this block.  Blocks go to the XCDs in turn; near: neighbouring tiles
+// to one XCD, where they share cache lines.
+__device__ __forceinline__ int tile_of_block(bool near) {
+  const int b = blockIdx.x, eighth = gridDim.x >> 3;
+  return near && b < eighth * 8 ? (b & 7) * eighth + (b >> 3) : b;
+}
+
 // The 8 pixels of a lane, from the tile's pixel `first` on.  In a row's last tile
 // the lanes that pass its end take the 8 before the end again (the same values in
 // the same places; pixels before the tile are left out), so that every load is a

@@ -29,7 +29,8 @@ struct Args {
   const int8_t* w;
   const float *wscale, *bias;
   char* out;
-  int M, K, P, pitch, strips, steps, packed, near;
+  int M, K, P, pitch, strips, steps, packed;
+  bool near;
   float floor;
 };
 
@@ -138,11 +139,7 @@ __global__ __launch_bounds__(kTileThreads, 4) void k_mix_i8_maps(Args p) {
   extern __shared__ __align__(16) unsigned char smem[];   // codes of the pixels
   __shared__ uint32_t tops[kTileThreads / 64 * PX];
   __shared__ RowScale rows[PX];
-  int b = blockIdx.x;
-  if (p.near) {   // blocks go to the XCDs in turn
-    const int eighth = gridDim.x >> 3;
-    if (b < eighth * 8) b = (b & 7) * eighth + (b >> 3);
-  }
+  const int b = tile_of_block(p.near);
   const int n = b / p.strips, pt = (b % p.strips) * PX;
   const uint32_t lds = (uint32_t)(uintptr_t)(BC_LDS unsigned char*)smem;
   if (p.P - pt >= PX) mix_tile<DT, OUT, PX, kLined, kHeld<DT>, true>(p, n, pt, lds, tops, rows);

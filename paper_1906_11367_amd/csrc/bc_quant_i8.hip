@@ -94,11 +94,11 @@ __device__ __forceinline__ void quant_tile(const char* base, long rs, const Pixe
 template <int DT, int PX>
 __global__ __launch_bounds__(kTileThreads, 4) void k_quant_maps(const char* src, long bs, long rs, int8_t* q,
                                                                 float* scale, int P, int K, int pitch, int strips,
-                                                                int steps) {
+                                                                int steps, bool near) {
   extern __shared__ __align__(16) unsigned char smem[];   // codes of the pixels
   __shared__ uint32_t tops[kTileThreads / 64 * PX];
   __shared__ RowScale rows[PX];
-  const int tid = threadIdx.x, n = blockIdx.x / strips, pt = (blockIdx.x % strips) * PX, left = P - pt;
+  const int b = tile_of_block(near), tid = threadIdx.x, n = b / strips, pt = (b % strips) * PX, left = P - pt;
   const Pixels at(tid % (PX / 8) * 8, left, P);
   const uint32_t lds = (uint32_t)(uintptr_t)(BC_LDS unsigned char*)smem;
   const char* base = src + ((long)n * bs + pt + at.first) * kBytes<DT>;
@@ -113,8 +113,12 @@ hipError_t launch_maps(const char* x, long bs, long rs, int8_t* q, float* scale,
                        hipStream_t s) {
   const int strips = (P + PX - 1) / PX, steps = (pitch + kStepK<PX> - 1) / kStepK<PX>;
   const size_t lds = (size_t)PX * std::min(steps, kPart<PX>) * kStepK<PX>;
+  // rows, or a strip's part of one, that are not whole 64 bytes (4096 x 64 x 64
+  // bf16, strips of 16: 16 us with neighbours, 28 in order; 2 x 957 x 1072 fp32,
+  // whole 64 bytes, 12 and 11)
+  const bool near = rs % (64 / kBytes<DT>) != 0 || PX * kBytes<DT> % 64 != 0;
   hipLaunchKernelGGL((k_quant_maps<DT, PX>), dim3((unsigned)((long)N * strips)), dim3(kTileThreads), lds, s, x, bs, rs,
-                     q, scale, P, K, pitch, strips, steps);
+                     q, scale, P, K, pitch, strips, steps, near);
   return hipGetLastError();
 }
 
