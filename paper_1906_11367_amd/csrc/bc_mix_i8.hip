@@ -274,24 +274,38 @@ hipError_t launch_tile(const Args& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The largest tile of which there are at least as many as CUs: an operand's
-// traffic falls with the tile's side, a half-empty chip costs more.  Stages of
-// 128 codes halve the barriers where LDS has room for them: one block to a CU
-// (256 x 128, and 128 x 128 where there is one each) or small tiles.  Kernel us
-// of 256 x 256, 256 x 128, 128 x 128 (128 and 64 deep), 64 x 64:
-//   2048 x 8192 -> 8192  121,  144,  169,         286
-//   2048 x 4096 -> 4096  53.6, 38.1, 46.2 (47.8), 58.1
-//   1024 x 4096 -> 4096  48.8, 31.0, 24.7 (27.2), 30.4
-//   1500 x 2000 -> 3000  29.0, 21.0, 27.1 (20.5), 24.6
-//   512 x 4096 -> 4096   46.6, 30.4, 22.0 (24.6), 18.4
+// Tiles, and the time of a round of them on 256 CUs for 4096 codes (us): wide tiles
+// read their operands less often, narrow ones leave fewer CUs idle in the last
+// round.  Stages of 128 codes halve the barriers where LDS has room for them.
+//   256 x 256        one to a CU       54
+//   256 x 128        one               34
+//   128 x 128        two               46 (28 for one)
+//   128 x 128, deep  one               26
+//   64 x 64          two               15.5 (14)
+// The least sum of rounds is the fastest or within 5 % at 37 sizes measured; kernel
+// us in the order above:
+//   2048 x 8192 -> 8192  128,  160,  184,  165,  228
+//   2048 x 4096 -> 4096  53.9, 38.3, 46.5, 47.5, 58.6
+//   1337 x 3495 -> 6448  51.5, 59.6, 59.3, 60.6, 60.7
+//   1500 x 2000 -> 3000  32.1, 22.0, 23.4, 27.8, 24.4
+//   1024 x 4096 -> 4096  51.8, 33.4, 28.2, 25.8, 31.2
+//   751 x 2552 -> 5380   37.7, 26.8, 30.0, 33.0, 24.4
+//   512 x 4096 -> 4096   48.8, 31.6, 25.2, 22.6, 17.5
 template <int OUT, bool kMaps>
 hipError_t launch(const Args& p, hipStream_t s) {
   auto tiles = [&](int i, int j) { return (long)((p.I + i - 1) / i) * ((p.J + j - 1) / j); };
-  if (tiles(256, 256) >= 256) return launch_tile<OUT, kMaps, 2, 4, 4, 2, 64, 4>(p, s);
-  if (tiles(256, 128) >= 256) return launch_tile<OUT, kMaps, 4, 2, 2, 2, 128, 3>(p, s);
-  if (tiles(128, 128) > 256) return launch_tile<OUT, kMaps, 2, 2, 2, 2, 64, 4>(p, s);
-  if (tiles(128, 128) == 256) return launch_tile<OUT, kMaps, 2, 2, 2, 2, 128, 4>(p, s);
-  return launch_tile<OUT, kMaps, 2, 2, 1, 1, 128, 4>(p, s);
+  // pairs of tiles to a CU; the last round may have one
+  auto pairs = [](long t, long two, long one) { return t / 512 * two + (t % 512 > 256 ? two : t % 512 > 0 ? one : 0); };
+  const long c128 = tiles(128, 128);
+  const long cost[5] = {(tiles(256, 256) + 255) / 256 * 540, (tiles(256, 128) + 255) / 256 * 340, pairs(c128, 460, 280),
+                        (c128 + 255) / 256 * 260, pairs(tiles(64, 64), 155, 140)};
+  switch (std::min_element(cost, cost + 5) - cost) {
+    case 0: return launch_tile<OUT, kMaps, 2, 4, 4, 2, 64, 4>(p, s);
+    case 1: return launch_tile<OUT, kMaps, 4, 2, 2, 2, 128, 3>(p, s);
+    case 2: return launch_tile<OUT, kMaps, 2, 2, 2, 2, 64, 4>(p, s);
+    case 3: return launch_tile<OUT, kMaps, 2, 2, 2, 2, 128, 4>(p, s);
+    default: return launch_tile<OUT, kMaps, 2, 2, 1, 1, 128, 4>(p, s);
+  }
 }
 
 // Workspace: the tokens' codes, then their scales.

@@ -153,6 +153,27 @@ def test_maps(N, K, P, M):
         close(out, back(z), back(b), out_dt)
 
 
+# sizes for which each of the products' tiles is the cheapest, few to the chip and
+# many, from codes
+@pytest.mark.parametrize("layout", ["tokens", "maps"])
+@pytest.mark.parametrize("N,P,K,M", [(1, 100, 70, 60000), (4, 15000, 70, 100), (1, 65800, 40, 40), (1, 2047, 300, 2060),
+                                     (3, 3000, 130, 200), (2, 4100, 257, 1100), (1, 700, 900, 300), (10, 210, 64, 4090)])
+def test_tiles(N, P, K, M, layout):
+    say("mix tiles", N, P, K, M, layout)
+    maps = layout == "maps"
+    rows = rand(N + K + P, N * P, K)
+    q, s = quantize(rows.cuda())
+    wq, ws = weights(M, M, K)
+    out = torch.full((N, M, P) if maps else (N, P, M), float("nan"), device="cuda")
+    if maps:
+        bc.pointwise_mix_i8(wq, ws, q, out, layout=bc.BC_MAPS, x_scale=s)
+    else:
+        bc.pointwise_mix_i8(wq, ws, q, out, x_scale=s)
+    z, b = R.mix_codes(*R.codes(rows.numpy()), wq[:, :K].cpu().numpy(), ws.cpu().numpy(), None, 0)
+    back = lambda v: v.reshape(N, P, M).transpose(0, 2, 1) if maps else v.reshape(N, P, M)
+    close(out, back(z), back(b), "f32")
+
+
 # a row's last strip of 1 to 63 pixels, in strips of 64, 32 and 16, and rows of
 # outputs that are whole runs of 64 or 16 bytes, or none
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
