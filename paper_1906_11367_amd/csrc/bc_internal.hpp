@@ -210,7 +210,7 @@ size_t mix_i8_maps_workspace_bytes(int N, int M, int K, int P);
 hipError_t launch_mix_i8_maps(const MixI8& m, hipStream_t s);
 // Few tokens, layout tokens (bc_mix_i8_few.hip): whether it takes so many, and
 // whether it makes their codes itself (otherwise x is codes already).
-bool mix_i8_few_takes(long rows, int K);
+bool mix_i8_few_takes(long rows, int K, int M);
 bool mix_i8_few_makes_codes(long rows, int K);
 hipError_t launch_mix_i8_few(const MixI8& m, hipStream_t s);
 size_t mix_i8_workspace_bytes(int N, int M, int K, int P, int dt, bool maps);

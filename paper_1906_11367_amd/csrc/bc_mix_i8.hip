@@ -324,7 +324,7 @@ size_t mix_i8_workspace_bytes(int N, int M, int K, int P, int dt, bool maps) {
 hipError_t launch_mix_i8(const MixI8& m, hipStream_t s) {
   if (m.maps && m.dt != 3 && mix_i8_maps_takes(m.N, m.M, m.K, m.P)) return launch_mix_i8_maps(m, s);
   const long rows = (long)m.N * m.P;
-  const bool few = !m.maps && mix_i8_few_takes(rows, m.K);
+  const bool few = !m.maps && mix_i8_few_takes(rows, m.K, m.M);
   const int8_t* x = static_cast<const int8_t*>(m.x);
   const float* xscale = m.xscale;
   if (few && (m.dt == 3 || mix_i8_few_makes_codes(rows, m.K))) return launch_mix_i8_few(m, s);

@@ -5,7 +5,9 @@
 // reduction, 128 codes at a time in turn, so that every wave has all of its
 // loads in flight at once, and add their int32 sums through LDS (exact, so in
 // any order).  A few tokens' codes are made in the block itself, while its
-// weights are on the way; more tokens' come from quantize_i8's kernel.
+// weights are on the way; more tokens' come from quantize_i8's kernel, and where
+// the weight rows leave CUs idle, blocks divide the tokens too.
+// 1 token 4096 -> 8192: 9 us (33.6 MB at 3.8 TB/s); 24 tokens 2048 -> 8192: 6.9.
 #include "bc_i8.hpp"
 
 #include <math.h>
@@ -41,6 +43,13 @@ __global__ __launch_bounds__(kThreads) void k_mix_i8_few(Args p) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m0 = blockIdx.x * 16 * MT, blocks = p.pitch / 128;
+  if constexpr (DT == 3) {   // this block's tokens
+    const int t0 = blockIdx.y * 16 * NT;
+    p.x += (long)t0 * p.pitch;
+    p.xscale += t0;
+    p.out += (long)t0 * p.M * kBytes<OUT>;
+    p.T = min(p.T - t0, 16 * NT);
+  }
   // chunk 4 s + lane / 16 of row lane % 16 in matrix instruction s of a block
   typedef i32x4_t Weights[MT][kAhead][2];
   Weights a;
@@ -176,11 +185,18 @@ __global__ __launch_bounds__(kThreads) void k_mix_i8_few(Args p) {
   }
 }
 
+long blocks_of(int M, int m, long T, int t) { return (long)((M + m - 1) / m) * ((T + t - 1) / t); }
+
 template <int DT, int OUT, int MT>
 hipError_t launch_rows(const Args& p, hipStream_t s) {
-  const int nt = (p.T + 15) / 16;
+  // tiles of tokens to a block: of codes as few as leave one block to a CU (200
+  // tokens 4096 -> 256: 6.2 us, with three each 9.8; 64 tokens 8192 -> 512: 9.8, 17)
+  int nt = min((p.T + 15) / 16, DT == 3 ? 3 : 2);
+  if (DT == 3)
+    for (int n = nt - 1; n > 0; --n)
+      if (blocks_of(p.M, 16 * MT, p.T, 16 * n) <= 256) nt = n;
   const size_t lds = (DT == 3 ? 0 : (size_t)p.T * (p.pitch + 16)) + (size_t)nt * (64 + kWaves * MT * 1024);
-  const dim3 grid((unsigned)((p.M + 16 * MT - 1) / (16 * MT)));
+  const dim3 grid((unsigned)((p.M + 16 * MT - 1) / (16 * MT)), (unsigned)((p.T + 16 * nt - 1) / (16 * nt)));
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, s, p); };
   switch (nt) {
     case 1: go(k_mix_i8_few<DT, OUT, 1, MT>); break;
@@ -206,8 +222,12 @@ hipError_t launch(const Args& p, hipStream_t s) {
 // Against the tiles of bc_mix_i8.hip, kernel us: 8 tokens 4096 -> 4096 5.7 and
 // 13.7, 32 tokens 8.6 and 13.9, 48 10.6 and 13.8, 64 tokens 4096 -> 8192 15.9
 // and 14.5, 33 tokens 8192 -> 8192 26.5 and 24.6: the tokens' codes, read by
-// every block, take over.
-bool mix_i8_few_takes(long rows, int K) { return rows <= (K <= 4096 ? 48 : 32); }
+// every block, take over.  Where few weight rows leave a CU no more than a block:
+// 64 tokens 4096 -> 1024 6.3 and 12.3, 600 tokens 4096 -> 256 10.2 and 12.4, 200
+// tokens 8192 -> 512 13.6 and 20; past it 100 tokens 2048 -> 2048 8.8 and 8.2.
+bool mix_i8_few_takes(long rows, int K, int M) {
+  return rows <= (K <= 4096 ? 48 : 32) || blocks_of(M, 16, rows, 48) <= 256;
+}
 
 // In the block: pieces of 512 values, kItems for each wave.
 bool mix_i8_few_makes_codes(long rows, int K) { return rows <= 32 && rows * ((K + 511) / 512) <= kItems * kWaves; }

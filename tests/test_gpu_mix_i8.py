@@ -153,6 +153,21 @@ def test_maps(N, K, P, M):
         close(out, back(z), back(b), out_dt)
 
 
+# more tokens than a block of the kernel for few takes: blocks of one to three
+# tiles of 16, and the last with fewer
+@pytest.mark.parametrize("T,K,M", [(49, 4096, 30), (64, 1000, 200), (97, 300, 513), (170, 5000, 130), (400, 700, 250),
+                                   (601, 200, 256), (1000, 128, 16), (4097, 260, 40), (33, 4200, 1024)])
+def test_several_blocks_of_tokens(T, K, M):
+    say("mix blocks of tokens", T, K, M)
+    wq, ws = weights(M, M, K)
+    x = rand(T + K, T, K).to(torch.bfloat16).cuda()
+    z, b = R.mix_codes(*R.codes(x.float().cpu().numpy()), wq[:, :K].cpu().numpy(), ws.cpu().numpy(), None, 0)
+    for out_dt in ("f32", "bf16"):
+        out = torch.full((T, M), float("nan"), dtype=DT[out_dt], device="cuda")
+        bc.pointwise_mix_i8(wq, ws, x, out)
+        close(out, z, b, out_dt)
+
+
 # sizes for which each of the products' tiles is the cheapest, few to the chip and
 # many, from codes
 @pytest.mark.parametrize("layout", ["tokens", "maps"])
