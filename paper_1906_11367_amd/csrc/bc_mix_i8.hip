@@ -353,7 +353,7 @@ hipError_t launch_mix_i8(const MixI8& m, hipStream_t s) {
   p.M = m.M;
   p.P = m.P;
   p.floor = m.relu ? 0.f : -INFINITY;
-  p.stream = streams((double)rows * m.M, m.maps ? m.P : m.M, m.out_dt, m.out, m.out);
+  p.stream = streams((double)rows * m.M, m.maps ? m.P : m.M, m.out_dt, m.out, m.out, 64);
   if (m.maps) {
     p.a = x; p.ascale = xscale; p.I = (int)rows;
     p.b = w; p.bscale = m.wscale; p.J = m.M;

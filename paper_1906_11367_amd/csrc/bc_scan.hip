@@ -710,7 +710,7 @@ hipError_t launch_scan_fwd(const ScanFwd& f, hipStream_t s) {
   p.N = f.N;
   p.T = f.T;
   p.C = f.C;
-  p.stream = streams((double)f.N * f.T * f.C, f.maps ? f.T : f.C, f.out_dt, f.y, f.y);
+  p.stream = streams((double)f.N * f.T * f.C, f.maps ? f.T : f.C, f.out_dt, f.y, f.y, f.maps ? 16 : 64);
   if (f.maps) return launch_scan_fwd_maps(p, f.in_dt, f.out_dt, f.form, s);
   if (f.in_dt == kBF16) return fwd_tokens<kBF16, kBF16>(p, f.form, f.ws, s);
   return f.out_dt == kBF16 ? fwd_tokens<kF32, kBF16>(p, f.form, f.ws, s) : fwd_tokens<kF32, kF32>(p, f.form, f.ws, s);
@@ -734,7 +734,7 @@ hipError_t launch_scan_bwd(const ScanBwd& f, hipStream_t s) {
   p.N = f.N;
   p.T = f.T;
   p.C = f.C;
-  p.stream = streams((double)f.N * f.T * f.C, f.grs, f.out_dt, f.ggate, f.gx) && f.gbs % 64 == 0;
+  p.stream = streams((double)f.N * f.T * f.C, f.grs, f.out_dt, f.ggate, f.gx, f.maps ? 16 : 64) && f.gbs % (f.maps ? 8 : 32) == 0;
   if (f.maps) return launch_scan_bwd_maps(p, f.in_dt, f.out_dt, f.form, s);
   if (f.in_dt == kBF16) return bwd_tokens<kBF16, kBF16>(p, f.form, f.ws, s);
   return f.out_dt == kBF16 ? bwd_tokens<kF32, kBF16>(p, f.form, f.ws, s) : bwd_tokens<kF32, kF32>(p, f.form, f.ws, s);

@@ -203,14 +203,16 @@ __device__ __forceinline__ int seq_len(const int* lengths, int n, int T) {
 }
 
 // Outputs of `elements` in rows of `rs` go past the caches where they are
-// larger than the XCDs' L2 and their rows are whole cache lines: parts of a
-// line that come from different waves would each cost a read of it.  Measured
-// with and without, us: forward 1 x 65536 x 1024 bf16 94 and 103, backward 8 x
-// 4096 x 2048 bf16 156 and 165, maps 32 x 512 x 4096 bf16 68 and 82; rows of 837
-// fp32: 32 and 24.
-inline bool streams(double elements, long rs, int dt, const void* a, const void* b) {
+// larger than the XCDs' L2 and their rows are whole runs of `run` bytes: 64 where
+// a row is written in parts, which would each cost a read of a line that they
+// share; 16, a lane's piece, where a wave writes 1 KiB of a row in one piece.
+// Measured with and without, us: forward 1 x 65536 x 1024 bf16 94 and 103, backward
+// 8 x 4096 x 2048 bf16 156 and 165, mix 16000 x 1024 to 4704 bf16 107 and 110;
+// rows of 837 fp32 32 and 24, of 1032 bf16 64 and 57; maps 32 x 512 x 4096 bf16 68
+// and 82, 32 x 256 x 4104 bf16 47 and 53.
+inline bool streams(double elements, long rs, int dt, const void* a, const void* b, int run) {
   const int e = dt == kBF16 ? 2 : 4;
-  return elements * e >= 32e6 && rs * e % 128 == 0 && ((uintptr_t)a | (uintptr_t)b) % 128 == 0;
+  return elements * e >= 32e6 && rs * e % run == 0 && ((uintptr_t)a | (uintptr_t)b) % run == 0;
 }
 
 }  // namespace scan
