@@ -4,6 +4,10 @@
 // whole 128 bytes; rows i of one and rows j of the other give out(i, j), i the
 // index that is contiguous in the output: tokens [T][M] take i = weight row,
 // j = token, maps [N][M][P] the reverse.
+// Bound by the matrix instructions where the sizes are large: 16384 x 4096 to
+// 8192 takes 490 to 540 us with the clocks' state (2250 to 2040 TOP/s; the
+// vendor's library 480 to 500), below by tiles that are not a whole round of
+// the chip, 1024 x 4096 to 4096 26 us (1330 TOP/s).
 #include "bc_internal.hpp"
 #include "bc_scan.hpp"
 

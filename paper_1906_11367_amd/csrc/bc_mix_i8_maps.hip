@@ -7,8 +7,9 @@
 // known (as many as fit; the rest is read again), turns the codes through LDS
 // into the rows that the matrix instructions read, and multiplies them with all
 // M weight rows, which come from the XCD's L2.  The codes never go to memory.
-// 32 images of 1024 x 64 x 64 bf16 to 256 fp32 maps: 95 us, 403 MB at 4.2 TB/s;
-// the products take 20 us of it, in which the block's loads stand still.
+// 32 images of 1024 x 64 x 64 bf16 to 256 fp32 maps: 111 us with other tensors in
+// every call, 403 MB at 3.6 TB/s (90 with the same); codes and products take a
+// third of it, in which the block's loads stand still.
 #include "bc_i8.hpp"
 
 #include <math.h>

@@ -1,7 +1,9 @@
 // 8-bit codes and scales of the rows a mix reduces over (gfx950; bc_i8.hpp has
 // the definition).  Rows of codes are padded with zeros to whole 128 bytes,
 // which leaves the products no tail along the reduction.
-// Bound by memory: one read of x and a byte out for each value.
+// Bound by memory: one read of x and a byte out for each value.  16384 rows of 4096
+// bf16: 33 us (201 MB at 6.1 TB/s, part of it from the last-level cache); 8 images
+// of 3000 x 64 x 64 bf16: 106 (295 MB, 2.8 TB/s: a strip's channels are 8 KB apart).
 #include "bc_i8.hpp"
 
 #include <algorithm>

@@ -5,10 +5,13 @@
 // reads three and writes two, with 10 to 40 operations per element.  A block
 // takes a slab of channels (whole cache lines of every row) by a tile of steps: a
 // lane holds a few channels of a few consecutive steps in registers, so every
-// element is read once.
-// 8 x 4096 x 2048 bf16: forward 90 us (4.5 TB/s), backward 146 (4.6 TB/s); 1 x
-// 65536 x 1024 bf16 forward 105 (3.8); 64 x 512 x 1024 fp32 82 and 122 (4.9, 5.5):
-// a copy of 1 GiB reaches 5.2 here.
+// element is read once.  A step is bound by its launch: 8 x 1024 2.5 us, 512 x
+// 4096 bf16 6 to 7 (29 MB at 4.4 TB/s).
+// 8 x 4096 x 2048 bf16: forward 89 us (4.5 TB/s), backward 143 (4.7 TB/s); 1 x
+// 65536 x 1024 bf16 forward 100 (4.0); 64 x 512 x 1024 fp32 82 and 122 (4.9, 5.5):
+// a copy of 1 GiB reaches 5.2 here.  No tensor is read or written twice (counted:
+// 1.01 of the bytes); a tile's loads, arithmetic and carries follow one another,
+// and other blocks fill the gaps but not all of them.
 #include "bc_scan.hpp"
 
 #include <algorithm>

