@@ -7,7 +7,7 @@
 // any order).  A few tokens' codes are made in the block itself, while its
 // weights are on the way; more tokens' come from quantize_i8's kernel, and where
 // the weight rows leave CUs idle, blocks divide the tokens too.
-// 1 token 4096 -> 8192: 9 us (33.6 MB at 3.8 TB/s); 24 tokens 2048 -> 8192: 6.9.
+// 1 token 4096 -> 8192: 9 to 10 us (33.6 MB at 3.5 TB/s); 24 tokens 2048 -> 8192: 6.8.
 #include "bc_i8.hpp"
 
 #include <math.h>
