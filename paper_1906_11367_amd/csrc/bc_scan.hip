@@ -237,6 +237,7 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdA
   __shared__ float totA[kWaves][CW], totB[kWaves][CW], carry[CW], last[CW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int grp = tid % kGroups, slot = tid / kGroups;
+  static_assert(!kChain || X::kThreads % CW == 0, "a chained tile's carries: a lane or more for each channel");
   constexpr int kParts = kChain ? X::kThreads / CW : 1;
   __shared__ float lookA[kParts][CW], lookB[kParts][CW];
   int unit, place = 0;
@@ -254,11 +255,15 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdA
   const char* xp = p.x + ((long)n * p.bs + c0) * kBytes<IN>;
   char* yp = p.y + ((long)n * p.T * p.C + c0) * kBytes<OUT>;
   const int S = (p.T + kScanSpan - 1) / kScanSpan;
+  auto start = [&](int ch) {
+    const int c = slab * CW + ch;
+    return p.h0 && c < p.C ? p.h0[(size_t)n * p.C + c] : 0.f;
+  };
   float first = 0.f;
-  if (tid < CW) {
-    const int c = slab * CW + tid;
-    if (place == 0) first = p.h0 && c < p.C ? p.h0[(size_t)n * p.C + c] : 0.f;
-    if (!kChain) carry[tid] = first;
+  if constexpr (kChain) {
+    if (tid < CW && place == 0) first = start(tid);
+  } else {   // a slab may have more channels than the block has lanes
+    for (int ch = tid; ch < CW; ch += X::kThreads) carry[ch] = start(ch);
   }
   const int tile = place;
   const int t0 = tile * kTile + slot * L;
@@ -344,11 +349,13 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdA
         publish(p.pre + groups + (long)(tile / kGroupTiles + 1) * CW, v, 0.f);
     }
     __syncthreads();
-  } else if (tid < CW) {
-    float h = first;
+  } else {
+    for (int ch = tid; ch < CW; ch += X::kThreads) {
+      float h = carry[ch];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) h = __fmaf_rn(totA[w][tid], h, totB[w][tid]);
-    last[tid] = h;
+      for (int w = 0; w < kWaves; ++w) h = __fmaf_rn(totA[w][ch], h, totB[w][ch]);
+      last[ch] = h;
+    }
   }
   float h[V];
 #pragma unroll
@@ -370,7 +377,9 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_fwd(FwdA
   }
   if (kChain && place + 1 < p.tiles) return;
   __syncthreads();
-  if (p.h_last && tid < CW && slab * CW + tid < p.C) p.h_last[(size_t)n * p.C + slab * CW + tid] = last[tid];
+  if (p.h_last)
+    for (int ch = tid; ch < CW && slab * CW + ch < p.C; ch += X::kThreads)
+      p.h_last[(size_t)n * p.C + slab * CW + ch] = last[ch];
 }
 
 template <class X, int IN, int OUT, int FORM, bool kChain>
@@ -379,6 +388,7 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_bwd(BwdA
   __shared__ float totA[kWaves][CW], totB[kWaves][CW], totR[kWaves][CW], carry[CW], last[CW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int grp = tid % kGroups, slot = tid / kGroups;
+  static_assert(!kChain || X::kThreads % CW == 0, "a chained tile's carries: a lane or more for each channel");
   constexpr int kParts = kChain ? X::kThreads / CW : 1;
   __shared__ float lookA[kParts][CW], lookB[kParts][CW];
   int unit, place = 0;
@@ -398,11 +408,15 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_bwd(BwdA
   char* ggate = p.ggate + ((long)n * p.gbs + c0) * kBytes<OUT>;
   char* gx = p.gx + ((long)n * p.gbs + c0) * kBytes<OUT>;
   const int S = (p.T + kScanSpan - 1) / kScanSpan;
+  auto start = [&](int ch) {
+    const int c = slab * CW + ch;
+    return p.gh_last && c < p.C ? p.gh_last[(size_t)n * p.C + c] : 0.f;
+  };
   float first = 0.f;
-  if (tid < CW) {
-    const int c = slab * CW + tid;
-    if (place == 0) first = p.gh_last && c < p.C ? p.gh_last[(size_t)n * p.C + c] : 0.f;
-    if (!kChain) carry[tid] = first;
+  if constexpr (kChain) {
+    if (tid < CW && place == 0) first = start(tid);
+  } else {   // a slab may have more channels than the block has lanes
+    for (int ch = tid; ch < CW; ch += X::kThreads) carry[ch] = start(ch);
   }
   const int o = place, tile = p.tiles - 1 - o;   // the chain runs backwards in time
   const int t0 = tile * kTile + slot * L;
@@ -502,11 +516,13 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_bwd(BwdA
         publish(p.pre + groups + (long)(o / kGroupTiles + 1) * CW, v, 0.f);
     }
     __syncthreads();
-  } else if (tid < CW) {
-    float r = first;
+  } else {
+    for (int ch = tid; ch < CW; ch += X::kThreads) {
+      float r = carry[ch];
 #pragma unroll
-    for (int w = kWaves - 1; w >= 0; --w) r = __fmaf_rn(totA[w][tid], r, totR[w][tid]);
-    last[tid] = r;
+      for (int w = kWaves - 1; w >= 0; --w) r = __fmaf_rn(totA[w][ch], r, totR[w][ch]);
+      last[ch] = r;
+    }
   }
   float h[L][V], r[V];
 #pragma unroll
@@ -553,7 +569,9 @@ __global__ __launch_bounds__(X::kThreads, X::kWavesPerSimd) void k_scan_bwd(BwdA
   }
   if (kChain && place + 1 < p.tiles) return;
   __syncthreads();
-  if (p.gh0 && tid < CW && slab * CW + tid < p.C) p.gh0[(size_t)n * p.C + slab * CW + tid] = last[tid];
+  if (p.gh0)
+    for (int ch = tid; ch < CW && slab * CW + ch < p.C; ch += X::kThreads)
+      p.gh0[(size_t)n * p.C + slab * CW + ch] = last[ch];
 }
 
 // One token for N sequences: state rows from one pool to another (or in place).

@@ -116,6 +116,17 @@ def test_tokens(N, T, C, dt, form):
     run_both(inputs(11, N, T, C, dt, "tokens", form), N, T, C, dt, "tokens", form)
 
 
+# a few steps of many channels: slabs of more channels than a block has lanes
+@pytest.mark.parametrize("form", ["logit", "value"])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("N,T,C", [(2, 1, 300), (3, 2, 513), (2, 3, 128), (2, 4, 256), (5, 5, 257), (1, 7, 1030),
+                                   (3, 8, 640)])
+def test_few_steps_of_many_channels(N, T, C, dt, form):
+    say("scan few steps", N, T, C, dt, form)
+    run_both(inputs(22, N, T, C, dt, "tokens", form), N, T, C, dt, "tokens", form)
+    run_both(inputs(23, N, T, C, dt, "tokens", form), N, T, C, dt, "tokens", form, [T // 2] * N, start=False)
+
+
 # few chains, long enough that the forward cuts them into longer tiles (256 steps)
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("N,T,C,lengths", [(1, 16385, 9, None), (1, 16640, 64, [16639]), (2, 17001, 70, [17001, 4353]),
