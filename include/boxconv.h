@@ -445,7 +445,12 @@ typedef enum { BC_GATE_LOGIT = 0, BC_GATE_VALUE = 1 } bc_gate_form;
  * states  : NULL, or device fp32, bc_gated_scan_states_bytes() bytes: the
  *           states the backward starts from (its layout is the library's).
  * ws      : >= bc_gated_scan_workspace_bytes(0, ...) bytes, NULL when that is 0.
- *           A workspace for more steps (T) serves fewer.
+ *           A workspace for more steps (T) serves fewer.  Blocks pass states to
+ *           one another through it: calls that may run at the same time need
+ *           one each.  If another call writes it meanwhile, the outputs are
+ *           undefined (NaN where a block gave up waiting, after about a second)
+ *           and the status is still BC_OK; nothing but the call's own outputs
+ *           and workspace is written.
  * Non-finite values spread as the recurrence spreads them: forward in time in
  * their own channel and sequence (also through a reset: 0 * infinity), nowhere
  * else.

@@ -13,6 +13,7 @@
 // 1.01 of the bytes); a tile's loads, arithmetic and carries follow one another,
 // and other blocks fill the gaps but not all of them.
 #include "bc_scan.hpp"
+#include "bc_scan_chain.hpp"
 
 #include <algorithm>
 
@@ -141,8 +142,10 @@ __device__ __forceinline__ void wave_suffix(const float (&A)[V], const float (&B
 constexpr int kGroupTiles = 16;
 constexpr unsigned long long kEmpty = ~0ull;
 constexpr long kTicketWords = 16;   // a cache line for each counter
-// A bound on the polls (about a second), in case the caller lets two calls
-// share a workspace: the outputs are then NaN rather than never.
+// A bound on the polls (about a second), past which a block goes on with a NaN.
+// It is reached only where another call writes this one's workspace meanwhile:
+// the outputs are then worthless, but every wait ends, and no access leaves the
+// tensors or the workspace (chain_has).
 constexpr int kMaxPolls = 1 << 20;
 
 __device__ __forceinline__ void publish(unsigned long long* at, float lo, float hi) {
@@ -213,22 +216,19 @@ __global__ __launch_bounds__(256) void k_scan_clear(unsigned long long* ws, long
   else if (i < words) ws[i] = kEmpty;
 }
 
-// This block's unit (a slab of a sequence) and its place in the unit's chain, a
-// ticket drawn from the unit's own counter: one counter for all serialised the
-// blocks (about 15 ns a draw; with 8192 tiles 115 us instead of 90).  false: a
-// block past the end (the grid's last row).
+// This block's unit and its place in the unit's chain, a ticket drawn from the
+// unit's own counter: one counter for all serialised the blocks (about 15 ns a
+// draw; with 8192 tiles 115 us instead of 90).  false, for the whole block: a
+// block past the end (the grid's last row), or no place of the chain.
 __device__ __forceinline__ bool draw_ticket(unsigned long long* tickets, int units, int tiles, int& unit, int& place) {
   __shared__ int t;
   const long b = (long)blockIdx.y * gridDim.x + blockIdx.x;
-  unit = (int)(b % units);
-  // blocks go to the XCDs in turn: neighbouring slabs to one XCD
-  const int eighth = units >> 3;
-  if (unit < eighth * 8) unit = (unit & 7) * eighth + (unit >> 3);
   if (b >= (long)units * tiles) return false;
+  unit = chain_unit(b, units);
   if (threadIdx.x == 0) t = (int)(atomicAdd(reinterpret_cast<unsigned*>(tickets + (long)unit * kTicketWords), 1u) + 1u);
   __syncthreads();
   place = t;
-  return true;
+  return chain_has(place, tiles);
 }
 
 template <class X, int IN, int OUT, int FORM, bool kChain>

@@ -1,0 +1,56 @@
+"""How the blocks of a chained scan share its tiles, run on the host: the
+functions the kernels call (csrc/bc_scan_chain.hpp), built without device code."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+from paper_1906_11367_amd import build as B
+
+pytestmark = pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"),
+                                reason="no hipcc")
+
+
+def run_host(tmp_path, body):
+    src, exe = tmp_path / "chain.cpp", str(tmp_path / "chain")
+    src.write_text('#include "bc_scan_chain.hpp"\n#include <climits>\n#include <cstdio>\n#include <vector>\n'
+                   f"using namespace bc::scan;\nint main() {{\n{body}\nreturn 0;\n}}\n")
+    for cmd in ([B.hipcc(), "-O1", "-std=c++17", "--offload-host-only", "-x", "hip", "-I", B.CSRC, str(src), "-o", exe],
+                [exe]):
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        assert r.returncode == 0, " ".join(cmd) + "\n" + r.stdout[-2000:] + r.stderr[-2000:]
+
+
+def test_every_unit_has_its_tiles_blocks(tmp_path):
+    run_host(tmp_path, """
+      for (int units : {1, 2, 7, 8, 9, 63, 64, 100, 1000})
+        for (int tiles : {2, 3, 17}) {
+          std::vector<int> blocks(units, 0);
+          for (long b = 0; b < (long)units * tiles; ++b) {
+            const int u = chain_unit(b, units);
+            if (u < 0 || u >= units) return 1;
+            ++blocks[u];
+          }
+          for (int n : blocks) if (n != tiles) return 2;
+        }""")
+
+
+def test_a_number_outside_the_chain_is_no_place(tmp_path):
+    """Whatever a counter holds that another call wrote over: a block goes on only
+    with a tile of its tensors, in both directions of time."""
+    run_host(tmp_path, """
+      for (int tiles : {2, 16, 17, 300}) {
+        for (long n = -3; n < 2L * tiles + 3; ++n)
+          if (chain_has((int)n, tiles) != (n >= 0 && n < tiles)) return 1;
+        for (int n : {INT_MIN, INT_MIN + 1, -1, INT_MAX, 0x3f800000}) if (chain_has(n, tiles)) return 2;
+        for (int n = 0; n < tiles; ++n) if (tiles - 1 - n < 0) return 3;   // the backward's tile
+      }""")
+
+
+def test_the_kernels_leave_where_there_is_no_place():
+    with open(os.path.join(B.CSRC, "bc_scan.hip")) as f:
+        text = f.read()
+    draw = text[text.index("bool draw_ticket("):]
+    assert "return chain_has(place, tiles);" in draw[:draw.index("\n}\n")]
+    assert text.count("draw_ticket(p.tickets") == text.count("if (!draw_ticket(p.tickets, p.N * p.slabs, p.tiles, unit, place)) return;") == 2
