@@ -103,7 +103,8 @@ class RecurrentPlan:
 class RecurrentServer:
     """Inference of the layer in 8-bit codes.  w_in [2D, C] and w_out [M, D] (fp32
     or bf16) are turned into codes once; the states of up to `slots` sequences
-    are rows of a pool, fp32, zero at first."""
+    are rows of a pool, fp32, zero at first.  A slot outside the pool marks an idle
+    row of a batch: it changes no state, and its z is that of a zero state (b_out)."""
 
     def __init__(self, w_in: torch.Tensor, w_out: torch.Tensor, slots: int, b_in: torch.Tensor | None = None,
                  b_out: torch.Tensor | None = None, form: int = bc.BC_GATE_LOGIT,
@@ -116,6 +117,18 @@ class RecurrentServer:
         self.w_in, self.w_out = self._codes(w_in), self._codes(w_out)
         self.state = torch.zeros((slots, self.D), dtype=torch.float32, device=w_in.device)
 
+    @property
+    def state(self) -> torch.Tensor:
+        """The pool [slots, D]: read and written in place, or set (copied)."""
+        return self._state
+
+    @state.setter
+    def state(self, value: torch.Tensor):
+        # a row more, always zero: prefill's idle rows start and end there
+        self._rows = torch.zeros((value.shape[0] + 1, self.D), dtype=torch.float32, device=value.device)
+        self._state = self._rows[:-1]
+        self._state.copy_(value)
+
     @staticmethod
     def _codes(w):
         q = torch.empty((w.shape[0], bc.i8_pitch(w.shape[1])), dtype=torch.int8, device=w.device)
@@ -126,27 +139,36 @@ class RecurrentServer:
 
     def prefill(self, x: torch.Tensor, slots: torch.Tensor, lengths: torch.Tensor | None = None,
                 layout: int = bc.BC_TOKENS, fresh: bool = True):
-        """Prompts x [N, T, C] (or maps [N, C, T]) of sequences slots [N] (int32,
-        distinct, inside the pool) -> z [N, T, M] (or [N, M, T]); their rows of
-        the pool take the states at each one's length.  fresh: from zero states,
-        otherwise from the pool's."""
+        """Prompts x [N, T, C] (or maps [N, C, T]) of sequences slots [N] (distinct,
+        but for idle rows) -> z [N, T, M] (or [N, M, T]); their rows of the pool
+        take the states at each one's length.  fresh: from zero states, otherwise
+        from the pool's."""
         D, N = self.D, x.shape[0]
         tokens = layout == bc.BC_TOKENS
         T = x.shape[1] if tokens else x.shape[2]
+        bc._need(slots, (N,), (torch.int32, torch.int64), "prefill", "slots")
+        bc._need(lengths, (N,), torch.int32, "prefill", "lengths")
         shape = (lambda c: (N, T, c)) if tokens else (lambda c: (N, c, T))
         p = bc.pointwise_mix_i8(*self.w_in, x, self._new(*shape(2 * D)), layout=layout, bias=self.b_in)
         gate, v = (p[..., :D], p[..., D:]) if tokens else (p[:, :D], p[:, D:])
-        rows = slots.long()
-        h = torch.empty((N, D), dtype=torch.float32, device=x.device) if fresh else self.state[rows]
+        # an idle row is a sequence of no steps in the pool's extra row: no steps
+        # leave that zero, whichever of several idle rows is stored last
+        S, rows = self._state.shape[0], slots.long()
+        idle = (rows < 0) | (rows >= S)
+        rows = rows.masked_fill(idle, S)
+        if lengths is None:
+            lengths = torch.full((N,), T, dtype=torch.int32, device=x.device)
+        lengths = lengths.masked_fill(idle, 0)
+        h = torch.empty((N, D), dtype=torch.float32, device=x.device) if fresh else self._rows[rows]
         y = bc.gated_scan_fwd(gate, v, self._new(*shape(D)), h0=None if fresh else h, h_last=h, lengths=lengths,
                               form=self.form, layout=layout)
-        self.state[rows] = h
+        self._rows[rows] = h
         return bc.pointwise_mix_i8(*self.w_out, y, self._new(*shape(self.M)), layout=layout, bias=self.b_out)
 
     def step(self, x: torch.Tensor, slots: torch.Tensor | None = None):
-        """One token x [N, C] of each of N sequences (slots [N] int32; an entry
-        outside the pool is an idle row) -> z [N, M]; the pool is updated."""
+        """One token x [N, C] of each of N sequences (slots [N] int32, or None:
+        the pool's first N rows) -> z [N, M]; the pool is updated."""
         D, N = self.D, x.shape[0]
         p = bc.pointwise_mix_i8(*self.w_in, x, self._new(N, 2 * D), bias=self.b_in)
-        y = bc.gated_scan_step(p[:, :D], p[:, D:], self.state, self._new(N, D), slots=slots, form=self.form)
+        y = bc.gated_scan_step(p[:, :D], p[:, D:], self._state, self._new(N, D), slots=slots, form=self.form)
         return bc.pointwise_mix_i8(*self.w_out, y, self._new(N, self.M), bias=self.b_out)
