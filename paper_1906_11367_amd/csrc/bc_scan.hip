@@ -15,8 +15,6 @@
 #include "bc_scan.hpp"
 #include "bc_scan_chain.hpp"
 
-#include <algorithm>
-
 namespace bc {
 namespace {
 
@@ -211,7 +209,7 @@ struct Lookback {
 
 // Fills the words of a chained call (the counters with them: they start at -1).
 __global__ __launch_bounds__(256) void k_scan_clear(unsigned long long* ws, long words) {
-  const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 2;
+  const long i = (((long)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x) * 2;
   if (i + 1 < words) *reinterpret_cast<ulonglong2*>(ws + i) = make_ulonglong2(kEmpty, kEmpty);
   else if (i < words) ws[i] = kEmpty;
 }
@@ -658,16 +656,16 @@ size_t words_of(int N, int T, int C) {
   });
 }
 
-// Launches the kernel of a cut; chained ones after a fill of their words.  A
-// grid has less than 2^32 threads along x; blocks past the end return.
+// Launches the kernel of a cut; chained ones after a fill of their words.  Blocks
+// past a grid's end return.
 template <class X, class Args, class Chained, class Single>
 hipError_t launch_cut(Args& p, Chained chained, Single single, void* ws, hipStream_t s) {
   const Plan q = plan_of<X>(p.N, p.T, p.C);
   p.slabs = (int)(q.units / p.N);
   p.tiles = q.tiles;
   p.groups = (q.tiles + kGroupTiles - 1) / kGroupTiles;
-  const long blocks = q.units * q.tiles, x = std::min(blocks, 1L << 22);
-  const dim3 grid((unsigned)x, (unsigned)((blocks + x - 1) / x));
+  const Grid g = grid_of(q.units * q.tiles);
+  const dim3 grid(g.x, g.y);
   if (q.words == 0) {
     hipLaunchKernelGGL(single, grid, dim3(X::kThreads), 0, s, p);
     return hipGetLastError();
@@ -676,7 +674,8 @@ hipError_t launch_cut(Args& p, Chained chained, Single single, void* ws, hipStre
   p.tickets = w;
   p.agg = w + q.units * kTicketWords;
   p.pre = p.agg + q.units * q.tiles * q.slab;
-  hipLaunchKernelGGL(k_scan_clear, dim3((unsigned)((q.words / 2 + 256) / 256)), dim3(256), 0, s, w, q.words);
+  const Grid c = grid_of(clear_blocks(q.words));
+  hipLaunchKernelGGL(k_scan_clear, dim3(c.x, c.y), dim3(256), 0, s, w, q.words);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(chained, grid, dim3(X::kThreads), 0, s, p);

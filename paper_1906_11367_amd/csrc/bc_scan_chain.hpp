@@ -19,5 +19,16 @@ __host__ __device__ inline int chain_unit(long b, int units) {
 // outside would lie outside the tensors.
 __host__ __device__ inline bool chain_has(int place, int tiles) { return (unsigned)place < (unsigned)tiles; }
 
+// The rows and columns of a grid of `blocks` or a few more (those return): a grid
+// has less than 2^32 threads along x, and blocks have 512 at most.
+struct Grid { unsigned x, y; };
+inline Grid grid_of(long blocks) {
+  const long x = blocks < 1L << 22 ? blocks : 1L << 22;
+  return {(unsigned)x, (unsigned)((blocks + x - 1) / x)};
+}
+
+// Blocks that fill a call's words, two to a thread of 256.
+inline long clear_blocks(long words) { return (words + 511) / 512; }
+
 }  // namespace scan
 }  // namespace bc

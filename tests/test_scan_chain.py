@@ -48,6 +48,22 @@ def test_a_number_outside_the_chain_is_no_place(tmp_path):
       }""")
 
 
+def test_grids_hold_every_word_and_stay_below_2_32_threads(tmp_path):
+    """Up to 65536 sequences of 2^20 steps (one word a channel and tile of 128,
+    64 channels: 2^36 words and more)."""
+    run_host(tmp_path, """
+      for (long words = 1; words < 1L << 38; words = words * 3 / 2 + 1) {
+        const Grid g = grid_of(clear_blocks(words));
+        if ((long)g.x * 256 >= 1L << 32 || g.y > 65535) return 1;
+        if ((long)g.x * g.y * 512 < words) return 2;
+        if ((long)g.x * (g.y - 1) * 512 >= words) return 3;   // no row of blocks for nothing
+      }
+      for (long blocks : {1L, 1000L, (1L << 22) - 1, 1L << 22, (1L << 22) + 1, 1L << 31}) {
+        const Grid g = grid_of(blocks);
+        if ((long)g.x * 512 >= 1L << 32 || (long)g.x * g.y < blocks) return 4;
+      }""")
+
+
 def test_the_kernels_leave_where_there_is_no_place():
     with open(os.path.join(B.CSRC, "bc_scan.hip")) as f:
         text = f.read()
