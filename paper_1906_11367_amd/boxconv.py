@@ -444,21 +444,26 @@ def pointwise_mix(mode: int, a: torch.Tensor, b: torch.Tensor, out: torch.Tensor
 _FLOATS = (torch.float32, torch.bfloat16)
 
 
-def _rows(t: torch.Tensor, what: str, name: str):
-    """Pointer, batch stride and row stride of a 3-D tensor whose last dimension
-    is contiguous (a slice of a larger tensor, for one).  Strides of dimensions
-    of one element are the contiguous ones."""
-    if not isinstance(t, torch.Tensor):
-        raise BoxConvError(f"{what}: {name} must be a tensor")
+def _data(t: torch.Tensor):
+    """The pointer of a tensor whose strides are passed along."""
     if not t.is_cuda:
         raise BoxConvError("tensors must be on the GPU")
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, what: str, name: str):
+    """Batch stride and row stride of a 3-D tensor whose last dimension is
+    contiguous (a slice of a larger tensor, for one).  Strides of dimensions of
+    one element are the contiguous ones."""
+    if not isinstance(t, torch.Tensor):
+        raise BoxConvError(f"{what}: {name} must be a tensor")
     n, r, c = t.shape
     sn, sr, sc = t.stride()
     if sc != 1 and c > 1:
         raise BoxConvError(f"{what}: {name} must be contiguous in its last dimension")
     if r == 1:
         sr = c
-    return t.data_ptr(), (sn if n > 1 else sr * r), sr
+    return (sn if n > 1 else sr * r), sr
 
 
 _CODES = {torch.int32: BC_I32, torch.float32: BC_F32, torch.bfloat16: BC_BF16, torch.int8: BC_I8}
@@ -511,15 +516,14 @@ def gated_scan_fwd(gate: torch.Tensor, x: torch.Tensor, y: torch.Tensor, h0: tor
     lib = load_library()
     if states is not None:
         _need_numel(states, lib.bc_gated_scan_states_bytes(N, T, C, layout) // 4, _F32, what, "states")
-    gp, bs, rs = _rows(gate, what, "gate")
-    xp, xbs, xrs = _rows(x, what, "x")
-    if (bs, rs) != (xbs, xrs):
+    bs, rs = _rows(gate, what, "gate")
+    if (bs, rs) != _rows(x, what, "x"):
         raise BoxConvError(f"{what}: gate and x must have the same strides")
     dt = _CODES[x.dtype]
     if ws is None:
         ws = _workspace(lib.bc_gated_scan_workspace_bytes(0, N, T, C, dt, layout), x.device)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check(lib.gated_scan_fwd(gp, xp, dt, bs, rs, _ptr(h0), _ptr(lengths), _ptr(y), dtype_code(y), _ptr(h_last),
+    _check(lib.gated_scan_fwd(_data(gate), _data(x), dt, bs, rs, _ptr(h0), _ptr(lengths), _ptr(y), dtype_code(y), _ptr(h_last),
                               _ptr(states), N, T, C, form, layout, _ptr(ws), nbytes, _stream()), what)
     return y
 
@@ -543,19 +547,17 @@ def gated_scan_bwd(gate: torch.Tensor, x: torch.Tensor, states: torch.Tensor, gr
         raise BoxConvError(f"{what}: states and grad_y must be tensors")
     lib = load_library()
     _need_numel(states, lib.bc_gated_scan_states_bytes(N, T, C, layout) // 4, _F32, what, "states")
-    gp, bs, rs = _rows(gate, what, "gate")
-    xp, xbs, xrs = _rows(x, what, "x")
-    ggp, gbs, grs = _rows(grad_gate, what, "grad_gate")
-    gxp, gxbs, gxrs = _rows(grad_x, what, "grad_x")
-    if (bs, rs) != (xbs, xrs) or (gbs, grs) != (gxbs, gxrs):
+    bs, rs = _rows(gate, what, "gate")
+    gbs, grs = _rows(grad_gate, what, "grad_gate")
+    if (bs, rs) != _rows(x, what, "x") or (gbs, grs) != _rows(grad_x, what, "grad_x"):
         raise BoxConvError(f"{what}: gate and x, and grad_gate and grad_x, must have the same strides")
     dt = _CODES[x.dtype]
     if ws is None:
         ws = _workspace(lib.bc_gated_scan_workspace_bytes(1, N, T, C, dt, layout), x.device)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check(lib.gated_scan_bwd(gp, xp, dt, bs, rs, _ptr(states), _ptr(lengths), _ptr(grad_y), _ptr(grad_h_last), ggp,
-                              gxp, dtype_code(grad_x), gbs, grs, _ptr(grad_h0), N, T, C, form, layout, _ptr(ws),
-                              nbytes, _stream()), what)
+    _check(lib.gated_scan_bwd(_data(gate), _data(x), dt, bs, rs, _ptr(states), _ptr(lengths), _ptr(grad_y),
+                              _ptr(grad_h_last), _data(grad_gate), _data(grad_x), dtype_code(grad_x), gbs, grs,
+                              _ptr(grad_h0), N, T, C, form, layout, _ptr(ws), nbytes, _stream()), what)
     return grad_gate, grad_x
 
 
@@ -578,14 +580,12 @@ def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, y:
     _need(state, (S, C), _F32, what, "state")
     _need(state_out, (S, C), _F32, what, "state_out")
     _need(slots, (N,), torch.int32, what, "slots")
-    if not gate.is_cuda or not x.is_cuda:
-        raise BoxConvError("tensors must be on the GPU")
     gs, xs = gate.stride(), x.stride()
     if N > 1 and gs[0] != xs[0] or C > 1 and (gs[1] != 1 or xs[1] != 1):
         raise BoxConvError(f"{what}: gate and x must be contiguous in their last dimension and of the same strides")
     sp = _ptr(state)
     lib = _lib or load_library()
-    st = lib.gated_scan_step(gate.data_ptr(), x.data_ptr(), _CODES[dtype], xs[0] if N > 1 else C, sp,
+    st = lib.gated_scan_step(_data(gate), _data(x), _CODES[dtype], xs[0] if N > 1 else C, sp,
                               sp if state_out is None else _ptr(state_out), _ptr(slots), _ptr(y), N, C, S, form,
                               _stream())
     if st:
@@ -603,7 +603,7 @@ def mix_i8_workspace_bytes(N, M, K, P, x_dt: int, layout: int = BC_TOKENS) -> in
 
 
 def _mix_input(x, layout, what, name):
-    """N, K, P, pointer and strides of a mix's input: tokens [T, K] or [N, P, K],
+    """N, K, P and strides of a mix's input: tokens [T, K] or [N, P, K],
     maps [N, K, P] or [N, K, H, W] (contiguous maps)."""
     if not isinstance(x, torch.Tensor) or x.dtype not in _FLOATS:
         raise BoxConvError(f"{what}: {name} must be an fp32 or bf16 tensor")
@@ -611,13 +611,11 @@ def _mix_input(x, layout, what, name):
         if x.dim() == 2:
             P, K = x.shape
             sr, sc = x.stride()
-            if not x.is_cuda:
-                raise BoxConvError("tensors must be on the GPU")
             if sc != 1 and K > 1:
                 raise BoxConvError(f"{what}: {name} must be contiguous in its last dimension")
             if P == 1:
                 sr = K
-            return 1, K, P, x.data_ptr(), sr * P, sr
+            return 1, K, P, sr * P, sr
         if x.dim() != 3:
             raise BoxConvError(f"{what}: {name} must be [T, K] or [N, P, K]")
         N, P, K = x.shape
@@ -638,13 +636,14 @@ def quantize_i8(src: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, layout:
     """8-bit codes q [rows, i8_pitch(K)] int8 and scales [rows] fp32 of src:
     tokens or weights [rows, K] ([N, P, K]), or maps [N, K, P] (rows = N * P)."""
     what = "quantize_i8"
-    N, K, P, sp, bs, rs = _mix_input(src, layout, what, "src")
+    N, K, P, bs, rs = _mix_input(src, layout, what, "src")
     if q is None or scale is None:
         raise BoxConvError(f"{what}: q and scale must be tensors")
     lib = load_library()
     _need(q, (N * P, lib.bc_i8_pitch(K)), torch.int8, what, "q")
     _need(scale, (N * P,), _F32, what, "scale")
-    _check(lib.quantize_i8(sp, dtype_code(src), bs, rs, _ptr(q), _ptr(scale), N, K, P, layout, _stream()), what)
+    _check(lib.quantize_i8(_data(src), dtype_code(src), bs, rs, _ptr(q), _ptr(scale), N, K, P, layout, _stream()),
+           what)
     return q, scale
 
 
@@ -676,9 +675,9 @@ def pointwise_mix_i8(wq: torch.Tensor, w_scale: torch.Tensor, x: torch.Tensor, o
             P = rows // max(N, 1)
         if N * P != rows:
             raise BoxConvError(f"{what}: {rows} rows of codes are not {N} maps")
-        xp, bs, rs = _ptr(x), 0, 0
+        bs = rs = 0
     else:
-        N, K, P, xp, bs, rs = _mix_input(x, layout, what, "x")
+        N, K, P, bs, rs = _mix_input(x, layout, what, "x")
     if (K + 127) // 128 * 128 != pitch:   # i8_pitch(K)
         raise BoxConvError(f"{what}: wq has rows of {pitch} codes, expected i8_pitch({K})")
     shape = out.shape
@@ -689,6 +688,7 @@ def pointwise_mix_i8(wq: torch.Tensor, w_scale: torch.Tensor, x: torch.Tensor, o
         raise BoxConvError(f"{what}: out has shape {tuple(shape)}, expected {(N, M, P)}")
     lib = _lib or load_library()
     dt = _CODES[x.dtype]
+    xp = _ptr(x) if dt == BC_I8 else _data(x)
     if ws is None:
         ws = _workspace(lib.bc_mix_i8_workspace_bytes(N, M, K, P, dt, layout), x.device)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
