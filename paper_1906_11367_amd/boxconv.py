@@ -508,6 +508,8 @@ def gated_scan_fwd(gate: torch.Tensor, x: torch.Tensor, y: torch.Tensor, h0: tor
     last dimension and of the same strides -> y, dense, of the same shape."""
     what = "gated_scan_fwd"
     N, T, C = _seq_sizes(x, layout, what)
+    if gate is None or y is None:
+        raise BoxConvError(f"{what}: gate and y must be tensors")
     _need(gate, x.shape, x.dtype, what, "gate")
     _need(y, x.shape, _out_types(x.dtype), what, "y")
     _need(h0, (N, C), _F32, what, "h0")
@@ -536,6 +538,8 @@ def gated_scan_bwd(gate: torch.Tensor, x: torch.Tensor, states: torch.Tensor, gr
     and grad_x share their strides too (halves of one gradient, for one)."""
     what = "gated_scan_bwd"
     N, T, C = _seq_sizes(x, layout, what)
+    if any(v is None for v in (gate, states, grad_y, grad_gate, grad_x)):
+        raise BoxConvError(f"{what}: gate, states, grad_y, grad_gate and grad_x must be tensors")
     _need(gate, x.shape, x.dtype, what, "gate")
     _need(grad_y, x.shape, x.dtype, what, "grad_y")
     _need(grad_x, x.shape, _out_types(x.dtype), what, "grad_x")
@@ -543,8 +547,6 @@ def gated_scan_bwd(gate: torch.Tensor, x: torch.Tensor, states: torch.Tensor, gr
     _need(grad_h_last, (N, C), _F32, what, "grad_h_last")
     _need(grad_h0, (N, C), _F32, what, "grad_h0")
     _need(lengths, (N,), torch.int32, what, "lengths")
-    if states is None or grad_y is None:
-        raise BoxConvError(f"{what}: states and grad_y must be tensors")
     lib = load_library()
     _need_numel(states, lib.bc_gated_scan_states_bytes(N, T, C, layout) // 4, _F32, what, "states")
     bs, rs = _rows(gate, what, "gate")
@@ -682,7 +684,7 @@ def pointwise_mix_i8(wq: torch.Tensor, w_scale: torch.Tensor, x: torch.Tensor, o
         raise BoxConvError(f"{what}: wq has rows of {pitch} codes, expected i8_pitch({K})")
     shape = out.shape
     if layout == BC_TOKENS:
-        if shape[-1] != M or out.numel() != N * P * M:
+        if len(shape) == 0 or shape[-1] != M or out.numel() != N * P * M:
             raise BoxConvError(f"{what}: out has shape {tuple(shape)}, expected {N * P} tokens of {M}")
     elif len(shape) not in (3, 4) or shape[0] != N or shape[1] != M or out.numel() != N * M * P:
         raise BoxConvError(f"{what}: out has shape {tuple(shape)}, expected {(N, M, P)}")

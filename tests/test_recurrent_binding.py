@@ -71,3 +71,18 @@ def test_a_call_without_a_fault_asks_for_the_gpu(call):
 def test_refusals_name_their_argument(call, bad, says):
     with pytest.raises(bc.BoxConvError, match=f"^{call}: .*{says}"):
         getattr(bc, call)(**{**CALLS[call], **bad})
+
+
+@pytest.mark.parametrize("call,missing", [
+    ("gated_scan_fwd", "gate x y"), ("gated_scan_bwd", "gate x states grad_y grad_gate grad_x"),
+    ("gated_scan_step", "gate x state y"), ("quantize_i8", "src q scale"), ("pointwise_mix_i8", "wq w_scale x out")])
+def test_what_a_call_needs_is_asked_for(call, missing):
+    for name in missing.split():
+        with pytest.raises(bc.BoxConvError, match=f"^{call}: .*{name}"):
+            getattr(bc, call)(**{**CALLS[call], name: None})
+
+
+def test_an_output_without_dimensions():
+    with pytest.raises(bc.BoxConvError, match="out has shape"):
+        bc.pointwise_mix_i8(**{**CALLS["pointwise_mix_i8"], "x": t(1, 8), "wq": t(1, 128, dtype=i8), "w_scale": t(1),
+                               "bias": None, "out": t()})
