@@ -31,7 +31,7 @@ class RecurrentPlan:
     D: int                 # states
     M: int                 # output channels
     mix_dtype: str = "f32"     # 'f32' | 'bf16': the mixes' compute type
-    x_dtype: torch.dtype = torch.float32   # or bf16, with a bf16 mix
+    x_dtype: torch.dtype | None = None     # the one type of x that is taken (None: fp32, or bf16 with a bf16 mix)
     form: int = bc.BC_GATE_LOGIT
     with_backward: bool = True
     device: str = "cuda"
@@ -39,8 +39,10 @@ class RecurrentPlan:
     def __post_init__(self):
         if self.mix_dtype not in ("f32", "bf16"):
             raise ValueError("mix_dtype must be 'f32' or 'bf16'")
-        if self.x_dtype != torch.float32 and not (self.x_dtype == torch.bfloat16 and self.mix_dtype == "bf16"):
+        types = (torch.float32, torch.bfloat16) if self.mix_dtype == "bf16" else (torch.float32,)
+        if self.x_dtype is not None and self.x_dtype not in types:
             raise ValueError("x must be fp32, or bf16 with a bf16 mix")
+        self.x_types = types if self.x_dtype is None else (self.x_dtype,)
         if self.D * self.T % 8:
             raise ValueError("D * T must be a multiple of 8 (gate and input are 16-byte aligned halves)")
         dev = torch.device(self.device)
@@ -80,6 +82,7 @@ class RecurrentPlan:
                 lengths: torch.Tensor | None = None):
         """x [N, C, T] -> (z [N, M, T], h_last [N, D])."""
         D = self.D
+        bc._need(x, None, self.x_types, "RecurrentPlan.forward", "x")
         self._mix(bc.BC_MIX_FWD, w_in, x, self.p, 2 * D, self.C)
         bc.gated_scan_fwd(self.p[:, :D], self.p[:, D:], self.h, h0=h0, h_last=self.h_last, lengths=lengths,
                           states=self.states, form=self.form, layout=bc.BC_MAPS, ws=self.ws)
@@ -90,6 +93,7 @@ class RecurrentPlan:
                  grad_h_last: torch.Tensor | None = None, lengths: torch.Tensor | None = None):
         """After the forward of the same arguments: (dx, dw_in, dw_out, dh0)."""
         D = self.D
+        bc._need(x, None, self.x_types, "RecurrentPlan.backward", "x")
         self._mix(bc.BC_MIX_BWD_WEIGHT, grad_z, self.h, self.dw_out, self.M, D)
         self._mix(bc.BC_MIX_BWD_DATA, w_out, grad_z, self.dh, self.M, D)
         bc.gated_scan_bwd(self.p[:, :D], self.p[:, D:], self.states, self.dh, self.dp[:, :D], self.dp[:, D:],
