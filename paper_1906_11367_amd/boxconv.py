@@ -158,8 +158,12 @@ def _maps_and_boxes(x, boxes, what):
 
 def _stream():
     # the current device's current stream, without building a Stream object (a
-    # microsecond of a small call)
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    # microsecond of a small call) where torch has the functions its own
+    # Stream is made from; they are not part of its interface
+    try:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    except AttributeError:
+        return torch.cuda.current_stream().cuda_stream
 
 
 def dtype_code(t: torch.Tensor) -> int:

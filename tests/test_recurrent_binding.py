@@ -86,3 +86,26 @@ def test_an_output_without_dimensions():
     with pytest.raises(bc.BoxConvError, match="out has shape"):
         bc.pointwise_mix_i8(**{**CALLS["pointwise_mix_i8"], "x": t(1, 8), "wq": t(1, 128, dtype=i8), "w_scale": t(1),
                                "bias": None, "out": t()})
+
+
+@pytest.mark.parametrize("gone", ["_cuda_getCurrentRawStream", "_cuda_getDevice"])
+def test_the_stream_without_torchs_own_functions(monkeypatch, gone):
+    """Every entry point asks for the current stream; it is the public one where a
+    torch does not have the shorter way."""
+    class Stream:
+        cuda_stream = 0x5000
+
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0x7000, raising=False)
+    assert bc._stream() == 0x7000
+    monkeypatch.delattr(torch._C, gone)
+    assert bc._stream() == 0x5000
+
+
+@pytest.mark.gpu
+def test_the_stream_is_torchs_current_one():
+    side = torch.cuda.Stream()
+    assert bc._stream() == torch.cuda.current_stream().cuda_stream
+    with torch.cuda.stream(side):
+        assert bc._stream() == side.cuda_stream
