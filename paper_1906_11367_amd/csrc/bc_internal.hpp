@@ -148,7 +148,7 @@ hipError_t launch_relu_cast_bf16(const float* g, const float* aux, void* dst, si
 // Gated scan over token sequences [N][T][C] (bc_scan.hip) and over maps
 // [N][C][T] (bc_scan_maps.hip).  Strides in elements: bs between batches, rs
 // between rows (steps of tokens, channels of maps); rows are contiguous.
-constexpr int kScanSpan = 64;        // steps between kept states, tokens: [N][spans][C]
+constexpr int kScanSpan = 128;       // steps between kept states, tokens: [N][spans][C]
 constexpr int kScanSpanMaps = 256;   // maps: [N][C][spans] (bf16 keeps every second)
 struct ScanFwd {
   const void *gate, *x;

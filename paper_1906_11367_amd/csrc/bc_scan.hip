@@ -72,9 +72,9 @@ template <> struct BwdCuts<kF32> {
   using list = CutList<Cut<4, 64, 64, 4, 4>, Cut<4, 8, 64, 4, 4>, Cut<4, 8, 128, 4, 4>, chained,
                        Cut<4, 8, 512, 4, 4>>;   // 4, 32, 64, 128, 256
 };
-// States are kept every kScanSpan steps: at every tile of the chained backward.
-static_assert(BwdCuts<kBF16>::chained::kTile % kScanSpan == 0 && BwdCuts<kF32>::chained::kTile % kScanSpan == 0,
-              "kept states");
+// States are kept every kScanSpan steps: before every tile of the chained backward
+// and before no other step (a sequence of one tile starts from its first state).
+static_assert(BwdCuts<kBF16>::chained::kTile == kScanSpan && BwdCuts<kF32>::chained::kTile == kScanSpan, "kept states");
 
 // (A, B) of the runs of lower slots of this wave (identity for the first), and
 // the inclusive pair.  Slots are kGroups lanes apart.
