@@ -628,19 +628,20 @@ Plan plan_of(int N, int T, int C) {
   return q;
 }
 
-// Calls f with the cut of N x C sequences of T steps and that of its chained
-// kernel: the first of the list that holds the steps, or one of the chained.
+// Calls f with the cut of N x C sequences of T steps and whether its tiles are
+// chained: the first of the list that holds the steps, or one of the chained.
 template <class Cuts, class F, class X, class... Xs>
 auto with_cut(int N, int T, int C, F f, CutList<X, Xs...>) {
   using Chained = typename Cuts::chained;
   using Far = typename Cuts::far;
-  if (T <= X::kTile) return f(X{}, Chained{});
+  if (T <= X::kTile) return f(X{}, std::false_type{});
   if constexpr (sizeof...(Xs) > 0) {
     return with_cut<Cuts>(N, T, C, f, CutList<Xs...>{});
   } else {
+    static_assert(X::kTile >= Chained::kTile, "more steps than the list holds: two tiles or more");
     const Plan q = plan_of<Chained>(N, T, C);
-    if (q.tiles >= 128 && q.tiles >= 16 * q.units) return f(Far{}, Far{});
-    return f(Chained{}, Chained{});
+    if (q.tiles >= 128 && q.tiles >= 16 * q.units) return f(Far{}, std::true_type{});
+    return f(Chained{}, std::true_type{});
   }
 }
 template <class Cuts, class F>
@@ -650,35 +651,31 @@ auto with_cut(int N, int T, int C, F f) { return with_cut<Cuts>(N, T, C, f, type
 // is taken too, so that a workspace for longer sequences serves shorter ones.
 template <class Cuts>
 size_t words_of(int N, int T, int C) {
-  return (size_t)with_cut<Cuts>(N, T, C, [&](auto x, auto) {
-    using X = decltype(x);
-    return X::kTile < T ? plan_of<typename Cuts::chained>(N, T, C).words : 0;
+  return (size_t)with_cut<Cuts>(N, T, C, [&](auto, auto chained) {
+    return decltype(chained)::value ? plan_of<typename Cuts::chained>(N, T, C).words : 0;
   });
 }
 
-// Launches the kernel of a cut; chained ones after a fill of their words.  Blocks
+// Launches the kernel of a cut; a chained one after a fill of its words.  Blocks
 // past a grid's end return.
-template <class X, class Args, class Chained, class Single>
-hipError_t launch_cut(Args& p, Chained chained, Single single, void* ws, hipStream_t s) {
+template <class X, bool kChain, class Args, class Kernel>
+hipError_t launch_cut(Args& p, Kernel kernel, void* ws, hipStream_t s) {
   const Plan q = plan_of<X>(p.N, p.T, p.C);
   p.slabs = (int)(q.units / p.N);
   p.tiles = q.tiles;
   p.groups = (q.tiles + kGroupTiles - 1) / kGroupTiles;
-  const Grid g = grid_of(q.units * q.tiles);
-  const dim3 grid(g.x, g.y);
-  if (q.words == 0) {
-    hipLaunchKernelGGL(single, grid, dim3(X::kThreads), 0, s, p);
-    return hipGetLastError();
+  if constexpr (kChain) {
+    unsigned long long* w = static_cast<unsigned long long*>(ws);
+    p.tickets = w;
+    p.agg = w + q.units * kTicketWords;
+    p.pre = p.agg + q.units * q.tiles * q.slab;
+    const Grid c = grid_of(clear_blocks(q.words));
+    hipLaunchKernelGGL(k_scan_clear, dim3(c.x, c.y), dim3(256), 0, s, w, q.words);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  unsigned long long* w = static_cast<unsigned long long*>(ws);
-  p.tickets = w;
-  p.agg = w + q.units * kTicketWords;
-  p.pre = p.agg + q.units * q.tiles * q.slab;
-  const Grid c = grid_of(clear_blocks(q.words));
-  hipLaunchKernelGGL(k_scan_clear, dim3(c.x, c.y), dim3(256), 0, s, w, q.words);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(chained, grid, dim3(X::kThreads), 0, s, p);
+  const Grid g = grid_of(q.units * q.tiles);
+  hipLaunchKernelGGL(kernel, dim3(g.x, g.y), dim3(X::kThreads), 0, s, p);
   return hipGetLastError();
 }
 
@@ -686,7 +683,8 @@ template <int IN, int OUT, int FORM>
 hipError_t fwd_form(FwdArgs& p, void* ws, hipStream_t s) {
   return with_cut<FwdCuts<IN>>(p.N, p.T, p.C, [&](auto x, auto chained) {
     using X = decltype(x);
-    return launch_cut<X>(p, k_scan_fwd<decltype(chained), IN, OUT, FORM, true>, k_scan_fwd<X, IN, OUT, FORM, false>, ws, s);
+    constexpr bool kChain = decltype(chained)::value;
+    return launch_cut<X, kChain>(p, k_scan_fwd<X, IN, OUT, FORM, kChain>, ws, s);
   });
 }
 
@@ -694,7 +692,8 @@ template <int IN, int OUT, int FORM>
 hipError_t bwd_form(BwdArgs& p, void* ws, hipStream_t s) {
   return with_cut<BwdCuts<IN>>(p.N, p.T, p.C, [&](auto x, auto chained) {
     using X = decltype(x);
-    return launch_cut<X>(p, k_scan_bwd<decltype(chained), IN, OUT, FORM, true>, k_scan_bwd<X, IN, OUT, FORM, false>, ws, s);
+    constexpr bool kChain = decltype(chained)::value;
+    return launch_cut<X, kChain>(p, k_scan_bwd<X, IN, OUT, FORM, kChain>, ws, s);
   });
 }
 

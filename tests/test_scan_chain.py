@@ -1,12 +1,14 @@
 """How the blocks of a chained scan share its tiles, run on the host: the
 functions the kernels call (csrc/bc_scan_chain.hpp), built without device code."""
 import os
+import re
 import shutil
 import subprocess
 
 import pytest
 
 from paper_1906_11367_amd import build as B
+from test_kernel_code import _kernels, device_code  # noqa: F401 (a fixture)
 
 pytestmark = pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"),
                                 reason="no hipcc")
@@ -70,3 +72,24 @@ def test_the_kernels_leave_where_there_is_no_place():
     draw = text[text.index("bool draw_ticket("):]
     assert "return chain_has(place, tiles);" in draw[:draw.index("\n}\n")]
     assert text.count("draw_ticket(p.tickets") == text.count("if (!draw_ticket(p.tickets, p.N * p.slabs, p.tiles, unit, place)) return;") == 2
+
+
+def test_every_scan_kernel_built_is_one_that_calls_reach(device_code):
+    """Cuts of the token kernels (channels a lane, lanes side by side, threads,
+    steps a lane): one tile a sequence, or chained."""
+    single = {("fwd", 1): {(4, 64, 64, 8), (4, 8, 64, 4), (4, 8, 128, 4), (4, 16, 512, 4), (4, 8, 512, 4)},
+              ("fwd", 2): {(4, 64, 64, 8), (4, 16, 64, 8), (4, 16, 128, 8), (4, 16, 256, 8), (4, 16, 512, 8)},
+              ("bwd", 1): {(4, 64, 64, 4), (4, 8, 64, 4), (4, 8, 128, 4), (4, 16, 512, 4), (4, 8, 512, 4)},
+              ("bwd", 2): {(2, 64, 64, 8), (2, 32, 64, 8), (2, 32, 128, 8), (2, 32, 256, 8), (2, 32, 512, 8)}}
+    chained = {("fwd", 1): {(4, 16, 512, 4), (4, 16, 512, 8)}, ("fwd", 2): {(4, 16, 256, 8), (4, 16, 512, 8)},
+               ("bwd", 1): {(4, 16, 512, 4)}, ("bwd", 2): {(2, 32, 512, 8)}}
+    found = {}
+    for _, name in _kernels(device_code, r"k_scan_(fwd|bwd)I"):
+        way, *n = re.search(r"k_scan_(fwd|bwd)INS0_3CutILi(\d+)ELi(\d+)ELi(\d+)ELi(\d+)ELi\d+EEELi(\d)ELi(\d)ELi(\d)ELb(\d)E",
+                            name).groups()
+        *cut, dt, out, form, chain = map(int, n)
+        found.setdefault((way, dt, chain), {}).setdefault((out, form), set()).add(tuple(cut))
+    for (way, dt), cuts in single.items():
+        kinds = [(out, form) for out in ((1, 2) if dt == 1 else (2,)) for form in (0, 1)]
+        assert found[way, dt, 0] == {k: cuts for k in kinds}
+        assert found[way, dt, 1] == {k: chained[way, dt] for k in kinds}
