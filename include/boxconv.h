@@ -424,10 +424,12 @@ typedef enum { BC_GATE_LOGIT = 0, BC_GATE_VALUE = 1 } bc_gate_form;
  *   BC_GATE_LOGIT: a_t = sigmoid(gate_t), h_t = a_t h_{t-1} + (1 - a_t) x_t;
  *   BC_GATE_VALUE: a_t = gate_t,          h_t = a_t h_{t-1} + x_t;
  *   y_t = h_t, h_last = h_{T-1}.
- * All arithmetic in fp32 (a and 1 - a each to fp32 accuracy; gate = -infinity
- * is an exact reset); only y is rounded to its type.  Runs of steps are
- * composed, so with BC_GATE_VALUE the products of consecutive coefficients
- * have to stay inside fp32's range (|a| <= 1 always does).
+ * All arithmetic in fp32; only y is rounded to its type.  BC_GATE_LOGIT: a and
+ * 1 - a come each from exp(-|gate|), to within 8 * 2^-24 of themselves for fp32
+ * tensors and (8 + 1.25 |gate|) * 2^-24 for bf16 ones, and are zero below
+ * 2^-126; gate = -infinity is an exact reset.  Runs of steps are composed, so
+ * with BC_GATE_VALUE the products of consecutive coefficients have to stay
+ * inside fp32's range (|a| <= 1 always does).
  *
  * gate, x : device, dtype dt = BC_F32 or BC_BF16, in the layout's order with
  *           batch_stride and row_stride elements between batches and rows

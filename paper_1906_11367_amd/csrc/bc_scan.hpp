@@ -138,7 +138,9 @@ __device__ __forceinline__ Raw<kWords<DT, V>> hold_gate() {
 }
 
 // exp(-v), v >= 0.  fp32 storage: the rounding of v / ln 2, which would grow
-// with v, is put back to first order.
+// with v, is put back to first order; 3 units of 2^-24 are left, of the exponential
+// (an ulp) and the last product.  bf16 storage, whose gates are off by 2^-9 of
+// themselves already, leaves it: 1.22 v units more.
 template <int DT>
 __device__ __forceinline__ float exp_neg(float v) {
   const float t = v * -1.44269504f;
@@ -150,7 +152,8 @@ __device__ __forceinline__ float exp_neg(float v) {
 
 // Coefficient a of the state and c of the input.  The logit form takes both
 // from exp(-|gate|), so that neither a nor 1 - a loses its digits where it is
-// small; gate = -infinity is an exact reset (a = 0, c = 1).
+// small: 4 units more, of the sum, the reciprocal (an ulp) and the product.
+// gate = -infinity is an exact reset (a = 0, c = 1).
 template <int DT, int FORM>
 __device__ __forceinline__ void coefficients(float gate, float& a, float& c) {
   if constexpr (FORM == kValue) {
