@@ -453,9 +453,11 @@ typedef enum { BC_GATE_LOGIT = 0, BC_GATE_VALUE = 1 } bc_gate_form;
  *           undefined (NaN where a block gave up waiting, after about a second)
  *           and the status is still BC_OK; nothing but the call's own outputs
  *           and workspace is written.
- * Non-finite values spread as the recurrence spreads them: forward in time in
- * their own channel and sequence (also through a reset: 0 * infinity), nowhere
- * else.
+ * Non-finite values spread as far as the recurrence spreads them: forward in
+ * time in their own channel and sequence (also through a reset: 0 * infinity),
+ * nowhere else; in the backward, grad_y's and a coefficient's backward in time,
+ * a state's to the coefficients after it.  Which of them are NaN may differ: an
+ * infinite state is one where the composed coefficients after it underflow.
  * Sizes: N, C <= 65536, T <= 2^30; tokens: N * ceil(C/32) * ceil(T/64) < 2^31;
  * maps: N * C <= 2^25 (BC_ERR_SHAPE).  Strides smaller than a row or a batch
  * are BC_ERR_SHAPE too.
