@@ -627,7 +627,8 @@ def _mix_input(x, layout, what, name):
         N, P, K = x.shape
     elif layout == BC_MAPS:
         if x.dim() == 4:
-            if x.stride(2) != x.shape[3] * x.stride(3) and x.shape[2] > 1:
+            # (a dimension of one element may have any stride)
+            if x.shape[2] > 1 and x.stride(2) != (x.shape[3] * x.stride(3) if x.shape[3] > 1 else 1):
                 raise BoxConvError(f"{what}: {name}'s maps must be contiguous")
             x = x.flatten(2)
         if x.dim() != 3:

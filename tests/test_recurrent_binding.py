@@ -88,6 +88,29 @@ def test_an_output_without_dimensions():
                                "bias": None, "out": t()})
 
 
+def test_maps_of_one_column():
+    """Contiguous maps [N, K, H, 1] whose last stride says nothing."""
+    x = t(2, 8, 1, 5).transpose(2, 3)
+    assert x.stride() == (40, 5, 1, 5) and x.is_contiguous()
+    call = {**CALLS["pointwise_mix_i8"], "x": x, "layout": bc.BC_MAPS, "out": t(2, 3, 5)}
+    with pytest.raises(bc.BoxConvError, match="must be on the GPU"):
+        bc.pointwise_mix_i8(**call)
+    with pytest.raises(bc.BoxConvError, match="x's maps must be contiguous"):
+        bc.pointwise_mix_i8(**{**call, "x": t(2, 8, 5, 4)[..., :1]})
+
+
+@pytest.mark.gpu
+def test_maps_of_one_column_are_read_as_they_stand():
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn((2, 8, 1, 5), generator=g).cuda().transpose(2, 3)
+    wq, ws = bc.quantize_i8(torch.randn((3, 8), generator=g).cuda(), torch.empty((3, 128), dtype=i8, device="cuda"),
+                            torch.empty(3, device="cuda"))
+    out, want = torch.empty((2, 3, 5), device="cuda"), torch.empty((2, 3, 5), device="cuda")
+    bc.pointwise_mix_i8(wq, ws, x, out, layout=bc.BC_MAPS)
+    bc.pointwise_mix_i8(wq, ws, x.reshape(2, 8, 5).clone(), want, layout=bc.BC_MAPS)
+    assert torch.equal(out, want) and torch.isfinite(out).all()
+
+
 @pytest.mark.parametrize("gone", ["_cuda_getCurrentRawStream", "_cuda_getDevice"])
 def test_the_stream_without_torchs_own_functions(monkeypatch, gone):
     """Every entry point asks for the current stream; it is the public one where a
