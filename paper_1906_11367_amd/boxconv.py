@@ -678,7 +678,7 @@ def pointwise_mix_i8(wq: torch.Tensor, w_scale: torch.Tensor, x: torch.Tensor, o
         if layout == BC_TOKENS:
             N, P = 1, rows
         else:
-            N = out.shape[0]
+            N = out.shape[0] if out.dim() else 0
             P = rows // max(N, 1)
         if N * P != rows:
             raise BoxConvError(f"{what}: {rows} rows of codes are not {N} maps")

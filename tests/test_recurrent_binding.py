@@ -88,6 +88,12 @@ def test_an_output_without_dimensions():
                                "bias": None, "out": t()})
 
 
+def test_an_output_without_dimensions_for_codes_of_maps():
+    with pytest.raises(bc.BoxConvError, match="5 rows of codes are not 0 maps"):
+        bc.pointwise_mix_i8(**{**CALLS["pointwise_mix_i8"], "x": t(5, 128, dtype=i8), "x_scale": t(5),
+                               "layout": bc.BC_MAPS, "out": t()})
+
+
 def test_maps_of_one_column():
     """Contiguous maps [N, K, H, 1] whose last stride says nothing."""
     x = t(2, 8, 1, 5).transpose(2, 3)
