@@ -6,8 +6,9 @@
 // j = token, maps [N][M][P] the reverse.
 // Bound by the matrix instructions where the sizes are large: 16384 x 4096 to
 // 8192 takes 490 to 540 us with the clocks' state (2250 to 2040 TOP/s; the
-// vendor's library 480 to 500), below by tiles that are not a whole round of
-// the chip, 1024 x 4096 to 4096 26 us (1330 TOP/s).
+// vendor's library 480 to 500).  Sizes that 256 x 256 tiles leave most CUs idle at
+// take smaller ones, up to twice as slow for each product (launch): 1024 x 4096
+// to 4096, one round of 256 tiles of 128 x 128, 26 us (1330 TOP/s).
 #include "bc_internal.hpp"
 #include "bc_scan.hpp"
 

@@ -6,12 +6,12 @@
 // takes a slab of channels (whole cache lines of every row) by a tile of steps: a
 // lane holds a few channels of a few consecutive steps in registers, so every
 // element is read once.  A step is bound by its launch: 8 x 1024 2.5 us, 512 x
-// 4096 bf16 6 to 7 (29 MB at 4.4 TB/s).
+// 4096 bf16 6 to 7.5 (29 MB at 4.4 TB/s).
 // 8 x 4096 x 2048 bf16: forward 89 us (4.5 TB/s), backward 143 (4.7 TB/s); 1 x
 // 65536 x 1024 bf16 forward 100 (4.0); 64 x 512 x 1024 fp32 82 and 122 (4.9, 5.5):
-// a copy of 1 GiB reaches 5.2 here.  No tensor is read or written twice (counted:
-// 1.01 of the bytes); a tile's loads, arithmetic and carries follow one another,
-// and other blocks fill the gaps but not all of them.
+// a copy of 1 GiB reaches 5.2 here, a plain elementwise kernel 6.2.  No tensor is
+// read or written twice (counted: 1.01 of the bytes); a tile's loads, arithmetic and
+// carries follow one another, and other blocks fill the gaps but not all of them.
 #include "bc_scan.hpp"
 #include "bc_scan_chain.hpp"
 
@@ -127,8 +127,9 @@ __device__ __forceinline__ void wave_suffix(const float (&A)[V], const float (&B
   }
 }
 
-// Chained tiles.  Every tile has a block of its own, and the state before a
-// tile comes from the tiles before it in one launch: each publishes its pair
+// Chained tiles, the published single-pass scan with decoupled look-back (Merrill and
+// Garland, 2016) in groups.  Every tile has a block of its own, and the state before
+// a tile comes from the tiles before it in one launch: each publishes its pair
 // (A, B), and a block combines the pairs back to the start of its group of
 // kGroupTiles with the state published there (by the last block of the group
 // before).  A block waits only on lower places of its chain, drawn as blocks
