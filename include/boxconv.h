@@ -417,7 +417,7 @@ size_t bc_noalloc_scratch_bytes(void);
  *              reads and writes its maps.
  * ---------------------------------------------------------------------- */
 typedef enum { BC_TOKENS = 0, BC_MAPS = 1 } bc_layout;
-typedef enum { BC_GATE_LOGIT = 0, BC_GATE_VALUE = 1 } bc_gate_form;
+typedef enum { BC_GATE_LOGIT = 0, BC_GATE_VALUE = 1, BC_GATE_LOG = 2 } bc_gate_form;
 
 /* ------------------------------------------------------------------------
  * gated_scan_fwd -- for every sequence n and channel c, from h_{-1} = h0:
@@ -548,6 +548,167 @@ bc_status pointwise_mix_i8(const void* wq, const float* w_scale, const void* x, 
                            hipStream_t stream);
 int bc_i8_pitch(int K);   /* bytes between rows of K codes: K rounded up to 128; 0 for K outside 1..65536 */
 size_t bc_mix_i8_workspace_bytes(int N, int M, int K, int P, int x_dt, int layout);
+
+/* ========================================================================
+ * Linear-attention blocks: a recurrence like the gated scan's whose state is a
+ * matrix for each head, between 1x1 mixes, and the norms around them.
+ * ---------------------------------------------------------------------- */
+
+/* Elements between batches (sequences), rows (tokens) and heads of a tensor
+ * [N][T][H][D] whose last dimension is contiguous: [N][T][H][D] itself is
+ * {T*H*D, H*D, D}, [N][H][T][D] is {H*T*D, D, T*D}, and a slice of a projection's
+ * rows has the projection's strides.  Not negative.  Inputs may repeat elements
+ * (a stride of 0); an output's elements are all distinct. */
+typedef struct { int64_t batch, row, head; } bc_strides;
+
+/* N sequences of T tokens; H heads of decays, states and outputs; Hq, Hk and Hv
+ * heads of q, k and v, divisors of H: head h reads head h / (H / Hq) of q, and so
+ * on.  Rows of Dk elements (q, k) and Dv (v, y), 1 to 128.  dt: BC_F32 or BC_BF16,
+ * the type of q, k, v, y and their gradients; gate_dt: BC_F32 or dt, the gate's and
+ * its gradient's; form: BC_GATE_LOGIT or BC_GATE_LOG; scale: any finite number. */
+typedef struct {
+  int N, T, H, Hq, Hk, Hv, Dk, Dv, dt, gate_dt, form;
+  float scale;
+} bc_attention;
+
+/* ------------------------------------------------------------------------
+ * linear_attention_fwd -- for every sequence n and head h, from S_{-1} = s0:
+ *   S_t = a_t S_{t-1} + k_t v_t^T   [Dk][Dv],   y_t = scale * S_t^T q_t,
+ *   BC_GATE_LOGIT: a_t = sigmoid(gate_t);  BC_GATE_LOG: a_t = exp(gate_t);
+ *   s_last = S_{T-1}.
+ * States, sums and decays are fp32 (running sums of log a in fp64); y alone is
+ * rounded to its type.  bf16: where the fp32 state or scores meet a bf16 operand
+ * on the matrix units they are taken as sums of bf16 parts, two for y (2^-17 of
+ * each product), three for the state (2^-25).  gate = -infinity is an exact reset
+ * (log a below -10000 is one too); with BC_GATE_LOG a_t > 1 is allowed while
+ * states stay inside fp32's range.
+ *
+ * q, k, v  : device [N][T][Hq][Dk], [N][T][Hk][Dk], [N][T][Hv][Dv] by their strides.
+ * gate     : device [N][T][H] by its strides (its heads gate_strides.head apart);
+ *            strides {0, 0, 1} on [H] numbers: a decay for each head, the same for
+ *            every token.  gate and grad_gate are aligned to their elements alone.
+ * s0       : device fp32 [N][H][Dk][Dv], or NULL: zero.
+ * lengths  : device int32 [N], or NULL: all T.  Sequence n ends after lengths[n]
+ *            tokens (clamped to [0, T]): nothing is read past it, y is zero there
+ *            and s_last is the state at it (s0 for an empty sequence).
+ * y        : device [N][T][H][Dv] by its strides; shares no memory with an input.
+ * s_last   : device fp32 [N][H][Dk][Dv], or NULL.  May be s0.
+ * states   : NULL, or device fp32, bc_linear_attention_states_bytes() bytes: the
+ *            states the backward starts from (its layout is the library's).
+ * ws       : >= bc_linear_attention_workspace_bytes(0, ...) bytes, NULL when that
+ *            is 0.  Calls that may run at the same time need one each.
+ * Results depend on nothing but the arguments (no atomics; every call gives the
+ * same bits).  Non-finite values in a token that exists make any output of their
+ * own sequence and head non-finite, before or after the token, and no others; past
+ * a sequence's end they are not read.
+ * Sizes: N * H <= 131072, T <= 2^30, N * H * ceil(T / 128) <= 2^23, tensors
+ * of extents below 2e18 elements (BC_ERR_SHAPE).
+ *
+ * linear_attention_bwd -- gradients of L = <grad_y, y> + <grad_s_last, s_last>:
+ * with R_T = grad_s_last, R_t = scale q_t grad_y_t^T + a_{t+1} R_{t+1} (a_T = 1),
+ *   grad_q_t = scale S_t grad_y_t,  grad_k_t = R_t v_t,  grad_v_t = R_t^T k_t,
+ *   d L / d log a_t = a_t <S_{t-1}, R_t>,  grad_s0 = a_0 R_0,
+ * and grad_gate_t is d L / d log a_t (BC_GATE_LOG) or (1 - a_t) times that
+ * (BC_GATE_LOGIT), zero where a_t is.  A head of q, k or v that several heads read
+ * gets the sum of their gradients, in fp32 and in order.  Past a sequence's end
+ * the gradients are zero and grad_y is not read.
+ * states      : the forward's, of the same q, k, v, gate, s0 and lengths.
+ * grad_y      : device [N][T][H][Dv] by its strides.
+ * grad_s_last : device fp32 [N][H][Dk][Dv], or NULL: zero.
+ * grad_q, grad_k, grad_v : device, shaped as q, k, v, by their own strides.
+ * grad_gate   : device [N][T][H] by its strides, or NULL (decays that are not
+ *               learned).  For a gate whose tokens share memory it is still one
+ *               number a token: their sum is the caller's.
+ * grad_s0     : device fp32 [N][H][Dk][Dv], or NULL.  May be grad_s_last.
+ * The other gradients share no memory with an input or with one another.
+ * ws          : >= bc_linear_attention_workspace_bytes(1, ...) bytes.
+ *
+ * linear_attention_step -- one token of N running sequences whose states are rows
+ * of a pool: with s = slots[n] (or n where slots is NULL),
+ *   state_out[s] = a[n] state[s] + k[n] v[n]^T,  y[n] = scale * state_out[s]^T q[n].
+ * q, k, v, gate : as above without the tokens (strides' row unused); T is not read.
+ * state, state_out : device fp32 [S][H][Dk][Dv]; they may be the same (in place)
+ *            or share nothing.  Rows that no sequence names are not written.
+ * slots    : device int32 [N], or NULL (then N <= S).  A slot outside [0, S) marks
+ *            an idle row: y is zero, no state is read or written.  Two rows may not
+ *            name one slot.
+ * y        : device, dense [N][H][Dv].
+ * ---------------------------------------------------------------------- */
+bc_status linear_attention_fwd(const bc_attention* sizes, const void* q, bc_strides q_strides, const void* k,
+                               bc_strides k_strides, const void* v, bc_strides v_strides, const void* gate,
+                               bc_strides gate_strides, const float* s0, const int* lengths, void* y,
+                               bc_strides y_strides, float* s_last, float* states, void* ws, size_t ws_bytes,
+                               hipStream_t stream);
+bc_status linear_attention_bwd(const bc_attention* sizes, const void* q, bc_strides q_strides, const void* k,
+                               bc_strides k_strides, const void* v, bc_strides v_strides, const void* gate,
+                               bc_strides gate_strides, const float* states, const int* lengths, const void* grad_y,
+                               bc_strides grad_y_strides, const float* grad_s_last, void* grad_q,
+                               bc_strides grad_q_strides, void* grad_k, bc_strides grad_k_strides, void* grad_v,
+                               bc_strides grad_v_strides, void* grad_gate, bc_strides grad_gate_strides,
+                               float* grad_s0, void* ws, size_t ws_bytes, hipStream_t stream);
+bc_status linear_attention_step(const bc_attention* sizes, const void* q, bc_strides q_strides, const void* k,
+                                bc_strides k_strides, const void* v, bc_strides v_strides, const void* gate,
+                                bc_strides gate_strides, const float* state, float* state_out, const int* slots,
+                                void* y, int S, hipStream_t stream);
+/* op: 0 = linear_attention_fwd, 1 = linear_attention_bwd; 0 for sizes the calls reject. */
+size_t bc_linear_attention_workspace_bytes(int op, const bc_attention* sizes);
+size_t bc_linear_attention_states_bytes(int N, int T, int H, int Dk, int Dv);
+
+/* ------------------------------------------------------------------------
+ * block_norm_fwd -- the norms around a block with its gate, residual sum and
+ * scale, for every row of C channels:
+ *   p = norm(z) * w_post within each of `groups` runs of C / groups channels
+ *       (p = z for groups = 0),
+ *   u = p * act(gate)     (u = p without a gate),
+ *   r = x + res_scale * u (r = res_scale * u without x),
+ *   y = norm(r) * w_pre,
+ *   BC_NORM_RMS:   norm(v) = v / sqrt(mean(v^2) + eps);
+ *   BC_NORM_LAYER: the same of v - mean(v);
+ *   BC_ACT_SILU:   act(g) = g * sigmoid(g);  BC_ACT_SIGMOID: sigmoid(g).
+ * The norm before a block alone is groups = 0 with y; a norm with a gate over the
+ * heads of an attention is groups = heads with r; after a block, groups = 1 with x,
+ * r and y give the residual stream and the next block's input in one pass.
+ * All arithmetic is fp32; r and y are rounded once, y from the r that is not
+ * rounded.  A row's outputs depend on that row alone (non-finite values too).  Mean
+ * squares have to stay inside fp32's range.
+ *
+ * z, gate, x : device [R][C], dt = BC_F32 or BC_BF16, contiguous rows, z_stride, ...
+ *              elements apart (>= C); gate, x or both may be NULL.
+ * w_post, res_scale, w_pre : device fp32 [C], or NULL: ones.
+ * r, y       : device [R][C], dt, rows r_stride and y_stride apart; one of them may
+ *              be NULL.
+ *
+ * block_norm_bwd -- gradients of L = <grad_r, r> + <grad_y, y>; grad_r or grad_y
+ * may be NULL: zero.  r and y are computed again, in fp32.
+ * grad_z, grad_gate, grad_x : device [R][C], dt, rows by their strides, or NULL
+ *              (not wanted); grad_gate and grad_x only with a gate and an x.
+ * grad_w_post (with groups), grad_res_scale, grad_w_pre (with grad_y) : device fp32
+ *              [C], or NULL.  Sums over rows are fp32, in an order that is a function
+ *              of the sizes: every call gives the same bits.
+ * ws         : >= bc_block_norm_workspace_bytes(R, C) bytes; may be NULL where no
+ *              weight's gradient is asked for.
+ *
+ * An output may be an input of the same row stride (in place); otherwise it shares
+ * no memory with one.  eps: positive, not below 2^-126.  Sizes: groups divides C,
+ * max(groups, 1) * ceil(C / max(groups, 1) / 8) <= 2048: C <= 16384 in runs of whole
+ * eights (BC_ERR_SHAPE).
+ * ---------------------------------------------------------------------- */
+typedef enum { BC_NORM_RMS = 0, BC_NORM_LAYER = 1 } bc_norm_kind;
+typedef enum { BC_ACT_SILU = 0, BC_ACT_SIGMOID = 1 } bc_act;
+typedef struct {
+  int R, C, groups, kind, act, dt;
+  float eps;
+} bc_norm;
+bc_status block_norm_fwd(const bc_norm* sizes, const void* z, int64_t z_stride, const void* gate, int64_t gate_stride,
+                         const void* x, int64_t x_stride, const float* w_post, const float* res_scale,
+                         const float* w_pre, void* r, int64_t r_stride, void* y, int64_t y_stride, hipStream_t stream);
+bc_status block_norm_bwd(const bc_norm* sizes, const void* z, int64_t z_stride, const void* gate, int64_t gate_stride,
+                         const void* x, int64_t x_stride, const float* w_post, const float* res_scale,
+                         const float* w_pre, const void* grad_r, int64_t grad_r_stride, const void* grad_y,
+                         int64_t grad_y_stride, void* grad_z, int64_t grad_z_stride, void* grad_gate,
+                         int64_t grad_gate_stride, void* grad_x, int64_t grad_x_stride, float* grad_w_post,
+                         float* grad_res_scale, float* grad_w_pre, void* ws, size_t ws_bytes, hipStream_t stream);
+size_t bc_block_norm_workspace_bytes(int R, int C);   /* 0 for sizes below 1 */
 
 /* Workspace sizes in bytes.  op: 0 = box_conv_fwd, 1 = box_conv_bwd (and
  * box_conv_bwd_relu_bf16); the _strided form for the strided entry points

@@ -11,7 +11,9 @@ box-parameter reparameterisation (box_params_from_unit, box_params_unit_grad,
 box_params_clip), kernel splitting (box_conv_split_fwd, box_conv_split_bwd),
 the bf16 helpers (bc_cast_bf16, bc_relu_grad_bf16), the gated scan of
 recurrent layers (gated_scan_fwd, gated_scan_bwd, gated_scan_step), the 8-bit
-mix (quantize_i8, pointwise_mix_i8), plus the workspace-size queries.
+mix (quantize_i8, pointwise_mix_i8), linear attention (linear_attention_fwd,
+linear_attention_bwd, linear_attention_step), the norms around a block
+(block_norm_fwd, block_norm_bwd), plus the workspace-size queries.
 """
 from __future__ import annotations
 
@@ -29,13 +31,30 @@ BC_FLAG_MEAN_OFFSET, BC_FLAG_FORCE_HBM, BC_FLAG_INTEGER_CORNERS = 1, 2, 4
 BC_SPLIT_2X, BC_SPLIT_2Y, BC_SPLIT_4 = 1, 2, 3
 BC_SPLIT_FORCE_HBM = 0x100
 BC_TOKENS, BC_MAPS = 0, 1
-BC_GATE_LOGIT, BC_GATE_VALUE = 0, 1
+BC_GATE_LOGIT, BC_GATE_VALUE, BC_GATE_LOG = 0, 1, 2
+BC_NORM_RMS, BC_NORM_LAYER = 0, 1
+BC_ACT_SILU, BC_ACT_SIGMOID = 0, 1
 STATUS = {0: "BC_OK", 1: "BC_ERR_NULL", 2: "BC_ERR_SHAPE", 3: "BC_ERR_DTYPE", 4: "BC_ERR_ALIGN",
           5: "BC_ERR_WORKSPACE", 6: "BC_ERR_HIP", 7: "BC_ERR_UNSUPPORTED"}
 
 # Exported symbols and their C signatures (kept in step with boxconv.h).
 _vp, _i, _u, _sz, _f = ctypes.c_void_p, ctypes.c_int, ctypes.c_uint, ctypes.c_size_t, ctypes.c_float
 _ll = ctypes.c_int64
+
+
+class bc_strides(ctypes.Structure):
+    _fields_ = [("batch", _ll), ("row", _ll), ("head", _ll)]
+
+
+class bc_attention(ctypes.Structure):
+    _fields_ = [(n, _i) for n in ("N", "T", "H", "Hq", "Hk", "Hv", "Dk", "Dv", "dt", "gate_dt", "form")] + [("scale", _f)]
+
+
+class bc_norm(ctypes.Structure):
+    _fields_ = [(n, _i) for n in ("R", "C", "groups", "kind", "act", "dt")] + [("eps", _f)]
+
+
+_st, _at, _nm = bc_strides, ctypes.POINTER(bc_attention), ctypes.POINTER(bc_norm)
 SIGNATURES = {
     "box_prep": (_i, [_vp, _i, _i, _u, _vp, _vp]),
     "sat_build": (_i, [_vp, _i, _vp, _vp, _i, _i, _i, _i, _vp]),
@@ -68,6 +87,16 @@ SIGNATURES = {
     "pointwise_mix_i8": (_i, [_vp, _vp, _vp, _i, _ll, _ll, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp, _sz, _vp]),
     "bc_i8_pitch": (_i, [_i]),
     "bc_mix_i8_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
+    "linear_attention_fwd": (_i, [_at, _vp, _st, _vp, _st, _vp, _st, _vp, _st, _vp, _vp, _vp, _st, _vp, _vp, _vp, _sz, _vp]),
+    "linear_attention_bwd": (_i, [_at, _vp, _st, _vp, _st, _vp, _st, _vp, _st, _vp, _vp, _vp, _st, _vp, _vp, _st, _vp, _st,
+                                  _vp, _st, _vp, _st, _vp, _vp, _sz, _vp]),
+    "linear_attention_step": (_i, [_at, _vp, _st, _vp, _st, _vp, _st, _vp, _st, _vp, _vp, _vp, _vp, _i, _vp]),
+    "bc_linear_attention_workspace_bytes": (_sz, [_i, _at]),
+    "bc_linear_attention_states_bytes": (_sz, [_i, _i, _i, _i, _i]),
+    "block_norm_fwd": (_i, [_nm, _vp, _ll, _vp, _ll, _vp, _ll, _vp, _vp, _vp, _vp, _ll, _vp, _ll, _vp]),
+    "block_norm_bwd": (_i, [_nm, _vp, _ll, _vp, _ll, _vp, _ll, _vp, _vp, _vp, _vp, _ll, _vp, _ll, _vp, _ll, _vp, _ll, _vp,
+                            _ll, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "bc_block_norm_workspace_bytes": (_sz, [_i, _i]),
     "bc_status_string": (ctypes.c_char_p, [_i]),
     "bc_abi_version": (_i, []),
 }
@@ -704,3 +733,246 @@ def pointwise_mix_i8(wq: torch.Tensor, w_scale: torch.Tensor, x: torch.Tensor, o
     if st:
         _check(st, what)
     return out
+
+
+# ---- linear-attention blocks --------------------------------------------------
+
+def _strides(t: torch.Tensor, what: str, name: str) -> bc_strides:
+    """Of a tensor [N, T, H, D] (or [N, H, D], one token) whose last dimension is
+    contiguous; strides of dimensions of one element are zero."""
+    shape, s = t.shape, t.stride()
+    if s[-1] != 1 and shape[-1] > 1:
+        raise BoxConvError(f"{what}: {name} must be contiguous in its last dimension")
+    if len(shape) == 3:
+        return bc_strides(s[0] if shape[0] > 1 else 0, 0, s[1] if shape[1] > 1 else 0)
+    return bc_strides(s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0, s[2] if shape[2] > 1 else 0)
+
+
+def _gate_strides(t: torch.Tensor) -> bc_strides:
+    """Of a gate [N, T, H], [N, H] (one token) or [H] (a decay for each head)."""
+    shape, s = t.shape, [a if n > 1 else 0 for n, a in zip(t.shape, t.stride())]
+    if len(shape) == 1:
+        return bc_strides(0, 0, s[0])
+    return bc_strides(s[0], s[1], s[2]) if len(shape) == 3 else bc_strides(s[0], 0, s[1])
+
+
+def _one_device(what, *tensors):
+    """The library launches on the current device's stream."""
+    here = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise BoxConvError("tensors must be on the GPU")
+        if here is None:
+            here = torch.cuda.current_device()
+        if t.get_device() != here:
+            raise BoxConvError(f"{what}: tensors must be on the current device ({here})")
+
+
+def _attention_sizes(q, k, v, gate, y, form, scale, what, tokens, yname="y"):
+    """The sizes of a call, its operands' shapes and types checked against them."""
+    dims = 4 if tokens else 3
+    for t, name in ((q, "q"), (k, "k"), (v, "v"), (y, yname)):
+        if not isinstance(t, torch.Tensor) or t.dim() != dims or t.dtype not in _FLOATS:
+            raise BoxConvError(f"{what}: {name} must be a {dims}-D fp32 or bf16 tensor")
+    dt, lead, H, Dv = y.dtype, tuple(y.shape[:-2]), y.shape[-2], y.shape[-1]
+    Dk = q.shape[-1]
+    _need(q, (*lead, q.shape[-2], Dk), dt, what, "q")
+    _need(k, (*lead, k.shape[-2], Dk), dt, what, "k")
+    _need(v, (*lead, v.shape[-2], Dv), dt, what, "v")
+    if not isinstance(gate, torch.Tensor) or gate.dtype not in (torch.float32, dt):
+        raise BoxConvError(f"{what}: gate must be a tensor, fp32 or of q's type")
+    if gate.dim() != 1:
+        _need(gate, (*lead, H), gate.dtype, what, "gate")
+    else:
+        _need(gate, (H,), gate.dtype, what, "gate")
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        if t.shape[-2] == 0 or H % t.shape[-2]:
+            raise BoxConvError(f"{what}: {name} has {t.shape[-2]} heads, not a divisor of {H}")
+    return bc_attention(lead[0], lead[1] if tokens else 1, H, q.shape[-2], k.shape[-2], v.shape[-2], Dk, Dv, _CODES[dt],
+                        _CODES[gate.dtype], form, float(scale))
+
+
+def linear_attention_workspace_bytes(op: int, N, T, H, Hq, Hk, Hv, Dk, Dv, dt: int) -> int:
+    """op: 0 = linear_attention_fwd, 1 = linear_attention_bwd; dt: dtype code of q."""
+    a = bc_attention(N, T, H, Hq, Hk, Hv, Dk, Dv, dt, BC_F32, BC_GATE_LOG, 1.0)
+    return int(load_library().bc_linear_attention_workspace_bytes(op, ctypes.byref(a)))
+
+
+def linear_attention_states(N, T, H, Dk, Dv, device="cuda") -> torch.Tensor:
+    """The buffer in which linear_attention_fwd keeps what linear_attention_bwd
+    starts from (its layout is the library's)."""
+    n = int(load_library().bc_linear_attention_states_bytes(N, T, H, Dk, Dv))
+    if n == 0:
+        raise BoxConvError("linear_attention_states: BC_ERR_SHAPE")
+    return torch.empty(n // 4, dtype=torch.float32, device=device)
+
+
+def linear_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, gate: torch.Tensor, y: torch.Tensor,
+                         s0: torch.Tensor | None = None, s_last: torch.Tensor | None = None,
+                         lengths: torch.Tensor | None = None, states: torch.Tensor | None = None,
+                         form: int = BC_GATE_LOGIT, scale: float = 1.0, ws: torch.Tensor | None = None):
+    """q [N, T, Hq, Dk], k [N, T, Hk, Dk], v [N, T, Hv, Dv] and y [N, T, H, Dv],
+    contiguous in the last dimension (views of other layouts are taken as they
+    are); gate [N, T, H], or [H]: a decay for each head."""
+    what = "linear_attention_fwd"
+    a = _attention_sizes(q, k, v, gate, y, form, scale, what, True)
+    cells = (a.N, a.H, a.Dk, a.Dv)
+    _need(s0, cells, _F32, what, "s0")
+    _need(s_last, cells, _F32, what, "s_last")
+    _need(lengths, (a.N,), torch.int32, what, "lengths")
+    lib = load_library()
+    if states is not None:
+        _need_numel(states, lib.bc_linear_attention_states_bytes(a.N, a.T, a.H, a.Dk, a.Dv) // 4, _F32, what, "states")
+    sq, sk, sv, sy = (_strides(t, what, n) for t, n in ((q, "q"), (k, "k"), (v, "v"), (y, "y")))
+    _one_device(what, q, k, v, gate, y, s0, s_last, lengths, states, ws)
+    if ws is None:
+        ws = _workspace(lib.bc_linear_attention_workspace_bytes(0, a), q.device)
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(lib.linear_attention_fwd(a, _data(q), sq, _data(k), sk, _data(v), sv, _data(gate), _gate_strides(gate),
+                                    _ptr(s0), _ptr(lengths), _data(y), sy, _ptr(s_last), _ptr(states), _ptr(ws), nbytes,
+                                    _stream()), what)
+    return y
+
+
+def linear_attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, gate: torch.Tensor, states: torch.Tensor,
+                         grad_y: torch.Tensor, grad_q: torch.Tensor, grad_k: torch.Tensor, grad_v: torch.Tensor,
+                         grad_gate: torch.Tensor | None = None, grad_s_last: torch.Tensor | None = None,
+                         grad_s0: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                         form: int = BC_GATE_LOGIT, scale: float = 1.0, ws: torch.Tensor | None = None):
+    """The gradients of linear_attention_fwd; states: what that call kept.
+    grad_gate [N, T, H] or None (a gate [H] is not learned here, or its gradient
+    is the sum of grad_gate over sequences and tokens)."""
+    what = "linear_attention_bwd"
+    a = _attention_sizes(q, k, v, gate, grad_y, form, scale, what, True, "grad_y")
+    grads = ((grad_q, q, "grad_q"), (grad_k, k, "grad_k"), (grad_v, v, "grad_v"))
+    for g, t, name in grads:
+        if not isinstance(g, torch.Tensor):
+            raise BoxConvError(f"{what}: {name} must be a tensor")
+        _need(g, tuple(t.shape), t.dtype, what, name)
+    _need(grad_gate, (a.N, a.T, a.H), gate.dtype, what, "grad_gate")
+    cells = (a.N, a.H, a.Dk, a.Dv)
+    _need(grad_s_last, cells, _F32, what, "grad_s_last")
+    _need(grad_s0, cells, _F32, what, "grad_s0")
+    _need(lengths, (a.N,), torch.int32, what, "lengths")
+    lib = load_library()
+    if not isinstance(states, torch.Tensor):
+        raise BoxConvError(f"{what}: states must be a tensor")
+    _need_numel(states, lib.bc_linear_attention_states_bytes(a.N, a.T, a.H, a.Dk, a.Dv) // 4, _F32, what, "states")
+    sq, sk, sv, sy = (_strides(t, what, n) for t, n in ((q, "q"), (k, "k"), (v, "v"), (grad_y, "grad_y")))
+    gq, gk, gv = (_strides(g, what, name) for g, _, name in grads)
+    _one_device(what, q, k, v, gate, states, grad_y, grad_q, grad_k, grad_v, grad_gate, grad_s_last, grad_s0, lengths, ws)
+    if ws is None:
+        ws = _workspace(lib.bc_linear_attention_workspace_bytes(1, a), q.device)
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(lib.linear_attention_bwd(a, _data(q), sq, _data(k), sk, _data(v), sv, _data(gate), _gate_strides(gate),
+                                    _ptr(states), _ptr(lengths), _data(grad_y), sy, _ptr(grad_s_last), _data(grad_q), gq,
+                                    _data(grad_k), gk, _data(grad_v), gv, None if grad_gate is None else _data(grad_gate),
+                                    bc_strides() if grad_gate is None else _gate_strides(grad_gate), _ptr(grad_s0),
+                                    _ptr(ws), nbytes, _stream()), what)
+    return grad_q, grad_k, grad_v
+
+
+def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, gate: torch.Tensor, state: torch.Tensor,
+                          y: torch.Tensor, slots: torch.Tensor | None = None, state_out: torch.Tensor | None = None,
+                          form: int = BC_GATE_LOGIT, scale: float = 1.0):
+    """One token of N sequences: q [N, Hq, Dk], k [N, Hk, Dk], v [N, Hv, Dv], gate
+    [N, H] or [H], state [S, H, Dk, Dv] fp32 (the pool; state_out, default itself,
+    takes the new states), slots [N] int32 -> y [N, H, Dv], dense."""
+    what = "linear_attention_step"
+    a = _attention_sizes(q, k, v, gate, y, form, scale, what, False)
+    S = state.shape[0] if isinstance(state, torch.Tensor) and state.dim() == 4 else None
+    if S is None:
+        raise BoxConvError(f"{what}: state must be a 4-D tensor")
+    _need(state, (S, a.H, a.Dk, a.Dv), _F32, what, "state")
+    _need(state_out, (S, a.H, a.Dk, a.Dv), _F32, what, "state_out")
+    _need(slots, (a.N,), torch.int32, what, "slots")
+    sq, sk, sv = _strides(q, what, "q"), _strides(k, what, "k"), _strides(v, what, "v")
+    _one_device(what, q, k, v, gate, state, state_out, slots, y)
+    sp = _ptr(state)
+    lib = _lib or load_library()
+    st = lib.linear_attention_step(a, _data(q), sq, _data(k), sk, _data(v), sv, _data(gate), _gate_strides(gate), sp,
+                                   sp if state_out is None else _ptr(state_out), _ptr(slots), _ptr(y), S, _stream())
+    if st:
+        _check(st, what)
+    return y
+
+
+def _norm_rows(t, shape, dtype, what, name):
+    """Pointer and row stride of [..., C], its leading dimensions one run of rows."""
+    if t is None:
+        return None, 0
+    _need(t, shape, dtype, what, name)
+    if t.dim() != 2:
+        try:
+            t = t.view(-1, t.shape[-1])
+        except RuntimeError:
+            raise BoxConvError(f"{what}: {name}'s rows must be equally far apart") from None
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        raise BoxConvError(f"{what}: {name} must be contiguous in its last dimension")
+    return t.data_ptr(), t.stride(0)
+
+
+def _norm_sizes(z, groups, kind, act, eps, what):
+    if not isinstance(z, torch.Tensor) or z.dim() < 2 or z.dtype not in _FLOATS:
+        raise BoxConvError(f"{what}: z must be an fp32 or bf16 tensor [..., C]")
+    C = z.shape[-1]
+    return tuple(z.shape), z.dtype, bc_norm(z.numel() // max(C, 1), C, groups, kind, act, _CODES[z.dtype], eps)
+
+
+def block_norm_workspace_bytes(R: int, C: int) -> int:
+    return int(load_library().bc_block_norm_workspace_bytes(R, C))
+
+
+def block_norm_fwd(z: torch.Tensor, gate: torch.Tensor | None = None, x: torch.Tensor | None = None,
+                   w_post: torch.Tensor | None = None, res_scale: torch.Tensor | None = None,
+                   w_pre: torch.Tensor | None = None, r: torch.Tensor | None = None, y: torch.Tensor | None = None,
+                   groups: int = 0, kind: int = BC_NORM_RMS, act: int = BC_ACT_SILU, eps: float = 1e-6):
+    """z, gate, x and the outputs r and y (either may be None): [..., C], rows
+    equally far apart; weights fp32 [C].  p = norm(z) * w_post by groups (0: z),
+    r = x + res_scale * p * act(gate), y = norm(r) * w_pre -> (r, y)."""
+    what = "block_norm_fwd"
+    shape, dt, n = _norm_sizes(z, groups, kind, act, eps, what)
+    rows = [_norm_rows(t, shape, dt, what, name) for t, name in ((z, "z"), (gate, "gate"), (x, "x"))]
+    for t, name in ((w_post, "w_post"), (res_scale, "res_scale"), (w_pre, "w_pre")):
+        _need(t, (n.C,), _F32, what, name)
+    outs = [_norm_rows(t, shape, dt, what, name) for t, name in ((r, "r"), (y, "y"))]
+    _one_device(what, z, gate, x, w_post, res_scale, w_pre, r, y)
+    lib = _lib or load_library()
+    st = lib.block_norm_fwd(n, *rows[0], *rows[1], *rows[2], _ptr(w_post), _ptr(res_scale), _ptr(w_pre), *outs[0],
+                            *outs[1], _stream())
+    if st:
+        _check(st, what)
+    return r, y
+
+
+def block_norm_bwd(z: torch.Tensor, gate: torch.Tensor | None = None, x: torch.Tensor | None = None,
+                   w_post: torch.Tensor | None = None, res_scale: torch.Tensor | None = None,
+                   w_pre: torch.Tensor | None = None, grad_r: torch.Tensor | None = None,
+                   grad_y: torch.Tensor | None = None, grad_z: torch.Tensor | None = None,
+                   grad_gate: torch.Tensor | None = None, grad_x: torch.Tensor | None = None,
+                   grad_w_post: torch.Tensor | None = None, grad_res_scale: torch.Tensor | None = None,
+                   grad_w_pre: torch.Tensor | None = None, groups: int = 0, kind: int = BC_NORM_RMS,
+                   act: int = BC_ACT_SILU, eps: float = 1e-6, ws: torch.Tensor | None = None):
+    """The gradients of block_norm_fwd of the same arguments, those that are given
+    a tensor -> (grad_z, grad_gate, grad_x)."""
+    what = "block_norm_bwd"
+    shape, dt, n = _norm_sizes(z, groups, kind, act, eps, what)
+    rows = [_norm_rows(t, shape, dt, what, name) for t, name in
+            ((z, "z"), (gate, "gate"), (x, "x"), (grad_r, "grad_r"), (grad_y, "grad_y"), (grad_z, "grad_z"),
+             (grad_gate, "grad_gate"), (grad_x, "grad_x"))]
+    weights = ((w_post, "w_post"), (res_scale, "res_scale"), (w_pre, "w_pre"), (grad_w_post, "grad_w_post"),
+               (grad_res_scale, "grad_res_scale"), (grad_w_pre, "grad_w_pre"))
+    for t, name in weights:
+        _need(t, (n.C,), _F32, what, name)
+    _one_device(what, z, gate, x, grad_r, grad_y, grad_z, grad_gate, grad_x, *(t for t, _ in weights), ws)
+    lib = load_library()
+    if ws is None and any(t is not None for t in (grad_w_post, grad_res_scale, grad_w_pre)):
+        ws = _workspace(lib.bc_block_norm_workspace_bytes(n.R, n.C), z.device)
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    flat = [v for pair in rows[3:] for v in pair]
+    _check(lib.block_norm_bwd(n, *rows[0], *rows[1], *rows[2], _ptr(w_post), _ptr(res_scale), _ptr(w_pre), *flat,
+                              _ptr(grad_w_post), _ptr(grad_res_scale), _ptr(grad_w_pre), _ptr(ws), nbytes, _stream()),
+           what)
+    return grad_z, grad_gate, grad_x

@@ -4,6 +4,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "../../include/boxconv.h"
 #include "bc_internal.hpp"
@@ -581,6 +582,284 @@ bc_status gated_scan_step(const void* gate, const void* x, int dt, int64_t row_s
     return BC_ERR_ALIGN;
   return hip_status(bc::launch_scan_step(gate, x, (long)row_stride, dt, state, state_out, slots, y, N, C, S, form,
                                          stream));
+}
+
+// ---- linear attention ------------------------------------------------------
+
+static bool heads_ok(int H, int Hx) { return Hx > 0 && Hx <= H && H % Hx == 0; }
+
+static bc_status attention_sizes(const bc_attention* a, bool tokens) {
+  if (!a) return BC_ERR_NULL;
+  if (a->form != BC_GATE_LOGIT && a->form != BC_GATE_LOG) return BC_ERR_UNSUPPORTED;
+  if (a->N <= 0 || a->H <= 0 || (long)a->N * a->H > (1L << 17)) return BC_ERR_SHAPE;
+  if (!heads_ok(a->H, a->Hq) || !heads_ok(a->H, a->Hk) || !heads_ok(a->H, a->Hv)) return BC_ERR_SHAPE;
+  if (a->Dk <= 0 || a->Dv <= 0 || a->Dk > 128 || a->Dv > 128) return BC_ERR_SHAPE;
+  if (tokens && (a->T <= 0 || a->T > (1 << 30) || (long)a->N * a->H * ((a->T + 127) / 128) > (1L << 23))) return BC_ERR_SHAPE;
+  if (a->dt != BC_F32 && a->dt != BC_BF16) return BC_ERR_DTYPE;
+  if (a->gate_dt != BC_F32 && a->gate_dt != a->dt) return BC_ERR_DTYPE;
+  // (a factor that is not a number would make every output one)
+  return a->scale - a->scale == 0.0f ? BC_OK : BC_ERR_UNSUPPORTED;
+}
+
+// Offsets in bytes stay below 2^63.
+static bool strides_in_range(const bc_strides& s, int N, int T, int H) {
+  if (s.batch < 0 || s.row < 0 || s.head < 0) return false;
+  return (double)s.batch * (N - 1) + (double)s.row * (T - 1) + (double)s.head * (H - 1) < 2e18;
+}
+
+// An output's elements are distinct: each stride at least the extent of what the
+// smaller ones span.  Strides of dimensions of one element do not matter.
+static bool strides_distinct(const bc_strides& s, int N, int T, int H, int D) {
+  if (!strides_in_range(s, N, T, H)) return false;
+  struct Dim { int64_t stride; int size; } d[3] = {{s.batch, N}, {s.row, T}, {s.head, H}};
+  std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+  double extent = D;   // may pass 2^63
+  for (const Dim& x : d) {
+    if (x.size == 1) continue;
+    if ((double)x.stride < extent) return false;
+    extent += (double)x.stride * (x.size - 1);
+  }
+  return true;
+}
+
+// Gates are read one by one: a slice of them may start anywhere.
+static bool aligned_gate(const void* p, const bc_attention& a) {
+  return ((uintptr_t)p & (a.gate_dt == BC_F32 ? 3u : 1u)) == 0;
+}
+
+// The operands' pointers and strides, of T tokens.
+static bc_status attention_inputs(const bc::Attention& f, int T) {
+  if (!f.q || !f.k || !f.v || !f.gate) return BC_ERR_NULL;
+  const bc_attention& a = *f.a;
+  if (!strides_in_range(f.qs, a.N, T, a.Hq) || !strides_in_range(f.ks, a.N, T, a.Hk) ||
+      !strides_in_range(f.vs, a.N, T, a.Hv) || !strides_in_range(f.gs, a.N, T, a.H))
+    return BC_ERR_SHAPE;
+  if (!aligned16(f.q) || !aligned16(f.k) || !aligned16(f.v) || !aligned_gate(f.gate, a)) return BC_ERR_ALIGN;
+  return BC_OK;
+}
+
+size_t bc_linear_attention_states_bytes(int N, int T, int H, int Dk, int Dv) {
+  const bc_attention a{N, T, H, H, H, H, Dk, Dv, BC_F32, BC_F32, BC_GATE_LOG, 1.0f};
+  return attention_sizes(&a, true) == BC_OK ? bc::linear_attention_states_bytes(N, T, H, Dk, Dv) : 0;
+}
+
+size_t bc_linear_attention_workspace_bytes(int op, const bc_attention* sizes) {
+  if ((op != 0 && op != 1) || attention_sizes(sizes, true) != BC_OK) return 0;
+  return bc::linear_attention_workspace_bytes(op == 1, *sizes);
+}
+
+static bc_status attention_workspace(bool bwd, const bc_attention& a, void* ws, size_t ws_bytes) {
+  const size_t need = bc::linear_attention_workspace_bytes(bwd, a);
+  if (need > 0 && (!ws || ws_bytes < need)) return BC_ERR_WORKSPACE;
+  return need > 0 && !aligned16(ws) ? BC_ERR_ALIGN : BC_OK;
+}
+
+bc_status linear_attention_fwd(const bc_attention* sizes, const void* q, bc_strides q_strides, const void* k,
+                               bc_strides k_strides, const void* v, bc_strides v_strides, const void* gate,
+                               bc_strides gate_strides, const float* s0, const int* lengths, void* y,
+                               bc_strides y_strides, float* s_last, float* states, void* ws, size_t ws_bytes,
+                               hipStream_t stream) {
+  bc_status st = attention_sizes(sizes, true);
+  if (st != BC_OK) return st;
+  bc::Attention f{};
+  f.a = sizes;
+  f.q = q;
+  f.k = k;
+  f.v = v;
+  f.gate = gate;
+  f.qs = q_strides;
+  f.ks = k_strides;
+  f.vs = v_strides;
+  f.gs = gate_strides;
+  f.s0 = s0;
+  f.lengths = lengths;
+  f.y = y;
+  f.ys = y_strides;
+  f.s_last = s_last;
+  f.states = states;
+  f.ws = ws;
+  if (!y) return BC_ERR_NULL;
+  if ((st = attention_inputs(f, sizes->T)) != BC_OK) return st;
+  if (!strides_distinct(y_strides, sizes->N, sizes->T, sizes->H, sizes->Dv)) return BC_ERR_SHAPE;
+  if (!aligned16(y) || !aligned16_or_null(s0) || !aligned16_or_null(lengths) || !aligned16_or_null(s_last) ||
+      !aligned16_or_null(states))
+    return BC_ERR_ALIGN;
+  if ((st = attention_workspace(false, *sizes, ws, ws_bytes)) != BC_OK) return st;
+  return hip_status(bc::launch_linear_attention_fwd(f, stream));
+}
+
+bc_status linear_attention_bwd(const bc_attention* sizes, const void* q, bc_strides q_strides, const void* k,
+                               bc_strides k_strides, const void* v, bc_strides v_strides, const void* gate,
+                               bc_strides gate_strides, const float* states, const int* lengths, const void* grad_y,
+                               bc_strides grad_y_strides, const float* grad_s_last, void* grad_q,
+                               bc_strides grad_q_strides, void* grad_k, bc_strides grad_k_strides, void* grad_v,
+                               bc_strides grad_v_strides, void* grad_gate, bc_strides grad_gate_strides,
+                               float* grad_s0, void* ws, size_t ws_bytes, hipStream_t stream) {
+  bc_status st = attention_sizes(sizes, true);
+  if (st != BC_OK) return st;
+  bc::Attention f{};
+  f.a = sizes;
+  f.q = q;
+  f.k = k;
+  f.v = v;
+  f.gate = gate;
+  f.qs = q_strides;
+  f.ks = k_strides;
+  f.vs = v_strides;
+  f.gs = gate_strides;
+  f.states = const_cast<float*>(states);
+  f.lengths = lengths;
+  f.gy = grad_y;
+  f.gys = grad_y_strides;
+  f.gs_last = grad_s_last;
+  f.gq = grad_q;
+  f.gk = grad_k;
+  f.gv = grad_v;
+  f.ggate = grad_gate;
+  f.gqs = grad_q_strides;
+  f.gks = grad_k_strides;
+  f.gvs = grad_v_strides;
+  f.ggs = grad_gate_strides;
+  f.gs0 = grad_s0;
+  f.ws = ws;
+  if (!states || !grad_y || !grad_q || !grad_k || !grad_v) return BC_ERR_NULL;
+  if ((st = attention_inputs(f, sizes->T)) != BC_OK) return st;
+  const bc_attention& a = *sizes;
+  if (!strides_in_range(grad_y_strides, a.N, a.T, a.H) || !strides_distinct(grad_q_strides, a.N, a.T, a.Hq, a.Dk) ||
+      !strides_distinct(grad_k_strides, a.N, a.T, a.Hk, a.Dk) || !strides_distinct(grad_v_strides, a.N, a.T, a.Hv, a.Dv) ||
+      (grad_gate && !strides_distinct(grad_gate_strides, a.N, a.T, a.H, 1)))
+    return BC_ERR_SHAPE;
+  if (!aligned16(states) || !aligned16(grad_y) || !aligned16(grad_q) || !aligned16(grad_k) || !aligned16(grad_v) ||
+      !aligned_gate(grad_gate, a) || !aligned16_or_null(lengths) || !aligned16_or_null(grad_s_last) ||
+      !aligned16_or_null(grad_s0))
+    return BC_ERR_ALIGN;
+  if ((st = attention_workspace(true, a, ws, ws_bytes)) != BC_OK) return st;
+  return hip_status(bc::launch_linear_attention_bwd(f, stream));
+}
+
+bc_status linear_attention_step(const bc_attention* sizes, const void* q, bc_strides q_strides, const void* k,
+                                bc_strides k_strides, const void* v, bc_strides v_strides, const void* gate,
+                                bc_strides gate_strides, const float* state, float* state_out, const int* slots,
+                                void* y, int S, hipStream_t stream) {
+  bc_status st = attention_sizes(sizes, false);
+  if (st != BC_OK) return st;
+  bc::Attention f{};
+  f.a = sizes;
+  f.q = q;
+  f.k = k;
+  f.v = v;
+  f.gate = gate;
+  f.qs = q_strides;
+  f.ks = k_strides;
+  f.vs = v_strides;
+  f.gs = gate_strides;
+  f.y = y;
+  if (!state || !state_out || !y) return BC_ERR_NULL;
+  if ((st = attention_inputs(f, 1)) != BC_OK) return st;
+  if (S <= 0 || (!slots && sizes->N > S)) return BC_ERR_SHAPE;
+  if (!aligned16(state) || !aligned16(state_out) || !aligned16(y) || !aligned16_or_null(slots)) return BC_ERR_ALIGN;
+  return hip_status(bc::launch_linear_attention_step(f, state, state_out, slots, S, stream));
+}
+
+// ---- block norms -------------------------------------------------------------
+
+static bc_status norm_sizes(const bc_norm* n) {
+  if (!n) return BC_ERR_NULL;
+  if (n->kind != BC_NORM_RMS && n->kind != BC_NORM_LAYER) return BC_ERR_UNSUPPORTED;
+  if (n->act != BC_ACT_SILU && n->act != BC_ACT_SIGMOID) return BC_ERR_UNSUPPORTED;
+  if (n->R <= 0 || n->C <= 0 || n->C > (1 << 14) || n->groups < 0 || n->groups > n->C) return BC_ERR_SHAPE;
+  if (n->groups > 0 && n->C % n->groups) return BC_ERR_SHAPE;
+  if (!bc::block_norm_takes(n->C, n->groups)) return BC_ERR_SHAPE;
+  if (n->dt != BC_F32 && n->dt != BC_BF16) return BC_ERR_DTYPE;
+  // (not below the smallest normal number: rows of zeros have no other size)
+  return n->eps >= 1.17549435e-38f && n->eps < 1e38f ? BC_OK : BC_ERR_UNSUPPORTED;
+}
+
+// Rows of C, `stride` apart.
+static bc_status norm_rows(const bc_norm& n, std::initializer_list<bc::NormRows> all) {
+  for (const bc::NormRows& t : all)
+    if (t.p && (t.stride < n.C || t.stride > (1L << 30)) && n.R > 1) return BC_ERR_SHAPE;
+  for (const bc::NormRows& t : all)
+    if (t.p && !aligned16(t.p)) return BC_ERR_ALIGN;
+  return BC_OK;
+}
+
+size_t bc_block_norm_workspace_bytes(int R, int C) {
+  return R <= 0 || C <= 0 || C > (1 << 14) ? 0 : bc::block_norm_workspace_bytes(R, C);
+}
+
+bc_status block_norm_fwd(const bc_norm* sizes, const void* z, int64_t z_stride, const void* gate, int64_t gate_stride,
+                         const void* x, int64_t x_stride, const float* w_post, const float* res_scale,
+                         const float* w_pre, void* r, int64_t r_stride, void* y, int64_t y_stride, hipStream_t stream) {
+  bc_status st = norm_sizes(sizes);
+  if (st != BC_OK) return st;
+  if (!z || (!r && !y)) return BC_ERR_NULL;
+  if (sizes->groups == 0 && w_post) return BC_ERR_UNSUPPORTED;
+  if (!y && w_pre) return BC_ERR_UNSUPPORTED;
+  bc::BlockNorm b{};
+  b.z = {z, z_stride};
+  b.gate = {gate, gate_stride};
+  b.x = {x, x_stride};
+  b.r = {r, r_stride};
+  b.y = {y, y_stride};
+  if ((st = norm_rows(*sizes, {b.z, b.gate, b.x, b.r, b.y})) != BC_OK) return st;
+  if (!aligned16_or_null(w_post) || !aligned16_or_null(res_scale) || !aligned16_or_null(w_pre)) return BC_ERR_ALIGN;
+  b.w_post = w_post;
+  b.scale = res_scale;
+  b.w_pre = w_pre;
+  b.R = sizes->R;
+  b.C = sizes->C;
+  b.groups = sizes->groups;
+  b.layer = sizes->kind == BC_NORM_LAYER;
+  b.sigmoid = sizes->act == BC_ACT_SIGMOID;
+  b.dt = sizes->dt;
+  b.eps = sizes->eps;
+  return hip_status(bc::launch_block_norm(b, false, stream));
+}
+
+bc_status block_norm_bwd(const bc_norm* sizes, const void* z, int64_t z_stride, const void* gate, int64_t gate_stride,
+                         const void* x, int64_t x_stride, const float* w_post, const float* res_scale,
+                         const float* w_pre, const void* grad_r, int64_t grad_r_stride, const void* grad_y,
+                         int64_t grad_y_stride, void* grad_z, int64_t grad_z_stride, void* grad_gate,
+                         int64_t grad_gate_stride, void* grad_x, int64_t grad_x_stride, float* grad_w_post,
+                         float* grad_res_scale, float* grad_w_pre, void* ws, size_t ws_bytes, hipStream_t stream) {
+  bc_status st = norm_sizes(sizes);
+  if (st != BC_OK) return st;
+  if (!z || (!grad_r && !grad_y) || (grad_gate && !gate) || (grad_x && !x)) return BC_ERR_NULL;
+  if (sizes->groups == 0 && (w_post || grad_w_post)) return BC_ERR_UNSUPPORTED;
+  if (!grad_y && grad_w_pre) return BC_ERR_UNSUPPORTED;
+  bc::BlockNorm b{};
+  b.z = {z, z_stride};
+  b.gate = {gate, gate_stride};
+  b.x = {x, x_stride};
+  b.dr = {grad_r, grad_r_stride};
+  b.dy = {grad_y, grad_y_stride};
+  b.dz = {grad_z, grad_z_stride};
+  b.dgate = {grad_gate, grad_gate_stride};
+  b.dx = {grad_x, grad_x_stride};
+  if ((st = norm_rows(*sizes, {b.z, b.gate, b.x, b.dr, b.dy, b.dz, b.dgate, b.dx})) != BC_OK) return st;
+  for (const float* w : {w_post, res_scale, w_pre, static_cast<const float*>(grad_w_post),
+                         static_cast<const float*>(grad_res_scale), static_cast<const float*>(grad_w_pre)})
+    if (!aligned16_or_null(w)) return BC_ERR_ALIGN;
+  if (grad_w_post || grad_res_scale || grad_w_pre) {
+    if (!ws || ws_bytes < bc::block_norm_workspace_bytes(sizes->R, sizes->C)) return BC_ERR_WORKSPACE;
+    if (!aligned16(ws)) return BC_ERR_ALIGN;
+  }
+  b.w_post = w_post;
+  b.scale = res_scale;
+  b.w_pre = w_pre;
+  b.dw_post = grad_w_post;
+  b.dscale = grad_res_scale;
+  b.dw_pre = grad_w_pre;
+  b.R = sizes->R;
+  b.C = sizes->C;
+  b.groups = sizes->groups;
+  b.layer = sizes->kind == BC_NORM_LAYER;
+  b.sigmoid = sizes->act == BC_ACT_SIGMOID;
+  b.dt = sizes->dt;
+  b.eps = sizes->eps;
+  b.ws = ws;
+  return hip_status(bc::launch_block_norm(b, true, stream));
 }
 
 // Grids below 2^32 threads: tiles of 64 x 64 outputs by 256 threads, strips of

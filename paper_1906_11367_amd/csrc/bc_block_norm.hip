@@ -1,0 +1,473 @@
+// The norms around a block, fused with its gate, residual sum and scale (gfx950).
+// For every row of C channels:
+//   p = norm(z) w_post within each of `groups` runs of channels (p = z without),
+//   u = p act(gate),  r = x + scale u,  y = norm(r) w_pre,
+// norm(v) = v rho, rho = (mean(v^2) + eps)^-1/2, of v less its mean for
+// BC_NORM_LAYER.  The gradient to v through n = v rho, given dn, is
+//   rho (dn - n mean(n dn) [- mean(dn)]).
+// What bounds it: every tensor is read or written once, a few dozen operations
+// an element, so memory.  A row stays in registers between its statistics: a team
+// of lanes takes a row, 8 consecutive channels (16 bytes of bf16) a slot, no slot
+// across two groups; rows of up to 512 slots' channels share waves, longer ones
+// take a block.  The backward computes the forward's values again (in fp32, none
+// read back rounded) and keeps each lane's share of the weights' gradients over
+// all rows of its block; a second kernel sums the blocks in order.
+#include <algorithm>
+
+#include "bc_internal.hpp"
+#include "bc_scan.hpp"
+
+namespace bc {
+namespace {
+
+using scan::kBF16;
+using scan::kF32;
+using scan::kBytes;
+
+struct Rows { const char* p; long stride; };   // of an input; null: none
+struct OutRows { char* p; long stride; };
+
+struct NormArgs {
+  Rows z, gate, x;
+  OutRows r, y;
+  const float *w_post, *scale, *w_pre;
+  Rows dr, dy;                  // backward
+  OutRows dz, dgate, dx;
+  float* part;                  // [blocks][3][C]: dw_post, dscale, dw_pre; or null
+  int R, C, groups, size;       // size: channels of a group
+  int per;                      // slots of a group
+  int lanes;                    // of a team that shares its wave
+  int mode;                     // how a group's slots are summed
+  int layer, sigmoid, post, pre;
+  float eps;
+};
+
+constexpr int kSumTeam = 0, kSumLanes = 1, kSumShared = 2;
+
+__device__ __forceinline__ float sigmoid(float g) {
+  const float e = expf(-fabsf(g)), r = __builtin_amdgcn_rcpf(1.0f + e);
+  return g >= 0.0f ? r : e * r;
+}
+
+// Sums over slots, by a team of W waves, or of `lanes` lanes (W = 1), NS slots a
+// lane: slot i * team + lane.
+template <int W, int NS> struct Team {
+  static constexpr int kSlots = W == 1 ? 256 : 64 * W * NS;   // of a block, where they meet in LDS
+  float* lds;       // [2][kSlots] slots, then [2][kSlots] groups
+  int lane, size;   // within the team; the team's lanes
+  int base;         // the team's first slot of the block's
+  int per, groups, mode;
+
+  template <int K> __device__ __forceinline__ void all(float (&v)[K]) const {
+    const int within = W == 1 ? size : 64;
+    for (int d = 1; d < within; d *= 2)
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], d);
+    if constexpr (W > 1) {
+      __syncthreads();   // the last sum has been read
+      if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int k = 0; k < K; ++k) lds[k * W + (threadIdx.x >> 6)] = v[k];
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        v[k] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) v[k] += lds[k * W + w];
+      }
+    }
+  }
+
+  // over the whole row
+  template <int K> __device__ __forceinline__ void row(float (&v)[NS][K]) const {
+    float s[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      s[k] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NS; ++i) s[k] += v[i][k];
+    }
+    all<K>(s);
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[i][k] = s[k];
+  }
+
+  // over each slot's group
+  template <int K> __device__ __forceinline__ void group(float (&v)[NS][K]) const {
+    if (mode == kSumTeam) {
+      row<K>(v);
+    } else if (mode == kSumLanes) {
+      for (int d = 1; d < per; d *= 2)
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+          for (int k = 0; k < K; ++k) v[i][k] += __shfl_xor(v[i][k], d);
+    } else {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+#pragma unroll
+        for (int k = 0; k < K; ++k) lds[k * kSlots + base + i * size + lane] = v[i][k];
+      __syncthreads();
+      // 8 lanes a group
+      float* sums = lds + 2 * kSlots;
+      const int eight = lane >> 3, l = lane & 7;
+      for (int g0 = 0; g0 < groups; g0 += size >> 3) {
+        const int g = g0 + eight;
+        float s[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          s[k] = 0.0f;
+          if (g < groups)
+            for (int j = l; j < per; j += 8) s[k] += lds[k * kSlots + base + g * per + j];
+          for (int d = 1; d < 8; d *= 2) s[k] += __shfl_xor(s[k], d);
+          if (g < groups && l == 0) sums[k * kSlots + base + g] = s[k];
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        const int j = i * size + lane, g = min(j / per, groups - 1);
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[i][k] = sums[k * kSlots + base + g];
+      }
+    }
+  }
+};
+
+template <int DT, int NS>
+__device__ __forceinline__ void load_row(const Rows& t, long row, const int (&col)[NS], const int (&avail)[NS],
+                                         float (&v)[NS][8]) {
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    const auto raw = scan::load_vec<DT, 8>(t.p + (row * t.stride + col[i]) * kBytes<DT>, avail[i]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[i][e] = scan::elem<DT, 8>(raw, e);
+  }
+}
+
+template <int DT, int NS>
+__device__ __forceinline__ void store_row(const OutRows& t, long row, const int (&col)[NS], const int (&avail)[NS],
+                                          const float (&v)[NS][8]) {
+#pragma unroll
+  for (int i = 0; i < NS; ++i)
+    if (avail[i] > 0) scan::store_vec<DT, 8>(t.p + (row * t.stride + col[i]) * kBytes<DT>, avail[i], v[i]);
+}
+
+template <int NS>
+__device__ __forceinline__ void load_weights(const float* w, float none, const int (&col)[NS], const int (&avail)[NS],
+                                             float (&v)[NS][8]) {
+#pragma unroll
+  for (int i = 0; i < NS; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[i][e] = w && e < avail[i] ? w[col[i] + e] : none;
+}
+
+// v -> v rho (less the mean), rho by slot.
+template <bool kGroup, class Team, int NS>
+__device__ __forceinline__ void normalise(const Team& team, bool layer, float inv, float eps, const int (&avail)[NS],
+                                          float (&v)[NS][8], float (&rho)[NS]) {
+  float s[NS][1];
+  auto sum = [&]() {
+    if constexpr (kGroup) team.template group<1>(s);
+    else team.template row<1>(s);
+  };
+  if (layer) {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      s[i][0] = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[i][0] += v[i][e];
+    }
+    sum();
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = e < avail[i] ? v[i][e] - s[i][0] * inv : 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    s[i][0] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[i][0] = fmaf(v[i][e], v[i][e], s[i][0]);
+  }
+  sum();
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    rho[i] = 1.0f / sqrtf(fmaf(s[i][0], inv, eps));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[i][e] *= rho[i];
+  }
+}
+
+// dn (the gradient to n = norm(v)) -> the gradient to v.
+template <bool kGroup, class Team, int NS>
+__device__ __forceinline__ void norm_grad(const Team& team, bool layer, float inv, const int (&avail)[NS],
+                                          const float (&n)[NS][8], const float (&rho)[NS], float (&dn)[NS][8]) {
+  float s[NS][2];
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    s[i][0] = s[i][1] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s[i][0] = fmaf(n[i][e], dn[i][e], s[i][0]);
+      s[i][1] += dn[i][e];
+    }
+  }
+  if constexpr (kGroup) team.template group<2>(s);
+  else team.template row<2>(s);
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    const float c = s[i][0] * inv, mean = layer ? s[i][1] * inv : 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dn[i][e] = e < avail[i] ? rho[i] * (dn[i][e] - mean - n[i][e] * c) : 0.0f;
+  }
+}
+
+template <int DT, int W, int NS, bool BWD>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a) {
+  using T = Team<W, NS>;
+  __shared__ float lds[4 * T::kSlots];
+  const int tid = threadIdx.x;
+  T team;
+  team.lds = lds;
+  team.size = W == 1 ? a.lanes : 64 * W;
+  team.lane = W == 1 ? tid & (a.lanes - 1) : tid;
+  const int which = W == 1 ? tid / a.lanes : 0, teams = W == 1 ? 256 / a.lanes : 1;
+  team.base = which * team.size;
+  team.per = a.per;
+  team.groups = max(a.groups, 1);
+  team.mode = a.mode;
+
+  int col[NS], avail[NS];
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    const int j = i * team.size + team.lane, g = j / a.per, k = j % a.per;
+    col[i] = g * a.size + k * 8;
+    avail[i] = g < team.groups ? min(a.size - k * 8, 8) : 0;
+    if (g >= team.groups) col[i] = 0;
+  }
+  float w_post[NS][8], scale[NS][8], w_pre[NS][8];
+  load_weights<NS>(a.w_post, 1.0f, col, avail, w_post);
+  load_weights<NS>(a.scale, 1.0f, col, avail, scale);
+  load_weights<NS>(a.w_pre, 1.0f, col, avail, w_pre);
+  const float inv_group = 1.0f / (float)a.size, inv_row = 1.0f / (float)a.C;
+
+  float sum[3][NS][8];
+  if constexpr (BWD) {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[k][i][e] = 0.0f;
+  }
+
+  for (long row0 = (long)blockIdx.x * teams; row0 < a.R; row0 += (long)gridDim.x * teams) {
+    const long row = min(row0 + which, (long)a.R - 1);   // (a team past the end follows the last row)
+    const bool on = row0 + which < a.R;
+    int here[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) here[i] = on ? avail[i] : 0;
+    float n[NS][8], g[NS][8], r[NS][8], dr[NS][8], dy[NS][8], rho1[NS], rho2[NS];
+    load_row<DT, NS>(a.z, row, col, here, n);
+    if (a.gate.p) load_row<DT, NS>(a.gate, row, col, here, g);
+    if (a.x.p) load_row<DT, NS>(a.x, row, col, here, r);
+    if constexpr (BWD) {
+      if (a.dr.p) load_row<DT, NS>(a.dr, row, col, here, dr);
+      if (a.dy.p) load_row<DT, NS>(a.dy, row, col, here, dy);
+    }
+    if (a.post) normalise<true>(team, a.layer, inv_group, a.eps, here, n, rho1);
+    float phi[NS][8], u[NS][8];
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        phi[i][e] = 1.0f;
+        if (a.gate.p) {
+          const float s = sigmoid(g[i][e]);
+          phi[i][e] = a.sigmoid ? s : g[i][e] * s;
+          if constexpr (BWD) g[i][e] = a.sigmoid ? s * (1.0f - s) : s * fmaf(g[i][e], 1.0f - s, 1.0f);   // the slope
+        }
+        u[i][e] = n[i][e] * w_post[i][e] * phi[i][e];
+        const float v = u[i][e] * scale[i][e];
+        r[i][e] = a.x.p ? r[i][e] + v : v;
+      }
+    if constexpr (!BWD) {
+      if (a.r.p) store_row<DT, NS>(a.r, row, col, here, r);
+      if (a.pre) {
+        normalise<false>(team, a.layer, inv_row, a.eps, here, r, rho2);
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) r[i][e] *= w_pre[i][e];
+        store_row<DT, NS>(a.y, row, col, here, r);
+      }
+    } else {
+      if (a.pre) {
+        normalise<false>(team, a.layer, inv_row, a.eps, here, r, rho2);
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            sum[2][i][e] = fmaf(dy[i][e], r[i][e], sum[2][i][e]);
+            dy[i][e] *= w_pre[i][e];
+          }
+        norm_grad<false>(team, a.layer, inv_row, here, r, rho2, dy);
+      }
+      float d[NS][8];
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[i][e] = (a.dr.p ? dr[i][e] : 0.0f) + (a.pre ? dy[i][e] : 0.0f);
+      if (a.dx.p) store_row<DT, NS>(a.dx, row, col, here, d);
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          sum[1][i][e] = fmaf(d[i][e], u[i][e], sum[1][i][e]);
+          const float du = d[i][e] * scale[i][e];
+          g[i][e] *= du * n[i][e] * w_post[i][e];
+          const float dp = du * phi[i][e];
+          sum[0][i][e] = fmaf(dp, n[i][e], sum[0][i][e]);
+          d[i][e] = dp * w_post[i][e];
+        }
+      if (a.dgate.p) store_row<DT, NS>(a.dgate, row, col, here, g);
+      if (a.dz.p) {
+        if (a.post) norm_grad<true>(team, a.layer, inv_group, here, n, rho1, d);
+        store_row<DT, NS>(a.dz, row, col, here, d);
+      }
+    }
+  }
+  if constexpr (BWD) {
+    if (a.part) {
+      float* out = a.part + (long)blockIdx.x * 3 * a.C;
+      // teams of one block: in order, through LDS
+      if (W == 1 && teams > 1) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            __syncthreads();
+            lds[tid] = sum[k][0][e];
+            __syncthreads();
+            if (which == 0) {
+              float s = 0.0f;
+              for (int t = 0; t < teams; ++t) s += lds[t * team.size + team.lane];
+              if (e < avail[0]) out[(long)k * a.C + col[0] + e] = s;
+            }
+          }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+          for (int i = 0; i < NS; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (e < avail[i]) out[(long)k * a.C + col[i] + e] = sum[k][i][e];
+      }
+    }
+  }
+}
+
+// The weights' gradients: blocks' shares part [P][3][C], 64 channels a block.
+__global__ __launch_bounds__(1024) void k_norm_weights(const float* part, int P, int C, float* dw_post, float* dscale,
+                                                       float* dw_pre) {
+  __shared__ float lds[16][64];
+  const int blocks = (C + 63) / 64, k = blockIdx.x / blocks, c = blockIdx.x % blocks * 64 + (threadIdx.x & 63);
+  float* out = k == 0 ? dw_post : k == 1 ? dscale : dw_pre;
+  if (!out) return;
+  const int row = threadIdx.x >> 6;
+  float s = 0.0f;
+  if (c < C)
+    for (int p = row; p < P; p += 16) s += part[((long)p * 3 + k) * C + c];
+  lds[row][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (row == 0 && c < C) {
+    float t = 0.0f;
+#pragma unroll
+    for (int u = 0; u < 16; ++u) t += lds[u][threadIdx.x];
+    out[c] = t;
+  }
+}
+
+constexpr int kPartBlocks = 512;   // blocks of the backward, and shares of the weights' gradients
+
+inline int slots_of(int C, int groups) {
+  const int G = std::max(groups, 1);
+  return G * ((C / G + 7) / 8);
+}
+
+template <int DT, bool BWD>
+hipError_t launch_norm(NormArgs& a, int* blocks, hipStream_t s) {
+  const int slots = slots_of(a.C, a.groups);
+  const int G = std::max(a.groups, 1);
+  a.size = a.C / G;
+  a.per = slots / G;
+  a.lanes = 64;
+  const bool pow2 = (a.per & (a.per - 1)) == 0 && a.per <= 64;
+  auto go = [&](auto kernel, int threads, int teams) {
+    const long want = ((long)a.R + teams - 1) / teams;
+    *blocks = (int)std::min<long>(want, BWD ? kPartBlocks : 2048);
+    a.mode = G == 1 ? kSumTeam : pow2 ? kSumLanes : kSumShared;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)*blocks), dim3((unsigned)threads), 0, s, a);
+    return hipGetLastError();
+  };
+  if (slots <= 64) {
+    a.lanes = 8;
+    while (a.lanes < slots) a.lanes *= 2;
+    return go(k_block_norm<DT, 1, 1, BWD>, 256, 256 / a.lanes);
+  }
+  if (slots <= 256) return go(k_block_norm<DT, 4, 1, BWD>, 256, 1);
+  if (slots <= 512) return go(k_block_norm<DT, 8, 1, BWD>, 512, 1);
+  if (slots <= 1024) return go(k_block_norm<DT, 16, 1, BWD>, 1024, 1);
+  return go(k_block_norm<DT, 16, 2, BWD>, 1024, 1);
+}
+
+}  // namespace
+
+bool block_norm_takes(int C, int groups) { return slots_of(C, groups) <= 2048; }
+
+size_t block_norm_workspace_bytes(int R, int C) { return (size_t)std::min(R, kPartBlocks) * 3 * C * 4; }
+
+static Rows rows(const NormRows& t) { return {static_cast<const char*>(t.p), t.stride}; }
+static OutRows out_rows(const NormRows& t) { return {static_cast<char*>(const_cast<void*>(t.p)), t.stride}; }
+
+hipError_t launch_block_norm(const BlockNorm& b, bool bwd, hipStream_t s) {
+  NormArgs a{};
+  a.z = rows(b.z);
+  a.gate = rows(b.gate);
+  a.x = rows(b.x);
+  a.r = out_rows(b.r);
+  a.y = out_rows(b.y);
+  a.w_post = b.w_post;
+  a.scale = b.scale;
+  a.w_pre = b.w_pre;
+  a.dr = rows(b.dr);
+  a.dy = rows(b.dy);
+  a.dz = out_rows(b.dz);
+  a.dgate = out_rows(b.dgate);
+  a.dx = out_rows(b.dx);
+  a.R = b.R;
+  a.C = b.C;
+  a.groups = b.groups;
+  a.layer = b.layer;
+  a.sigmoid = b.sigmoid;
+  a.post = b.groups > 0;
+  a.pre = bwd ? b.dy.p != nullptr : b.y.p != nullptr;
+  a.eps = b.eps;
+  int blocks = 0;
+  if (!bwd) return b.dt == kBF16 ? launch_norm<kBF16, false>(a, &blocks, s) : launch_norm<kF32, false>(a, &blocks, s);
+  const bool weights = b.dw_post || b.dscale || b.dw_pre;
+  a.part = weights ? static_cast<float*>(b.ws) : nullptr;
+  const hipError_t e = b.dt == kBF16 ? launch_norm<kBF16, true>(a, &blocks, s) : launch_norm<kF32, true>(a, &blocks, s);
+  if (e != hipSuccess || !weights) return e;
+  hipLaunchKernelGGL(k_norm_weights, dim3((unsigned)(3 * ((b.C + 63) / 64))), dim3(1024), 0, s,
+                     static_cast<const float*>(b.ws), blocks, b.C, b.dw_post, b.dscale, b.dw_pre);
+  return hipGetLastError();
+}
+
+}  // namespace bc

@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/boxconv.h"
+
 namespace bc {
 
 // Row pitch (elements) of a table kept in LDS: W+1 columns plus 3 columns of
@@ -183,6 +185,46 @@ hipError_t launch_scan_bwd_maps(const scan::BwdArgs& p, int in_dt, int out_dt, i
 hipError_t launch_scan_step(const void* gate, const void* x, long rs, int dt, const float* state, float* state_out,
                             const int* slots, void* y, int N, int C, int S, int form, hipStream_t s);
 size_t scan_workspace_bytes(bool bwd, int N, int T, int C, int in_dt, bool maps);
+
+// Linear attention with a decay for each head (bc_linattn.hip).
+struct Attention {
+  const bc_attention* a;
+  const void *q, *k, *v, *gate;
+  bc_strides qs, ks, vs, gs;
+  const float* s0;
+  const int* lengths;
+  void* y;                 // forward and step (there dense)
+  bc_strides ys;
+  float *s_last, *states;
+  const void* gy;          // backward
+  bc_strides gys;
+  const float* gs_last;
+  void *gq, *gk, *gv, *ggate;
+  bc_strides gqs, gks, gvs, ggs;
+  float* gs0;
+  void* ws;
+};
+long linear_attention_blocks(int N, int T, int H);   // the backward's largest grid
+size_t linear_attention_states_bytes(int N, int T, int H, int Dk, int Dv);
+size_t linear_attention_workspace_bytes(bool bwd, const bc_attention& a);
+hipError_t launch_linear_attention_fwd(const Attention& f, hipStream_t s);
+hipError_t launch_linear_attention_bwd(const Attention& f, hipStream_t s);
+hipError_t launch_linear_attention_step(const Attention& f, const float* state, float* state_out, const int* slots, int S,
+                                        hipStream_t s);
+
+// The norms around a block (bc_block_norm.hip).  Rows: stride elements apart.
+struct NormRows { const void* p; long stride; };
+struct BlockNorm {
+  NormRows z, gate, x, r, y, dr, dy, dz, dgate, dx;   // null where there is none
+  const float *w_post, *scale, *w_pre;
+  float *dw_post, *dscale, *dw_pre;
+  int R, C, groups, layer, sigmoid, dt;
+  float eps;
+  void* ws;
+};
+bool block_norm_takes(int C, int groups);
+size_t block_norm_workspace_bytes(int R, int C);
+hipError_t launch_block_norm(const BlockNorm& b, bool bwd, hipStream_t s);
 
 // 1x1 mix of 8-bit codes (bc_mix_i8.hip).
 constexpr int kI8Pad = 128;   // rows of codes are padded with zeros to whole 128 bytes

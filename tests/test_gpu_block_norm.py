@@ -1,0 +1,237 @@
+"""The norms around a block against their 64-bit oracle, forward and backward.
+
+Tolerances are counted: units of 2^-24 of each value's magnitude and half a step
+of the output's type (oracle/attention_oracle.py)."""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention_oracle as A
+from paper_1906_11367_amd import boxconv as bc
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+KIND = {False: bc.BC_NORM_RMS, True: bc.BC_NORM_LAYER}
+ACT = {"silu": bc.BC_ACT_SILU, "sigmoid": bc.BC_ACT_SIGMOID}
+EPS = 2.0 ** -20   # the same in 32 and in 64 bits
+
+
+def say(*a):
+    print(*a, flush=True)
+    sys.stdout.flush()
+
+
+def to64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def rand(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed))
+
+
+def check(name, got, want, mag, units, dt):
+    g = to64(got)
+    bound = units * A.EPS * mag + A.HALF_STEP[dt] * np.abs(want) * (1 + 2.0 ** -7) + 1e-37
+    err = np.abs(g - want)
+    assert np.isfinite(g).all(), name
+    say(f"{name}: {(err / bound).max():.3f} of the bound")
+    assert (err <= bound).all(), (name, (err / bound).max(), np.unravel_index((err / bound).argmax(), err.shape))
+
+
+class Case:
+    def __init__(self, R, C, dt="f32", groups=0, layer=False, gate="", x=False, weights=True, pre=True, r=True, pad=0,
+                 zero_rows=True, seed=1):
+        self.R, self.C, self.dt, self.groups, self.layer, self.act = R, C, dt, groups, layer, gate or "silu"
+        t = DT[dt]
+        z = rand(seed, R, C) * torch.exp(rand(seed + 1, R, 1)) + (1.0 if layer else 0.0)
+        if zero_rows and R > 2:
+            z[R // 2] = 0
+        rows = [z, rand(seed + 2, R, C) * 2 if gate else None, rand(seed + 3, R, C) if x else None,
+                rand(seed + 4, R, C) if r else None, rand(seed + 5, R, C) if pre else None]
+        rows = [None if v is None else v.to(t) for v in rows]
+        w = [1 + 0.3 * rand(seed + 6 + i, C) if on else None for i, on in
+             enumerate((weights and groups > 0, weights, weights and pre))]
+        f = lambda v: None if v is None else to64(v)
+        self.ref = A.block_norm(*(f(v) for v in rows[:3]), *(f(v) for v in w), groups, layer, self.act, EPS, pre,
+                                f(rows[3]), f(rows[4]))
+        self.pad = pad
+        self.z, self.gate, self.x, self.dr, self.dy = (self.place(v) for v in rows)
+        self.w = dict(zip(("w_post", "res_scale", "w_pre"), (None if v is None else v.cuda() for v in w)))
+        new = lambda on: self.place(torch.full((R, C), 7.0, dtype=t)) if on else None
+        self.r, self.y = new(r), new(pre)
+        self.dz, self.dgate, self.dx = new(True), new(bool(gate)), new(x)
+        vec = lambda on: torch.full((C,), 7.0, device="cuda") if on else None
+        self.dw_post, self.dres_scale, self.dw_pre = vec(groups > 0), vec(True), vec(pre)
+
+    def place(self, v):
+        if v is None:
+            return None
+        if not self.pad:
+            return v.cuda()
+        rows = torch.full((v.shape[0], self.C + self.pad), 7.0, dtype=v.dtype, device="cuda")
+        rows[:, :self.C] = v
+        return rows[:, :self.C]
+
+    def how(self):
+        return dict(gate=self.gate, x=self.x, **self.w, groups=self.groups, kind=KIND[self.layer], act=ACT[self.act],
+                    eps=EPS)
+
+    def forward(self):
+        bc.block_norm_fwd(self.z, r=self.r, y=self.y, **self.how())
+
+    def backward(self):
+        bc.block_norm_bwd(self.z, grad_r=self.dr, grad_y=self.dy, grad_z=self.dz, grad_gate=self.dgate, grad_x=self.dx,
+                          grad_w_post=self.dw_post, grad_res_scale=self.dres_scale, grad_w_pre=self.dw_pre, **self.how())
+
+    NAMES = ("r", "y", "dz", "dgate", "dx", "dw_post", "dres_scale", "dw_pre")
+
+    def check(self, names=NAMES):
+        u = A.norm_units(self.C)
+        torch.cuda.synchronize()
+        for name in names:
+            got = getattr(self, name)
+            if got is None:
+                continue
+            weight = name.startswith("dw") or name == "dres_scale"
+            # a weight's gradient: R terms, summed in order at the worst
+            check(name, got, *self.ref[name], u + (self.R + 16 if weight else 0), "f32" if weight else self.dt)
+            if self.pad and not weight:
+                whole = torch.as_strided(got, (self.R, self.C + self.pad), (self.C + self.pad, 1))
+                assert (whole[:, self.C:] == 7).all(), name
+
+
+ALL = dict(gate="silu", x=True)
+CASES = [
+    dict(R=1, C=1), dict(R=1, C=8, dt="bf16"), dict(R=3, C=5, layer=True, x=True), dict(R=2, C=64, dt="bf16", groups=1, **ALL),
+    dict(R=7, C=63, groups=3, layer=True, **ALL), dict(R=9, C=96, dt="bf16", groups=12, **ALL),
+    dict(R=33, C=72, groups=3, gate="sigmoid"), dict(R=5, C=100, groups=100, gate="sigmoid", x=True),
+    dict(R=40, C=128, dt="bf16", groups=1, layer=True, **ALL), dict(R=17, C=300, groups=4, **ALL),
+    dict(R=6, C=512, dt="bf16", groups=8, pre=False, gate="silu"), dict(R=6, C=513, dt="bf16", x=True),
+    dict(R=5, C=837, groups=3, layer=True, gate="sigmoid", x=True), dict(R=11, C=1024, dt="bf16"),
+    dict(R=4, C=2048, dt="bf16", groups=16, gate="silu", pre=False), dict(R=3, C=2049, x=True, layer=True),
+    dict(R=5, C=2500, groups=20, dt="bf16", **ALL), dict(R=3, C=4096, dt="bf16", groups=1, x=True),
+    dict(R=3, C=4100, groups=4, layer=True, **ALL), dict(R=2, C=8192, dt="bf16", groups=64, **ALL),
+    dict(R=2, C=8180, groups=20, **ALL), dict(R=3, C=16384, dt="bf16", groups=1, layer=True, **ALL),
+    dict(R=2, C=16384, groups=128, x=True), dict(R=700, C=48, dt="bf16", groups=2, **ALL),
+    dict(R=3000, C=20, groups=1, layer=True, x=True), dict(R=1100, C=520, dt="bf16", groups=1, **ALL),
+    dict(R=30, C=200, dt="bf16", groups=4, pad=3, **ALL), dict(R=30, C=201, pad=7, layer=True, groups=3, **ALL),
+    dict(R=5, C=640, weights=False, groups=2, **ALL), dict(R=5, C=640, r=False, groups=2, dt="bf16", **ALL),
+]
+
+
+@pytest.mark.parametrize("kw", CASES, ids=lambda kw: "-".join(f"{k}{v}" for k, v in kw.items()))
+def test_against_the_oracle(kw):
+    say(kw)
+    c = Case(**kw)
+    c.forward()
+    c.check(("r", "y"))
+    c.backward()
+    c.check()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_in_place(dt):
+    """r over x, and the gradients over the gradients they come from."""
+    c = Case(50, 264, dt, groups=3, gate="silu", x=True)
+    c.forward()
+    x, keep = c.x.clone(), c.r.clone()
+    bc.block_norm_fwd(c.z, r=c.x, y=c.y, **c.how())
+    assert torch.equal(c.x, keep)
+    c.check(("y",))
+    c.x = x
+    c.backward()
+    want = [t.clone() for t in (c.dz, c.dgate, c.dx)]
+    g = c.how()
+    bc.block_norm_bwd(c.z, grad_r=c.dr, grad_y=c.dy, grad_z=c.dy, grad_gate=g["gate"], grad_x=c.dr, **g)
+    for a, b in zip(want, (c.dy, c.gate, c.dr)):
+        assert torch.equal(a, b)
+
+
+def test_single_gradients():
+    """Each output asked for alone is the one of the whole call, bit for bit."""
+    c = Case(600, 264, "bf16", groups=3, gate="silu", x=True)
+    c.backward()
+    whole = {n: getattr(c, n) for n in Case.NAMES[2:]}
+    for n, want in whole.items():
+        got = torch.full_like(want, 7.0)
+        bc.block_norm_bwd(c.z, grad_r=c.dr, grad_y=c.dy, **{"grad_" + n[1:]: got}, **c.how())
+        assert torch.equal(got, want), n
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [40, 1000])
+def test_non_finite_rows_stay_by_themselves(dt, C):
+    c = Case(9, C, dt, groups=5, layer=True, gate="silu", x=True)
+    c.forward()
+    c.backward()
+    names = ("r", "y", "dz", "dgate", "dx")
+    clean = {n: getattr(c, n).clone() for n in names}
+    c.z[3, 1], c.gate[4, 2], c.x[5, 3] = float("nan"), float("inf"), -float("inf")
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    rows = [0, 1, 2, 6, 7, 8]
+    for n in names:
+        assert torch.equal(getattr(c, n)[rows], clean[n][rows]), n
+    assert torch.isnan(c.y[3]).any() and not torch.isfinite(c.r[5, 3])
+
+
+def test_extremes():
+    """Rows of zeros, of one value, of subnormal and of large values; gates far out."""
+    C = 100
+    z = torch.zeros(6, C)
+    z[1], z[2], z[3], z[4, 7] = 3.0, 1e-41, 1e18, 5.0
+    gate = torch.tensor([0.0, 1e4, -1e4, 100.0, -100.0, float("-inf")]).repeat(C // 4 + 1)[:C].expand(6, C).contiguous()
+    z, gate = z.cuda(), gate.cuda()
+    r, y = torch.empty_like(z), torch.empty_like(z)
+    for layer in (False, True):
+        bc.block_norm_fwd(z, gate=gate, r=r, y=y, groups=1, kind=KIND[layer], act=bc.BC_ACT_SIGMOID, eps=EPS)
+        assert torch.isfinite(r).all() and torch.isfinite(y).all()
+        ref = A.block_norm(to64(z), np.maximum(to64(gate), -700.0), groups=1, layer=layer, act="sigmoid", eps=EPS)
+        check("r", r, *ref["r"], A.norm_units(C), "f32")
+
+
+def test_bits_are_the_same_every_time_and_under_a_graph():
+    c = Case(1300, 2056, "bf16", groups=8, gate="silu", x=True)
+    c.forward()
+    c.backward()
+    first = {n: getattr(c, n).clone() for n in Case.NAMES}
+    ws = torch.empty(bc.block_norm_workspace_bytes(c.R, c.C), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.forward()
+        bc.block_norm_bwd(c.z, grad_r=c.dr, grad_y=c.dy, grad_z=c.dz, grad_gate=c.dgate, grad_x=c.dx,
+                          grad_w_post=c.dw_post, grad_res_scale=c.dres_scale, grad_w_pre=c.dw_pre, ws=ws, **c.how())
+    for _ in range(3):
+        for n in Case.NAMES:
+            getattr(c, n).fill_(7)
+        ws.fill_(0xff)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for n, v in first.items():
+            assert torch.equal(getattr(c, n), v), n
+
+
+def test_offsets_past_32_bits():
+    R, C, far = 3, 64, 2 ** 30
+    buf = torch.zeros(2 * far + C, dtype=torch.bfloat16, device="cuda")
+    z = torch.as_strided(buf, (R, C), (far, 1))
+    z.copy_(rand(1, R, C))
+    y = [torch.empty((R, C), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    bc.block_norm_fwd(z, y=y[0])
+    bc.block_norm_fwd(z.contiguous(), y=y[1])
+    assert torch.equal(*y) and y[0].abs().max() > 0
+
+
+def test_more_dimensions():
+    """[N, T, C] rows of a wider buffer."""
+    rows = rand(1, 4, 9, 64).cuda()
+    z, y = rows[..., :32], torch.empty((4, 9, 32), device="cuda")
+    bc.block_norm_fwd(z, y=y, eps=EPS)
+    want = A.block_norm(to64(z).reshape(36, 32), eps=EPS)["y"]
+    check("y", y.reshape(36, 32), *want, A.norm_units(32), "f32")
