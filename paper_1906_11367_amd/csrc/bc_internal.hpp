@@ -204,7 +204,6 @@ struct Attention {
   float* gs0;
   void* ws;
 };
-long linear_attention_blocks(int N, int T, int H);   // the backward's largest grid
 size_t linear_attention_states_bytes(int N, int T, int H, int Dk, int Dv);
 size_t linear_attention_workspace_bytes(bool bwd, const bc_attention& a);
 hipError_t launch_linear_attention_fwd(const Attention& f, hipStream_t s);

@@ -10,12 +10,13 @@ namespace bc {
 namespace linattn {
 namespace {
 
-// States at the segments' borders from the segments' own: with one entry a
-// border, forward (entry idx(s) holds what segment s leaves by itself) from the
-// first on, backward in time from the last.  entries -> states, in place.
+// States at the segments' borders from what the segments leave by themselves, in
+// place: entry i is border i; forward, entry s + 1 holds segment s's own state, and
+// the states follow from the first border on; backward in time, entry s, from the
+// last.
 struct Joint {
   float* entry;
-  long entry_nh;           // elements between (sequence, head)s
+  long entry_nh;           // (segs + 1) cells
   const float* start;      // [nh][cells], or null: zero
   const float* decay;      // [nh][segs]
   float* last;             // [nh][cells], or null
@@ -23,7 +24,7 @@ struct Joint {
   Str gs;
   int gate_f32, form;
   const int* lengths;
-  int H, segs, step, border, cells, rev;   // forward: entry min((s + 1) step, border) ends segment s
+  int H, segs, cells, rev;
 };
 
 constexpr int kJointAhead = 8;   // segments whose entries are on their way
@@ -34,8 +35,8 @@ __global__ __launch_bounds__(256) void k_join(Joint j) {
   float* p = j.entry + nh * j.entry_nh + cell;
   const float* dec = j.decay + (long)nh * j.segs;
   float s = j.start ? j.start[(long)nh * j.cells + cell] : 0.0f;
-  p[j.rev ? (long)j.border * j.cells : 0] = s;
-  auto at = [&](int i) { return (long)(j.rev ? j.segs - 1 - i : min((i + 1) * j.step, j.border)) * j.cells; };
+  p[j.rev ? (long)j.segs * j.cells : 0] = s;
+  auto at = [&](int i) { return (long)(j.rev ? j.segs - 1 - i : i + 1) * j.cells; };
   for (int i0 = 0; i0 < j.segs; i0 += kJointAhead) {
     float add[kJointAhead], d[kJointAhead];
 #pragma unroll
@@ -61,34 +62,34 @@ __global__ __launch_bounds__(256) void k_join(Joint j) {
   }
 }
 
-// The gates' gradients of one span: the sum of q . dq - k . dk from a token to
-// the span's end, and what crosses that end, <state, gradient> of the border.
+// The gates' gradients of one segment: the sum of q . dq - k . dk from a token to
+// the segment's end, and what crosses that end, <state, gradient> of the border.
 struct GateGrad {
   const float *dq, *dk;          // [nh][T]: q_t . dq_t, k_t . dk_t
-  const float* state;            // the state after the span: entry nh * state_nh + (span + 1) cells
+  const float* state;            // after segment s: at nh * state_nh + (s + 1) cells
   long state_nh;
   const float* grad;             // its gradient, before the next token's decay; null: zero
-  long grad_nh, grad_span;
+  long grad_nh, grad_seg;
   const char* gate;
   Str gs;
   int gate_f32, form;
   char* out;
   Str os;
   const int* lengths;
-  int T, H, span, spans, cells;
+  int T, H, seg, segs, cells;
 };
 
 __global__ __launch_bounds__(256) void k_gate_grad(GateGrad a) {
   __shared__ double part[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int sp = blockIdx.x % a.spans, nh = blockIdx.x / a.spans, n = nh / a.H, h = nh % a.H;
+  const int sp = blockIdx.x % a.segs, nh = blockIdx.x / a.segs, n = nh / a.H, h = nh % a.H;
   const int len = a.lengths ? min(max(a.lengths[n], 0), a.T) : a.T;
-  const int b = sp * a.span, e = min(b + a.span, a.T);
+  const int b = sp * a.seg, e = min(b + a.seg, a.T);
   const long g0 = n * a.gs.n + h * a.gs.h;
   double carry = 0.0;
   if (a.grad && b < len) {
     const float* x = a.state + nh * a.state_nh + (long)(sp + 1) * a.cells;
-    const float* y = a.grad + nh * a.grad_nh + sp * a.grad_span;
+    const float* y = a.grad + nh * a.grad_nh + sp * a.grad_seg;
     double s = 0.0;
     int i = tid * 4;
     for (; i + 3 < a.cells; i += 1024) {
@@ -244,47 +245,50 @@ inline Str str(const bc_strides& s) { return {(long)s.batch, (long)s.row, (long)
 inline size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
 
-// How a call is divided.  Spans: the backward's segments, between kept states;
-// as long as two blocks on each of 256 CUs allow, 128 to 1024 tokens (the gates'
-// gradients sum over a span).  The forward's segments are whole spans.
-struct Plan { int span, spans, seg, segs; };
-Plan plan_of(int N, int T, int H) {
-  const long nh = (long)N * H;
+// How a call is divided: segments of whole chunks, a block each, as long as two
+// blocks on each of 256 CUs allow and 128 tokens at least.  The backward's are the
+// forward's that kept its states, and no longer than 2048 tokens (the gates'
+// gradients are sums over a segment).
+struct Plan { int seg, segs, chunks; };
+Plan plan_of(const bc_attention& a, bool keeps) {
+  const long nh = (long)a.N * a.H;
   Plan p;
-  p.span = (int)std::min(1024L, std::max(128L, nh * T / 512 / 64 * 64));
-  p.spans = (int)ceil_div(T, p.span);
-  const long want = std::min<long>(p.spans, std::max(1L, 512 / nh));
-  const int per = (int)ceil_div(p.spans, want);
-  p.seg = per * p.span;
-  p.segs = (int)ceil_div(p.spans, per);
+  const long want = std::max(128L, (nh * a.T + 511) / 512);
+  p.seg = (int)std::min((want + 63) / 64 * 64, keeps ? 2048L : 1L << 30);
+  p.segs = (int)ceil_div(a.T, p.seg);
+  p.chunks = (int)ceil_div(a.T, chunk_of(a.dt));
   return p;
 }
 
-struct FwdWs { size_t decay, entries, total; };
-FwdWs fwd_ws(const bc_attention& a, const Plan& p) {
-  FwdWs w{};
-  if (p.segs == 1) return w;
+// Workspaces.  Decays of the chunks, then what joins the segments: their own
+// decays, and states at their borders.
+struct Ws { size_t rows[2], end[2], whole[2], decay, entries, dots, part, total; };
+Ws ws_of(const bc_attention& a, const Plan& p, bool bwd) {
   const size_t nh = (size_t)a.N * a.H;
-  w.entries = up(nh * p.segs * 4);
-  w.total = w.entries + up(nh * (p.segs + 1) * a.Dk * a.Dv * 4);
-  return w;
-}
-
-struct BwdWs { size_t decay, entries, dots, part, total; };
-BwdWs bwd_ws(const bc_attention& a, const Plan& p) {
-  BwdWs w{};
-  const size_t nh = (size_t)a.N * a.H;
+  Ws w{};
   size_t at = 0;
-  if (p.spans > 1) {
-    w.entries = up(nh * p.spans * 4);
-    at = w.entries + up(nh * (p.spans + 1) * a.Dk * a.Dv * 4);
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += up(bytes);
+    return here;
+  };
+  for (int r = 0; r < (bwd ? 2 : 1); ++r) {
+    w.rows[r] = take(nh * p.chunks * chunk_of(a.dt) * 16);
+    w.end[r] = take(nh * p.chunks * 8);
+    w.whole[r] = take(nh * p.chunks * 4);
   }
-  w.dots = at;
-  w.part = at + up(nh * a.T * 4) * 2;
-  size_t d = 0;   // gradients by reading head, summed afterwards; one at a time
-  if (a.Hq < a.H || a.Hk < a.H) d = a.Dk;
-  if (a.Hv < a.H) d = std::max(d, (size_t)a.Dv);
-  w.total = w.part + up(nh * a.T * d * 4);
+  if (p.segs > 1) {
+    w.decay = take(nh * p.segs * 4);
+    w.entries = take(nh * (p.segs + 1) * a.Dk * a.Dv * 4);
+  }
+  if (bwd) {
+    w.dots = take(up(nh * a.T * 4) * 2);
+    size_t d = 0;   // gradients by reading head, summed afterwards; one at a time
+    if (a.Hq < a.H || a.Hk < a.H) d = a.Dk;
+    if (a.Hv < a.H) d = std::max(d, (size_t)a.Dv);
+    w.part = take(nh * a.T * d * 4);
+  }
+  w.total = at;
   return w;
 }
 
@@ -299,18 +303,22 @@ Walk walk_of(const Attention& f) {
   w.N = a.N;
   w.T = a.T;
   w.H = a.H;
+  w.chunks = (int)ceil_div(a.T, chunk_of(a.dt));
   w.scale = w.kv = 1.0f;
   return w;
 }
+
+// A single token's rows may have any stride.
+inline Str rows_str(const bc_strides& s, int T, int len) { return {(long)s.batch, T > 1 ? (long)s.row : len, (long)s.head}; }
 
 struct Operand { const void* p; bc_strides s; int div, len; };
 void set(Walk& w, const Operand& q, const Operand& k, const Operand& v) {
   w.q = static_cast<const char*>(q.p);
   w.k = static_cast<const char*>(k.p);
   w.v = static_cast<const char*>(v.p);
-  w.qs = str(q.s);
-  w.ks = str(k.s);
-  w.vs = str(v.s);
+  w.qs = rows_str(q.s, w.T, q.len);
+  w.ks = rows_str(k.s, w.T, k.len);
+  w.vs = rows_str(v.s, w.T, v.len);
   w.qd = q.div;
   w.kd = k.div;
   w.vd = v.div;
@@ -324,62 +332,87 @@ void set(Walk& w, const Operand& q, const Operand& k, const Operand& v) {
 
 using namespace linattn;
 
+
 #define BC_TRY(call)                      \
   do {                                    \
     const hipError_t e_ = (call);         \
     if (e_ != hipSuccess) return e_;      \
   } while (0)
 
-long linear_attention_blocks(int N, int T, int H) { return (long)N * H * plan_of(N, T, H).spans; }
+static Decays decays_at(const Ws& ws, char* wsp, int rev) {
+  return {reinterpret_cast<f32x4_t*>(wsp + ws.rows[rev]), reinterpret_cast<float*>(wsp + ws.whole[rev]),
+          reinterpret_cast<double*>(wsp + ws.end[rev])};
+}
+
+// The decays of every chunk, forward and (bwd) backward in time.
+static hipError_t launch_decays(const Attention& f, const Plan& p, const Ws& ws, bool bwd, hipStream_t s) {
+  const bc_attention& a = *f.a;
+  DecayArgs d{};
+  for (int r = 0; r < (bwd ? 2 : 1); ++r) d.to[r] = decays_at(ws, static_cast<char*>(f.ws), r);
+  d.kv[0] = 1.0f;
+  d.kv[1] = a.scale;
+  d.gate = static_cast<const char*>(f.gate);
+  d.gs = str(f.gs);
+  d.gate_f32 = a.gate_dt == kF32;
+  d.form = a.form;
+  d.lengths = f.lengths;
+  d.T = a.T;
+  d.H = a.H;
+  d.chunks = p.chunks;
+  d.units = (long)a.N * a.H * p.chunks;
+  return a.dt == kBF16 ? launch_decays_bf16(d, s) : launch_decays_f32(d, s);
+}
 
 size_t linear_attention_states_bytes(int N, int T, int H, int Dk, int Dv) {
-  return (size_t)N * H * (plan_of(N, T, H).spans + 1) * Dk * Dv * 4;
+  bc_attention a{};
+  a.N = N;
+  a.T = T;
+  a.H = H;
+  a.dt = kF32;
+  return (size_t)N * H * (plan_of(a, true).segs + 1) * Dk * Dv * 4;
 }
 
 size_t linear_attention_workspace_bytes(bool bwd, const bc_attention& a) {
-  const Plan p = plan_of(a.N, a.T, a.H);
-  return bwd ? bwd_ws(a, p).total : fwd_ws(a, p).total;
+  const size_t keeps = ws_of(a, plan_of(a, true), bwd).total;
+  return bwd ? keeps : std::max(keeps, ws_of(a, plan_of(a, false), false).total);
 }
 
 hipError_t launch_linear_attention_fwd(const Attention& f, hipStream_t s) {
   const bc_attention& a = *f.a;
-  const Plan p = plan_of(a.N, a.T, a.H);
-  const FwdWs ws = fwd_ws(a, p);
-  const long cells = (long)a.Dk * a.Dv;
+  const Plan p = plan_of(a, f.states != nullptr);
+  const Ws ws = ws_of(a, p, false);
+  const long cells = (long)a.Dk * a.Dv, nh = (long)a.N * a.H;
   char* wsp = static_cast<char*>(f.ws);
+  BC_TRY(launch_decays(f, p, ws, false, s));
   Walk w = walk_of(f);
   set(w, {f.q, f.qs, a.H / a.Hq, a.Dk}, {f.k, f.ks, a.H / a.Hk, a.Dk}, {f.v, f.vs, a.H / a.Hv, a.Dv});
+  w.dec = decays_at(ws, wsp, 0);
   w.seg = p.seg;
   w.segs = p.segs;
-  w.sk = a.Dv;
-  w.sv = 1;
-  w.span = p.span;
+  w.rows_first = 1;
+  const long border = (p.segs + 1) * cells;   // states of one sequence and head
   if (p.segs > 1) {
-    const int per = p.seg / p.span;
-    Joint j{};
-    j.entry = f.states ? f.states : reinterpret_cast<float*>(wsp + ws.entries);
-    j.step = f.states ? per : 1;
-    j.border = f.states ? p.spans : p.segs;
-    j.entry_nh = (j.border + 1) * cells;
-    // the segments' own states and decays, in the entries of their ends.  The
-    // last one's entry is the border's.
-    w.last = j.entry + j.step * cells;
-    w.last_nh = j.entry_nh;
-    w.last_seg = j.step * cells;
-    w.last_max = (j.border - j.step) * cells;
+    // the segments' own states, each where the state at its end belongs
+    float* entry = f.states ? f.states : reinterpret_cast<float*>(wsp + ws.entries);
+    w.last = entry + cells;
+    w.last_nh = border;
+    w.last_seg = cells;
     w.decay = reinterpret_cast<float*>(wsp + ws.decay);
     BC_TRY(launch_walk(w, a.dt, s));
+    Joint j{};
+    j.entry = entry;
+    j.entry_nh = border;
     j.start = f.s0;
     j.decay = w.decay;
     j.last = f.s_last;
     j.H = a.H;
     j.segs = p.segs;
     j.cells = (int)cells;
-    hipLaunchKernelGGL(k_join, dim3((unsigned)(ceil_div(cells, 256) * a.N * a.H)), dim3(256), 0, s, j);
+    hipLaunchKernelGGL(k_join, dim3((unsigned)(ceil_div(cells, 256) * nh)), dim3(256), 0, s, j);
     BC_TRY(hipGetLastError());
-    w.init = j.entry;
-    w.init_nh = j.entry_nh;
-    w.init_seg = j.step * cells;
+    w.init = entry;
+    w.init_nh = border;
+    w.init_seg = cells;
     w.last = nullptr;
     w.decay = nullptr;
   } else {
@@ -388,79 +421,77 @@ hipError_t launch_linear_attention_fwd(const Attention& f, hipStream_t s) {
     w.last = f.s_last;
     w.last_nh = cells;
     if (f.states) {
-      w.last2 = f.states + p.spans * cells;
-      w.last2_nh = (p.spans + 1) * cells;
+      w.first = f.states;
+      w.last2 = f.states + cells;
+      w.last2_nh = border;
     }
   }
-  if (f.states) {
-    w.save = f.states;
-    w.save_nh = (p.spans + 1) * cells;
-  }
   w.y = static_cast<char*>(f.y);
-  w.ys = str(f.ys);
+  w.ys = rows_str(f.ys, a.T, a.Dv);
   w.scale = a.scale;
   return launch_walk(w, a.dt, s);
 }
 
 hipError_t launch_linear_attention_bwd(const Attention& f, hipStream_t s) {
   const bc_attention& a = *f.a;
-  const Plan p = plan_of(a.N, a.T, a.H);
-  const BwdWs ws = bwd_ws(a, p);
-  const long cells = (long)a.Dk * a.Dv, nh = (long)a.N * a.H;
+  const Plan p = plan_of(a, true);
+  const Ws ws = ws_of(a, p, true);
+  const long cells = (long)a.Dk * a.Dv, nh = (long)a.N * a.H, border = (p.segs + 1) * cells;
   char* wsp = static_cast<char*>(f.ws);
   const Operand q{f.q, f.qs, a.H / a.Hq, a.Dk}, k{f.k, f.ks, a.H / a.Hk, a.Dk}, v{f.v, f.vs, a.H / a.Hv, a.Dv},
       dy{f.gy, f.gys, 1, a.Dv};
-  float* dots = f.ggate ? reinterpret_cast<float*>(wsp + ws.dots) : nullptr;
-  float* dots_k = f.ggate ? reinterpret_cast<float*>(wsp + ws.dots + up(nh * a.T * 4)) : nullptr;
-  Walk base = walk_of(f);
-  base.seg = p.span;
-  base.segs = p.spans;
-  base.span = p.span;
+  float* dots = reinterpret_cast<float*>(wsp + ws.dots);
+  float* dots_k = reinterpret_cast<float*>(wsp + ws.dots + up(nh * a.T * 4));
+  BC_TRY(launch_decays(f, p, ws, true, s));
+  Walk forward = walk_of(f);
+  forward.seg = p.seg;
+  forward.segs = p.segs;
+  forward.dec = decays_at(ws, wsp, 0);
+  Walk back = forward;
+  back.rev = 1;
+  back.kv = a.scale;
+  back.dec = decays_at(ws, wsp, 1);
 
-  // R at the spans' ends
-  const float* grad = f.gs_last;
-  long grad_nh = cells, grad_span = 0;
-  if (p.spans > 1) {
+  // R at the segments' ends
+  back.init = f.gs_last;
+  back.init_nh = cells;
+  if (p.segs > 1) {
     float* entry = reinterpret_cast<float*>(wsp + ws.entries);
-    Walk w = base;
+    Walk w = back;
     set(w, dy, q, dy);
-    w.rev = 1;
-    w.sk = a.Dv;
-    w.sv = 1;
-    w.kv = a.scale;
+    w.init = nullptr;
+    w.rows_first = 1;
     w.last = entry;
-    w.last_nh = (p.spans + 1) * cells;
+    w.last_nh = border;
     w.last_seg = cells;
-    w.last_max = p.spans * cells;
     w.decay = reinterpret_cast<float*>(wsp + ws.decay);
     BC_TRY(launch_walk(w, a.dt, s));
     Joint j{};
     j.entry = entry;
-    j.entry_nh = (p.spans + 1) * cells;
+    j.entry_nh = border;
     j.start = f.gs_last;
     j.decay = w.decay;
     j.last = f.gs0;
-    j.gate = base.gate;
-    j.gs = base.gs;
-    j.gate_f32 = base.gate_f32;
-    j.form = base.form;
+    j.gate = w.gate;
+    j.gs = w.gs;
+    j.gate_f32 = w.gate_f32;
+    j.form = w.form;
     j.lengths = f.lengths;
     j.H = a.H;
-    j.segs = p.spans;
-    j.border = p.spans;
+    j.segs = p.segs;
     j.cells = (int)cells;
     j.rev = 1;
     hipLaunchKernelGGL(k_join, dim3((unsigned)(ceil_div(cells, 256) * nh)), dim3(256), 0, s, j);
     BC_TRY(hipGetLastError());
-    grad = entry + cells;
-    grad_nh = j.entry_nh;
-    grad_span = cells;
+    back.init = entry + cells;
+    back.init_nh = border;
+    back.init_seg = cells;
   }
 
-  auto out = [&](Walk& w, void* g, const bc_strides& gs, int share, int D) -> hipError_t {
+  auto run = [&](Walk& w, void* g, const bc_strides& gs, int share, int D) -> hipError_t {
     w.y = static_cast<char*>(share > 1 ? static_cast<void*>(wsp + ws.part) : g);
-    w.ys = share > 1 ? Str{(long)a.T * a.H * D, (long)a.H * D, D} : str(gs);
-    w.y_f32 = share > 1 || a.dt == kF32;
+    w.ys = share > 1 ? Str{(long)a.T * a.H * D, (long)a.H * D, D} : rows_str(gs, a.T, D);
+    w.y_f32 = share > 1;
     BC_TRY(launch_walk(w, a.dt, s));
     if (share == 1) return hipSuccess;
     const long count = (long)a.N * a.T * (a.H / share) * D;
@@ -469,80 +500,62 @@ hipError_t launch_linear_attention_bwd(const Attention& f, hipStream_t s) {
                        D, share, count);
     return hipGetLastError();
   };
+  auto with_dots = [&](Walk& w, const Operand& x, float* to) {
+    if (!f.ggate) return;
+    w.x = static_cast<const char*>(x.p);
+    w.xs = rows_str(x.s, a.T, x.len);
+    w.xd = x.div;
+    w.dots = to;
+  };
 
-  Walk w = base;   // dq
+  Walk w = forward;   // dq
   set(w, dy, v, k);
   w.init = f.states;
-  w.init_nh = (p.spans + 1) * cells;
+  w.init_nh = border;
   w.init_seg = cells;
-  w.sk = 1;
-  w.sv = a.Dv;
   w.scale = a.scale;
-  if (dots) {
-    w.x = static_cast<const char*>(q.p);
-    w.xs = str(q.s);
-    w.xd = q.div;
-    w.dots = dots;
-  }
-  BC_TRY(out(w, f.gq, f.gqs, q.div, a.Dk));
+  with_dots(w, q, dots);
+  BC_TRY(run(w, f.gq, f.gqs, q.div, a.Dk));
 
-  w = base;   // dk
+  w = back;           // dk
   set(w, v, dy, q);
-  w.rev = 1;
-  w.kv = a.scale;
-  w.init = grad;
-  w.init_nh = grad_nh;
-  w.init_seg = grad_span;
-  w.sk = 1;
-  w.sv = a.Dv;
-  if (dots) {
-    w.x = static_cast<const char*>(k.p);
-    w.xs = str(k.s);
-    w.xd = k.div;
-    w.dots = dots_k;
-  }
-  BC_TRY(out(w, f.gk, f.gks, k.div, a.Dk));
+  with_dots(w, k, dots_k);
+  BC_TRY(run(w, f.gk, f.gks, k.div, a.Dk));
 
   if (f.ggate) {
     GateGrad d{};
     d.dq = dots;
     d.dk = dots_k;
     d.state = f.states;
-    d.state_nh = (p.spans + 1) * cells;
-    d.grad = grad;
-    d.grad_nh = grad_nh;
-    d.grad_span = grad_span;
-    d.gate = base.gate;
-    d.gs = base.gs;
-    d.gate_f32 = base.gate_f32;
-    d.form = base.form;
+    d.state_nh = border;
+    d.grad = back.init;
+    d.grad_nh = back.init_nh;
+    d.grad_seg = back.init_seg;
+    d.gate = back.gate;
+    d.gs = back.gs;
+    d.gate_f32 = back.gate_f32;
+    d.form = back.form;
     d.out = static_cast<char*>(f.ggate);
     d.os = str(f.ggs);
     d.lengths = f.lengths;
     d.T = a.T;
     d.H = a.H;
-    d.span = p.span;
-    d.spans = p.spans;
+    d.seg = p.seg;
+    d.segs = p.segs;
     d.cells = (int)cells;
-    hipLaunchKernelGGL(k_gate_grad, dim3((unsigned)(nh * p.spans)), dim3(256), 0, s, d);
+    hipLaunchKernelGGL(k_gate_grad, dim3((unsigned)(nh * p.segs)), dim3(256), 0, s, d);
     BC_TRY(hipGetLastError());
   }
 
-  w = base;   // dv, last: grad_s0 may be grad_s_last, which the others read
+  w = back;           // dv, last: grad_s0 may be grad_s_last, which the others read
   set(w, k, q, dy);
-  w.rev = 1;
-  w.kv = a.scale;
-  w.init = grad;
-  w.init_nh = grad_nh;
-  w.init_seg = grad_span;
-  w.sk = a.Dv;
-  w.sv = 1;
-  if (p.spans == 1) {
+  w.rows_first = 1;
+  if (p.segs == 1) {
     w.last = f.gs0;
     w.last_nh = cells;
     w.last_a0 = 1;
   }
-  return out(w, f.gv, f.gvs, v.div, a.Dv);
+  return run(w, f.gv, f.gvs, v.div, a.Dv);
 }
 
 hipError_t launch_linear_attention_step(const Attention& f, const float* state, float* state_out, const int* slots, int S,

@@ -62,6 +62,16 @@ __device__ __forceinline__ float exp2_parts(double x) {
   return fmaf(e, (float)(x - (double)hi) * 0.6931472f, e);
 }
 
+// What the decays of a chunk of CH tokens make, for one direction of time: a row
+// {hi, lo, here, rest} for each token in the order of the walk, with L the running
+// sum of log2 a up to it, hi + lo = L, here = 2^L, rest = 2^(end - L) (times the
+// factor of k v^T); and of the whole chunk 2^end and end.
+struct Decays {
+  f32x4_t* rows;     // [nh][chunks][CH]
+  float* whole;      // [nh][chunks]
+  double* end;       // [nh][chunks]
+};
+
 // The walk of one block over a segment of one sequence and head: operands are
 // named as in the forward.
 struct Walk {
@@ -73,19 +83,19 @@ struct Walk {
   const int* lengths;
   int N, T, H;
   int rev;                   // backward in time, with the decay of the token after
-  int seg, segs;             // tokens of a segment, segments
+  int seg, segs;             // tokens of a segment (whole chunks), segments
+  Decays dec;
+  int chunks;                // of a sequence
   const float* init;         // state before a segment, or null: zero
   long init_nh, init_seg;
-  long sk, sv;               // strides of a state in memory
-  float* save;               // states every `span` tokens (entries nh * save_nh + t / span), or null
-  long save_nh;
-  int span;
+  float* first;              // the initial state once more (one segment), entries last2_nh apart
+  int rows_first;            // states in memory are [K][V]; else [V][K]
   float* last;               // state after a segment, or null
-  long last_nh, last_seg, last_max;   // segment's offset: min(seg * last_seg, last_max)
+  long last_nh, last_seg;
   float* last2;              // the same once more (one segment), entries last2_nh apart
   long last2_nh;
-  int last_a0;               // rev: times the first token's decay
-  float* decay;              // [N * H][segs]: the segments' decays (states only)
+  int last_a0;               // rev: `last` is times the first token's decay
+  float* decay;              // [nh][segs]: the segments' decays, or null
   char* y;                   // null: states only
   Str ys;
   int y_f32;
@@ -97,6 +107,22 @@ struct Walk {
   float* dots;
 };
 
+// A wave a chunk; both directions of time in one launch where both are wanted.
+struct DecayArgs {
+  Decays to[2];            // forward, backward; rows null: not wanted
+  float kv[2];
+  const char* gate;
+  Str gs;
+  int gate_f32, form;
+  const int* lengths;
+  int T, H, chunks;
+  long units;              // nh * chunks
+};
+
+constexpr int chunk_of(int) { return 32; }   // tokens of a chunk
+
+hipError_t launch_decays_bf16(const DecayArgs& a, hipStream_t s);
+hipError_t launch_decays_f32(const DecayArgs& a, hipStream_t s);
 hipError_t launch_walk_bf16(const Walk& w, hipStream_t s);
 hipError_t launch_walk_f32(const Walk& w, hipStream_t s);
 

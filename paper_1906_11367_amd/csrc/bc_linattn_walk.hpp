@@ -1,9 +1,9 @@
 // The walk of linear attention over a segment (bc_linattn.hpp), on MFMA.
 //
-// A block of four waves takes a segment of one sequence and head, chunk by
-// chunk: q, k and v of a chunk go through LDS, each wave owns a quarter of the
-// state's columns (v's), which stay in its registers as fp32 accumulators, and
-// the chunk's scores, one 16 x 16 tile at a time, are shared through LDS.
+// A block takes a segment of one sequence and head, chunk by chunk: q, k and v of
+// a chunk go through LDS, each wave owns 16 of the state's columns (v's), which
+// stay in its registers as fp32 accumulators, and the chunk's scores, one 16 x 16
+// tile at a time, are shared through LDS.
 //
 // The matrix instruction (16 x 16 outputs) wants both operands by rows of the
 // reduction, 4 or 8 consecutive per lane, and leaves 4 consecutive rows of its
@@ -19,6 +19,8 @@
 // decayed v that the state takes in into three (2^-25: the state is fp32).
 // fp32: the fp32 matrix instruction.
 #pragma once
+#include <initializer_list>
+
 #include "bc_linattn.hpp"
 
 namespace bc {
@@ -27,12 +29,12 @@ namespace {
 
 template <int DT> struct Traits;
 template <> struct Traits<kBF16> {
-  static constexpr int kChunk = 64, kGroup = 32;   // tokens of a chunk; reduction of one operand pair
+  static constexpr int kChunk = chunk_of(kBF16), kGroup = 32;   // tokens of a chunk; reduction of one operand pair
   using Frag = bf16x8_t;
   using Elem = uint16_t;
 };
 template <> struct Traits<kF32> {
-  static constexpr int kChunk = 32, kGroup = 16;
+  static constexpr int kChunk = chunk_of(kF32), kGroup = 16;
   using Frag = f32x4_t;
   using Elem = float;
 };
@@ -44,6 +46,13 @@ __device__ __forceinline__ f32x4_t mma(const f32x4_t& a, const f32x4_t& b, f32x4
 #pragma unroll
   for (int r = 0; r < 4; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], b[r], c, 0, 0, 0);
   return c;
+}
+
+// Two values to a bf16 pair, nearest even, in one instruction.
+__device__ __forceinline__ uint32_t round_pair(float lo, float hi) {
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
 }
 
 // fp32 values as a sum of P operands.
@@ -58,12 +67,16 @@ __device__ __forceinline__ Split<kBF16, P> split(const float (&x)[8]) {
   for (int e = 0; e < 8; ++e) rest[e] = x[e];
 #pragma unroll
   for (int p = 0; p < P; ++p) {
+    Raw<4> w;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const __bf16 h = (__bf16)rest[e];
-      s.part[p][e] = h;
-      if (p + 1 < P) rest[e] -= (float)h;
+    for (int i = 0; i < 4; ++i) {   // two values an instruction
+      w[i] = round_pair(rest[2 * i], rest[2 * i + 1]);
+      if (p + 1 < P) {
+        rest[2 * i] -= __uint_as_float(w[i] << 16);
+        rest[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+      }
     }
+    s.part[p] = __builtin_bit_cast(bf16x8_t, w);
   }
   return s;
 }
@@ -74,49 +87,72 @@ __device__ __forceinline__ Split<kF32, P> split(const float (&x)[4]) {
   for (int e = 0; e < 4; ++e) s.part[0][e] = x[e];
   return s;
 }
-template <int DT, int P>
-__device__ __forceinline__ f32x4_t mma(const Split<DT, P>& a, const typename Traits<DT>::Frag& b, f32x4_t c) {
-#pragma unroll
-  for (int p = (DT == kBF16 ? P : 1) - 1; p >= 0; --p) c = mma(a.part[p], b, c);
-  return c;
+// (fp32 needs but one; smaller parts are added first)
+template <int DT, int P> constexpr int kParts = DT == kBF16 ? P : 1;
+
+// Rows [0, rows) of `width` bytes, `step` >= width apart, from p: what a buffer
+// operation reads past them is zero, and what it would write there is dropped.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const char* p, int rows, int step, int width) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0, rows > 0 ? (rows - 1) * step + width : 0, 0x00020000);
 }
-template <int DT, int P>
-__device__ __forceinline__ f32x4_t mma(const typename Traits<DT>::Frag& a, const Split<DT, P>& b, f32x4_t c) {
-#pragma unroll
-  for (int p = (DT == kBF16 ? P : 1) - 1; p >= 0; --p) c = mma(a, b.part[p], c);
-  return c;
+constexpr uint32_t kNoColumn = 0x80000000u;   // past every row: such offsets stay below 2^32
+
+template <int W> __device__ __forceinline__ Raw<W> buffer_load(__amdgpu_buffer_rsrc_t rs, uint32_t at) {
+  if constexpr (W == 2) return __builtin_bit_cast(Raw<2>, __builtin_amdgcn_raw_buffer_load_b64(rs, (int)at, 0, 0));
+  else if constexpr (W == 4) return __builtin_bit_cast(Raw<4>, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)at, 0, 0));
+  else {
+    const Raw<4> a = buffer_load<4>(rs, at), b = buffer_load<4>(rs, at + 16);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+}
+template <int W> __device__ __forceinline__ void buffer_store(__amdgpu_buffer_rsrc_t rs, uint32_t at, const Raw<W>& v) {
+  if constexpr (W == 2) __builtin_amdgcn_raw_buffer_store_b64(v, rs, (int)at, 0, 0);
+  else if constexpr (W == 4) __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)at, 0, 0);
+  else {
+    buffer_store<4>(rs, at, __builtin_shufflevector(v, v, 0, 1, 2, 3));
+    buffer_store<4>(rs, at + 16, __builtin_shufflevector(v, v, 4, 5, 6, 7));
+  }
 }
 
 // A chunk's rows of one operand: from memory to registers, then to LDS.
-template <int DT, int W> struct Tile {
-  static constexpr int kVec = 16 / kBytes<DT>, kPerRow = W / kVec, kRows = 256 / kPerRow;
-  static constexpr int kPasses = Traits<DT>::kChunk / kRows;
+// VEC: whole aligned 16-byte vectors, a chunk's rows within 2^31 bytes.
+template <int DT, int W, int THREADS, bool VEC> struct Tile {
+  static constexpr int kVec = 16 / kBytes<DT>, kPerRow = W / kVec, kRows = THREADS / kPerRow;
+  static constexpr int CH = Traits<DT>::kChunk, kPasses = (CH + kRows - 1) / kRows;
   static constexpr int kPitch = W + 16;   // elements
+  static_assert(kPasses * kRows == CH || kRows > CH, "whole passes, or one of which threads are idle");
   Raw<4> r[kPasses];
 
-  // row i is token t0 + dt * i, which exists within [lo, hi)
-  __device__ __forceinline__ void load(const char* base, long row_stride, int D, int t0, int dt, int lo, int hi) {
-    const int col = (threadIdx.x % kPerRow) * kVec, row = threadIdx.x / kPerRow;
-    if (D % kVec == 0) {
+  static __device__ __forceinline__ int col() { return (threadIdx.x % kPerRow) * kVec; }
+  static __device__ __forceinline__ bool busy() { return kRows <= CH || threadIdx.x < CH * kPerRow; }
+  // row i of the tile is token t0 + i, or t0 + CH - 1 - i (rev)
+  static __device__ __forceinline__ int row(int pass, bool rev) {
+    const int k = threadIdx.x / kPerRow + pass * kRows;
+    return rev ? CH - 1 - k : k;
+  }
+
+  // tokens from hi (> t0) on do not exist: zeros
+  __device__ __forceinline__ void load(const char* base, long row_stride, int D, int t0, bool rev, int hi) {
+    if constexpr (VEC) {
+      const int step = (int)row_stride * kBytes<DT>;
+      const auto rs = rows_of(base + t0 * row_stride * kBytes<DT>, min(hi - t0, CH), step, D * kBytes<DT>);
+      const uint32_t at = col() < D && busy() ? (uint32_t)(row(0, rev) * step + col() * kBytes<DT>) : kNoColumn;
+      const int skip = rev ? -kRows * step : kRows * step;
 #pragma unroll
-      for (int i = 0; i < kPasses; ++i) {
-        const int t = t0 + dt * (row + i * kRows);
-        r[i] = Raw<4>{0, 0, 0, 0};
-        if (t >= lo && t < hi && col < D) r[i] = scan::load_wide<DT, kVec>(base + ((long)t * row_stride + col) * kBytes<DT>);
-      }
+      for (int i = 0; i < kPasses; ++i) r[i] = buffer_load<4>(rs, at + (uint32_t)(i * skip));
     } else {
 #pragma unroll
       for (int i = 0; i < kPasses; ++i) {
-        const int t = t0 + dt * (row + i * kRows);
-        const int avail = t >= lo && t < hi ? D - col : 0;
-        r[i] = scan::load_vec<DT, kVec>(base + ((long)t * row_stride + col) * kBytes<DT>, avail);
+        const int t = t0 + row(i, rev);
+        r[i] = scan::load_vec<DT, kVec>(base + ((long)t * row_stride + col()) * kBytes<DT>, t < hi && busy() ? D - col() : 0);
       }
     }
   }
   __device__ __forceinline__ void store(typename Traits<DT>::Elem* lds) const {
-    const int col = (threadIdx.x % kPerRow) * kVec, row = threadIdx.x / kPerRow;
+    if (!busy()) return;
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) *reinterpret_cast<Raw<4>*>(lds + (row + i * kRows) * kPitch + col) = r[i];
+    for (int i = 0; i < kPasses; ++i)
+      *reinterpret_cast<Raw<4>*>(lds + (threadIdx.x / kPerRow + i * kRows) * kPitch + col()) = r[i];
   }
 };
 
@@ -148,56 +184,32 @@ __device__ __forceinline__ f32x4_t col_frag(const float* p, int lane, int step) 
 template <int DT>
 __device__ __forceinline__ constexpr int col_token(int g, int e) { return (e >> 2) * 16 + 4 * g + (e & 3); }
 
-// What a chunk's decays make, in LDS.
-template <int CH> struct Decays {
-  float hi[CH], lo[CH];   // L, log2
-  float here[CH];         // exp(L_i)
-  float rest[CH];         // exp(L_end - L_i), with the factor of k v^T
-  float whole;            // exp(L_end)
-};
-
-// By one wave: the decay of row `lane`'s token (0 for rows past the chunk).
-template <int CH>
-__device__ __forceinline__ void make_decays(Decays<CH>* d, double l2, float kv, int lane, double& total) {
-#pragma unroll
-  for (int s = 1; s < CH; s *= 2) {
-    const double o = __shfl_up(l2, s);
-    if (lane >= s) l2 += o;
-  }
-  const double end = __shfl(l2, CH - 1);
-  total += end;
-  if (lane < CH) {
-    const float hi = (float)l2;
-    d->hi[lane] = hi;
-    d->lo[lane] = (float)(l2 - (double)hi);
-    d->here[lane] = exp2_parts(l2);
-    d->rest[lane] = kv * exp2_parts(end - l2);
-    if (lane == 0) d->whole = exp2_parts(end);
-  }
-}
-
-template <int DT, int KP, int VP>
+template <int DT, int KP, int VP, int NT>
 struct Smem {
-  static constexpr int CH = Traits<DT>::kChunk, IT = CH / 16, kTiles = IT * (IT + 1) / 2;
+  static constexpr int CH = Traits<DT>::kChunk, IT = CH / 16, kTiles = IT * (IT + 1) / 2, kWaves = VP / 16 / NT;
   using E = typename Traits<DT>::Elem;
-  alignas(16) E q[CH * Tile<DT, KP>::kPitch];
-  alignas(16) E k[CH * Tile<DT, KP>::kPitch];
-  alignas(16) E v[CH * Tile<DT, VP>::kPitch];
+  alignas(16) E q[CH * (KP + 16)];
+  alignas(16) E k[CH * (KP + 16)];
+  alignas(16) E v[CH * (VP + 16)];
   alignas(16) char p[kTiles * 1024];   // score tiles: fp32, or two bf16 parts
-  alignas(16) Decays<CH> dec[2];
-  alignas(16) float dots[4][CH];
+  alignas(16) float dec[2][4][CH];     // hi, lo, here, rest of Decays
+  alignas(16) float dots[kWaves][CH];
 };
 
-template <int DT, int KP, int VP, bool OUT>
-__global__ __launch_bounds__(256, 2) void k_walk(Walk w) {
+// MODE: the states alone, with outputs, or with outputs and their products with x.
+constexpr int kStates = 0, kOut = 1, kOutDots = 2;
+
+template <int DT, int KP, int VP, int NT, int MODE, bool VEC>
+__global__ __launch_bounds__(VP / NT * 4, KP == 64 && VP == 64 ? 3 : 2) void k_walk(Walk w) {
+  constexpr bool OUT = MODE != kStates, DOTS = MODE == kOutDots;
   using Tr = Traits<DT>;
   using Frag = typename Tr::Frag;
-  using E = typename Tr::Elem;
+  using SM = Smem<DT, KP, VP, NT>;
   constexpr int CH = Tr::kChunk, KG = Tr::kGroup, IT = CH / 16, PG = CH / KG, TPG = KG / 16;
-  constexpr int NT = VP / 64, KT = KP / 16, FE = KG / 4;
-  constexpr int KPITCH = Tile<DT, KP>::kPitch, VPITCH = Tile<DT, VP>::kPitch;
+  constexpr int KT = KP / 16, FE = KG / 4, THREADS = VP / NT * 4, WAVES = VP / 16 / NT;
+  constexpr int KPITCH = KP + 16, VPITCH = VP + 16;
   extern __shared__ char smem_raw[];
-  auto& sm = *reinterpret_cast<Smem<DT, KP, VP>*>(smem_raw);
+  SM& sm = *reinterpret_cast<SM*>(smem_raw);
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, m = lane & 15;
@@ -205,87 +217,109 @@ __global__ __launch_bounds__(256, 2) void k_walk(Walk w) {
   const int len = w.lengths ? min(max(w.lengths[n], 0), w.T) : w.T;
   const int b = seg * w.seg, e = min(b + w.seg, w.T);
   const int chunks = (e - b + CH - 1) / CH;
-  const int dt = w.rev ? -1 : 1, hi = min(e, len);
+  const bool rev = w.rev;
+  const int hi = min(e, len);
 
   const char* qp = w.q + (n * w.qs.n + (h / w.qd) * w.qs.h) * kBytes<DT>;
   const char* kp = w.k + (n * w.ks.n + (h / w.kd) * w.ks.h) * kBytes<DT>;
   const char* vp = w.v + (n * w.vs.n + (h / w.vd) * w.vs.h) * kBytes<DT>;
-  const long g0 = n * w.gs.n + h * w.gs.h;
 
-  Tile<DT, KP> tq, tk;
-  Tile<DT, VP> tv;
-  double l2 = 0.0, total = 0.0;
-  auto first = [&](int c) { return w.rev ? e - 1 - c * CH : b + c * CH; };
+  Tile<DT, KP, THREADS, VEC> tq, tk;
+  Tile<DT, VP, THREADS, VEC> tv;
+  // the first token of chunk c in memory (its last in time, rev)
+  auto first = [&](int c) { return b + (rev ? chunks - 1 - c : c) * CH; };
+  // a chunk of which nothing exists: its outputs are zero, the state stays
+  auto dead = [&](int t0) { return t0 >= len; };
+  f32x4_t td;
+  const long d0 = (long)nh * w.chunks;
   auto load = [&](int c) {
     const int t0 = first(c);
-    if constexpr (OUT) tq.load(qp, w.qs.t, w.K, t0, dt, b, hi);
-    tk.load(kp, w.ks.t, w.K, t0, dt, b, hi);
-    tv.load(vp, w.vs.t, w.V, t0, dt, b, hi);
-    if (wave == 0) {
-      const int t = t0 + dt * lane, gt = w.rev ? t + 1 : t;
-      l2 = 0.0;
-      if (lane < CH && t >= b && t < e && gt < len) l2 = log2_decay(load_elem(w.gate, g0 + gt * w.gs.t, w.gate_f32), w.form);
-    }
+    if (c >= chunks || dead(t0)) return;
+    if constexpr (OUT) tq.load(qp, w.qs.t, w.K, t0, rev, hi);
+    tk.load(kp, w.ks.t, w.K, t0, rev, hi);
+    tv.load(vp, w.vs.t, w.V, t0, rev, hi);
+    if (wave == WAVES - 1 && lane < CH) td = w.dec.rows[(d0 + t0 / CH) * CH + lane];
   };
 
-  // the wave's columns: lane m of tile nt has column c0 + vcol(nt, m), so that a
-  // lane's outputs of both tiles are consecutive
+  // the wave's 16 columns of the state, c0 + m; its rows that lane group g holds
+  // of tile kt: krow(kt, g) + 0..3, so that an operand's are consecutive
   const int c0 = wave * 16 * NT;
   auto vcol = [&](int nt, int mm) { return NT == 2 ? 8 * (mm >> 2) + 4 * nt + (mm & 3) : mm; };
-  constexpr int VSTEP = NT == 2 ? 8 : 4;
-  // rows of S that lane group g holds of tile kt: krow(kt) + 0..3
+  constexpr int VSTEP = 4 * NT;
   auto krow = [&](int kt, int gg) { return DT == kBF16 ? 32 * (kt >> 1) + 8 * gg + 4 * (kt & 1) : 16 * kt + 4 * gg; };
   constexpr int KSTEP = DT == kBF16 ? 8 : 4;
   auto kcol = [&](int kt) { return DT == kBF16 ? 32 * (kt >> 1) + 4 * (kt & 1) : 16 * kt; };
 
+  load(0);
+  // A state in memory: element (kk, vv) at kk sk + vv sv.  What the tile has past K
+  // rows or V columns reads as zero and is not written.
+  const int sk = w.rows_first ? w.V : 1, sv = w.rows_first ? 1 : w.K, cells = w.K * w.V * 4;
+  auto cell = [&](int kk, int vv) { return kk < w.K && vv < w.V ? (uint32_t)(kk * sk + vv * sv) * 4u : kNoColumn; };
   f32x4_t S[KT][NT];
-  {
-    const float* p = w.init ? w.init + nh * w.init_nh + seg * w.init_seg : nullptr;
+  if (w.init) {
+    const auto rs = rows_of(reinterpret_cast<const char*>(w.init + nh * w.init_nh + seg * w.init_seg), 1, 0, cells);
+    if (VEC && sk == 1) {   // four rows are one vector
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          S[kt][nt] = __builtin_bit_cast(f32x4_t, buffer_load<4>(rs, cell(krow(kt, g), c0 + vcol(nt, m))));
+    } else {
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            S[kt][nt][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, (int)cell(krow(kt, g) + r, c0 + vcol(nt, m)), 0, 0));
+    }
+  } else {
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int kk = krow(kt, g) + r, vv = c0 + vcol(nt, m);
-          S[kt][nt][r] = p && kk < w.K && vv < w.V ? p[kk * w.sk + vv * w.sv] : 0.0f;
-        }
+      for (int nt = 0; nt < NT; ++nt) S[kt][nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
   auto put_state = [&](float* p, float f) {
+    const auto rs = rows_of(reinterpret_cast<const char*>(p), 1, 0, cells);
+    // (offsets made here, not kept from above through the loop: 64 registers)
+    int gg = g, mm = m;
+    asm volatile("" : "+v"(gg), "+v"(mm));
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int kk = krow(kt, g) + r, vv = c0 + vcol(nt, m);
-          if (kk < w.K && vv < w.V) p[kk * w.sk + vv * w.sv] = S[kt][nt][r] * f;
-        }
+        for (int r = 0; r < 4; ++r)
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[kt][nt][r] * f), rs,
+                                                (int)cell(krow(kt, gg) + r, c0 + vcol(nt, mm)), 0, 0);
   };
 
-  load(0);
-  if (wave == 0) make_decays<CH>(&sm.dec[0], l2, w.kv, lane, total);
+  if (w.first) put_state(w.first + nh * w.last2_nh, 1.0f);
+
+  const float reach = w.kv * w.scale;   // of the scores
+  const int out_bytes = DT == kF32 || w.y_f32 ? 4 : 2;
   for (int c = 0; c < chunks; ++c) {
     const int t0 = first(c);
-    // nothing of the chunk exists: its outputs are zero, the state stays
-    const bool dead = (w.rev ? t0 - CH + 1 : t0) >= len;
-    const Decays<CH>& d = sm.dec[c & 1];
-    if (!dead) {
+    const bool live = !dead(t0);
+    const float(&d)[4][CH] = sm.dec[c & 1];
+    if (live) {
       if constexpr (OUT) tq.store(sm.q);
       tk.store(sm.k);
       tv.store(sm.v);
+      if (wave == WAVES - 1 && lane < CH)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sm.dec[c & 1][u][lane] = td[u];
     }
+    const float whole = w.dec.whole[d0 + t0 / CH];
     __syncthreads();
-    if (c + 1 < chunks) load(c + 1);
-    if constexpr (OUT) {
-      if (w.save && (t0 - b) % w.span == 0 && t0 % w.span == 0) put_state(w.save + nh * w.save_nh + (t0 / w.span) * (long)w.K * w.V, 1.0f);
-    }
+    load(c + 1);
+    __builtin_amdgcn_sched_barrier(0);
     f32x4_t acc[IT][NT];
     Frag vf[PG][NT];
-    if (!dead) {
+    if (live) {
       if constexpr (OUT) {
         // scores of the causal tiles, transposed: rows j, columns i
-        for (int i = wave; i < IT * (IT + 1) / 2; i += 4) {
+        for (int i = wave; i < SM::kTiles; i += WAVES) {
           const int it = (i >= 1) + (i >= 3) + (i >= 6), jt = i - it * (it + 1) / 2;
           f32x4_t s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -293,20 +327,20 @@ __global__ __launch_bounds__(256, 2) void k_walk(Walk w) {
             s = mma(row_frag<DT>(sm.k + (jt * 16 + m) * KPITCH + kg * KG + g * FE),
                     row_frag<DT>(sm.q + (it * 16 + m) * KPITCH + kg * KG + g * FE), s);
           const int ii = it * 16 + m, jj = jt * 16 + 4 * g;
-          const float ih = d.hi[ii], il = d.lo[ii];
-          const f32x4_t jh = *reinterpret_cast<const f32x4_t*>(&d.hi[jj]), jl = *reinterpret_cast<const f32x4_t*>(&d.lo[jj]);
+          const float ih = d[0][ii], il = d[1][ii];
+          const f32x4_t jh = *reinterpret_cast<const f32x4_t*>(&d[0][jj]), jl = *reinterpret_cast<const f32x4_t*>(&d[1][jj]);
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            s[r] = jj + r <= ii ? s[r] * (w.kv * __builtin_amdgcn_exp2f((ih - jh[r]) + (il - jl[r]))) : 0.0f;
+            s[r] = jj + r <= ii ? s[r] * (reach * __builtin_amdgcn_exp2f((ih - jh[r]) + (il - jl[r]))) : 0.0f;
           if constexpr (DT == kBF16) {
-            bf16x4_t h4, l4;
+            Raw<2> h2, l2;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              h4[r] = (__bf16)s[r];
-              l4[r] = (__bf16)(s[r] - (float)h4[r]);
+            for (int r = 0; r < 2; ++r) {
+              h2[r] = round_pair(s[2 * r], s[2 * r + 1]);
+              l2[r] = round_pair(s[2 * r] - __uint_as_float(h2[r] << 16), s[2 * r + 1] - __uint_as_float(h2[r] & 0xffff0000u));
             }
-            reinterpret_cast<bf16x4_t*>(sm.p)[i * 128 + lane] = h4;
-            reinterpret_cast<bf16x4_t*>(sm.p)[i * 128 + 64 + lane] = l4;
+            reinterpret_cast<Raw<2>*>(sm.p)[i * 128 + lane] = h2;
+            reinterpret_cast<Raw<2>*>(sm.p)[i * 128 + 64 + lane] = l2;
           } else {
             reinterpret_cast<f32x4_t*>(sm.p)[i * 64 + lane] = s;
           }
@@ -323,19 +357,22 @@ __global__ __launch_bounds__(256, 2) void k_walk(Walk w) {
           for (int nt = 0; nt < NT; ++nt) {
             float x[FE];
 #pragma unroll
-            for (int q = 0; q < FE; ++q) x[q] = S[kg * TPG + q / 4][nt][q & 3];
+            for (int u = 0; u < FE; ++u) x[u] = S[kg * TPG + u / 4][nt][u & 3];
             sp[nt] = split<2>(x);
           }
+          Frag f[IT];
 #pragma unroll
-          for (int it = 0; it < IT; ++it) {
-            const Frag f = row_frag<DT>(sm.q + (it * 16 + m) * KPITCH + kg * KG + g * FE);
+          for (int it = 0; it < IT; ++it) f[it] = row_frag<DT>(sm.q + (it * 16 + m) * KPITCH + kg * KG + g * FE);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) acc[it][nt] = mma<DT, 2>(sp[nt], f, acc[it][nt]);
-          }
+          for (int part = kParts<DT, 2> - 1; part >= 0; --part)
+#pragma unroll
+            for (int it = 0; it < IT; ++it)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) acc[it][nt] = mma(sp[nt].part[part], f[it], acc[it][nt]);
         }
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
-          const float f = d.here[it * 16 + m];
+          const float f = w.scale * d[2][it * 16 + m];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) acc[it][nt] *= f;
         }
@@ -343,18 +380,16 @@ __global__ __launch_bounds__(256, 2) void k_walk(Walk w) {
 #pragma unroll
       for (int p = 0; p < PG; ++p)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          vf[p][nt] = col_frag<VPITCH>(sm.v + p * KG * VPITCH + c0 + (NT == 2 ? 4 * nt : 0), lane, VSTEP);
+        for (int nt = 0; nt < NT; ++nt) vf[p][nt] = col_frag<VPITCH>(sm.v + p * KG * VPITCH + c0 + 4 * nt * (NT - 1), lane, VSTEP);
     }
     if constexpr (OUT) {
       __syncthreads();
-      if (!dead) {
+      if (live) {
 #pragma unroll
-        for (int it = 0; it < IT; ++it)
+        for (int p = 0; p < PG; ++p) {
+          Split<DT, 2> pf[IT];
 #pragma unroll
-          for (int p = 0; p < PG; ++p) {
-            if (p * TPG > it) continue;
-            Split<DT, 2> pf;
+          for (int it = p * TPG; it < IT; ++it) {
             if constexpr (DT == kBF16) {
               const bf16x4_t z = {};
 #pragma unroll
@@ -362,45 +397,67 @@ __global__ __launch_bounds__(256, 2) void k_walk(Walk w) {
                 const int i = it * (it + 1) / 2 + 2 * p;
                 const bf16x4_t a = reinterpret_cast<const bf16x4_t*>(sm.p)[i * 128 + u * 64 + lane];
                 const bf16x4_t bb = 2 * p + 1 <= it ? reinterpret_cast<const bf16x4_t*>(sm.p)[(i + 1) * 128 + u * 64 + lane] : z;
-                pf.part[u] = __builtin_shufflevector(a, bb, 0, 1, 2, 3, 4, 5, 6, 7);
+                pf[it].part[u] = __builtin_shufflevector(a, bb, 0, 1, 2, 3, 4, 5, 6, 7);
               }
             } else {
-              pf.part[0] = reinterpret_cast<const f32x4_t*>(sm.p)[(it * (it + 1) / 2 + p) * 64 + lane];
+              pf[it].part[0] = reinterpret_cast<const f32x4_t*>(sm.p)[(it * (it + 1) / 2 + p) * 64 + lane];
             }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) acc[it][nt] = mma<DT, 2>(vf[p][nt], pf, acc[it][nt]);
           }
+#pragma unroll
+          for (int part = kParts<DT, 2> - 1; part >= 0; --part)
+#pragma unroll
+            for (int it = p * TPG; it < IT; ++it)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) acc[it][nt] = mma(vf[p][nt], pf[it].part[part], acc[it][nt]);
+        }
       }
-      // outputs: a lane has 4 NT consecutive columns of row it * 16 + m
+      // outputs: a lane has 4 NT consecutive columns of row it * 16 + m.  VEC: whole
+      // vectors exist or nothing, and a chunk's rows are within 2^31 bytes.
       constexpr int V = 4 * NT;
-      const int col = c0 + (NT == 2 ? 8 * g : 4 * g), avail = w.V - col;
+      const int col = c0 + V * g, avail = w.V - col;
+      char* yp = w.y + (n * w.ys.n + t0 * w.ys.t + h * w.ys.h) * out_bytes;
+      const char* xp = w.x + (n * w.xs.n + t0 * w.xs.t + (h / w.xd) * w.xs.h) * kBytes<DT>;
+      const int ystep = (int)w.ys.t * out_bytes, xstep = (int)w.xs.t * kBytes<DT>;
+      const auto yr = rows_of(yp, VEC ? min(e - t0, CH) : 0, ystep, w.V * out_bytes);
+      const auto xr = rows_of(xp, VEC && DOTS ? min(hi - t0, CH) : 0, xstep, w.V * kBytes<DT>);
+      if (t0 + CH > hi) {   // rows that do not exist
+#pragma unroll
+        for (int it = 0; it < IT; ++it)
+          if (t0 + (rev ? CH - 1 - it * 16 - m : it * 16 + m) >= hi)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) acc[it][nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      }
 #pragma unroll
       for (int it = 0; it < IT; ++it) {
-        const int t = t0 + dt * (it * 16 + m);
-        const bool exists = t >= b && t < e, live = exists && t < len;
-        float o[V], dot = 0.0f;
+        const int row = rev ? CH - 1 - it * 16 - m : it * 16 + m;
+        float o[V];
 #pragma unroll
-        for (int q = 0; q < V; ++q) o[q] = live ? acc[it][q / 4][q & 3] * w.scale : 0.0f;
-        if (w.x && live) {
-          const Raw<scan::kWords<DT, V>> xr =
-              scan::load_vec<DT, V>(w.x + (n * w.xs.n + t * w.xs.t + (h / w.xd) * w.xs.h + col) * kBytes<DT>, avail);
+        for (int u = 0; u < V; ++u) o[u] = acc[it][u / 4][u & 3];
+        if constexpr (VEC) {
+          if (out_bytes == 4)
+            buffer_store<V>(yr, avail > 0 ? (uint32_t)(row * ystep + col * 4) : kNoColumn, scan::rounded<kF32, V>(o));
+          else
+            buffer_store<V / 2>(yr, avail > 0 ? (uint32_t)(row * ystep + col * 2) : kNoColumn, scan::rounded<kBF16, V>(o));
+        } else if (t0 + row < e && avail > 0) {
+          const long at = (row * w.ys.t + col) * out_bytes;
+          if (out_bytes == 4) scan::store_vec<kF32, V>(yp + at, avail, o);
+          else scan::store_vec<kBF16, V>(yp + at, avail, o);
+        }
+        if constexpr (DOTS) {
+          Raw<scan::kWords<DT, V>> x;
+          if constexpr (VEC) x = buffer_load<scan::kWords<DT, V>>(xr, avail > 0 ? (uint32_t)(row * xstep + col * kBytes<DT>) : kNoColumn);
+          else x = scan::load_vec<DT, V>(xp + (row * w.xs.t + col) * kBytes<DT>, t0 + row < hi ? avail : 0);
+          float dot = 0.0f;
 #pragma unroll
-          for (int q = 0; q < V; ++q) dot = fmaf(o[q], scan::elem<DT, V>(xr, q), dot);
-        }
-        if (exists && avail > 0) {
-          const long at = n * w.ys.n + t * w.ys.t + h * w.ys.h + col;
-          if (DT == kF32 || w.y_f32) scan::store_vec<kF32, V>(w.y + at * 4, avail, o);
-          else scan::store_vec<kBF16, V>(w.y + at * 2, avail, o);
-        }
-        if (w.x) {
+          for (int u = 0; u < V; ++u) dot = fmaf(o[u], scan::elem<DT, V>(x, u), dot);
           dot += __shfl_xor(dot, 16);
           dot += __shfl_xor(dot, 32);
           if (g == 0) sm.dots[wave][it * 16 + m] = dot;
         }
       }
     }
-    if (!dead) {
-      const float whole = d.whole;
+    __builtin_amdgcn_sched_barrier(0);
+    if (live) {
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -412,42 +469,111 @@ __global__ __launch_bounds__(256, 2) void k_walk(Walk w) {
         for (int nt = 0; nt < NT; ++nt) {
           float x[FE];
 #pragma unroll
-          for (int q = 0; q < FE; ++q) x[q] = (float)vf[p][nt][q] * d.rest[p * KG + col_token<DT>(g, q)];
+          for (int u = 0; u < FE; ++u) x[u] = (float)vf[p][nt][u] * d[3][p * KG + col_token<DT>(g, u)];
           sp[nt] = split<3>(x);
         }
+        // four tiles of rows at a time, part by part: products that follow one another
+        // add to different accumulators
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-          const Frag f = col_frag<KPITCH>(sm.k + p * KG * KPITCH + kcol(kt), lane, KSTEP);
+        for (int kt0 = 0; kt0 < KT; kt0 += 4) {
+          Frag f[4];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) S[kt][nt] = mma<DT, 3>(f, sp[nt], S[kt][nt]);
+          for (int i = 0; i < 4; ++i) f[i] = col_frag<KPITCH>(sm.k + p * KG * KPITCH + kcol(kt0 + i), lane, KSTEP);
+#pragma unroll
+          for (int part = kParts<DT, 3> - 1; part >= 0; --part)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) S[kt0 + i][nt] = mma(f[i], sp[nt].part[part], S[kt0 + i][nt]);
         }
       }
     }
-    if (c + 1 < chunks && wave == 0) make_decays<CH>(&sm.dec[(c + 1) & 1], l2, w.kv, lane, total);
     __syncthreads();
-    if constexpr (OUT) {
-      if (w.x && tid < CH) {
-        const int t = t0 + dt * tid;
-        if (t >= b && t < e) w.dots[(long)nh * w.T + t] = (sm.dots[0][tid] + sm.dots[1][tid]) + (sm.dots[2][tid] + sm.dots[3][tid]);
+    if constexpr (DOTS) {
+      if (tid < CH) {
+        const int t = t0 + (rev ? CH - 1 - tid : tid);
+        float s = 0.0f;
+#pragma unroll
+        for (int u = 0; u < WAVES; ++u) s += sm.dots[u][tid];
+        if (t >= b && t < e) w.dots[(long)nh * w.T + t] = s;
       }
     }
   }
-  if (w.last) {
-    float f = 1.0f;
-    if (w.last_a0 && len > 0) f = exp2_parts(log2_decay(load_elem(w.gate, g0, w.gate_f32), w.form));
-    put_state(w.last + nh * w.last_nh + min(seg * w.last_seg, w.last_max), f);
+  float f = 1.0f;
+  if (w.last_a0 && len > 0)
+    f = exp2_parts(log2_decay(load_elem(w.gate, n * w.gs.n + h * w.gs.h, w.gate_f32), w.form));
+  float* to = w.last ? w.last + nh * w.last_nh + seg * w.last_seg : nullptr;
+  float* more = w.last2 ? w.last2 + nh * w.last2_nh : nullptr;
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i) {
+    if (to) put_state(to, f);
+    to = more;
   }
-  if (w.last2) put_state(w.last2 + nh * w.last2_nh, 1.0f);
-  if (w.decay && tid == 0) w.decay[(long)nh * w.segs + seg] = exp2_parts(total);
+  if (w.decay && tid == 0) {
+    double sum = 0.0;
+    for (int c = 0; c < chunks; ++c) sum += w.dec.end[d0 + first(c) / CH];
+    w.decay[(long)nh * w.segs + seg] = exp2_parts(sum);
+  }
 }
 
+#ifndef NTX
+#define NTX 2
+#endif
 template <int DT, int KP, int VP>
 hipError_t launch_walk_sized(const Walk& w, hipStream_t s) {
-  auto go = [&](auto kernel, size_t lds) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((long)w.N * w.H * w.segs)), dim3(256), (unsigned)lds, s, w);
+  constexpr int NT = VP == 128 ? NTX : 1;
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((long)w.N * w.H * w.segs)), dim3(VP / NT * 4), sizeof(Smem<DT, KP, VP, NT>), s, w);
     return hipGetLastError();
   };
-  return w.y ? go(k_walk<DT, KP, VP, true>, sizeof(Smem<DT, KP, VP>)) : go(k_walk<DT, KP, VP, false>, sizeof(Smem<DT, KP, VP>));
+  // whole vectors, rows that do not overlap (a row past the last that exists is
+  // then past its end too), 64 of them within 2^31 bytes
+  constexpr int kVec = 16 / kBytes<DT>;
+  auto fits = [](const Str& t, int len) {
+    return len % kVec == 0 && (t.n | t.t | t.h) % kVec == 0 && t.t >= len && t.t < (1L << 31) / 4 / 64;
+  };
+  const bool vec = fits(w.qs, w.K) && fits(w.ks, w.K) && fits(w.vs, w.V) && (!w.y || fits(w.ys, w.V)) && (!w.x || fits(w.xs, w.V));
+  if (!w.y) return vec ? go(k_walk<DT, KP, VP, NT, kStates, true>) : go(k_walk<DT, KP, VP, NT, kStates, false>);
+  if (!w.x) return vec ? go(k_walk<DT, KP, VP, NT, kOut, true>) : go(k_walk<DT, KP, VP, NT, kOut, false>);
+  return vec ? go(k_walk<DT, KP, VP, NT, kOutDots, true>) : go(k_walk<DT, KP, VP, NT, kOutDots, false>);
+}
+
+template <int CH>
+__global__ __launch_bounds__(256) void k_decays(DecayArgs a) {
+  const long unit = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (unit >= a.units) return;
+  const int nh = (int)(unit / a.chunks), c = (int)(unit % a.chunks), n = nh / a.H, h = nh % a.H;
+  const int len = a.lengths ? min(max(a.lengths[n], 0), a.T) : a.T;
+#pragma unroll
+  for (int rev = 0; rev < 2; ++rev) {
+    const Decays& to = a.to[rev];
+    if (!to.rows) continue;
+    // backward in time a token's own decay lies behind it: the next one's is between
+    const int t = c * CH + (rev ? CH - lane : lane);
+    double l2 = 0.0;
+    if (lane < CH && t < len) l2 = log2_decay(load_elem(a.gate, n * a.gs.n + t * a.gs.t + h * a.gs.h, a.gate_f32), a.form);
+#pragma unroll
+    for (int s = 1; s < CH; s *= 2) {
+      const double o = __shfl_up(l2, s);
+      if (lane >= s) l2 += o;
+    }
+    const double end = __shfl(l2, CH - 1);
+    if (lane < CH) {
+      const float hi = (float)l2;
+      to.rows[unit * CH + lane] = f32x4_t{hi, (float)(l2 - (double)hi), exp2_parts(l2), a.kv[rev] * exp2_parts(end - l2)};
+      if (lane == 0) {
+        to.whole[unit] = exp2_parts(end);
+        to.end[unit] = end;
+      }
+    }
+  }
+}
+
+template <int DT>
+hipError_t launch_decays_dt(const DecayArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(k_decays<Traits<DT>::kChunk>, dim3((unsigned)((a.units + 3) / 4)), dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 template <int DT>
