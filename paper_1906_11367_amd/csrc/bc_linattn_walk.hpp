@@ -314,6 +314,22 @@ __global__ __launch_bounds__(VP / NT * 4, KP == 64 && VP == 64 ? 3 : 2) void k_w
     __syncthreads();
     load(c + 1);
     __builtin_amdgcn_sched_barrier(0);
+    // the rows that outputs are multiplied with, on their way from here
+    constexpr int V = 4 * NT;
+    const int col = c0 + V * g, avail = w.V - col;
+    Raw<scan::kWords<DT, V>> x[DOTS ? IT : 1];
+    if constexpr (DOTS) {
+      const char* xp = w.x + (n * w.xs.n + t0 * w.xs.t + (h / w.xd) * w.xs.h) * kBytes<DT>;
+      const int xstep = (int)w.xs.t * kBytes<DT>;
+      const auto xr = rows_of(xp, VEC ? min(hi - t0, CH) : 0, xstep, w.V * kBytes<DT>);
+#pragma unroll
+      for (int it = 0; it < IT; ++it) {
+        const int row = rev ? CH - 1 - it * 16 - m : it * 16 + m;
+        if constexpr (VEC) x[it] = buffer_load<scan::kWords<DT, V>>(xr, avail > 0 ? (uint32_t)(row * xstep + col * kBytes<DT>) : kNoColumn);
+        else x[it] = scan::load_vec<DT, V>(xp + (row * w.xs.t + col) * kBytes<DT>, t0 + row < hi ? avail : 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
     f32x4_t acc[IT][NT];
     Frag vf[PG][NT];
     if (live) {
@@ -411,15 +427,10 @@ __global__ __launch_bounds__(VP / NT * 4, KP == 64 && VP == 64 ? 3 : 2) void k_w
               for (int nt = 0; nt < NT; ++nt) acc[it][nt] = mma(vf[p][nt], pf[it].part[part], acc[it][nt]);
         }
       }
-      // outputs: a lane has 4 NT consecutive columns of row it * 16 + m.  VEC: whole
-      // vectors exist or nothing, and a chunk's rows are within 2^31 bytes.
-      constexpr int V = 4 * NT;
-      const int col = c0 + V * g, avail = w.V - col;
+      // outputs: a lane has V consecutive columns of row it * 16 + m
       char* yp = w.y + (n * w.ys.n + t0 * w.ys.t + h * w.ys.h) * out_bytes;
-      const char* xp = w.x + (n * w.xs.n + t0 * w.xs.t + (h / w.xd) * w.xs.h) * kBytes<DT>;
-      const int ystep = (int)w.ys.t * out_bytes, xstep = (int)w.xs.t * kBytes<DT>;
+      const int ystep = (int)w.ys.t * out_bytes;
       const auto yr = rows_of(yp, VEC ? min(e - t0, CH) : 0, ystep, w.V * out_bytes);
-      const auto xr = rows_of(xp, VEC && DOTS ? min(hi - t0, CH) : 0, xstep, w.V * kBytes<DT>);
       if (t0 + CH > hi) {   // rows that do not exist
 #pragma unroll
         for (int it = 0; it < IT; ++it)
@@ -444,12 +455,9 @@ __global__ __launch_bounds__(VP / NT * 4, KP == 64 && VP == 64 ? 3 : 2) void k_w
           else scan::store_vec<kBF16, V>(yp + at, avail, o);
         }
         if constexpr (DOTS) {
-          Raw<scan::kWords<DT, V>> x;
-          if constexpr (VEC) x = buffer_load<scan::kWords<DT, V>>(xr, avail > 0 ? (uint32_t)(row * xstep + col * kBytes<DT>) : kNoColumn);
-          else x = scan::load_vec<DT, V>(xp + (row * w.xs.t + col) * kBytes<DT>, t0 + row < hi ? avail : 0);
           float dot = 0.0f;
 #pragma unroll
-          for (int u = 0; u < V; ++u) dot = fmaf(o[u], scan::elem<DT, V>(x, u), dot);
+          for (int u = 0; u < V; ++u) dot = fmaf(o[u], scan::elem<DT, V>(x[it], u), dot);
           dot += __shfl_xor(dot, 16);
           dot += __shfl_xor(dot, 32);
           if (g == 0) sm.dots[wave][it * 16 + m] = dot;
