@@ -23,6 +23,7 @@ namespace {
 using scan::kBF16;
 using scan::kF32;
 using scan::kBytes;
+using scan::Raw;
 
 struct Rows { const char* p; long stride; };   // of an input; null: none
 struct OutRows { char* p; long stride; };
@@ -49,37 +50,42 @@ __device__ __forceinline__ float sigmoid(float g) {
   return g >= 0.0f ? r : e * r;
 }
 
-// Sums over slots, by a team of W waves, or of `lanes` lanes (W = 1), NS slots a
-// lane: slot i * team + lane.
+// Sums over slots, by a team of W waves, or of `size` lanes of one (W = 1), NS
+// slots a lane: slot i * size + lane.
 template <int W, int NS> struct Team {
   static constexpr int kSlots = W == 1 ? 256 : 64 * W * NS;   // of a block, where they meet in LDS
-  float* lds;       // [2][kSlots] slots, then [2][kSlots] groups
+  static constexpr int kRing = W > 1 ? 2 * 2 * W : 0;         // two places for the waves' sums
+  static constexpr int kFloats = kRing + 4 * kSlots;
+  float* lds;
   int lane, size;   // within the team; the team's lanes
   int base;         // the team's first slot of the block's
   int per, groups, mode;
+  int turn = 0;
 
-  template <int K> __device__ __forceinline__ void all(float (&v)[K]) const {
+  template <int K> __device__ __forceinline__ void all(float (&v)[K]) {
     const int within = W == 1 ? size : 64;
     for (int d = 1; d < within; d *= 2)
 #pragma unroll
       for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], d);
     if constexpr (W > 1) {
-      __syncthreads();   // the last sum has been read
+      // a place is written again after the next sum's barrier, when all have read it
+      float* at = lds + turn * 2 * W;
+      turn ^= 1;
       if ((threadIdx.x & 63) == 0)
 #pragma unroll
-        for (int k = 0; k < K; ++k) lds[k * W + (threadIdx.x >> 6)] = v[k];
+        for (int k = 0; k < K; ++k) at[k * W + (threadIdx.x >> 6)] = v[k];
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         v[k] = 0.0f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) v[k] += lds[k * W + w];
+        for (int w = 0; w < W; ++w) v[k] += at[k * W + w];
       }
     }
   }
 
   // over the whole row
-  template <int K> __device__ __forceinline__ void row(float (&v)[NS][K]) const {
+  template <int K> __device__ __forceinline__ void row(float (&v)[NS][K]) {
     float s[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -95,7 +101,7 @@ template <int W, int NS> struct Team {
   }
 
   // over each slot's group
-  template <int K> __device__ __forceinline__ void group(float (&v)[NS][K]) const {
+  template <int K> __device__ __forceinline__ void group(float (&v)[NS][K]) {
     if (mode == kSumTeam) {
       row<K>(v);
     } else if (mode == kSumLanes) {
@@ -105,14 +111,15 @@ template <int W, int NS> struct Team {
 #pragma unroll
           for (int k = 0; k < K; ++k) v[i][k] += __shfl_xor(v[i][k], d);
     } else {
-      __syncthreads();
+      float* slots = lds + kRing;
+      float* sums = slots + 2 * kSlots;
+      __syncthreads();   // the last sums have been read
 #pragma unroll
       for (int i = 0; i < NS; ++i)
 #pragma unroll
-        for (int k = 0; k < K; ++k) lds[k * kSlots + base + i * size + lane] = v[i][k];
+        for (int k = 0; k < K; ++k) slots[k * kSlots + base + i * size + lane] = v[i][k];
       __syncthreads();
       // 8 lanes a group
-      float* sums = lds + 2 * kSlots;
       const int eight = lane >> 3, l = lane & 7;
       for (int g0 = 0; g0 < groups; g0 += size >> 3) {
         const int g = g0 + eight;
@@ -121,7 +128,7 @@ template <int W, int NS> struct Team {
         for (int k = 0; k < K; ++k) {
           s[k] = 0.0f;
           if (g < groups)
-            for (int j = l; j < per; j += 8) s[k] += lds[k * kSlots + base + g * per + j];
+            for (int j = l; j < per; j += 8) s[k] += slots[k * kSlots + base + g * per + j];
           for (int d = 1; d < 8; d *= 2) s[k] += __shfl_xor(s[k], d);
           if (g < groups && l == 0) sums[k * kSlots + base + g] = s[k];
         }
@@ -137,66 +144,95 @@ template <int W, int NS> struct Team {
   }
 };
 
+// A lane's slots: 8 channels from col on, of which [lo, hi) are the slot's.  A
+// group's last slot ends with the group and leaves to the one before what is that
+// one's, so that every slot is read whole (groups below 8 channels: one slot, and
+// its channels one by one).
+template <int NS> struct Slots { int col[NS], lo[NS], hi[NS]; };
+
+template <int DT> using Eight = Raw<scan::kWords<DT, 8>>;
+
 template <int DT, int NS>
-__device__ __forceinline__ void load_row(const Rows& t, long row, const int (&col)[NS], const int (&avail)[NS],
-                                         float (&v)[NS][8]) {
+__device__ __forceinline__ void fetch(const Rows& t, long row, bool on, bool tiny, const Slots<NS>& s, Eight<DT> (&v)[NS]) {
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
-    const auto raw = scan::load_vec<DT, 8>(t.p + (row * t.stride + col[i]) * kBytes<DT>, avail[i]);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[i][e] = scan::elem<DT, 8>(raw, e);
+    const char* p = t.p + (row * t.stride + s.col[i]) * kBytes<DT>;
+    if (tiny) {
+      v[i] = scan::load_vec<DT, 8>(p, on ? s.hi[i] : 0);
+    } else {
+      v[i] = {};
+      if (on && s.hi[i] > 0) v[i] = scan::load_wide<DT, 8>(p);
+    }
   }
 }
 
 template <int DT, int NS>
-__device__ __forceinline__ void store_row(const OutRows& t, long row, const int (&col)[NS], const int (&avail)[NS],
-                                          const float (&v)[NS][8]) {
+__device__ __forceinline__ void unpack(const Eight<DT> (&raw)[NS], const Slots<NS>& s, float (&v)[NS][8]) {
 #pragma unroll
   for (int i = 0; i < NS; ++i)
-    if (avail[i] > 0) scan::store_vec<DT, 8>(t.p + (row * t.stride + col[i]) * kBytes<DT>, avail[i], v[i]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[i][e] = e >= s.lo[i] ? scan::elem<DT, 8>(raw[i], e) : 0.0f;
+}
+
+template <int DT, int NS>
+__device__ __forceinline__ void store_row(const OutRows& t, long row, bool on, const Slots<NS>& s, const float (&v)[NS][8]) {
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    char* p = t.p + (row * t.stride + s.col[i]) * kBytes<DT>;
+    if (!on || s.hi[i] == 0) continue;
+    if (s.lo[i] == 0 && s.hi[i] == 8) {
+      scan::store_wide<DT, 8>(p, v[i], false);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e >= s.lo[i] && e < s.hi[i]) {
+          if constexpr (DT == kF32) reinterpret_cast<float*>(p)[e] = v[i][e];
+          else reinterpret_cast<__bf16*>(p)[e] = (__bf16)v[i][e];
+        }
+    }
+  }
 }
 
 template <int NS>
-__device__ __forceinline__ void load_weights(const float* w, float none, const int (&col)[NS], const int (&avail)[NS],
-                                             float (&v)[NS][8]) {
+__device__ __forceinline__ void load_weights(const float* w, const Slots<NS>& s, float (&v)[NS][8]) {
 #pragma unroll
   for (int i = 0; i < NS; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[i][e] = w && e < avail[i] ? w[col[i] + e] : none;
+    for (int e = 0; e < 8; ++e) v[i][e] = w && e < s.hi[i] ? w[s.col[i] + e] : 1.0f;
 }
 
 // v -> v rho (less the mean), rho by slot.
 template <bool kGroup, class Team, int NS>
-__device__ __forceinline__ void normalise(const Team& team, bool layer, float inv, float eps, const int (&avail)[NS],
+__device__ __forceinline__ void normalise(Team& team, bool layer, float inv, float eps, const Slots<NS>& s,
                                           float (&v)[NS][8], float (&rho)[NS]) {
-  float s[NS][1];
+  float t[NS][1];
   auto sum = [&]() {
-    if constexpr (kGroup) team.template group<1>(s);
-    else team.template row<1>(s);
+    if constexpr (kGroup) team.template group<1>(t);
+    else team.template row<1>(t);
   };
   if (layer) {
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-      s[i][0] = 0.0f;
+      t[i][0] = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[i][0] += v[i][e];
+      for (int e = 0; e < 8; ++e) t[i][0] += v[i][e];
     }
     sum();
 #pragma unroll
     for (int i = 0; i < NS; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = e < avail[i] ? v[i][e] - s[i][0] * inv : 0.0f;
+      for (int e = 0; e < 8; ++e) v[i][e] = e >= s.lo[i] && e < s.hi[i] ? v[i][e] - t[i][0] * inv : 0.0f;
   }
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
-    s[i][0] = 0.0f;
+    t[i][0] = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[i][0] = fmaf(v[i][e], v[i][e], s[i][0]);
+    for (int e = 0; e < 8; ++e) t[i][0] = fmaf(v[i][e], v[i][e], t[i][0]);
   }
   sum();
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
-    rho[i] = 1.0f / sqrtf(fmaf(s[i][0], inv, eps));
+    rho[i] = 1.0f / sqrtf(fmaf(t[i][0], inv, eps));
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[i][e] *= rho[i];
   }
@@ -204,32 +240,48 @@ __device__ __forceinline__ void normalise(const Team& team, bool layer, float in
 
 // dn (the gradient to n = norm(v)) -> the gradient to v.
 template <bool kGroup, class Team, int NS>
-__device__ __forceinline__ void norm_grad(const Team& team, bool layer, float inv, const int (&avail)[NS],
-                                          const float (&n)[NS][8], const float (&rho)[NS], float (&dn)[NS][8]) {
-  float s[NS][2];
+__device__ __forceinline__ void norm_grad(Team& team, bool layer, float inv, const Slots<NS>& s, const float (&n)[NS][8],
+                                          const float (&rho)[NS], float (&dn)[NS][8]) {
+  if (!layer) {
+    float t[NS][1];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      t[i][0] = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[i][0] = fmaf(n[i][e], dn[i][e], t[i][0]);
+    }
+    if constexpr (kGroup) team.template group<1>(t);
+    else team.template row<1>(t);
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dn[i][e] = rho[i] * (dn[i][e] - n[i][e] * (t[i][0] * inv));
+    return;
+  }
+  float t[NS][2];
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
-    s[i][0] = s[i][1] = 0.0f;
+    t[i][0] = t[i][1] = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      s[i][0] = fmaf(n[i][e], dn[i][e], s[i][0]);
-      s[i][1] += dn[i][e];
+      t[i][0] = fmaf(n[i][e], dn[i][e], t[i][0]);
+      t[i][1] += dn[i][e];
     }
   }
-  if constexpr (kGroup) team.template group<2>(s);
-  else team.template row<2>(s);
+  if constexpr (kGroup) team.template group<2>(t);
+  else team.template row<2>(t);
 #pragma unroll
-  for (int i = 0; i < NS; ++i) {
-    const float c = s[i][0] * inv, mean = layer ? s[i][1] * inv : 0.0f;
+  for (int i = 0; i < NS; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dn[i][e] = e < avail[i] ? rho[i] * (dn[i][e] - mean - n[i][e] * c) : 0.0f;
-  }
+    for (int e = 0; e < 8; ++e)
+      dn[i][e] = e >= s.lo[i] && e < s.hi[i] ? rho[i] * (dn[i][e] - t[i][1] * inv - n[i][e] * (t[i][0] * inv)) : 0.0f;
 }
 
-template <int DT, int W, int NS, bool BWD>
+// GATE, PRE: there is a gate; there is a y (or its gradient).
+template <int DT, int W, int NS, bool BWD, bool GATE, bool PRE>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a) {
   using T = Team<W, NS>;
-  __shared__ float lds[4 * T::kSlots];
+  __shared__ float lds[T::kFloats];
   const int tid = threadIdx.x;
   T team;
   team.lds = lds;
@@ -240,19 +292,21 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a
   team.per = a.per;
   team.groups = max(a.groups, 1);
   team.mode = a.mode;
+  const bool tiny = a.size < 8;
 
-  int col[NS], avail[NS];
+  Slots<NS> s;
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
     const int j = i * team.size + team.lane, g = j / a.per, k = j % a.per;
-    col[i] = g * a.size + k * 8;
-    avail[i] = g < team.groups ? min(a.size - k * 8, 8) : 0;
-    if (g >= team.groups) col[i] = 0;
+    const int over = tiny ? 0 : max(k * 8 + 8 - a.size, 0);   // past the group's end
+    s.col[i] = g < team.groups ? g * a.size + k * 8 - over : 0;
+    s.lo[i] = over;
+    s.hi[i] = g < team.groups ? min(a.size, 8) : 0;
   }
   float w_post[NS][8], scale[NS][8], w_pre[NS][8];
-  load_weights<NS>(a.w_post, 1.0f, col, avail, w_post);
-  load_weights<NS>(a.scale, 1.0f, col, avail, scale);
-  load_weights<NS>(a.w_pre, 1.0f, col, avail, w_pre);
+  load_weights<NS>(a.w_post, s, w_post);
+  load_weights<NS>(a.scale, s, scale);
+  if constexpr (PRE) load_weights<NS>(a.w_pre, s, w_pre);
   const float inv_group = 1.0f / (float)a.size, inv_row = 1.0f / (float)a.C;
 
   float sum[3][NS][8];
@@ -265,49 +319,65 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a
         for (int e = 0; e < 8; ++e) sum[k][i][e] = 0.0f;
   }
 
-  for (long row0 = (long)blockIdx.x * teams; row0 < a.R; row0 += (long)gridDim.x * teams) {
-    const long row = min(row0 + which, (long)a.R - 1);   // (a team past the end follows the last row)
-    const bool on = row0 + which < a.R;
-    int here[NS];
-#pragma unroll
-    for (int i = 0; i < NS; ++i) here[i] = on ? avail[i] : 0;
-    float n[NS][8], g[NS][8], r[NS][8], dr[NS][8], dy[NS][8], rho1[NS], rho2[NS];
-    load_row<DT, NS>(a.z, row, col, here, n);
-    if (a.gate.p) load_row<DT, NS>(a.gate, row, col, here, g);
-    if (a.x.p) load_row<DT, NS>(a.x, row, col, here, r);
-    if constexpr (BWD) {
-      if (a.dr.p) load_row<DT, NS>(a.dr, row, col, here, dr);
-      if (a.dy.p) load_row<DT, NS>(a.dy, row, col, here, dy);
-    }
-    if (a.post) normalise<true>(team, a.layer, inv_group, a.eps, here, n, rho1);
-    float phi[NS][8], u[NS][8];
+  // a row's inputs are on their way while the row before it is worked on (but for
+  // blocks of 1024 threads, whose 128 registers hold no more)
+  constexpr bool AHEAD = NS == 1 && !(W == 16 && BWD && PRE);
+  constexpr bool X = PRE || !BWD;   // x is read
+  Eight<DT> rz[NS], rg[NS], rx[NS], rdr[NS], rdy[NS];
+  auto get = [&](long row0) {
+    const long row = row0 + which;
+    const bool on = row < a.R;
+    fetch<DT, NS>(a.z, row, on, tiny, s, rz);
+    if constexpr (GATE) fetch<DT, NS>(a.gate, row, on, tiny, s, rg);
+    if constexpr (X) fetch<DT, NS>(a.x, row, on && a.x.p, tiny, s, rx);
+    if constexpr (BWD) fetch<DT, NS>(a.dr, row, on && a.dr.p, tiny, s, rdr);
+    if constexpr (BWD && PRE) fetch<DT, NS>(a.dy, row, on, tiny, s, rdy);
+  };
+  const long step = (long)gridDim.x * teams;
+  long row0 = (long)blockIdx.x * teams;
+  if (AHEAD && row0 < a.R) get(row0);
+  for (; row0 < a.R; row0 += step) {
+    const long row = row0 + which;
+    const bool on = row < a.R;
+    if constexpr (!AHEAD) get(row0);
+    float n[NS][8], g[NS][8], r[NS][8], d[NS][8], dy[NS][8], rho1[NS], rho2[NS];
+    unpack<DT, NS>(rz, s, n);
+    if constexpr (GATE) unpack<DT, NS>(rg, s, g);
+    if constexpr (X) unpack<DT, NS>(rx, s, r);
+    if constexpr (BWD) unpack<DT, NS>(rdr, s, d);
+    if constexpr (BWD && PRE) unpack<DT, NS>(rdy, s, dy);
+    if (AHEAD && row0 + step < a.R) get(row0 + step);
+    if (a.post) normalise<true>(team, a.layer, inv_group, a.eps, s, n, rho1);
+    float phi[NS][8];
+    auto u_of = [&](int i, int e) {
+      const float p = n[i][e] * w_post[i][e];
+      if constexpr (GATE) return p * phi[i][e];
+      else return p;
+    };
 #pragma unroll
     for (int i = 0; i < NS; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        phi[i][e] = 1.0f;
-        if (a.gate.p) {
-          const float s = sigmoid(g[i][e]);
-          phi[i][e] = a.sigmoid ? s : g[i][e] * s;
-          if constexpr (BWD) g[i][e] = a.sigmoid ? s * (1.0f - s) : s * fmaf(g[i][e], 1.0f - s, 1.0f);   // the slope
+        if constexpr (GATE) {
+          const float sg = sigmoid(g[i][e]);
+          phi[i][e] = a.sigmoid ? sg : g[i][e] * sg;
+          if constexpr (BWD) g[i][e] = a.sigmoid ? sg * (1.0f - sg) : sg * fmaf(g[i][e], 1.0f - sg, 1.0f);   // the slope
         }
-        u[i][e] = n[i][e] * w_post[i][e] * phi[i][e];
-        const float v = u[i][e] * scale[i][e];
-        r[i][e] = a.x.p ? r[i][e] + v : v;
+        if constexpr (X) r[i][e] = r[i][e] + u_of(i, e) * scale[i][e];
       }
     if constexpr (!BWD) {
-      if (a.r.p) store_row<DT, NS>(a.r, row, col, here, r);
-      if (a.pre) {
-        normalise<false>(team, a.layer, inv_row, a.eps, here, r, rho2);
+      if (a.r.p) store_row<DT, NS>(a.r, row, on, s, r);
+      if constexpr (PRE) {
+        normalise<false>(team, a.layer, inv_row, a.eps, s, r, rho2);
 #pragma unroll
         for (int i = 0; i < NS; ++i)
 #pragma unroll
           for (int e = 0; e < 8; ++e) r[i][e] *= w_pre[i][e];
-        store_row<DT, NS>(a.y, row, col, here, r);
+        store_row<DT, NS>(a.y, row, on, s, r);
       }
     } else {
-      if (a.pre) {
-        normalise<false>(team, a.layer, inv_row, a.eps, here, r, rho2);
+      if constexpr (PRE) {
+        normalise<false>(team, a.layer, inv_row, a.eps, s, r, rho2);
 #pragma unroll
         for (int i = 0; i < NS; ++i)
 #pragma unroll
@@ -315,29 +385,31 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a
             sum[2][i][e] = fmaf(dy[i][e], r[i][e], sum[2][i][e]);
             dy[i][e] *= w_pre[i][e];
           }
-        norm_grad<false>(team, a.layer, inv_row, here, r, rho2, dy);
+        norm_grad<false>(team, a.layer, inv_row, s, r, rho2, dy);
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) d[i][e] += dy[i][e];
       }
-      float d[NS][8];
-#pragma unroll
-      for (int i = 0; i < NS; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[i][e] = (a.dr.p ? dr[i][e] : 0.0f) + (a.pre ? dy[i][e] : 0.0f);
-      if (a.dx.p) store_row<DT, NS>(a.dx, row, col, here, d);
+      if (a.dx.p) store_row<DT, NS>(a.dx, row, on, s, d);
 #pragma unroll
       for (int i = 0; i < NS; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          sum[1][i][e] = fmaf(d[i][e], u[i][e], sum[1][i][e]);
-          const float du = d[i][e] * scale[i][e];
-          g[i][e] *= du * n[i][e] * w_post[i][e];
-          const float dp = du * phi[i][e];
-          sum[0][i][e] = fmaf(dp, n[i][e], sum[0][i][e]);
-          d[i][e] = dp * w_post[i][e];
+          sum[1][i][e] = fmaf(d[i][e], u_of(i, e), sum[1][i][e]);
+          d[i][e] *= scale[i][e];
+          if constexpr (GATE) {
+            g[i][e] *= d[i][e] * n[i][e] * w_post[i][e];
+            d[i][e] *= phi[i][e];
+          }
+          sum[0][i][e] = fmaf(d[i][e], n[i][e], sum[0][i][e]);
+          d[i][e] *= w_post[i][e];
         }
-      if (a.dgate.p) store_row<DT, NS>(a.dgate, row, col, here, g);
+      if constexpr (GATE)
+        if (a.dgate.p) store_row<DT, NS>(a.dgate, row, on, s, g);
       if (a.dz.p) {
-        if (a.post) norm_grad<true>(team, a.layer, inv_group, here, n, rho1, d);
-        store_row<DT, NS>(a.dz, row, col, here, d);
+        if (a.post) norm_grad<true>(team, a.layer, inv_group, s, n, rho1, d);
+        store_row<DT, NS>(a.dz, row, on, s, d);
       }
     }
   }
@@ -354,9 +426,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a
             lds[tid] = sum[k][0][e];
             __syncthreads();
             if (which == 0) {
-              float s = 0.0f;
-              for (int t = 0; t < teams; ++t) s += lds[t * team.size + team.lane];
-              if (e < avail[0]) out[(long)k * a.C + col[0] + e] = s;
+              float t = 0.0f;
+              for (int u = 0; u < teams; ++u) t += lds[u * team.size + team.lane];
+              if (e >= s.lo[0] && e < s.hi[0]) out[(long)k * a.C + s.col[0] + e] = t;
             }
           }
         }
@@ -367,7 +439,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a
           for (int i = 0; i < NS; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              if (e < avail[i]) out[(long)k * a.C + col[i] + e] = sum[k][i][e];
+              if (e >= s.lo[i] && e < s.hi[i]) out[(long)k * a.C + s.col[i] + e] = sum[k][i][e];
       }
     }
   }
@@ -401,7 +473,7 @@ inline int slots_of(int C, int groups) {
   return G * ((C / G + 7) / 8);
 }
 
-template <int DT, bool BWD>
+template <int DT, bool BWD, bool GATE, bool PRE>
 hipError_t launch_norm(NormArgs& a, int* blocks, hipStream_t s) {
   const int slots = slots_of(a.C, a.groups);
   const int G = std::max(a.groups, 1);
@@ -419,12 +491,18 @@ hipError_t launch_norm(NormArgs& a, int* blocks, hipStream_t s) {
   if (slots <= 64) {
     a.lanes = 8;
     while (a.lanes < slots) a.lanes *= 2;
-    return go(k_block_norm<DT, 1, 1, BWD>, 256, 256 / a.lanes);
+    return go(k_block_norm<DT, 1, 1, BWD, GATE, PRE>, 256, 256 / a.lanes);
   }
-  if (slots <= 256) return go(k_block_norm<DT, 4, 1, BWD>, 256, 1);
-  if (slots <= 512) return go(k_block_norm<DT, 8, 1, BWD>, 512, 1);
-  if (slots <= 1024) return go(k_block_norm<DT, 16, 1, BWD>, 1024, 1);
-  return go(k_block_norm<DT, 16, 2, BWD>, 1024, 1);
+  if (slots <= 256) return go(k_block_norm<DT, 4, 1, BWD, GATE, PRE>, 256, 1);
+  if (slots <= 512) return go(k_block_norm<DT, 8, 1, BWD, GATE, PRE>, 512, 1);
+  if (slots <= 1024) return go(k_block_norm<DT, 16, 1, BWD, GATE, PRE>, 1024, 1);
+  return go(k_block_norm<DT, 16, 2, BWD, GATE, PRE>, 1024, 1);
+}
+
+template <int DT, bool BWD>
+hipError_t launch_norm(NormArgs& a, int* blocks, hipStream_t s) {
+  if (a.gate.p) return a.pre ? launch_norm<DT, BWD, true, true>(a, blocks, s) : launch_norm<DT, BWD, true, false>(a, blocks, s);
+  return a.pre ? launch_norm<DT, BWD, false, true>(a, blocks, s) : launch_norm<DT, BWD, false, false>(a, blocks, s);
 }
 
 }  // namespace
