@@ -14,6 +14,7 @@
 // all rows of its block; a second kernel sums the blocks in order.
 #include <algorithm>
 
+#include "bc_common.hpp"
 #include "bc_internal.hpp"
 #include "bc_scan.hpp"
 
@@ -34,7 +35,8 @@ struct NormArgs {
   const float *w_post, *scale, *w_pre;
   Rows dr, dy;                  // backward
   OutRows dz, dgate, dx;
-  float* part;                  // [blocks][3][C]: dw_post, dscale, dw_pre; or null
+  float* part;                  // [blocks][2][C]: sums over rows of d n act(gate) and of dy norm(r); or null
+  int wanted;                   // bit k: sum k is read
   int R, C, groups, size;       // size: channels of a group
   int per;                      // slots of a group
   int lanes;                    // of a team that shares its wave
@@ -43,9 +45,13 @@ struct NormArgs {
   float eps;
 };
 
-constexpr int kSumTeam = 0, kSumLanes = 1, kSumShared = 2;
+constexpr int kSumTeam = 0, kSumLanes = 1, kSumFew = 2, kSumShared = 3;
+constexpr int kFew = 4;   // groups whose sums go side by side
 
-__device__ __forceinline__ float sigmoid(float g) {
+// 1 / (1 + e^-g).  bf16: the exponential's argument is rounded once, which costs
+// |g| 2^-24 of it; fp32: to a few units of 2^-24.
+template <int DT> __device__ __forceinline__ float sigmoid(float g) {
+  if constexpr (DT == kBF16) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.442695041f));
   const float e = expf(-fabsf(g)), r = __builtin_amdgcn_rcpf(1.0f + e);
   return g >= 0.0f ? r : e * r;
 }
@@ -54,7 +60,7 @@ __device__ __forceinline__ float sigmoid(float g) {
 // slots a lane: slot i * size + lane.
 template <int W, int NS> struct Team {
   static constexpr int kSlots = W == 1 ? 256 : 64 * W * NS;   // of a block, where they meet in LDS
-  static constexpr int kRing = W > 1 ? 2 * 2 * W : 0;         // two places for the waves' sums
+  static constexpr int kRing = W > 1 ? 2 * 2 * kFew * W : 0;  // two places for the waves' sums
   static constexpr int kFloats = kRing + 4 * kSlots;
   float* lds;
   int lane, size;   // within the team; the team's lanes
@@ -63,13 +69,11 @@ template <int W, int NS> struct Team {
   int turn = 0;
 
   template <int K> __device__ __forceinline__ void all(float (&v)[K]) {
-    const int within = W == 1 ? size : 64;
-    for (int d = 1; d < within; d *= 2)
 #pragma unroll
-      for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], d);
+    for (int k = 0; k < K; ++k) v[k] = run_sum(v[k], W == 1 ? size : 64);
     if constexpr (W > 1) {
       // a place is written again after the next sum's barrier, when all have read it
-      float* at = lds + turn * 2 * W;
+      float* at = lds + turn * 2 * kFew * W;
       turn ^= 1;
       if ((threadIdx.x & 63) == 0)
 #pragma unroll
@@ -83,6 +87,8 @@ template <int W, int NS> struct Team {
       }
     }
   }
+
+  __device__ __forceinline__ int of(int i) const { return min((i * size + lane) / per, groups - 1); }   // slot i's group
 
   // over the whole row
   template <int K> __device__ __forceinline__ void row(float (&v)[NS][K]) {
@@ -105,11 +111,29 @@ template <int W, int NS> struct Team {
     if (mode == kSumTeam) {
       row<K>(v);
     } else if (mode == kSumLanes) {
-      for (int d = 1; d < per; d *= 2)
 #pragma unroll
-        for (int i = 0; i < NS; ++i)
+      for (int i = 0; i < NS; ++i)
 #pragma unroll
-          for (int k = 0; k < K; ++k) v[i][k] += __shfl_xor(v[i][k], d);
+        for (int k = 0; k < K; ++k) v[i][k] = run_sum(v[i][k], per);
+    } else if (mode == kSumFew) {
+      float t[kFew * K];
+#pragma unroll
+      for (int f = 0; f < kFew; ++f)
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          t[f * K + k] = 0.0f;
+#pragma unroll
+          for (int i = 0; i < NS; ++i) t[f * K + k] += of(i) == f ? v[i][k] : 0.0f;
+        }
+      all<kFew * K>(t);
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          v[i][k] = t[k];
+#pragma unroll
+          for (int f = 1; f < kFew; ++f) v[i][k] = of(i) == f ? t[f * K + k] : v[i][k];
+        }
     } else {
       float* slots = lds + kRing;
       float* sums = slots + 2 * kSlots;
@@ -129,16 +153,15 @@ template <int W, int NS> struct Team {
           s[k] = 0.0f;
           if (g < groups)
             for (int j = l; j < per; j += 8) s[k] += slots[k * kSlots + base + g * per + j];
-          for (int d = 1; d < 8; d *= 2) s[k] += __shfl_xor(s[k], d);
+          s[k] = run_sum(s[k], 8);
           if (g < groups && l == 0) sums[k * kSlots + base + g] = s[k];
         }
       }
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        const int j = i * size + lane, g = min(j / per, groups - 1);
 #pragma unroll
-        for (int k = 0; k < K; ++k) v[i][k] = sums[k * kSlots + base + g];
+        for (int k = 0; k < K; ++k) v[i][k] = sums[k * kSlots + base + of(i)];
       }
     }
   }
@@ -167,31 +190,45 @@ __device__ __forceinline__ void fetch(const Rows& t, long row, bool on, bool tin
 }
 
 template <int DT, int NS>
-__device__ __forceinline__ void unpack(const Eight<DT> (&raw)[NS], const Slots<NS>& s, float (&v)[NS][8]) {
+__device__ __forceinline__ void unpack(const Eight<DT> (&raw)[NS], bool whole, const Slots<NS>& s, float (&v)[NS][8]) {
 #pragma unroll
   for (int i = 0; i < NS; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[i][e] = e >= s.lo[i] ? scan::elem<DT, 8>(raw[i], e) : 0.0f;
-}
-
-template <int DT, int NS>
-__device__ __forceinline__ void store_row(const OutRows& t, long row, bool on, const Slots<NS>& s, const float (&v)[NS][8]) {
+    for (int e = 0; e < 8; ++e) v[i][e] = scan::elem<DT, 8>(raw[i], e);
+  if (!whole) {
 #pragma unroll
-  for (int i = 0; i < NS; ++i) {
-    char* p = t.p + (row * t.stride + s.col[i]) * kBytes<DT>;
-    if (!on || s.hi[i] == 0) continue;
-    if (s.lo[i] == 0 && s.hi[i] == 8) {
-      scan::store_wide<DT, 8>(p, v[i], false);
-    } else {
+    for (int i = 0; i < NS; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e >= s.lo[i] && e < s.hi[i]) {
-          if constexpr (DT == kF32) reinterpret_cast<float*>(p)[e] = v[i][e];
-          else reinterpret_cast<__bf16*>(p)[e] = (__bf16)v[i][e];
-        }
-    }
+      for (int e = 0; e < 8; ++e) v[i][e] = e >= s.lo[i] ? v[i][e] : 0.0f;
   }
 }
+
+// A row's values as they are stored, and the store of them.
+template <int DT, int NS> struct Packed {
+  Eight<DT> v[NS];
+  __device__ __forceinline__ void set(const float (&x)[NS][8]) {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) v[i] = scan::rounded<DT, 8>(x[i]);
+  }
+  __device__ __forceinline__ void store(const OutRows& t, long row, bool on, bool whole, const Slots<NS>& s) const {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      char* p = t.p + (row * t.stride + s.col[i]) * kBytes<DT>;
+      if (!on || s.hi[i] == 0) continue;
+      if (whole || (s.lo[i] == 0 && s.hi[i] == 8)) {
+        *reinterpret_cast<scan::Loose<scan::kWords<DT, 8>, kBytes<DT>>*>(p) =
+            __builtin_bit_cast(scan::Loose<scan::kWords<DT, 8>, kBytes<DT>>, v[i]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e >= s.lo[i] && e < s.hi[i]) {
+            if constexpr (DT == kF32) reinterpret_cast<uint32_t*>(p)[e] = v[i][e];
+            else reinterpret_cast<uint16_t*>(p)[e] = (uint16_t)(v[i][e / 2] >> (16 * (e & 1)));
+          }
+      }
+    }
+  }
+};
 
 template <int NS>
 __device__ __forceinline__ void load_weights(const float* w, const Slots<NS>& s, float (&v)[NS][8]) {
@@ -277,9 +314,22 @@ __device__ __forceinline__ void norm_grad(Team& team, bool layer, float inv, con
       dn[i][e] = e >= s.lo[i] && e < s.hi[i] ? rho[i] * (dn[i][e] - t[i][1] * inv - n[i][e] * (t[i][0] * inv)) : 0.0f;
 }
 
+// Blocks of the forward: as many as the card holds at once, each with a run of rows
+// (its weights are loaded once, and the next row's inputs ahead).  8192 rows of
+// 4096 bf16 with residual and both norms: 58 us, with 2048 blocks 76.
+constexpr int fwd_blocks(int W) { return W <= 2 ? 2048 : W == 4 ? 1536 : W == 8 ? 768 : 256; }
+
+// Waves a SIMD: what the registers of the variant allow without a spill (a reload
+// waits for the loads ahead too).
+constexpr int waves_of(int dt, int W, bool bwd, bool both) {
+  if (W == 16) return 4;
+  if (bwd) return dt == kBF16 && !both ? 4 : 2;
+  return dt == kBF16 ? (both ? 5 : 6) : 4;
+}
+
 // GATE, PRE: there is a gate; there is a y (or its gradient).
 template <int DT, int W, int NS, bool BWD, bool GATE, bool PRE>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a) {
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, waves_of(DT, W, BWD, GATE && PRE)) void k_block_norm(NormArgs a) {
   using T = Team<W, NS>;
   __shared__ float lds[T::kFloats];
   const int tid = threadIdx.x;
@@ -292,7 +342,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a
   team.per = a.per;
   team.groups = max(a.groups, 1);
   team.mode = a.mode;
-  const bool tiny = a.size < 8;
+  const bool tiny = a.size < 8, whole = a.size % 8 == 0;
 
   Slots<NS> s;
 #pragma unroll
@@ -303,16 +353,23 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a
     s.lo[i] = over;
     s.hi[i] = g < team.groups ? min(a.size, 8) : 0;
   }
-  float w_post[NS][8], scale[NS][8], w_pre[NS][8];
-  load_weights<NS>(a.w_post, s, w_post);
-  load_weights<NS>(a.scale, s, scale);
+  float w[NS][8], w_pre[NS][8];   // w_post scale, w_pre
+  {
+    float scale[NS][8];
+    load_weights<NS>(a.w_post, s, w);
+    load_weights<NS>(a.scale, s, scale);
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[i][e] *= scale[i][e];
+  }
   if constexpr (PRE) load_weights<NS>(a.w_pre, s, w_pre);
   const float inv_group = 1.0f / (float)a.size, inv_row = 1.0f / (float)a.C;
 
-  float sum[3][NS][8];
+  float sum[2][NS][8];
   if constexpr (BWD) {
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int i = 0; i < NS; ++i)
 #pragma unroll
@@ -341,39 +398,37 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a
     const bool on = row < a.R;
     if constexpr (!AHEAD) get(row0);
     float n[NS][8], g[NS][8], r[NS][8], d[NS][8], dy[NS][8], rho1[NS], rho2[NS];
-    unpack<DT, NS>(rz, s, n);
-    if constexpr (GATE) unpack<DT, NS>(rg, s, g);
-    if constexpr (X) unpack<DT, NS>(rx, s, r);
-    if constexpr (BWD) unpack<DT, NS>(rdr, s, d);
-    if constexpr (BWD && PRE) unpack<DT, NS>(rdy, s, dy);
+    unpack<DT, NS>(rz, whole, s, n);
+    if constexpr (GATE) unpack<DT, NS>(rg, whole, s, g);
+    if constexpr (X) unpack<DT, NS>(rx, whole, s, r);
+    if constexpr (BWD) unpack<DT, NS>(rdr, whole, s, d);
+    if constexpr (BWD && PRE) unpack<DT, NS>(rdy, whole, s, dy);
     if (AHEAD && row0 + step < a.R) get(row0 + step);
     if (a.post) normalise<true>(team, a.layer, inv_group, a.eps, s, n, rho1);
     float phi[NS][8];
-    auto u_of = [&](int i, int e) {
-      const float p = n[i][e] * w_post[i][e];
-      if constexpr (GATE) return p * phi[i][e];
-      else return p;
-    };
 #pragma unroll
     for (int i = 0; i < NS; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if constexpr (GATE) {
-          const float sg = sigmoid(g[i][e]);
+          const float sg = sigmoid<DT>(g[i][e]);
           phi[i][e] = a.sigmoid ? sg : g[i][e] * sg;
           if constexpr (BWD) g[i][e] = a.sigmoid ? sg * (1.0f - sg) : sg * fmaf(g[i][e], 1.0f - sg, 1.0f);   // the slope
         }
-        if constexpr (X) r[i][e] = r[i][e] + u_of(i, e) * scale[i][e];
+        if constexpr (X) r[i][e] = fmaf(GATE ? n[i][e] * phi[i][e] : n[i][e], w[i][e], r[i][e]);
       }
+    // what goes to memory is kept until the row's end: the next row's loads are
+    // waited for before any store is on its way, since such waits count both
+    Packed<DT, NS> o[3];
     if constexpr (!BWD) {
-      if (a.r.p) store_row<DT, NS>(a.r, row, on, s, r);
+      o[0].set(r);
       if constexpr (PRE) {
         normalise<false>(team, a.layer, inv_row, a.eps, s, r, rho2);
 #pragma unroll
         for (int i = 0; i < NS; ++i)
 #pragma unroll
           for (int e = 0; e < 8; ++e) r[i][e] *= w_pre[i][e];
-        store_row<DT, NS>(a.y, row, on, s, r);
+        o[1].set(r);
       }
     } else {
       if constexpr (PRE) {
@@ -382,7 +437,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a
         for (int i = 0; i < NS; ++i)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            sum[2][i][e] = fmaf(dy[i][e], r[i][e], sum[2][i][e]);
+            sum[1][i][e] = fmaf(dy[i][e], r[i][e], sum[1][i][e]);
             dy[i][e] *= w_pre[i][e];
           }
         norm_grad<false>(team, a.layer, inv_row, s, r, rho2, dy);
@@ -391,35 +446,52 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a
 #pragma unroll
           for (int e = 0; e < 8; ++e) d[i][e] += dy[i][e];
       }
-      if (a.dx.p) store_row<DT, NS>(a.dx, row, on, s, d);
+      o[0].set(d);
 #pragma unroll
       for (int i = 0; i < NS; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          sum[1][i][e] = fmaf(d[i][e], u_of(i, e), sum[1][i][e]);
-          d[i][e] *= scale[i][e];
           if constexpr (GATE) {
-            g[i][e] *= d[i][e] * n[i][e] * w_post[i][e];
+            g[i][e] *= d[i][e] * w[i][e] * n[i][e];
             d[i][e] *= phi[i][e];
           }
           sum[0][i][e] = fmaf(d[i][e], n[i][e], sum[0][i][e]);
-          d[i][e] *= w_post[i][e];
+          d[i][e] *= w[i][e];
         }
-      if constexpr (GATE)
-        if (a.dgate.p) store_row<DT, NS>(a.dgate, row, on, s, g);
+      if constexpr (GATE) o[1].set(g);
       if (a.dz.p) {
         if (a.post) norm_grad<true>(team, a.layer, inv_group, s, n, rho1, d);
-        store_row<DT, NS>(a.dz, row, on, s, d);
+        o[2].set(d);
       }
+    }
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        asm volatile("" : "+v"(rz[i]));
+        if constexpr (GATE) asm volatile("" : "+v"(rg[i]));
+        if constexpr (X) asm volatile("" : "+v"(rx[i]));
+        if constexpr (BWD) asm volatile("" : "+v"(rdr[i]));
+        if constexpr (BWD && PRE) asm volatile("" : "+v"(rdy[i]));
+      }
+    }
+    if constexpr (!BWD) {
+      if (a.r.p) o[0].store(a.r, row, on, whole, s);
+      if constexpr (PRE) o[1].store(a.y, row, on, whole, s);
+    } else {
+      if (a.dx.p) o[0].store(a.dx, row, on, whole, s);
+      if constexpr (GATE)
+        if (a.dgate.p) o[1].store(a.dgate, row, on, whole, s);
+      if (a.dz.p) o[2].store(a.dz, row, on, whole, s);
     }
   }
   if constexpr (BWD) {
     if (a.part) {
-      float* out = a.part + (long)blockIdx.x * 3 * a.C;
+      float* out = a.part + (long)blockIdx.x * 2 * a.C;
       // teams of one block: in order, through LDS
       if (W == 1 && teams > 1) {
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
+        for (int k = 0; k < 2; ++k) {
+          if (!(a.wanted >> k & 1)) continue;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             __syncthreads();
@@ -434,7 +506,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a
         }
       } else {
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
+        for (int k = 0; k < 2; ++k)
+          if (a.wanted >> k & 1)
 #pragma unroll
           for (int i = 0; i < NS; ++i)
 #pragma unroll
@@ -445,28 +518,39 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_block_norm(NormArgs a
   }
 }
 
-// The weights' gradients: blocks' shares part [P][3][C], 64 channels a block.
-__global__ __launch_bounds__(1024) void k_norm_weights(const float* part, int P, int C, float* dw_post, float* dscale,
-                                                       float* dw_pre) {
-  __shared__ float lds[16][64];
-  const int blocks = (C + 63) / 64, k = blockIdx.x / blocks, c = blockIdx.x % blocks * 64 + (threadIdx.x & 63);
-  float* out = k == 0 ? dw_post : k == 1 ? dscale : dw_pre;
-  if (!out) return;
-  const int row = threadIdx.x >> 6;
-  float s = 0.0f;
-  if (c < C)
-    for (int p = row; p < P; p += 16) s += part[((long)p * 3 + k) * C + c];
-  lds[row][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (row == 0 && c < C) {
-    float t = 0.0f;
+constexpr int kPartBlocks = 512;   // blocks of the backward, and shares of the weights' gradients
+
+// The weights' gradients from the blocks' sums part [P][2][C], 32 channels a block,
+// a lane of 32 the blocks p, p + 32, ..., all on their way at once.  With A the sum
+// of d n act(gate), the gradient to w_post is scale A and that to scale w_post A.
+struct WeightGrads {
+  const float *part, *w_post, *scale;
+  float *dw_post, *dscale, *dw_pre;
+  int P, C;
+};
+__global__ __launch_bounds__(1024) void k_norm_weights(WeightGrads a) {
+  __shared__ float lds[32][33];
+  const int blocks = (a.C + 31) / 32, k = blockIdx.x / blocks, col = threadIdx.x & 31, row = threadIdx.x >> 5;
+  const int c = min((int)(blockIdx.x % blocks) * 32 + col, a.C - 1);
+  if (k == 0 ? !a.dw_post && !a.dscale : !a.dw_pre) return;
+  float v[kPartBlocks / 32], s = 0.0f;
 #pragma unroll
-    for (int u = 0; u < 16; ++u) t += lds[u][threadIdx.x];
-    out[c] = t;
+  for (int i = 0; i < kPartBlocks / 32; ++i) v[i] = a.part[((long)min(row + 32 * i, a.P - 1) * 2 + k) * a.C + c];
+#pragma unroll
+  for (int i = 0; i < kPartBlocks / 32; ++i) s += row + 32 * i < a.P ? v[i] : 0.0f;
+  lds[col][row] = s;
+  __syncthreads();
+  // 32 lanes a channel
+  const float t = run_sum(lds[row][col], 32);
+  const int to = (int)(blockIdx.x % blocks) * 32 + row;
+  if (col != 0 || to >= a.C) return;
+  if (k == 1) {
+    a.dw_pre[to] = t;
+  } else {
+    if (a.dw_post) a.dw_post[to] = a.scale ? t * a.scale[to] : t;
+    if (a.dscale) a.dscale[to] = a.w_post ? t * a.w_post[to] : t;
   }
 }
-
-constexpr int kPartBlocks = 512;   // blocks of the backward, and shares of the weights' gradients
 
 inline int slots_of(int C, int groups) {
   const int G = std::max(groups, 1);
@@ -481,22 +565,23 @@ hipError_t launch_norm(NormArgs& a, int* blocks, hipStream_t s) {
   a.per = slots / G;
   a.lanes = 64;
   const bool pow2 = (a.per & (a.per - 1)) == 0 && a.per <= 64;
-  auto go = [&](auto kernel, int threads, int teams) {
+  auto go = [&](auto kernel, int threads, int teams, int cap) {
     const long want = ((long)a.R + teams - 1) / teams;
-    *blocks = (int)std::min<long>(want, BWD ? kPartBlocks : 2048);
-    a.mode = G == 1 ? kSumTeam : pow2 ? kSumLanes : kSumShared;
+    *blocks = (int)std::min<long>(want, BWD ? kPartBlocks : cap);
+    a.mode = G == 1 ? kSumTeam : pow2 ? kSumLanes : G <= kFew ? kSumFew : kSumShared;
     hipLaunchKernelGGL(kernel, dim3((unsigned)*blocks), dim3((unsigned)threads), 0, s, a);
     return hipGetLastError();
   };
   if (slots <= 64) {
     a.lanes = 8;
     while (a.lanes < slots) a.lanes *= 2;
-    return go(k_block_norm<DT, 1, 1, BWD, GATE, PRE>, 256, 256 / a.lanes);
+    return go(k_block_norm<DT, 1, 1, BWD, GATE, PRE>, 256, 256 / a.lanes, fwd_blocks(1));
   }
-  if (slots <= 256) return go(k_block_norm<DT, 4, 1, BWD, GATE, PRE>, 256, 1);
-  if (slots <= 512) return go(k_block_norm<DT, 8, 1, BWD, GATE, PRE>, 512, 1);
-  if (slots <= 1024) return go(k_block_norm<DT, 16, 1, BWD, GATE, PRE>, 1024, 1);
-  return go(k_block_norm<DT, 16, 2, BWD, GATE, PRE>, 1024, 1);
+  if (slots <= 128) return go(k_block_norm<DT, 2, 1, BWD, GATE, PRE>, 128, 1, fwd_blocks(2));
+  if (slots <= 256) return go(k_block_norm<DT, 4, 1, BWD, GATE, PRE>, 256, 1, fwd_blocks(4));
+  if (slots <= 512) return go(k_block_norm<DT, 8, 1, BWD, GATE, PRE>, 512, 1, fwd_blocks(8));
+  if (slots <= 1024) return go(k_block_norm<DT, 16, 1, BWD, GATE, PRE>, 1024, 1, fwd_blocks(16));
+  return go(k_block_norm<DT, 16, 2, BWD, GATE, PRE>, 1024, 1, fwd_blocks(16));
 }
 
 template <int DT, bool BWD>
@@ -509,7 +594,7 @@ hipError_t launch_norm(NormArgs& a, int* blocks, hipStream_t s) {
 
 bool block_norm_takes(int C, int groups) { return slots_of(C, groups) <= 2048; }
 
-size_t block_norm_workspace_bytes(int R, int C) { return (size_t)std::min(R, kPartBlocks) * 3 * C * 4; }
+size_t block_norm_workspace_bytes(int R, int C) { return (size_t)std::min(R, kPartBlocks) * 2 * C * 4; }
 
 static Rows rows(const NormRows& t) { return {static_cast<const char*>(t.p), t.stride}; }
 static OutRows out_rows(const NormRows& t) { return {static_cast<char*>(const_cast<void*>(t.p)), t.stride}; }
@@ -541,10 +626,11 @@ hipError_t launch_block_norm(const BlockNorm& b, bool bwd, hipStream_t s) {
   if (!bwd) return b.dt == kBF16 ? launch_norm<kBF16, false>(a, &blocks, s) : launch_norm<kF32, false>(a, &blocks, s);
   const bool weights = b.dw_post || b.dscale || b.dw_pre;
   a.part = weights ? static_cast<float*>(b.ws) : nullptr;
+  a.wanted = (b.dw_post || b.dscale ? 1 : 0) | (b.dw_pre ? 2 : 0);
   const hipError_t e = b.dt == kBF16 ? launch_norm<kBF16, true>(a, &blocks, s) : launch_norm<kF32, true>(a, &blocks, s);
   if (e != hipSuccess || !weights) return e;
-  hipLaunchKernelGGL(k_norm_weights, dim3((unsigned)(3 * ((b.C + 63) / 64))), dim3(1024), 0, s,
-                     static_cast<const float*>(b.ws), blocks, b.C, b.dw_post, b.dscale, b.dw_pre);
+  const WeightGrads w{a.part, b.w_post, b.scale, b.dw_post, b.dscale, b.dw_pre, blocks, b.C};
+  hipLaunchKernelGGL(k_norm_weights, dim3((unsigned)(2 * ((b.C + 31) / 32))), dim3(1024), 0, s, w);
   return hipGetLastError();
 }
 

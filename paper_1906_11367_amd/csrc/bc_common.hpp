@@ -367,6 +367,28 @@ __device__ __forceinline__ float row16_sum(float v) {
   return v;
 }
 
+// v of this lane and of the one 16, or 32, lanes away, in both.
+__device__ __forceinline__ float pair16_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float pair32_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Sum over each run of n lanes (a power of two up to 64, the same in all lanes),
+// in every lane of the run, without LDS.
+__device__ __forceinline__ float run_sum(float v, int n) {
+  if (n >= 2) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, false));
+  if (n >= 4) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xF, 0xF, false));
+  if (n >= 8) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xF, 0xF, false));
+  if (n >= 16) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, false));
+  if (n >= 32) v = pair16_sum(v);
+  if (n >= 64) v = pair32_sum(v);
+  return v;
+}
+
 // Wave-level sum (wave64), result valid in every lane.
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll

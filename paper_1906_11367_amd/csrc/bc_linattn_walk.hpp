@@ -21,6 +21,7 @@
 #pragma once
 #include <initializer_list>
 
+#include "bc_common.hpp"
 #include "bc_linattn.hpp"
 
 namespace bc {
@@ -458,8 +459,7 @@ __global__ __launch_bounds__(VP / NT * 4, KP == 64 && VP == 64 ? 3 : 2) void k_w
           float dot = 0.0f;
 #pragma unroll
           for (int u = 0; u < V; ++u) dot = fmaf(o[u], scan::elem<DT, V>(x[it], u), dot);
-          dot += __shfl_xor(dot, 16);
-          dot += __shfl_xor(dot, 32);
+          dot = pair32_sum(pair16_sum(dot));
           if (g == 0) sm.dots[wave][it * 16 + m] = dot;
         }
       }
