@@ -247,8 +247,8 @@ __global__ __launch_bounds__(256) void k_step(Step a) {
   }
 }
 
-hipError_t launch_walk(const Walk& w, int dt, hipStream_t s) {
-  return dt == kBF16 ? launch_walk_bf16(w, s) : launch_walk_f32(w, s);
+hipError_t launch_walk(const Walk& w, const Walk* beside, int dt, hipStream_t s) {
+  return dt == kBF16 ? launch_walk_bf16(w, beside, s) : launch_walk_f32(w, beside, s);
 }
 
 inline Str str(const bc_strides& s) { return {(long)s.batch, (long)s.row, (long)s.head}; }
@@ -259,20 +259,19 @@ inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
 // blocks on each of 256 CUs allow and 128 tokens at least.  The backward's are the
 // forward's that kept its states, and no longer than 2048 tokens (the gates'
 // gradients are sums over a segment).
-struct Plan { int seg, segs, chunks; };
+struct Plan { int seg, segs; };
 Plan plan_of(const bc_attention& a, bool keeps) {
   const long nh = (long)a.N * a.H;
   Plan p;
-  const long want = std::max(128L, (nh * a.T + 511) / 512);
+  const long want = std::max(a.T <= 512 ? 512L : 128L, (nh * a.T + 511) / 512);
   p.seg = (int)std::min((want + 63) / 64 * 64, keeps ? 2048L : 1L << 30);
   p.segs = (int)ceil_div(a.T, p.seg);
-  p.chunks = (int)ceil_div(a.T, chunk_of(a.dt));
   return p;
 }
 
-// Workspaces.  Decays of the chunks, then what joins the segments: their own
-// decays, and states at their borders.
-struct Ws { size_t rows[2], end[2], whole[2], decay, entries, dots, part, total; };
+// Workspaces.  What joins the segments: their decays and the states at their
+// borders; backward, what the gates' gradients are made from, and shared heads'.
+struct Ws { size_t decay, entries, dots, part, part_v, total; };
 Ws ws_of(const bc_attention& a, const Plan& p, bool bwd) {
   const size_t nh = (size_t)a.N * a.H;
   Ws w{};
@@ -282,21 +281,15 @@ Ws ws_of(const bc_attention& a, const Plan& p, bool bwd) {
     at += up(bytes);
     return here;
   };
-  for (int r = 0; r < (bwd ? 2 : 1); ++r) {
-    w.rows[r] = take(nh * p.chunks * chunk_of(a.dt) * 16);
-    w.end[r] = take(nh * p.chunks * 8);
-    w.whole[r] = take(nh * p.chunks * 4);
-  }
   if (p.segs > 1) {
     w.decay = take(nh * p.segs * 4);
     w.entries = take(nh * (p.segs + 1) * a.Dk * a.Dv * 4);
   }
   if (bwd) {
     w.dots = take(up(nh * a.T * 4) * 2);
-    size_t d = 0;   // gradients by reading head, summed afterwards; one at a time
-    if (a.Hq < a.H || a.Hk < a.H) d = a.Dk;
-    if (a.Hv < a.H) d = std::max(d, (size_t)a.Dv);
-    w.part = take(nh * a.T * d * 4);
+    // gradients by reading head: q's, then k's; and v's
+    if (a.Hq < a.H || a.Hk < a.H) w.part = take(nh * a.T * a.Dk * 4);
+    if (a.Hv < a.H) w.part_v = take(nh * a.T * a.Dv * 4);
   }
   w.total = at;
   return w;
@@ -313,7 +306,6 @@ Walk walk_of(const Attention& f) {
   w.N = a.N;
   w.T = a.T;
   w.H = a.H;
-  w.chunks = (int)ceil_div(a.T, chunk_of(a.dt));
   w.scale = w.kv = 1.0f;
   return w;
 }
@@ -349,30 +341,6 @@ using namespace linattn;
     if (e_ != hipSuccess) return e_;      \
   } while (0)
 
-static Decays decays_at(const Ws& ws, char* wsp, int rev) {
-  return {reinterpret_cast<f32x4_t*>(wsp + ws.rows[rev]), reinterpret_cast<float*>(wsp + ws.whole[rev]),
-          reinterpret_cast<double*>(wsp + ws.end[rev])};
-}
-
-// The decays of every chunk, forward and (bwd) backward in time.
-static hipError_t launch_decays(const Attention& f, const Plan& p, const Ws& ws, bool bwd, hipStream_t s) {
-  const bc_attention& a = *f.a;
-  DecayArgs d{};
-  for (int r = 0; r < (bwd ? 2 : 1); ++r) d.to[r] = decays_at(ws, static_cast<char*>(f.ws), r);
-  d.kv[0] = 1.0f;
-  d.kv[1] = a.scale;
-  d.gate = static_cast<const char*>(f.gate);
-  d.gs = str(f.gs);
-  d.gate_f32 = a.gate_dt == kF32;
-  d.form = a.form;
-  d.lengths = f.lengths;
-  d.T = a.T;
-  d.H = a.H;
-  d.chunks = p.chunks;
-  d.units = (long)a.N * a.H * p.chunks;
-  return a.dt == kBF16 ? launch_decays_bf16(d, s) : launch_decays_f32(d, s);
-}
-
 size_t linear_attention_states_bytes(int N, int T, int H, int Dk, int Dv) {
   bc_attention a{};
   a.N = N;
@@ -393,10 +361,8 @@ hipError_t launch_linear_attention_fwd(const Attention& f, hipStream_t s) {
   const Ws ws = ws_of(a, p, false);
   const long cells = (long)a.Dk * a.Dv, nh = (long)a.N * a.H;
   char* wsp = static_cast<char*>(f.ws);
-  BC_TRY(launch_decays(f, p, ws, false, s));
   Walk w = walk_of(f);
   set(w, {f.q, f.qs, a.H / a.Hq, a.Dk}, {f.k, f.ks, a.H / a.Hk, a.Dk}, {f.v, f.vs, a.H / a.Hv, a.Dv});
-  w.dec = decays_at(ws, wsp, 0);
   w.seg = p.seg;
   w.segs = p.segs;
   w.rows_first = 1;
@@ -408,7 +374,7 @@ hipError_t launch_linear_attention_fwd(const Attention& f, hipStream_t s) {
     w.last_nh = border;
     w.last_seg = cells;
     w.decay = reinterpret_cast<float*>(wsp + ws.decay);
-    BC_TRY(launch_walk(w, a.dt, s));
+    BC_TRY(launch_walk(w, nullptr, a.dt, s));
     Joint j{};
     j.entry = entry;
     j.entry_nh = border;
@@ -439,7 +405,7 @@ hipError_t launch_linear_attention_fwd(const Attention& f, hipStream_t s) {
   w.y = static_cast<char*>(f.y);
   w.ys = rows_str(f.ys, a.T, a.Dv);
   w.scale = a.scale;
-  return launch_walk(w, a.dt, s);
+  return launch_walk(w, nullptr, a.dt, s);
 }
 
 hipError_t launch_linear_attention_bwd(const Attention& f, hipStream_t s) {
@@ -452,17 +418,50 @@ hipError_t launch_linear_attention_bwd(const Attention& f, hipStream_t s) {
       dy{f.gy, f.gys, 1, a.Dv};
   float* dots = reinterpret_cast<float*>(wsp + ws.dots);
   float* dots_k = reinterpret_cast<float*>(wsp + ws.dots + up(nh * a.T * 4));
-  BC_TRY(launch_decays(f, p, ws, true, s));
   Walk forward = walk_of(f);
   forward.seg = p.seg;
   forward.segs = p.segs;
-  forward.dec = decays_at(ws, wsp, 0);
   Walk back = forward;
   back.rev = 1;
   back.kv = a.scale;
-  back.dec = decays_at(ws, wsp, 1);
 
-  // R at the segments' ends
+  // outputs of a walk: the gradient itself, or by reading head in the workspace,
+  // to be summed
+  auto out = [&](Walk& w, void* g, const bc_strides& gs, const Operand& like, size_t part) {
+    const int D = like.len;
+    const bool shared = like.div > 1;
+    w.y = static_cast<char*>(shared ? static_cast<void*>(wsp + part) : g);
+    w.ys = shared ? Str{(long)a.T * a.H * D, (long)a.H * D, D} : rows_str(gs, a.T, D);
+    w.y_f32 = shared;
+  };
+  auto sum_heads = [&](void* g, const bc_strides& gs, const Operand& like, size_t part) -> hipError_t {
+    if (like.div == 1) return hipSuccess;
+    const long count = (long)a.N * a.T * (a.H / like.div) * like.len;
+    hipLaunchKernelGGL(k_sum_heads, dim3((unsigned)std::min(ceil_div(count, 256), 1L << 16)), dim3(256), 0, s,
+                       reinterpret_cast<const float*>(wsp + part), static_cast<char*>(g), str(gs), a.dt == kF32, a.T, a.H,
+                       like.len, like.div, count);
+    return hipGetLastError();
+  };
+  auto with_dots = [&](Walk& w, const Operand& x, float* to) {
+    if (!f.ggate) return;
+    w.x = static_cast<const char*>(x.p);
+    w.xs = rows_str(x.s, a.T, x.len);
+    w.xd = x.div;
+    w.dots = to;
+  };
+
+  // two walks at a time where one leaves CUs without a second block
+  const bool pairs = nh * p.segs < 512;
+  Walk dq = forward;
+  set(dq, dy, v, k);
+  dq.init = f.states;
+  dq.init_nh = border;
+  dq.init_seg = cells;
+  dq.scale = a.scale;
+  with_dots(dq, q, dots);
+  out(dq, f.gq, f.gqs, q, ws.part);
+
+  // beside it R at the segments' ends, as far as the segments make it themselves
   back.init = f.gs_last;
   back.init_nh = cells;
   if (p.segs > 1) {
@@ -475,7 +474,12 @@ hipError_t launch_linear_attention_bwd(const Attention& f, hipStream_t s) {
     w.last_nh = border;
     w.last_seg = cells;
     w.decay = reinterpret_cast<float*>(wsp + ws.decay);
-    BC_TRY(launch_walk(w, a.dt, s));
+    if (pairs) {
+      BC_TRY(launch_walk(dq, &w, a.dt, s));
+    } else {
+      BC_TRY(launch_walk(dq, nullptr, a.dt, s));
+      BC_TRY(launch_walk(w, nullptr, a.dt, s));
+    }
     Joint j{};
     j.entry = entry;
     j.entry_nh = border;
@@ -496,41 +500,29 @@ hipError_t launch_linear_attention_bwd(const Attention& f, hipStream_t s) {
     back.init = entry + cells;
     back.init_nh = border;
     back.init_seg = cells;
+  } else {
+    BC_TRY(launch_walk(dq, nullptr, a.dt, s));
   }
+  BC_TRY(sum_heads(f.gq, f.gqs, q, ws.part));
 
-  auto run = [&](Walk& w, void* g, const bc_strides& gs, int share, int D) -> hipError_t {
-    w.y = static_cast<char*>(share > 1 ? static_cast<void*>(wsp + ws.part) : g);
-    w.ys = share > 1 ? Str{(long)a.T * a.H * D, (long)a.H * D, D} : rows_str(gs, a.T, D);
-    w.y_f32 = share > 1;
-    BC_TRY(launch_walk(w, a.dt, s));
-    if (share == 1) return hipSuccess;
-    const long count = (long)a.N * a.T * (a.H / share) * D;
-    hipLaunchKernelGGL(k_sum_heads, dim3((unsigned)std::min(ceil_div(count, 256), 1L << 16)), dim3(256), 0, s,
-                       reinterpret_cast<const float*>(wsp + ws.part), static_cast<char*>(g), str(gs), a.dt == kF32, a.T, a.H,
-                       D, share, count);
-    return hipGetLastError();
-  };
-  auto with_dots = [&](Walk& w, const Operand& x, float* to) {
-    if (!f.ggate) return;
-    w.x = static_cast<const char*>(x.p);
-    w.xs = rows_str(x.s, a.T, x.len);
-    w.xd = x.div;
-    w.dots = to;
-  };
-
-  Walk w = forward;   // dq
-  set(w, dy, v, k);
-  w.init = f.states;
-  w.init_nh = border;
-  w.init_seg = cells;
-  w.scale = a.scale;
-  with_dots(w, q, dots);
-  BC_TRY(run(w, f.gq, f.gqs, q.div, a.Dk));
-
-  w = back;           // dk
-  set(w, v, dy, q);
-  with_dots(w, k, dots_k);
-  BC_TRY(run(w, f.gk, f.gks, k.div, a.Dk));
+  Walk dk = back;
+  set(dk, v, dy, q);
+  with_dots(dk, k, dots_k);
+  out(dk, f.gk, f.gks, k, ws.part);
+  Walk dv = back;
+  set(dv, k, q, dy);
+  dv.rows_first = 1;
+  out(dv, f.gv, f.gvs, v, ws.part_v);
+  // grad_s0, unless k_join had it.  It may be grad_s_last, which the others read:
+  // then this walk is the last.
+  const bool by_dv = p.segs == 1 && f.gs0, alone = by_dv && f.gs0 == f.gs_last;
+  if (by_dv) {
+    dv.last = f.gs0;
+    dv.last_nh = cells;
+    dv.last_a0 = 1;
+  }
+  BC_TRY(launch_walk(dk, alone || !pairs ? nullptr : &dv, a.dt, s));
+  BC_TRY(sum_heads(f.gk, f.gks, k, ws.part));
 
   if (f.ggate) {
     GateGrad d{};
@@ -556,16 +548,8 @@ hipError_t launch_linear_attention_bwd(const Attention& f, hipStream_t s) {
     hipLaunchKernelGGL(k_gate_grad, dim3((unsigned)(nh * p.segs)), dim3(256), 0, s, d);
     BC_TRY(hipGetLastError());
   }
-
-  w = back;           // dv, last: grad_s0 may be grad_s_last, which the others read
-  set(w, k, q, dy);
-  w.rows_first = 1;
-  if (p.segs == 1) {
-    w.last = f.gs0;
-    w.last_nh = cells;
-    w.last_a0 = 1;
-  }
-  return run(w, f.gv, f.gvs, v.div, a.Dv);
+  if (alone || !pairs) BC_TRY(launch_walk(dv, nullptr, a.dt, s));
+  return sum_heads(f.gv, f.gvs, v, ws.part_v);
 }
 
 hipError_t launch_linear_attention_step(const Attention& f, const float* state, float* state_out, const int* slots, int S,

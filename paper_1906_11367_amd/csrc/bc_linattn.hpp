@@ -62,16 +62,6 @@ __device__ __forceinline__ float exp2_parts(double x) {
   return fmaf(e, (float)(x - (double)hi) * 0.6931472f, e);
 }
 
-// What the decays of a chunk of CH tokens make, for one direction of time: a row
-// {hi, lo, here, rest} for each token in the order of the walk, with L the running
-// sum of log2 a up to it, hi + lo = L, here = 2^L, rest = 2^(end - L) (times the
-// factor of k v^T); and of the whole chunk 2^end and end.
-struct Decays {
-  f32x4_t* rows;     // [nh][chunks][CH]
-  float* whole;      // [nh][chunks]
-  double* end;       // [nh][chunks]
-};
-
 // The walk of one block over a segment of one sequence and head: operands are
 // named as in the forward.
 struct Walk {
@@ -84,8 +74,6 @@ struct Walk {
   int N, T, H;
   int rev;                   // backward in time, with the decay of the token after
   int seg, segs;             // tokens of a segment (whole chunks), segments
-  Decays dec;
-  int chunks;                // of a sequence
   const float* init;         // state before a segment, or null: zero
   long init_nh, init_seg;
   float* first;              // the initial state once more (one segment), entries last2_nh apart
@@ -107,24 +95,12 @@ struct Walk {
   float* dots;
 };
 
-// A wave a chunk; both directions of time in one launch where both are wanted.
-struct DecayArgs {
-  Decays to[2];            // forward, backward; rows null: not wanted
-  float kv[2];
-  const char* gate;
-  Str gs;
-  int gate_f32, form;
-  const int* lengths;
-  int T, H, chunks;
-  long units;              // nh * chunks
-};
+constexpr int kChunk = 32;   // tokens of a chunk
 
-constexpr int chunk_of(int) { return 32; }   // tokens of a chunk
-
-hipError_t launch_decays_bf16(const DecayArgs& a, hipStream_t s);
-hipError_t launch_decays_f32(const DecayArgs& a, hipStream_t s);
-hipError_t launch_walk_bf16(const Walk& w, hipStream_t s);
-hipError_t launch_walk_f32(const Walk& w, hipStream_t s);
+// Walks of their own, or two over the same segments in one launch, block beside
+// block on one XCD: what both read is fetched once.
+hipError_t launch_walk_bf16(const Walk& w, const Walk* beside, hipStream_t s);
+hipError_t launch_walk_f32(const Walk& w, const Walk* beside, hipStream_t s);
 
 }  // namespace linattn
 }  // namespace bc

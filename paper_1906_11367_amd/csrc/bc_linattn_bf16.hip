@@ -3,7 +3,6 @@
 
 namespace bc {
 namespace linattn {
-hipError_t launch_decays_bf16(const DecayArgs& a, hipStream_t s) { return launch_decays_dt<kBF16>(a, s); }
-hipError_t launch_walk_bf16(const Walk& w, hipStream_t s) { return launch_walk_dt<kBF16>(w, s); }
+hipError_t launch_walk_bf16(const Walk& w, const Walk* beside, hipStream_t s) { return launch_walk_dt<kBF16>(w, beside, s); }
 }  // namespace linattn
 }  // namespace bc

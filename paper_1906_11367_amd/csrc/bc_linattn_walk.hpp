@@ -30,12 +30,12 @@ namespace {
 
 template <int DT> struct Traits;
 template <> struct Traits<kBF16> {
-  static constexpr int kChunk = chunk_of(kBF16), kGroup = 32;   // tokens of a chunk; reduction of one operand pair
+  static constexpr int kGroup = 32;   // the reduction of one operand pair
   using Frag = bf16x8_t;
   using Elem = uint16_t;
 };
 template <> struct Traits<kF32> {
-  static constexpr int kChunk = chunk_of(kF32), kGroup = 16;
+  static constexpr int kGroup = 16;
   using Frag = f32x4_t;
   using Elem = float;
 };
@@ -119,7 +119,7 @@ template <int W> __device__ __forceinline__ void buffer_store(__amdgpu_buffer_rs
 // VEC: whole aligned 16-byte vectors, a chunk's rows within 2^31 bytes.
 template <int DT, int W, int THREADS, bool VEC> struct Tile {
   static constexpr int kVec = 16 / kBytes<DT>, kPerRow = W / kVec, kRows = THREADS / kPerRow;
-  static constexpr int CH = Traits<DT>::kChunk, kPasses = (CH + kRows - 1) / kRows;
+  static constexpr int CH = kChunk, kPasses = (CH + kRows - 1) / kRows;
   static constexpr int kPitch = W + 16;   // elements
   static_assert(kPasses * kRows == CH || kRows > CH, "whole passes, or one of which threads are idle");
   Raw<4> r[kPasses];
@@ -185,15 +185,22 @@ __device__ __forceinline__ f32x4_t col_frag(const float* p, int lane, int step) 
 template <int DT>
 __device__ __forceinline__ constexpr int col_token(int g, int e) { return (e >> 2) * 16 + 4 * g + (e & 3); }
 
+constexpr int kAhead = 32;   // chunks whose decays are made at a time
+
 template <int DT, int KP, int VP, int NT>
 struct Smem {
-  static constexpr int CH = Traits<DT>::kChunk, IT = CH / 16, kTiles = IT * (IT + 1) / 2, kWaves = VP / 16 / NT;
+  static constexpr int CH = kChunk, IT = CH / 16, kTiles = IT * (IT + 1) / 2, kWaves = VP / 16 / NT;
   using E = typename Traits<DT>::Elem;
   alignas(16) E q[CH * (KP + 16)];
   alignas(16) E k[CH * (KP + 16)];
   alignas(16) E v[CH * (VP + 16)];
   alignas(16) char p[kTiles * 1024];   // score tiles: fp32, or two bf16 parts
-  alignas(16) float dec[2][4][CH];     // hi, lo, here, rest of Decays
+  // What the decays make, of kAhead chunks: rows {hi, lo, here, rest}, with L the
+  // running sum of log2 a over the chunk up to a token, in the order of the walk:
+  // hi + lo = L, here = 2^L, rest = 2^(end - L) times the factor of k v^T; and 2^end.
+  alignas(16) float dec[kAhead][4][CH];
+  float whole[kAhead];
+  double totals[kWaves];
   alignas(16) float dots[kWaves][CH];
 };
 
@@ -201,20 +208,19 @@ struct Smem {
 constexpr int kStates = 0, kOut = 1, kOutDots = 2;
 
 template <int DT, int KP, int VP, int NT, int MODE, bool VEC>
-__global__ __launch_bounds__(VP / NT * 4, KP == 64 && VP == 64 ? 3 : 2) void k_walk(Walk w) {
+__device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
   constexpr bool OUT = MODE != kStates, DOTS = MODE == kOutDots;
   using Tr = Traits<DT>;
   using Frag = typename Tr::Frag;
   using SM = Smem<DT, KP, VP, NT>;
-  constexpr int CH = Tr::kChunk, KG = Tr::kGroup, IT = CH / 16, PG = CH / KG, TPG = KG / 16;
+  constexpr int CH = kChunk, KG = Tr::kGroup, IT = CH / 16, PG = CH / KG, TPG = KG / 16;
   constexpr int KT = KP / 16, FE = KG / 4, THREADS = VP / NT * 4, WAVES = VP / 16 / NT;
   constexpr int KPITCH = KP + 16, VPITCH = VP + 16;
-  extern __shared__ char smem_raw[];
   SM& sm = *reinterpret_cast<SM*>(smem_raw);
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, m = lane & 15;
-  const int seg = blockIdx.x % w.segs, nh = blockIdx.x / w.segs, n = nh / w.H, h = nh % w.H;
+  const int seg = block % w.segs, nh = block / w.segs, n = nh / w.H, h = nh % w.H;
   const int len = w.lengths ? min(max(w.lengths[n], 0), w.T) : w.T;
   const int b = seg * w.seg, e = min(b + w.seg, w.T);
   const int chunks = (e - b + CH - 1) / CH;
@@ -231,15 +237,56 @@ __global__ __launch_bounds__(VP / NT * 4, KP == 64 && VP == 64 ? 3 : 2) void k_w
   auto first = [&](int c) { return b + (rev ? chunks - 1 - c : c) * CH; };
   // a chunk of which nothing exists: its outputs are zero, the state stays
   auto dead = [&](int t0) { return t0 >= len; };
-  f32x4_t td;
-  const long d0 = (long)nh * w.chunks;
   auto load = [&](int c) {
     const int t0 = first(c);
     if (c >= chunks || dead(t0)) return;
     if constexpr (OUT) tq.load(qp, w.qs.t, w.K, t0, rev, hi);
     tk.load(kp, w.ks.t, w.K, t0, rev, hi);
     tv.load(vp, w.vs.t, w.V, t0, rev, hi);
-    if (wave == WAVES - 1 && lane < CH) td = w.dec.rows[(d0 + t0 / CH) * CH + lane];
+  };
+
+  // The decays of chunks c .. c + kAhead - 1, half a wave each.  Backward in time a
+  // token's own decay lies behind it: the next one's is between.
+  double total = 0.0;
+  auto decays = [&](int c) {
+    const int half = lane >> 5, i = lane & 31;
+    constexpr int N2 = kAhead / 2 / WAVES;
+    float gate[N2];
+    bool on[N2];
+#pragma unroll
+    for (int u = 0; u < N2; ++u) {
+      const int ch = c + 2 * (wave + u * WAVES) + half, t = first(ch) + (rev ? CH - i : i);
+      on[u] = ch < chunks && t < len;
+      gate[u] = 0.0f;
+      if (on[u]) gate[u] = load_elem(w.gate, n * w.gs.n + t * w.gs.t + h * w.gs.h, w.gate_f32);
+    }
+#pragma unroll 1
+    for (int u = 0; u < N2; ++u) {
+      const int at = 2 * (wave + u * WAVES) + half;
+      if (c + 2 * (wave + u * WAVES) >= chunks) break;
+      float gu = gate[0];
+      bool ou = on[0];
+#pragma unroll
+      for (int v = 1; v < N2; ++v) {
+        gu = u == v ? gate[v] : gu;
+        ou = u == v ? on[v] : ou;
+      }
+      double l2 = ou ? log2_decay(gu, w.form) : 0.0;
+#pragma unroll
+      for (int s = 1; s < CH; s *= 2) {
+        const double o = __shfl_up(l2, s, 32);
+        if (i >= s) l2 += o;
+      }
+      const double end = __shfl(l2, 31, 32);
+      total += end;
+      const float hi = (float)l2;
+      float(&d)[4][CH] = sm.dec[at];
+      d[0][i] = hi;
+      d[1][i] = (float)(l2 - (double)hi);
+      d[2][i] = exp2_parts(l2);
+      d[3][i] = w.kv * exp2_parts(end - l2);
+      if (i == 0) sm.whole[at] = exp2_parts(end);
+    }
   };
 
   // the wave's 16 columns of the state, c0 + m; its rows that lane group g holds
@@ -255,7 +302,7 @@ __global__ __launch_bounds__(VP / NT * 4, KP == 64 && VP == 64 ? 3 : 2) void k_w
   // A state in memory: element (kk, vv) at kk sk + vv sv.  What the tile has past K
   // rows or V columns reads as zero and is not written.
   const int sk = w.rows_first ? w.V : 1, sv = w.rows_first ? 1 : w.K, cells = w.K * w.V * 4;
-  auto cell = [&](int kk, int vv) { return kk < w.K && vv < w.V ? (uint32_t)(kk * sk + vv * sv) * 4u : kNoColumn; };
+  auto cell = [&](int kk, int vv) { return (kk < w.K) & (vv < w.V) ? (uint32_t)(kk * sk + vv * sv) * 4u : kNoColumn; };
   f32x4_t S[KT][NT];
   if (w.init) {
     const auto rs = rows_of(reinterpret_cast<const char*>(w.init + nh * w.init_nh + seg * w.init_seg), 1, 0, cells);
@@ -280,6 +327,7 @@ __global__ __launch_bounds__(VP / NT * 4, KP == 64 && VP == 64 ? 3 : 2) void k_w
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) S[kt][nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
+  decays(0);
   auto put_state = [&](float* p, float f) {
     const auto rs = rows_of(reinterpret_cast<const char*>(p), 1, 0, cells);
     // (offsets made here, not kept from above through the loop: 64 registers)
@@ -302,17 +350,15 @@ __global__ __launch_bounds__(VP / NT * 4, KP == 64 && VP == 64 ? 3 : 2) void k_w
   for (int c = 0; c < chunks; ++c) {
     const int t0 = first(c);
     const bool live = !dead(t0);
-    const float(&d)[4][CH] = sm.dec[c & 1];
+    if (c > 0 && c % kAhead == 0) decays(c);
+    const float(&d)[4][CH] = sm.dec[c % kAhead];
     if (live) {
       if constexpr (OUT) tq.store(sm.q);
       tk.store(sm.k);
       tv.store(sm.v);
-      if (wave == WAVES - 1 && lane < CH)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) sm.dec[c & 1][u][lane] = td[u];
     }
-    const float whole = w.dec.whole[d0 + t0 / CH];
     __syncthreads();
+    const float whole = sm.whole[c % kAhead];
     load(c + 1);
     __builtin_amdgcn_sched_barrier(0);
     // the rows that outputs are multiplied with, on their way from here
@@ -517,77 +563,92 @@ __global__ __launch_bounds__(VP / NT * 4, KP == 64 && VP == 64 ? 3 : 2) void k_w
     if (to) put_state(to, f);
     to = more;
   }
-  if (w.decay && tid == 0) {
-    double sum = 0.0;
-    for (int c = 0; c < chunks; ++c) sum += w.dec.end[d0 + first(c) / CH];
-    w.decay[(long)nh * w.segs + seg] = exp2_parts(sum);
+  if (w.decay) {
+    total += __shfl_xor(total, 32);
+    if (lane == 0) sm.totals[wave] = total;
+    __syncthreads();
+    if (tid == 0) {
+      double sum = 0.0;
+#pragma unroll
+      for (int u = 0; u < WAVES; ++u) sum += sm.totals[u];
+      w.decay[(long)nh * w.segs + seg] = exp2_parts(sum);
+    }
   }
 }
 
-#ifndef NTX
-#define NTX 2
-#endif
-template <int DT, int KP, int VP>
-hipError_t launch_walk_sized(const Walk& w, hipStream_t s) {
-  constexpr int NT = VP == 128 ? NTX : 1;
-  auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((long)w.N * w.H * w.segs)), dim3(VP / NT * 4), sizeof(Smem<DT, KP, VP, NT>), s, w);
-    return hipGetLastError();
-  };
-  // whole vectors, rows that do not overlap (a row past the last that exists is
-  // then past its end too), 64 of them within 2^31 bytes
+// Columns of the state to a wave, in tiles of 16: blocks of four waves either way.
+template <int VP> constexpr int kTilesOf = VP / 64;
+template <int DT, int KP, int VP> using SmemOf = Smem<DT, KP, VP, kTilesOf<VP>>;
+
+template <int DT, int KP, int VP, int MODE, bool VEC>
+__global__ __launch_bounds__(256, KP == 64 && VP == 64 ? 3 : 2) void k_walk(Walk w) {
+  extern __shared__ char smem[];
+  walk<DT, KP, VP, kTilesOf<VP>, MODE, VEC>(w, blockIdx.x, smem);
+}
+
+// A walk with state [K][V] and one with [V][K], of `units` blocks each: of 16
+// blocks in a row eight are the one's, on all XCDs, and eight the other's.
+template <int DT, int KP, int VP, int MODE, int MODE2>
+__global__ __launch_bounds__(256, KP == 64 && VP == 64 ? 3 : 2) void k_walk2(Walk w, Walk w2, int units) {
+  extern __shared__ char smem[];
+  const int unit = (int)(blockIdx.x >> 4) * 8 + (int)(blockIdx.x & 7);
+  if (unit >= units) return;
+  if ((blockIdx.x & 8) == 0) walk<DT, KP, VP, kTilesOf<VP>, MODE, true>(w, unit, smem);
+  else walk<DT, VP, KP, kTilesOf<KP>, MODE2, true>(w2, unit, smem);
+}
+
+// Whole vectors, rows that do not overlap (a row past the last that exists is then
+// past its end too), 64 of them within 2^31 bytes.
+template <int DT> bool vectors(const Walk& w) {
   constexpr int kVec = 16 / kBytes<DT>;
   auto fits = [](const Str& t, int len) {
     return len % kVec == 0 && (t.n | t.t | t.h) % kVec == 0 && t.t >= len && t.t < (1L << 31) / 4 / 64;
   };
-  const bool vec = fits(w.qs, w.K) && fits(w.ks, w.K) && fits(w.vs, w.V) && (!w.y || fits(w.ys, w.V)) && (!w.x || fits(w.xs, w.V));
-  if (!w.y) return vec ? go(k_walk<DT, KP, VP, NT, kStates, true>) : go(k_walk<DT, KP, VP, NT, kStates, false>);
-  if (!w.x) return vec ? go(k_walk<DT, KP, VP, NT, kOut, true>) : go(k_walk<DT, KP, VP, NT, kOut, false>);
-  return vec ? go(k_walk<DT, KP, VP, NT, kOutDots, true>) : go(k_walk<DT, KP, VP, NT, kOutDots, false>);
+  return (!w.y || fits(w.qs, w.K)) && fits(w.ks, w.K) && fits(w.vs, w.V) && (!w.y || fits(w.ys, w.V)) && (!w.x || fits(w.xs, w.V));
 }
 
-template <int CH>
-__global__ __launch_bounds__(256) void k_decays(DecayArgs a) {
-  const long unit = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (unit >= a.units) return;
-  const int nh = (int)(unit / a.chunks), c = (int)(unit % a.chunks), n = nh / a.H, h = nh % a.H;
-  const int len = a.lengths ? min(max(a.lengths[n], 0), a.T) : a.T;
-#pragma unroll
-  for (int rev = 0; rev < 2; ++rev) {
-    const Decays& to = a.to[rev];
-    if (!to.rows) continue;
-    // backward in time a token's own decay lies behind it: the next one's is between
-    const int t = c * CH + (rev ? CH - lane : lane);
-    double l2 = 0.0;
-    if (lane < CH && t < len) l2 = log2_decay(load_elem(a.gate, n * a.gs.n + t * a.gs.t + h * a.gs.h, a.gate_f32), a.form);
-#pragma unroll
-    for (int s = 1; s < CH; s *= 2) {
-      const double o = __shfl_up(l2, s);
-      if (lane >= s) l2 += o;
-    }
-    const double end = __shfl(l2, CH - 1);
-    if (lane < CH) {
-      const float hi = (float)l2;
-      to.rows[unit * CH + lane] = f32x4_t{hi, (float)(l2 - (double)hi), exp2_parts(l2), a.kv[rev] * exp2_parts(end - l2)};
-      if (lane == 0) {
-        to.whole[unit] = exp2_parts(end);
-        to.end[unit] = end;
-      }
-    }
-  }
+inline int mode_of(const Walk& w) { return !w.y ? kStates : w.x ? kOutDots : kOut; }
+
+template <int DT, int KP, int VP>
+hipError_t launch_walk_sized(const Walk& w, hipStream_t s) {
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((long)w.N * w.H * w.segs)), dim3(256), sizeof(SmemOf<DT, KP, VP>), s, w);
+    return hipGetLastError();
+  };
+  const int mode = mode_of(w);
+  if (vectors<DT>(w))
+    return mode == kStates ? go(k_walk<DT, KP, VP, kStates, true>)
+                           : mode == kOut ? go(k_walk<DT, KP, VP, kOut, true>) : go(k_walk<DT, KP, VP, kOutDots, true>);
+  return mode == kStates ? go(k_walk<DT, KP, VP, kStates, false>)
+                         : mode == kOut ? go(k_walk<DT, KP, VP, kOut, false>) : go(k_walk<DT, KP, VP, kOutDots, false>);
+}
+
+// w: outputs; w2: states or outputs.
+template <int DT, int KP, int VP>
+hipError_t launch_walk2_sized(const Walk& w, const Walk& w2, hipStream_t s) {
+  const long units = (long)w.N * w.H * w.segs;
+  auto go = [&](auto kernel) {
+    constexpr size_t lds = sizeof(SmemOf<DT, KP, VP>) > sizeof(SmemOf<DT, VP, KP>) ? sizeof(SmemOf<DT, KP, VP>) : sizeof(SmemOf<DT, VP, KP>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((units + 7) / 8 * 16)), dim3(256), lds, s, w, w2, (int)units);
+    return hipGetLastError();
+  };
+  if (mode_of(w2) == kStates) return w.x ? go(k_walk2<DT, KP, VP, kOutDots, kStates>) : go(k_walk2<DT, KP, VP, kOut, kStates>);
+  return w.x ? go(k_walk2<DT, KP, VP, kOutDots, kOut>) : go(k_walk2<DT, KP, VP, kOut, kOut>);
 }
 
 template <int DT>
-hipError_t launch_decays_dt(const DecayArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(k_decays<Traits<DT>::kChunk>, dim3((unsigned)((a.units + 3) / 4)), dim3(256), 0, s, a);
-  return hipGetLastError();
-}
-
-template <int DT>
-hipError_t launch_walk_dt(const Walk& w, hipStream_t s) {
-  if (w.K <= 64) return w.V <= 64 ? launch_walk_sized<DT, 64, 64>(w, s) : launch_walk_sized<DT, 64, 128>(w, s);
-  return w.V <= 64 ? launch_walk_sized<DT, 128, 64>(w, s) : launch_walk_sized<DT, 128, 128>(w, s);
+hipError_t launch_walk_dt(const Walk& w, const Walk* beside, hipStream_t s) {
+  auto sized = [&](auto one, auto two) {   // the rounded sizes of K and V
+    constexpr int KP = decltype(one)::value, VP = decltype(two)::value;
+    if (!beside) return launch_walk_sized<DT, KP, VP>(w, s);
+    if (vectors<DT>(w) && vectors<DT>(*beside)) return launch_walk2_sized<DT, KP, VP>(w, *beside, s);
+    const hipError_t e = launch_walk_sized<DT, KP, VP>(w, s);
+    return e != hipSuccess ? e : launch_walk_sized<DT, VP, KP>(*beside, s);
+  };
+  using A = std::integral_constant<int, 64>;
+  using B = std::integral_constant<int, 128>;
+  if (w.K <= 64) return w.V <= 64 ? sized(A{}, A{}) : sized(A{}, B{});
+  return w.V <= 64 ? sized(B{}, A{}) : sized(B{}, B{});
 }
 
 }  // namespace
