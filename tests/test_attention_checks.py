@@ -292,3 +292,30 @@ def test_oracles_hold_by_hand():
     assert np.allclose(n, np.array([[3, 4]]) / np.sqrt(12.5))
     n = A.block_norm(np.array([[3.0, 5.0]]), layer=True, eps=0.0)["y"][0]
     assert np.allclose(n, [[-1, 1]])
+
+
+def test_sizes_of_2_31_are_refused():
+    """(A size that the library's 32 bits cannot hold; the tensors are one element seen often.)"""
+    one = torch.zeros(1)
+    many = one.expand(2 ** 31, 8)
+    with pytest.raises(bc.BoxConvError, match="2\\^31"):
+        bc.block_norm_fwd(many, r=many)
+    with pytest.raises(bc.BoxConvError, match="2\\^31"):
+        bc.block_norm_bwd(many, grad_r=many, grad_z=many)
+    t = one.expand(2 ** 31, 1, 8)
+    with pytest.raises(bc.BoxConvError, match="2\\^31"):
+        bc.linear_attention_step(t, t, t, one.expand(2 ** 31, 1), one.expand(1, 1, 8, 8), t)
+    t = one.expand(1, 2 ** 31, 1, 8)
+    with pytest.raises(bc.BoxConvError, match="2\\^31"):
+        bc.linear_attention_fwd(t, t, t, one.expand(1, 2 ** 31, 1), t)
+
+
+def test_arguments_that_are_no_tensors_are_refused():
+    t, g, s = torch.zeros(1, 1, 8), torch.zeros(1, 1), torch.zeros(1, 1, 8, 8)
+    for bad in (None, 3.0, [1.0], t.numpy(), t.to_sparse()):
+        with pytest.raises((bc.BoxConvError, RuntimeError)):
+            bc.linear_attention_step(bad, t, t, g, s, t)
+        with pytest.raises((bc.BoxConvError, RuntimeError)):
+            bc.linear_attention_fwd(t[None], bad, t[None], g[None], t[None])
+        with pytest.raises((bc.BoxConvError, RuntimeError)):
+            bc.block_norm_fwd(bad, r=t)

@@ -406,3 +406,28 @@ def test_steps_follow_a_prompt(dt):
         c.y[:, t] = y
     c.s_last = pool
     c.check(("y", "s_last"))
+
+
+def test_calls_of_one_layout():
+    """Layouts are checked when they are met first: later calls of the same layout take
+    their own tensors, numbers and pointers, and another layout is checked again."""
+    N, H, D = 2, 3, 16
+    mk = lambda seed: torch.randn(N, H, D, generator=torch.Generator().manual_seed(seed)).cuda()
+    q, k, v, y = mk(1), mk(2), mk(3), torch.empty(N, H, D, device="cuda")
+    g, pool = torch.zeros(N, H, device="cuda"), torch.zeros(N, H, D, D, device="cuda")
+    scale = torch.tensor(1.0)
+    one = bc.linear_attention_step(q, k, v, g, pool, y, scale=scale).clone()
+    scale.fill_(2.0)
+    pool.zero_()
+    # (the same tensor for scale, another value; another q in the same place)
+    assert torch.equal(bc.linear_attention_step(q, k, v, g, pool, y, scale=scale), 2 * one)
+    pool.zero_()
+    q.mul_(-1)
+    assert torch.equal(bc.linear_attention_step(q, k, v, g, pool, y, scale=1.0), -one)
+    with pytest.raises(bc.BoxConvError):      # a view that starts off the vectors' alignment
+        flat = torch.zeros(N * H * D + 1, device="cuda")
+        bc.linear_attention_step(flat[1:].view(N, H, D), k, v, g, pool, y)
+    with pytest.raises(bc.BoxConvError):      # of the same shape, rows in another order
+        bc.linear_attention_step(q, k, v, g, torch.zeros(N, D, H, D, device="cuda").transpose(1, 2), y)
+    with pytest.raises(bc.BoxConvError):
+        bc.linear_attention_step(q.cpu(), k, v, g, pool, y)
