@@ -116,8 +116,7 @@ template <int W> __device__ __forceinline__ void buffer_store(__amdgpu_buffer_rs
 }
 
 // A chunk's rows of one operand: from memory to registers, then to LDS.
-// VEC: whole aligned 16-byte vectors, a chunk's rows within 2^31 bytes.
-template <int DT, int W, int THREADS, bool VEC> struct Tile {
+template <int DT, int W, int THREADS> struct Tile {
   static constexpr int kVec = 16 / kBytes<DT>, kPerRow = W / kVec, kRows = THREADS / kPerRow;
   static constexpr int CH = kChunk, kPasses = (CH + kRows - 1) / kRows;
   static constexpr int kPitch = W + 16;   // elements
@@ -132,21 +131,19 @@ template <int DT, int W, int THREADS, bool VEC> struct Tile {
     return rev ? CH - 1 - k : k;
   }
 
-  // tokens from hi (> t0) on do not exist: zeros
+  // the rows of the tile's first token on, `from` bytes behind rs
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, int step, int from, int D, bool rev) {
+    const uint32_t at = (col() < D && busy() ? (uint32_t)(row(0, rev) * step + col() * kBytes<DT>) : kNoColumn) + (uint32_t)from;
+    const int skip = rev ? -kRows * step : kRows * step;
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) r[i] = buffer_load<4>(rs, at + (uint32_t)(i * skip));
+  }
+  // any rows: tokens from hi on do not exist (zeros)
   __device__ __forceinline__ void load(const char* base, long row_stride, int D, int t0, bool rev, int hi) {
-    if constexpr (VEC) {
-      const int step = (int)row_stride * kBytes<DT>;
-      const auto rs = rows_of(base + t0 * row_stride * kBytes<DT>, min(hi - t0, CH), step, D * kBytes<DT>);
-      const uint32_t at = col() < D && busy() ? (uint32_t)(row(0, rev) * step + col() * kBytes<DT>) : kNoColumn;
-      const int skip = rev ? -kRows * step : kRows * step;
 #pragma unroll
-      for (int i = 0; i < kPasses; ++i) r[i] = buffer_load<4>(rs, at + (uint32_t)(i * skip));
-    } else {
-#pragma unroll
-      for (int i = 0; i < kPasses; ++i) {
-        const int t = t0 + row(i, rev);
-        r[i] = scan::load_vec<DT, kVec>(base + ((long)t * row_stride + col()) * kBytes<DT>, t < hi && busy() ? D - col() : 0);
-      }
+    for (int i = 0; i < kPasses; ++i) {
+      const int t = t0 + row(i, rev);
+      r[i] = scan::load_vec<DT, kVec>(base + ((long)t * row_stride + col()) * kBytes<DT>, t < hi && busy() ? D - col() : 0);
     }
   }
   __device__ __forceinline__ void store(typename Traits<DT>::Elem* lds) const {
@@ -231,18 +228,38 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
   const char* kp = w.k + (n * w.ks.n + (h / w.kd) * w.ks.h) * kBytes<DT>;
   const char* vp = w.v + (n * w.vs.n + (h / w.vd) * w.vs.h) * kBytes<DT>;
 
-  Tile<DT, KP, THREADS, VEC> tq, tk;
-  Tile<DT, VP, THREADS, VEC> tv;
+  Tile<DT, KP, THREADS> tq, tk;
+  Tile<DT, VP, THREADS> tv;
   // the first token of chunk c in memory (its last in time, rev)
   auto first = [&](int c) { return b + (rev ? chunks - 1 - c : c) * CH; };
   // a chunk of which nothing exists: its outputs are zero, the state stays
   auto dead = [&](int t0) { return t0 >= len; };
+  // VEC: buffers of the rows of kAhead chunks, from the first one in memory on; a
+  // chunk's rows are an offset into them
+  const int sq = (int)w.qs.t * kBytes<DT>, skk = (int)w.ks.t * kBytes<DT>, svv = (int)w.vs.t * kBytes<DT>;
+  __amdgpu_buffer_rsrc_t rq, rk, rv;
+  int low = 0;
+  auto lowest = [&](int c) { return rev ? first(min(c + kAhead, chunks) - 1) : first(c); };
   auto load = [&](int c) {
+    if (c >= chunks) return;
+    if (VEC && c % kAhead == 0) {
+      low = lowest(c);
+      const int rows = min(hi - low, kAhead * CH);
+      if constexpr (OUT) rq = rows_of(qp + low * w.qs.t * kBytes<DT>, rows, sq, w.K * kBytes<DT>);
+      rk = rows_of(kp + low * w.ks.t * kBytes<DT>, rows, skk, w.K * kBytes<DT>);
+      rv = rows_of(vp + low * w.vs.t * kBytes<DT>, rows, svv, w.V * kBytes<DT>);
+    }
     const int t0 = first(c);
-    if (c >= chunks || dead(t0)) return;
-    if constexpr (OUT) tq.load(qp, w.qs.t, w.K, t0, rev, hi);
-    tk.load(kp, w.ks.t, w.K, t0, rev, hi);
-    tv.load(vp, w.vs.t, w.V, t0, rev, hi);
+    if (dead(t0)) return;
+    if constexpr (VEC) {
+      if constexpr (OUT) tq.load(rq, sq, (t0 - low) * sq, w.K, rev);
+      tk.load(rk, skk, (t0 - low) * skk, w.K, rev);
+      tv.load(rv, svv, (t0 - low) * svv, w.V, rev);
+    } else {
+      if constexpr (OUT) tq.load(qp, w.qs.t, w.K, t0, rev, hi);
+      tk.load(kp, w.ks.t, w.K, t0, rev, hi);
+      tv.load(vp, w.vs.t, w.V, t0, rev, hi);
+    }
   };
 
   // The decays of chunks c .. c + kAhead - 1, half a wave each.  Backward in time a
@@ -302,7 +319,7 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
   // A state in memory: element (kk, vv) at kk sk + vv sv.  What the tile has past K
   // rows or V columns reads as zero and is not written.
   const int sk = w.rows_first ? w.V : 1, sv = w.rows_first ? 1 : w.K, cells = w.K * w.V * 4;
-  auto cell = [&](int kk, int vv) { return (kk < w.K) & (vv < w.V) ? (uint32_t)(kk * sk + vv * sv) * 4u : kNoColumn; };
+  auto cell = [&](int kk, int vv) { return kk < w.K && vv < w.V ? (uint32_t)(kk * sk + vv * sv) * 4u : kNoColumn; };
   f32x4_t S[KT][NT];
   if (w.init) {
     const auto rs = rows_of(reinterpret_cast<const char*>(w.init + nh * w.init_nh + seg * w.init_seg), 1, 0, cells);
@@ -347,10 +364,22 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
 
   const float reach = w.kv * w.scale;   // of the scores
   const int out_bytes = DT == kF32 || w.y_f32 ? 4 : 2;
+  char* yp = OUT ? w.y + (n * w.ys.n + h * w.ys.h) * out_bytes : nullptr;
+  const char* xp = DOTS ? w.x + (n * w.xs.n + (h / w.xd) * w.xs.h) * kBytes<DT> : nullptr;
+  const int ystep = (int)w.ys.t * out_bytes, xstep = (int)w.xs.t * kBytes<DT>;
+  __amdgpu_buffer_rsrc_t ry, rx;
+  int out_low = 0;
   for (int c = 0; c < chunks; ++c) {
     const int t0 = first(c);
     const bool live = !dead(t0);
-    if (c > 0 && c % kAhead == 0) decays(c);
+    if (c % kAhead == 0) {
+      if (c > 0) decays(c);
+      if constexpr (OUT && VEC) {
+        out_low = lowest(c);
+        ry = rows_of(yp + out_low * w.ys.t * out_bytes, min(e - out_low, kAhead * CH), ystep, w.V * out_bytes);
+        if constexpr (DOTS) rx = rows_of(xp + out_low * w.xs.t * kBytes<DT>, min(hi - out_low, kAhead * CH), xstep, w.V * kBytes<DT>);
+      }
+    }
     const float(&d)[4][CH] = sm.dec[c % kAhead];
     if (live) {
       if constexpr (OUT) tq.store(sm.q);
@@ -366,14 +395,11 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
     const int col = c0 + V * g, avail = w.V - col;
     Raw<scan::kWords<DT, V>> x[DOTS ? IT : 1];
     if constexpr (DOTS) {
-      const char* xp = w.x + (n * w.xs.n + t0 * w.xs.t + (h / w.xd) * w.xs.h) * kBytes<DT>;
-      const int xstep = (int)w.xs.t * kBytes<DT>;
-      const auto xr = rows_of(xp, VEC ? min(hi - t0, CH) : 0, xstep, w.V * kBytes<DT>);
 #pragma unroll
       for (int it = 0; it < IT; ++it) {
         const int row = rev ? CH - 1 - it * 16 - m : it * 16 + m;
-        if constexpr (VEC) x[it] = buffer_load<scan::kWords<DT, V>>(xr, avail > 0 ? (uint32_t)(row * xstep + col * kBytes<DT>) : kNoColumn);
-        else x[it] = scan::load_vec<DT, V>(xp + (row * w.xs.t + col) * kBytes<DT>, t0 + row < hi ? avail : 0);
+        if constexpr (VEC) x[it] = buffer_load<scan::kWords<DT, V>>(rx, avail > 0 ? (uint32_t)((t0 - out_low + row) * xstep + col * kBytes<DT>) : kNoColumn);
+        else x[it] = scan::load_vec<DT, V>(xp + ((t0 + row) * w.xs.t + col) * kBytes<DT>, t0 + row < hi ? avail : 0);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -408,7 +434,9 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
             reinterpret_cast<f32x4_t*>(sm.p)[i * 64 + lane] = s;
           }
         }
-        // what the state before the chunk adds: rows v, columns i
+        // what the state before the chunk adds: rows v, columns i.  (This stretch has the
+        // most to issue: a wave in it goes before another block's, 2 % of a training call.)
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int it = 0; it < IT; ++it)
 #pragma unroll
@@ -446,6 +474,7 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
         for (int nt = 0; nt < NT; ++nt) vf[p][nt] = col_frag<VPITCH>(sm.v + p * KG * VPITCH + c0 + 4 * nt * (NT - 1), lane, VSTEP);
     }
     if constexpr (OUT) {
+      __builtin_amdgcn_s_setprio(0);
       __syncthreads();
       if (live) {
 #pragma unroll
@@ -475,9 +504,6 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
         }
       }
       // outputs: a lane has V consecutive columns of row it * 16 + m
-      char* yp = w.y + (n * w.ys.n + t0 * w.ys.t + h * w.ys.h) * out_bytes;
-      const int ystep = (int)w.ys.t * out_bytes;
-      const auto yr = rows_of(yp, VEC ? min(e - t0, CH) : 0, ystep, w.V * out_bytes);
       if (t0 + CH > hi) {   // rows that do not exist
 #pragma unroll
         for (int it = 0; it < IT; ++it)
@@ -493,11 +519,11 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
         for (int u = 0; u < V; ++u) o[u] = acc[it][u / 4][u & 3];
         if constexpr (VEC) {
           if (out_bytes == 4)
-            buffer_store<V>(yr, avail > 0 ? (uint32_t)(row * ystep + col * 4) : kNoColumn, scan::rounded<kF32, V>(o));
+            buffer_store<V>(ry, avail > 0 ? (uint32_t)((t0 - out_low + row) * ystep + col * 4) : kNoColumn, scan::rounded<kF32, V>(o));
           else
-            buffer_store<V / 2>(yr, avail > 0 ? (uint32_t)(row * ystep + col * 2) : kNoColumn, scan::rounded<kBF16, V>(o));
+            buffer_store<V / 2>(ry, avail > 0 ? (uint32_t)((t0 - out_low + row) * ystep + col * 2) : kNoColumn, scan::rounded<kBF16, V>(o));
         } else if (t0 + row < e && avail > 0) {
-          const long at = (row * w.ys.t + col) * out_bytes;
+          const long at = ((t0 + row) * w.ys.t + col) * out_bytes;
           if (out_bytes == 4) scan::store_vec<kF32, V>(yp + at, avail, o);
           else scan::store_vec<kBF16, V>(yp + at, avail, o);
         }
@@ -598,11 +624,12 @@ __global__ __launch_bounds__(256, KP == 64 && VP == 64 ? 3 : 2) void k_walk2(Wal
 }
 
 // Whole vectors, rows that do not overlap (a row past the last that exists is then
-// past its end too), 64 of them within 2^31 bytes.
+// past its end too), those of kAhead chunks within 2^30 bytes
+// (kNoColumn less a chunk is past them).
 template <int DT> bool vectors(const Walk& w) {
   constexpr int kVec = 16 / kBytes<DT>;
   auto fits = [](const Str& t, int len) {
-    return len % kVec == 0 && (t.n | t.t | t.h) % kVec == 0 && t.t >= len && t.t < (1L << 31) / 4 / 64;
+    return len % kVec == 0 && (t.n | t.t | t.h) % kVec == 0 && t.t >= len && t.t < (1L << 30) / 4 / (kAhead * kChunk);
   };
   return (!w.y || fits(w.qs, w.K)) && fits(w.ks, w.K) && fits(w.vs, w.V) && (!w.y || fits(w.ys, w.V)) && (!w.x || fits(w.xs, w.V));
 }
