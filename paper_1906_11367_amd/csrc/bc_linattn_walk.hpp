@@ -60,33 +60,41 @@ __device__ __forceinline__ uint32_t round_pair(float lo, float hi) {
 template <int DT, int P> struct Split {
   typename Traits<DT>::Frag part[DT == kBF16 ? P : 1];
 };
+// x: the values of an operand as two tiles of accumulators.  What a part leaves is the
+// tile less that part, exactly: the matrix unit subtracts (minus_of).
 template <int P>
-__device__ __forceinline__ Split<kBF16, P> split(const float (&x)[8]) {
+__device__ __forceinline__ Split<kBF16, P> split(const f32x4_t (&x)[2], const bf16x8_t (&minus)[2]) {
   Split<kBF16, P> s;
-  float rest[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) rest[e] = x[e];
+  f32x4_t rest[2] = {x[0], x[1]};
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     Raw<4> w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {   // two values an instruction
-      w[i] = round_pair(rest[2 * i], rest[2 * i + 1]);
-      if (p + 1 < P) {
-        rest[2 * i] -= __uint_as_float(w[i] << 16);
-        rest[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
-      }
-    }
+    for (int i = 0; i < 4; ++i) w[i] = round_pair(rest[i / 2][2 * (i & 1)], rest[i / 2][2 * (i & 1) + 1]);
     s.part[p] = __builtin_bit_cast(bf16x8_t, w);
+    if (p + 1 < P) {
+      rest[0] = mma(minus[0], s.part[p], rest[0]);
+      rest[1] = mma(minus[1], s.part[p], rest[1]);
+    }
   }
   return s;
 }
 template <int P>
-__device__ __forceinline__ Split<kF32, P> split(const float (&x)[4]) {
+__device__ __forceinline__ Split<kF32, P> split(const f32x4_t (&x)[1], const f32x4_t (&)[2]) {
   Split<kF32, P> s;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) s.part[0][e] = x[e];
+  s.part[0] = x[0];
   return s;
+}
+// The operands that take an operand from its two tiles: row 4 g + r of tile i is the
+// operand's element 8 g + 4 i + r, so there they have -1, and zeros elsewhere.
+template <int DT> __device__ __forceinline__ void minus_of(typename Traits<DT>::Frag (&minus)[2], int lane) {
+  if constexpr (DT == kBF16) {
+    const bool on = lane >> 4 == (lane & 15) >> 2;
+    const Raw<2> w = {on && (lane & 2) == 0 ? (lane & 1 ? 0xbf800000u : 0xbf80u) : 0u,
+                      on && (lane & 2) != 0 ? (lane & 1 ? 0xbf800000u : 0xbf80u) : 0u};
+    minus[0] = __builtin_bit_cast(bf16x8_t, Raw<4>{w[0], w[1], 0u, 0u});
+    minus[1] = __builtin_bit_cast(bf16x8_t, Raw<4>{0u, 0u, w[0], w[1]});
+  }
 }
 // (fp32 needs but one; smaller parts are added first)
 template <int DT, int P> constexpr int kParts = DT == kBF16 ? P : 1;
@@ -362,6 +370,8 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
 
   if (w.first) put_state(w.first + nh * w.last2_nh, 1.0f);
 
+  Frag minus[2];
+  minus_of<DT>(minus, lane);
   const float reach = w.kv * w.scale;   // of the scores
   const int out_bytes = DT == kF32 || w.y_f32 ? 4 : 2;
   char* yp = OUT ? w.y + (n * w.ys.n + h * w.ys.h) * out_bytes : nullptr;
@@ -446,10 +456,10 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
           Split<DT, 2> sp[NT];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            float x[FE];
+            f32x4_t x[TPG];
 #pragma unroll
-            for (int u = 0; u < FE; ++u) x[u] = S[kg * TPG + u / 4][nt][u & 3];
-            sp[nt] = split<2>(x);
+            for (int u = 0; u < TPG; ++u) x[u] = S[kg * TPG + u][nt];
+            sp[nt] = split<2>(x, minus);
           }
           Frag f[IT];
 #pragma unroll
@@ -547,10 +557,10 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
         Split<DT, 3> sp[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float x[FE];
+          f32x4_t x[TPG];
 #pragma unroll
-          for (int u = 0; u < FE; ++u) x[u] = (float)vf[p][nt][u] * d[3][p * KG + col_token<DT>(g, u)];
-          sp[nt] = split<3>(x);
+          for (int u = 0; u < FE; ++u) x[u / 4][u & 3] = (float)vf[p][nt][u] * d[3][p * KG + col_token<DT>(g, u)];
+          sp[nt] = split<3>(x, minus);
         }
         // four tiles of rows at a time, part by part: products that follow one another
         // add to different accumulators
