@@ -518,7 +518,13 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, waves_of(DT, W, BWD, GATE &&
   }
 }
 
-constexpr int kPartBlocks = 512;   // blocks of the backward, and shares of the weights' gradients
+// Blocks of the backward, and shares of the weights' gradients: 2048 waves or more.
+// With both norms and the weights' gradients, bf16, 65536 rows of 640 (blocks of two
+// waves): 150 us, with 512 blocks 293; 8192 rows of 4096: 98, with 1024 blocks 110.
+constexpr int part_blocks(int W) { return W == 2 ? 1024 : 512; }
+// Rows a block takes at least: a share costs more than a row or two.  600 rows of
+// 4096: 27 us, a block a row 32 to 41; 300 rows of 1024: 12.1, 12.8.
+constexpr int part_rows(int W) { return W == 1 ? 1 : W < 8 ? 2 : 4; }
 
 // The weights' gradients from the blocks' sums part [P][2][C], 32 channels a block,
 // a lane of 32 the blocks p, p + 32, ..., all on their way at once.  With A the sum
@@ -528,16 +534,16 @@ struct WeightGrads {
   float *dw_post, *dscale, *dw_pre;
   int P, C;
 };
-__global__ __launch_bounds__(1024) void k_norm_weights(WeightGrads a) {
+template <int BLOCKS> __global__ __launch_bounds__(1024) void k_norm_weights(WeightGrads a) {
   __shared__ float lds[32][33];
   const int blocks = (a.C + 31) / 32, k = blockIdx.x / blocks, col = threadIdx.x & 31, row = threadIdx.x >> 5;
   const int c = min((int)(blockIdx.x % blocks) * 32 + col, a.C - 1);
   if (k == 0 ? !a.dw_post && !a.dscale : !a.dw_pre) return;
-  float v[kPartBlocks / 32], s = 0.0f;
+  float v[BLOCKS / 32], s = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kPartBlocks / 32; ++i) v[i] = a.part[((long)min(row + 32 * i, a.P - 1) * 2 + k) * a.C + c];
+  for (int i = 0; i < BLOCKS / 32; ++i) v[i] = a.part[((long)min(row + 32 * i, a.P - 1) * 2 + k) * a.C + c];
 #pragma unroll
-  for (int i = 0; i < kPartBlocks / 32; ++i) s += row + 32 * i < a.P ? v[i] : 0.0f;
+  for (int i = 0; i < BLOCKS / 32; ++i) s += row + 32 * i < a.P ? v[i] : 0.0f;
   lds[col][row] = s;
   __syncthreads();
   // 32 lanes a channel
@@ -565,9 +571,9 @@ hipError_t launch_norm(NormArgs& a, int* blocks, hipStream_t s) {
   a.per = slots / G;
   a.lanes = 64;
   const bool pow2 = (a.per & (a.per - 1)) == 0 && a.per <= 64;
-  auto go = [&](auto kernel, int threads, int teams, int cap) {
-    const long want = ((long)a.R + teams - 1) / teams;
-    *blocks = (int)std::min<long>(want, BWD ? kPartBlocks : cap);
+  auto go = [&](auto kernel, int threads, int teams, int W) {
+    const long run = (long)teams * (BWD ? part_rows(W) : 1), want = (a.R + run - 1) / run;
+    *blocks = (int)std::min<long>(want, BWD ? part_blocks(W) : fwd_blocks(W));
     a.mode = G == 1 ? kSumTeam : pow2 ? kSumLanes : G <= kFew ? kSumFew : kSumShared;
     hipLaunchKernelGGL(kernel, dim3((unsigned)*blocks), dim3((unsigned)threads), 0, s, a);
     return hipGetLastError();
@@ -575,13 +581,13 @@ hipError_t launch_norm(NormArgs& a, int* blocks, hipStream_t s) {
   if (slots <= 64) {
     a.lanes = 8;
     while (a.lanes < slots) a.lanes *= 2;
-    return go(k_block_norm<DT, 1, 1, BWD, GATE, PRE>, 256, 256 / a.lanes, fwd_blocks(1));
+    return go(k_block_norm<DT, 1, 1, BWD, GATE, PRE>, 256, 256 / a.lanes, 1);
   }
-  if (slots <= 128) return go(k_block_norm<DT, 2, 1, BWD, GATE, PRE>, 128, 1, fwd_blocks(2));
-  if (slots <= 256) return go(k_block_norm<DT, 4, 1, BWD, GATE, PRE>, 256, 1, fwd_blocks(4));
-  if (slots <= 512) return go(k_block_norm<DT, 8, 1, BWD, GATE, PRE>, 512, 1, fwd_blocks(8));
-  if (slots <= 1024) return go(k_block_norm<DT, 16, 1, BWD, GATE, PRE>, 1024, 1, fwd_blocks(16));
-  return go(k_block_norm<DT, 16, 2, BWD, GATE, PRE>, 1024, 1, fwd_blocks(16));
+  if (slots <= 128) return go(k_block_norm<DT, 2, 1, BWD, GATE, PRE>, 128, 1, 2);
+  if (slots <= 256) return go(k_block_norm<DT, 4, 1, BWD, GATE, PRE>, 256, 1, 4);
+  if (slots <= 512) return go(k_block_norm<DT, 8, 1, BWD, GATE, PRE>, 512, 1, 8);
+  if (slots <= 1024) return go(k_block_norm<DT, 16, 1, BWD, GATE, PRE>, 1024, 1, 16);
+  return go(k_block_norm<DT, 16, 2, BWD, GATE, PRE>, 1024, 1, 16);
 }
 
 template <int DT, bool BWD>
@@ -594,7 +600,7 @@ hipError_t launch_norm(NormArgs& a, int* blocks, hipStream_t s) {
 
 bool block_norm_takes(int C, int groups) { return slots_of(C, groups) <= 2048; }
 
-size_t block_norm_workspace_bytes(int R, int C) { return (size_t)std::min(R, kPartBlocks) * 2 * C * 4; }
+size_t block_norm_workspace_bytes(int R, int C) { return (size_t)std::min(R, C <= 1024 ? part_blocks(2) : part_blocks(4)) * 2 * C * 4; }
 
 static Rows rows(const NormRows& t) { return {static_cast<const char*>(t.p), t.stride}; }
 static OutRows out_rows(const NormRows& t) { return {static_cast<char*>(const_cast<void*>(t.p)), t.stride}; }
@@ -630,7 +636,7 @@ hipError_t launch_block_norm(const BlockNorm& b, bool bwd, hipStream_t s) {
   const hipError_t e = b.dt == kBF16 ? launch_norm<kBF16, true>(a, &blocks, s) : launch_norm<kF32, true>(a, &blocks, s);
   if (e != hipSuccess || !weights) return e;
   const WeightGrads w{a.part, b.w_post, b.scale, b.dw_post, b.dscale, b.dw_pre, blocks, b.C};
-  hipLaunchKernelGGL(k_norm_weights, dim3((unsigned)(2 * ((b.C + 31) / 32))), dim3(1024), 0, s, w);
+  hipLaunchKernelGGL(blocks > 512 ? k_norm_weights<1024> : k_norm_weights<512>, dim3((unsigned)(2 * ((b.C + 31) / 32))), dim3(1024), 0, s, w);
   return hipGetLastError();
 }
 
