@@ -578,8 +578,8 @@ typedef struct {
  *   s_last = S_{T-1}.
  * States, sums and decays are fp32 (running sums of log a in fp64); y alone is
  * rounded to its type.  bf16: where the fp32 state or scores meet a bf16 operand
- * on the matrix units they are taken as sums of bf16 parts, two for y (2^-17 of
- * each product), three for the state (2^-25).  gate = -infinity is an exact reset
+ * on the matrix units they are taken as sums of bf16 parts, two for y (2^-16 of
+ * each product), three for the state (2^-24).  gate = -infinity is an exact reset
  * (log a below -10000 is one too); with BC_GATE_LOG a_t > 1 is allowed while
  * states stay inside fp32's range.
  *

@@ -30,14 +30,14 @@ def gather(v, Hx):
 
 def attention_units(T, Dk, Dv, dt, span=1024):
     """Units of 2^-24 of the magnitudes.  Products over Dk or Dv channels, over a
-    chunk's 64 tokens and, in the state, a multiplication and an addition a chunk;
+    chunk's tokens (64 allowed for) and, in the state, a multiplication and an addition a chunk;
     heads that share (at most 16) and the gates' sums over a span of tokens come on
     top (twice a span: q dq less k dk); the decays' logarithms are right to a few
     units of themselves, and x e^-x < 1/2, or e^-x is small enough to lie below the
     rest.  bf16: each score, and each state that a query reads, is a sum of two bf16
-    parts, off by 2^-17 or 128 units of itself."""
+    parts, off by 2^-16 or 256 units of itself."""
     c = Dk + Dv + 64 + 2 * (T // 32 + 1) + 64
-    return c + (256 if dt == "bf16" else 0)
+    return c + (512 if dt == "bf16" else 0)
 
 
 def attention(q, k, v, gate, form, scale, s0=None, lengths=None, dy=None, ds=None):

@@ -8,10 +8,14 @@
 // What bounds it: every tensor is read or written once, a few dozen operations
 // an element, so memory.  A row stays in registers between its statistics: a team
 // of lanes takes a row, 8 consecutive channels (16 bytes of bf16) a slot, no slot
-// across two groups; rows of up to 512 slots' channels share waves, longer ones
-// take a block.  The backward computes the forward's values again (in fp32, none
-// read back rounded) and keeps each lane's share of the weights' gradients over
-// all rows of its block; a second kernel sums the blocks in order.
+// across two groups; rows of up to 64 slots (512 channels) share waves or take one,
+// longer ones take a block.  The backward computes the forward's values again (in
+// fp32, none read back rounded) and keeps each lane's share of the weights'
+// gradients over all rows of its block; a second kernel sums the blocks in order.
+// bf16: a norm with a gate of 16 heads of 128, 16384 rows: 43 us (201 MB, 4.7 TB/s),
+// its gradients 74 (335 MB, 4.5); both norms with the residual sum of 8192 rows of
+// 4096: 58 us (268 MB, 4.7 TB/s), the gradients 98 (403 MB, 4.1).  fp32, 777 rows of
+// 3 x 279: 11 and 18 us, a row's chain of sums.  8 rows: 3.7 us, 7 us with the call.
 #include <algorithm>
 
 #include "bc_common.hpp"
@@ -527,8 +531,9 @@ constexpr int part_blocks(int W) { return W == 2 ? 1024 : 512; }
 constexpr int part_rows(int W) { return W == 1 ? 1 : W < 8 ? 2 : 4; }
 
 // The weights' gradients from the blocks' sums part [P][2][C], 32 channels a block,
-// a lane of 32 the blocks p, p + 32, ..., all on their way at once.  With A the sum
-// of d n act(gate), the gradient to w_post is scale A and that to scale w_post A.
+// a lane of 32 the blocks p, p + 32, ..., all on their way at once (16 MB of 512 x 4096 in
+// 5 us).  With A the sum of d n act(gate), the gradient to w_post is scale A and that to
+// scale w_post A.
 struct WeightGrads {
   const float *part, *w_post, *scale;
   float *dw_post, *dscale, *dw_pre;
