@@ -945,7 +945,7 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, gat
                           form: int = BC_GATE_LOGIT, scale: float = 1.0):
     """One token of N sequences: q [N, Hq, Dk], k [N, Hk, Dk], v [N, Hv, Dv], gate
     [N, H] or [H], state [S, H, Dk, Dv] fp32 (the pool; state_out, default itself,
-    takes the new states), slots [N] int32 -> y [N, H, Dv], dense."""
+    takes the new states), slots [N] int32, none named twice -> y [N, H, Dv], dense."""
     what = "linear_attention_step"
     scale = float(scale)
     tensors = (q, k, v, gate, y, state, state_out, slots)

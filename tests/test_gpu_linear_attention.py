@@ -159,6 +159,23 @@ def test_against_the_oracle(kw):
     c.check()
 
 
+@pytest.mark.parametrize("dt,D", [("f32", 4), ("bf16", 8)])
+def test_segments_of_many_chunks(dt, D):
+    """Heads enough for segments of 2048 tokens, without kept states of all 2113: what is
+    made for 32 chunks at a time is made again within a segment, and sequences end
+    before, at and after such a place."""
+    say(dt)
+    c = Case(8, 2113, 64, D, D, dt, start=True, lengths=[2113, 2048, 1025, 1024, 1023, 0, 1500, 33])
+    c.forward()
+    c.check(("y", "s_last"))
+    c.backward()
+    c.check()
+    c.states = None
+    c.y.fill_(float("nan"))
+    c.forward()
+    c.check(("y", "s_last"))
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_without_kept_states_and_optional_outputs(dt):
     """Inference: the same outputs without states, last state or lengths."""
