@@ -22,10 +22,11 @@
 // What bounds it: the walk itself, a chunk's steps one after the other with two waves
 // a SIMD (S takes 64 registers of a wave, the chunk on its way 24).  bf16, rows of
 // 128, 64 heads of 4096 tokens in 512 segments: 77 us for outputs (300 MB, 3.9 TB/s;
-// the matrix units are busy 45 % of the time, the vector units 50 %), 42 us for states
+// the matrix units are busy 40 % of the time, the vector units 44 %), 42 us for states
 // alone (167 MB, 4.0 TB/s); 8 heads of 65536 tokens, 165 and 83 us.  fp32, 8 heads of
 // 8192 tokens, rows of 64 and 128: 38 and 20 us.  Chunks of 64 tokens halve the work on
 // S but leave no registers: 487 us for a training call of the first size, of 32 436.
+// Two places in LDS for a chunk's rows, and so a barrier less, make no difference.
 #pragma once
 #include <initializer_list>
 
