@@ -261,23 +261,23 @@ inline Str str(const bc_strides& s) { return {(long)s.batch, (long)s.row, (long)
 inline size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
 
-// How a call is divided: segments of whole chunks, a block each, as long as two
-// blocks on each of 256 CUs allow and 128 tokens at least; one segment up to 512
-// tokens, where the passes that join segments cost more than they save.  The
-// backward's are the forward's that kept its states, and no longer than 2048 tokens
-// (the gates' gradients are sums over a segment).
-// 64 heads of 4096 tokens in training, bf16 rows of 128: 436 us; for 256 blocks 475,
-// for 1024 blocks 521 (8 heads of 65536 tokens, forward: 229, 269, 262).  18 heads of
-// 1531: 117 us; segments of 256 tokens at least 145, of 64 113, with twice the states.
-// 256 sequences and heads of 200 tokens: 15.5 us; in two segments 31.
+// How a call is divided: segments of whole chunks, a block each.  Joining them costs a
+// pass over keys and values and one over states, so a sequence stays whole up to 512
+// tokens and where each CU has one as it is; else two blocks a CU where segments keep 256
+// tokens (more would be a second round), or one where they keep 128.  With kept states
+// a segment has 2048 tokens at most: the gates' gradients are sums over it.
+// In training, bf16, rows of 128: 64 heads of 4096 tokens 436 us (8 segments), as 4 475, as
+// 16 521; 384 heads of 1024 522 us, as two segments 903; rows of 64, 16 heads of 4096
+// 87 us (256 tokens), of 128 tokens 93.  fp32, 18 heads of 1531, 40 and 72: 117 us, of
+// 256 tokens 145, of 64 113 with twice the states.
 struct Plan { int seg, segs; };
 Plan plan_of(const bc_attention& a, bool keeps) {
-  const long nh = (long)a.N * a.H;
-  Plan p;
-  const long want = std::max(a.T <= 512 ? 512L : 128L, (nh * a.T + 511) / 512);
-  p.seg = (int)std::min((want + 63) / 64 * 64, keeps ? 2048L : 1L << 30);
-  p.segs = (int)ceil_div(a.T, p.seg);
-  return p;
+  const long nh = (long)a.N * a.H, T = a.T;
+  long segs = 1;
+  if (nh < 256 && T > 512) segs = std::max(std::min(512 / nh, T / 256), std::min(256 / nh, ceil_div(T, 128)));
+  if (keeps) segs = std::max(segs, ceil_div(T, 2048));
+  const long seg = ceil_div(ceil_div(T, segs), kChunk) * kChunk;
+  return {(int)seg, (int)ceil_div(T, seg)};
 }
 
 // Workspaces.  What joins the segments: their decays and the states at their
