@@ -262,19 +262,20 @@ inline size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
 
 // How a call is divided: segments of whole chunks, a block each.  Joining them costs a
-// pass over keys and values and one over states, so a sequence stays whole up to 512
-// tokens and where each CU has one as it is; else two blocks a CU where segments keep 256
-// tokens (more would be a second round), or one where they keep 128.  With kept states
-// a segment has 2048 tokens at most: the gates' gradients are sums over it.
+// pass over keys and values and one over states, so a sequence stays whole up to 256
+// tokens (512 where it would have three segments at most) and where each CU has one as
+// it is; else two blocks a CU where segments keep 256 tokens (more would be a second
+// round), or one where they keep 64.  With kept states a segment has 2048 tokens at
+// most: the gates' gradients are sums over it.
 // In training, bf16, rows of 128: 64 heads of 4096 tokens 436 us (8 segments), as 4 475, as
-// 16 521; 384 heads of 1024 522 us, as two segments 903; rows of 64, 16 heads of 4096
-// 87 us (256 tokens), of 128 tokens 93.  fp32, 18 heads of 1531, 40 and 72: 117 us, of
-// 256 tokens 145, of 64 113 with twice the states.
+// 16 521; 384 heads of 1024 522 us, as two segments 903; 128 heads of 400 137 us, as two
+// 152; 3 heads of 432 59 us (7 segments), as 4 75, whole 137.  Rows of 64, 16 heads of
+// 4096 87 us (256 tokens), of 128 tokens 93.
 struct Plan { int seg, segs; };
 Plan plan_of(const bc_attention& a, bool keeps) {
   const long nh = (long)a.N * a.H, T = a.T;
   long segs = 1;
-  if (nh < 256 && T > 512) segs = std::max(std::min(512 / nh, T / 256), std::min(256 / nh, ceil_div(T, 128)));
+  if (nh < 256 && T > (nh > 64 ? 512 : 256)) segs = std::max(std::min(512 / nh, T / 256), std::min(256 / nh, ceil_div(T, 64)));
   if (keeps) segs = std::max(segs, ceil_div(T, 2048));
   const long seg = ceil_div(ceil_div(T, segs), kChunk) * kChunk;
   return {(int)seg, (int)ceil_div(T, seg)};
