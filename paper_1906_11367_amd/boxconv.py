@@ -801,7 +801,7 @@ def _layout(tensors):
         return None
 
 
-_forward_calls, _step_calls, _norm_calls = _Layouts(), _Layouts(), _Layouts()
+_forward_calls, _backward_calls, _step_calls, _norm_calls, _norm_grad_calls = (_Layouts() for _ in range(5))
 
 
 def _here(what, tensors):
@@ -911,32 +911,42 @@ def linear_attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, gate
     grad_gate [N, T, H] or None (a gate [H] is not learned here, or its gradient
     is the sum of grad_gate over sequences and tokens)."""
     what = "linear_attention_bwd"
-    a = _attention_sizes(q, k, v, gate, grad_y, form, scale, what, True, "grad_y")
-    grads = ((grad_q, q, "grad_q"), (grad_k, k, "grad_k"), (grad_v, v, "grad_v"))
-    for g, t, name in grads:
-        if not isinstance(g, torch.Tensor):
-            raise BoxConvError(f"{what}: {name} must be a tensor")
-        _need(g, tuple(t.shape), t.dtype, what, name)
-    _need(grad_gate, (a.N, a.T, a.H), gate.dtype, what, "grad_gate")
-    cells = (a.N, a.H, a.Dk, a.Dv)
-    _need(grad_s_last, cells, _F32, what, "grad_s_last")
-    _need(grad_s0, cells, _F32, what, "grad_s0")
-    _need(lengths, (a.N,), torch.int32, what, "lengths")
-    lib = load_library()
-    if not isinstance(states, torch.Tensor):
-        raise BoxConvError(f"{what}: states must be a tensor")
-    _need_numel(states, lib.bc_linear_attention_states_bytes(a.N, a.T, a.H, a.Dk, a.Dv) // 4, _F32, what, "states")
-    sq, sk, sv, sy = (_strides(t, what, n) for t, n in ((q, "q"), (k, "k"), (v, "v"), (grad_y, "grad_y")))
-    gq, gk, gv = (_strides(g, what, name) for g, _, name in grads)
-    _one_device(what, q, k, v, gate, states, grad_y, grad_q, grad_k, grad_v, grad_gate, grad_s_last, grad_s0, lengths, ws)
+    scale = float(scale)
+    tensors = (q, k, v, gate, states, grad_y, grad_q, grad_k, grad_v, grad_gate, grad_s_last, grad_s0, lengths, ws)
+    layout = _layout(tensors)
+    call = _backward_calls.get((form, scale, layout))
+    lib = _lib or load_library()
+    if call is None:
+        a = _attention_sizes(q, k, v, gate, grad_y, form, scale, what, True, "grad_y")
+        grads = ((grad_q, q, "grad_q"), (grad_k, k, "grad_k"), (grad_v, v, "grad_v"))
+        for g, t, name in grads:
+            if not isinstance(g, torch.Tensor):
+                raise BoxConvError(f"{what}: {name} must be a tensor")
+            _need(g, tuple(t.shape), t.dtype, what, name)
+        _need(grad_gate, (a.N, a.T, a.H), gate.dtype, what, "grad_gate")
+        cells = (a.N, a.H, a.Dk, a.Dv)
+        _need(grad_s_last, cells, _F32, what, "grad_s_last")
+        _need(grad_s0, cells, _F32, what, "grad_s0")
+        _need(lengths, (a.N,), torch.int32, what, "lengths")
+        if not isinstance(states, torch.Tensor):
+            raise BoxConvError(f"{what}: states must be a tensor")
+        _need_numel(states, lib.bc_linear_attention_states_bytes(a.N, a.T, a.H, a.Dk, a.Dv) // 4, _F32, what, "states")
+        strides = [_strides(t, what, n) for t, n in ((q, "q"), (k, "k"), (v, "v"), (grad_y, "grad_y"))]
+        strides += [_gate_strides(gate)] + [_strides(g, what, name) for g, _, name in grads]
+        strides += [bc_strides() if grad_gate is None else _gate_strides(grad_gate)]
+        _one_device(what, *tensors)
+        _dense(what, layout, states, lengths, grad_s_last, grad_s0, ws)
+        nbytes = lib.bc_linear_attention_workspace_bytes(1, a) if ws is None else ws.numel() * ws.element_size()
+        call = _backward_calls.put((form, scale, layout), (ctypes.byref(a), *strides, nbytes))
+    _here(what, tensors)
+    a, sq, sk, sv, sy, sg, gq, gk, gv, gg, nbytes = call
     if ws is None:
-        ws = _workspace(lib.bc_linear_attention_workspace_bytes(1, a), q.device)
-    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check(lib.linear_attention_bwd(a, _data(q), sq, _data(k), sk, _data(v), sv, _data(gate), _gate_strides(gate),
-                                    _ptr(states), _ptr(lengths), _data(grad_y), sy, _ptr(grad_s_last), _data(grad_q), gq,
-                                    _data(grad_k), gk, _data(grad_v), gv, None if grad_gate is None else _data(grad_gate),
-                                    bc_strides() if grad_gate is None else _gate_strides(grad_gate), _ptr(grad_s0),
-                                    _ptr(ws), nbytes, _stream()), what)
+        ws = _workspace(nbytes, q.device)
+    pq, pk, pv, pg, ps, py, pdq, pdk, pdv, pdg, p_last, p0, pn = [None if t is None else t.data_ptr() for t in tensors[:-1]]
+    st = lib.linear_attention_bwd(a, pq, sq, pk, sk, pv, sv, pg, sg, ps, pn, py, sy, p_last, pdq, gq, pdk, gk, pdv, gv, pdg,
+                                  gg, p0, None if ws is None else ws.data_ptr(), nbytes, _stream())
+    if st:
+        _check(st, what)
     return grad_q, grad_k, grad_v
 
 
@@ -1045,21 +1055,33 @@ def block_norm_bwd(z: torch.Tensor, gate: torch.Tensor | None = None, x: torch.T
     """The gradients of block_norm_fwd of the same arguments, those that are given
     a tensor -> (grad_z, grad_gate, grad_x)."""
     what = "block_norm_bwd"
-    shape, dt, n = _norm_sizes(z, groups, kind, act, eps, what)
-    rows = [_norm_rows(t, shape, dt, what, name) for t, name in
-            ((z, "z"), (gate, "gate"), (x, "x"), (grad_r, "grad_r"), (grad_y, "grad_y"), (grad_z, "grad_z"),
-             (grad_gate, "grad_gate"), (grad_x, "grad_x"))]
-    weights = ((w_post, "w_post"), (res_scale, "res_scale"), (w_pre, "w_pre"), (grad_w_post, "grad_w_post"),
-               (grad_res_scale, "grad_res_scale"), (grad_w_pre, "grad_w_pre"))
-    for t, name in weights:
-        _need(t, (n.C,), _F32, what, name)
-    _one_device(what, z, gate, x, grad_r, grad_y, grad_z, grad_gate, grad_x, *(t for t, _ in weights), ws)
-    lib = load_library()
-    if ws is None and any(t is not None for t in (grad_w_post, grad_res_scale, grad_w_pre)):
-        ws = _workspace(lib.bc_block_norm_workspace_bytes(n.R, n.C), z.device)
-    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    flat = [v for pair in rows[3:] for v in pair]
-    _check(lib.block_norm_bwd(n, *rows[0], *rows[1], *rows[2], _ptr(w_post), _ptr(res_scale), _ptr(w_pre), *flat,
-                              _ptr(grad_w_post), _ptr(grad_res_scale), _ptr(grad_w_pre), _ptr(ws), nbytes, _stream()),
-           what)
+    eps = float(eps)
+    tensors = (z, gate, x, grad_r, grad_y, grad_z, grad_gate, grad_x, w_post, res_scale, w_pre, grad_w_post, grad_res_scale,
+               grad_w_pre, ws)
+    layout = _layout(tensors)
+    call = _norm_grad_calls.get((groups, kind, act, eps, layout))
+    lib = _lib or load_library()
+    if call is None:
+        shape, dt, n = _norm_sizes(z, groups, kind, act, eps, what)
+        names = ("z", "gate", "x", "grad_r", "grad_y", "grad_z", "grad_gate", "grad_x")
+        steps = [_norm_rows(t, shape, dt, what, name)[1] for t, name in zip(tensors, names)]
+        weights = (w_post, res_scale, w_pre, grad_w_post, grad_res_scale, grad_w_pre)
+        for t, name in zip(weights, ("w_post", "res_scale", "w_pre", "grad_w_post", "grad_res_scale", "grad_w_pre")):
+            _need(t, (n.C,), _F32, what, name)
+        _one_device(what, *tensors)
+        _dense(what, layout, *weights, ws)
+        if ws is not None:
+            nbytes = ws.numel() * ws.element_size()
+        else:
+            nbytes = lib.bc_block_norm_workspace_bytes(n.R, n.C) if any(t is not None for t in weights[3:]) else 0
+        call = _norm_grad_calls.put((groups, kind, act, eps, layout), (ctypes.byref(n), *steps, nbytes))
+    _here(what, tensors)
+    n, sz, sg, sx, sr, sy, sdz, sdg, sdx, nbytes = call
+    if ws is None:
+        ws = _workspace(nbytes, z.device)
+    pz, pg, px, pr, py, pdz, pdg, pdx, *pw = [None if t is None else t.data_ptr() for t in tensors[:-1]]
+    st = lib.block_norm_bwd(n, pz, sz, pg, sg, px, sx, *pw[:3], pr, sr, py, sy, pdz, sdz, pdg, sdg, pdx, sdx, *pw[3:],
+                            None if ws is None else ws.data_ptr(), nbytes, _stream())
+    if st:
+        _check(st, what)
     return grad_z, grad_gate, grad_x

@@ -633,13 +633,13 @@ __global__ __launch_bounds__(256, KP == 64 && VP == 64 ? 3 : 2) void k_walk(Walk
 
 // A walk with state [K][V] and one with [V][K], of `units` blocks each: of 16
 // blocks in a row eight are the one's, on all XCDs, and eight the other's.
-template <int DT, int KP, int VP, int MODE, int MODE2>
+template <int DT, int KP, int VP, int MODE, int MODE2, bool VEC>
 __global__ __launch_bounds__(256, KP == 64 && VP == 64 ? 3 : 2) void k_walk2(Walk w, Walk w2, int units) {
   extern __shared__ char smem[];
   const int unit = (int)(blockIdx.x >> 4) * 8 + (int)(blockIdx.x & 7);
   if (unit >= units) return;
-  if ((blockIdx.x & 8) == 0) walk<DT, KP, VP, kTilesOf<VP>, MODE, true>(w, unit, smem);
-  else walk<DT, VP, KP, kTilesOf<KP>, MODE2, true>(w2, unit, smem);
+  if ((blockIdx.x & 8) == 0) walk<DT, KP, VP, kTilesOf<VP>, MODE, VEC>(w, unit, smem);
+  else walk<DT, VP, KP, kTilesOf<KP>, MODE2, VEC>(w2, unit, smem);
 }
 
 // Whole vectors, rows that do not overlap (a row past the last that exists is then
@@ -670,7 +670,7 @@ hipError_t launch_walk_sized(const Walk& w, hipStream_t s) {
 }
 
 // w: outputs; w2: states or outputs.
-template <int DT, int KP, int VP>
+template <int DT, int KP, int VP, bool VEC>
 hipError_t launch_walk2_sized(const Walk& w, const Walk& w2, hipStream_t s) {
   const long units = (long)w.N * w.H * w.segs;
   auto go = [&](auto kernel) {
@@ -678,8 +678,8 @@ hipError_t launch_walk2_sized(const Walk& w, const Walk& w2, hipStream_t s) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)((units + 7) / 8 * 16)), dim3(256), lds, s, w, w2, (int)units);
     return hipGetLastError();
   };
-  if (mode_of(w2) == kStates) return w.x ? go(k_walk2<DT, KP, VP, kOutDots, kStates>) : go(k_walk2<DT, KP, VP, kOut, kStates>);
-  return w.x ? go(k_walk2<DT, KP, VP, kOutDots, kOut>) : go(k_walk2<DT, KP, VP, kOut, kOut>);
+  if (mode_of(w2) == kStates) return w.x ? go(k_walk2<DT, KP, VP, kOutDots, kStates, VEC>) : go(k_walk2<DT, KP, VP, kOut, kStates, VEC>);
+  return w.x ? go(k_walk2<DT, KP, VP, kOutDots, kOut, VEC>) : go(k_walk2<DT, KP, VP, kOut, kOut, VEC>);
 }
 
 template <int DT>
@@ -687,9 +687,8 @@ hipError_t launch_walk_dt(const Walk& w, const Walk* beside, hipStream_t s) {
   auto sized = [&](auto one, auto two) {   // the rounded sizes of K and V
     constexpr int KP = decltype(one)::value, VP = decltype(two)::value;
     if (!beside) return launch_walk_sized<DT, KP, VP>(w, s);
-    if (vectors<DT>(w) && vectors<DT>(*beside)) return launch_walk2_sized<DT, KP, VP>(w, *beside, s);
-    const hipError_t e = launch_walk_sized<DT, KP, VP>(w, s);
-    return e != hipSuccess ? e : launch_walk_sized<DT, VP, KP>(*beside, s);
+    return vectors<DT>(w) && vectors<DT>(*beside) ? launch_walk2_sized<DT, KP, VP, true>(w, *beside, s)
+                                                   : launch_walk2_sized<DT, KP, VP, false>(w, *beside, s);
   };
   using A = std::integral_constant<int, 64>;
   using B = std::integral_constant<int, 128>;
