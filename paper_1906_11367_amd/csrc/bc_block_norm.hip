@@ -526,9 +526,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, waves_of(DT, W, BWD, GATE &&
 // With both norms and the weights' gradients, bf16, 65536 rows of 640 (blocks of two
 // waves): 150 us, with 512 blocks 293; 8192 rows of 4096: 98, with 1024 blocks 110.
 constexpr int part_blocks(int W) { return W == 2 ? 1024 : 512; }
-// Rows a block takes at least: a share costs more than a row or two.  600 rows of
-// 4096: 27 us, a block a row 32 to 41; 300 rows of 1024: 12.1, 12.8.
+// Rows a block takes at least, past kFewBlocks blocks: a share costs more than a row or
+// two.  600 rows of 4096: 27 us, a block a row 32 to 41; 300 rows of 1024: 12.1, 12.8.
+// Fewer rows follow one another for nothing: 11 rows of 5272 in 11 blocks 21 us, in 3 30.
 constexpr int part_rows(int W) { return W == 1 ? 1 : W < 8 ? 2 : 4; }
+constexpr long kFewBlocks = 128;
 
 // The weights' gradients from the blocks' sums part [P][2][C], 32 channels a block,
 // a lane of 32 the blocks p, p + 32, ..., all on their way at once (16 MB of 512 x 4096 in
@@ -577,7 +579,8 @@ hipError_t launch_norm(NormArgs& a, int* blocks, hipStream_t s) {
   a.lanes = 64;
   const bool pow2 = (a.per & (a.per - 1)) == 0 && a.per <= 64;
   auto go = [&](auto kernel, int threads, int teams, int W) {
-    const long run = (long)teams * (BWD ? part_rows(W) : 1), want = (a.R + run - 1) / run;
+    long want = ((long)a.R + teams - 1) / teams;
+    if (BWD) want = std::max((want + part_rows(W) - 1) / part_rows(W), std::min(want, kFewBlocks));
     *blocks = (int)std::min<long>(want, BWD ? part_blocks(W) : fwd_blocks(W));
     a.mode = G == 1 ? kSumTeam : pow2 ? kSumLanes : G <= kFew ? kSumFew : kSumShared;
     hipLaunchKernelGGL(kernel, dim3((unsigned)*blocks), dim3((unsigned)threads), 0, s, a);
