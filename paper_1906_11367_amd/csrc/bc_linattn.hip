@@ -463,8 +463,9 @@ hipError_t launch_linear_attention_bwd(const Attention& f, hipStream_t s) {
   };
 
   // Two walks at a time where one leaves CUs without a second block: 18 heads of 1531
-  // tokens, 216 segments, 117 us, one by one 124.  Where each fills the card they only
-  // stand in one another's way: 512 segments 437 us one by one, 471 in twos.
+  // tokens, 216 segments, 117 us, one by one 124; 384 segments 522 us, 540.  Where each
+  // fills the card they only stand in one another's way: 512 segments 437 us one by
+  // one, 471 in twos.
   const bool pairs = nh * p.segs < 512;
   Walk dq = forward;
   set(dq, dy, v, k);

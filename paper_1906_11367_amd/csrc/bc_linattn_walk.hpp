@@ -24,7 +24,10 @@
 // 128, 64 heads of 4096 tokens in 512 segments: 77 us for outputs (300 MB, 3.9 TB/s;
 // the matrix units are busy 40 % of the time, the vector units 44 %), 42 us for states
 // alone (167 MB, 4.0 TB/s); 8 heads of 65536 tokens, 165 and 83 us.  fp32, 8 heads of
-// 8192 tokens, rows of 64 and 128: 38 and 20 us.  Chunks of 64 tokens halve the work on
+// 8192 tokens in 256 segments, rows of 64 and 128: 40 and 21 us (the matrix units 55 %
+// busy where there are two blocks a CU).  Rows that are not whole vectors (VEC false)
+// cost about a sixth more: in training 64 heads of 4096 with 128 x 122 in place of
+// 128 x 120, 488 us for 420.  Chunks of 64 tokens halve the work on
 // S but leave no registers: 487 us for a training call of the first size, of 32 436.
 // Two places in LDS for a chunk's rows, and so a barrier less, make no difference.
 #pragma once
@@ -132,6 +135,22 @@ template <int W> __device__ __forceinline__ void buffer_store(__amdgpu_buffer_rs
   }
 }
 
+// Element e of the result is element e + over of v, zero past its end; over <= V.
+template <int DT, int V>
+__device__ __forceinline__ Raw<scan::kWords<DT, V>> shift_down(Raw<scan::kWords<DT, V>> v, int over) {
+  constexpr int W = scan::kWords<DT, V>;
+  if constexpr (DT == kBF16) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = over & 1 ? __builtin_amdgcn_alignbit(i + 1 < W ? v[i + 1] : 0u, v[i], 16) : v[i];
+    over >>= 1;
+  }
+#pragma unroll
+  for (int s = 1; s <= W; s *= 2)
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = over & s ? (i + s < W ? v[i + s] : 0u) : v[i];
+  return v;
+}
+
 // A chunk's rows of one operand: from memory to registers, then to LDS.
 template <int DT, int W, int THREADS> struct Tile {
   static constexpr int kVec = 16 / kBytes<DT>, kPerRow = W / kVec, kRows = THREADS / kPerRow;
@@ -155,13 +174,24 @@ template <int DT, int W, int THREADS> struct Tile {
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) r[i] = buffer_load<4>(rs, at + (uint32_t)(i * skip));
   }
-  // any rows: tokens from hi on do not exist (zeros)
+  // Any rows, tokens from hi (> t0) on do not exist.  A vector past the row's end is the
+  // row's last one, and that of a token that does not exist the last token's: every
+  // load is whole and in range, none waits for another, and settle() puts in order
+  // what has arrived.  (Rows shorter than a vector: element by element.)
   __device__ __forceinline__ void load(const char* base, long row_stride, int D, int t0, bool rev, int hi) {
+    const int c = min(col(), D - kVec);
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
       const int t = t0 + row(i, rev);
-      r[i] = scan::load_vec<DT, kVec>(base + ((long)t * row_stride + col()) * kBytes<DT>, t < hi && busy() ? D - col() : 0);
+      if (D < kVec) r[i] = scan::load_vec<DT, kVec>(base + ((long)t * row_stride + col()) * kBytes<DT>, t < hi && busy() ? D - col() : 0);
+      else r[i] = scan::load_wide<DT, kVec>(base + ((long)max(min(t, hi - 1), t0) * row_stride + c) * kBytes<DT>);
     }
+  }
+  __device__ __forceinline__ void settle(int D, int t0, bool rev, int hi) {
+    if (D < kVec) return;
+    const int over = min(col() - min(col(), D - kVec), kVec);
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) r[i] = shift_down<DT, kVec>(r[i], t0 + row(i, rev) < hi ? over : kVec);
   }
   __device__ __forceinline__ void store(typename Traits<DT>::Elem* lds) const {
     if (!busy()) return;
@@ -401,6 +431,11 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
     }
     const float(&d)[4][CH] = sm.dec[c % kAhead];
     if (live) {
+      if constexpr (!VEC) {
+        if constexpr (OUT) tq.settle(w.K, t0, rev, hi);
+        tk.settle(w.K, t0, rev, hi);
+        tv.settle(w.V, t0, rev, hi);
+      }
       if constexpr (OUT) tq.store(sm.q);
       tk.store(sm.k);
       tv.store(sm.v);
@@ -418,7 +453,8 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
       for (int it = 0; it < IT; ++it) {
         const int row = rev ? CH - 1 - it * 16 - m : it * 16 + m;
         if constexpr (VEC) x[it] = buffer_load<scan::kWords<DT, V>>(rx, avail > 0 ? (uint32_t)((t0 - out_low + row) * xstep + col * kBytes<DT>) : kNoColumn);
-        else x[it] = scan::load_vec<DT, V>(xp + ((t0 + row) * w.xs.t + col) * kBytes<DT>, t0 + row < hi ? avail : 0);
+        else if (w.V < V) x[it] = scan::load_vec<DT, V>(xp + ((t0 + row) * w.xs.t + col) * kBytes<DT>, t0 + row < hi ? avail : 0);
+        else x[it] = scan::load_wide<DT, V>(xp + (max(min(t0 + row, hi - 1), t0) * w.xs.t + min(col, w.V - V)) * kBytes<DT>);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -548,6 +584,10 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
         }
         if constexpr (DOTS) {
           float dot = 0.0f;
+          if (!VEC && w.V >= V) {   // (as Tile::settle)
+            const int over = min(col - min(col, w.V - V), V);
+            x[it] = shift_down<DT, V>(x[it], t0 + row < hi ? over : V);
+          }
 #pragma unroll
           for (int u = 0; u < V; ++u) dot = fmaf(o[u], scan::elem<DT, V>(x[it], u), dot);
           dot = pair32_sum(pair16_sum(dot));
