@@ -24,8 +24,8 @@
 // 128, 64 heads of 4096 tokens in 512 segments: 77 us for outputs (300 MB, 3.9 TB/s;
 // the matrix units are busy 40 % of the time, the vector units 44 %), 42 us for states
 // alone (167 MB, 4.0 TB/s); 8 heads of 65536 tokens, 165 and 83 us.  fp32, 8 heads of
-// 8192 tokens in 256 segments, rows of 64 and 128: 40 and 21 us (the matrix units 55 %
-// busy where there are two blocks a CU).  Rows that are not whole vectors (VEC false)
+// 8192 tokens in 256 segments, rows of 64 and 128: 40 and 21 us (the matrix units 49 %
+// busy, 61 to 65 % where two walks share a launch).  Rows that are not whole vectors (VEC false)
 // cost about a sixth more: in training 64 heads of 4096 with 128 x 122 in place of
 // 128 x 120, 488 us for 420.  Chunks of 64 tokens halve the work on
 // S but leave no registers: 487 us for a training call of the first size, of 32 436.
