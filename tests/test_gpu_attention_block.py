@@ -113,6 +113,28 @@ def test_training_against_the_oracle(dtype, bar, Hk, lengths):
         assert err <= bar, (name, err)
 
 
+def test_training_of_odd_sizes():
+    """No size a whole vector, a few tokens, an empty sequence; fp32 and its bar."""
+    N, T, C, H, Dk, Dv = 3, 5, 33, 3, 7, 5
+    plan = LinearAttentionPlan(N, T, C, H, Dk, Dv, Hk=1)
+    w = weights(plan.shape, C, H, Dv)
+    x, dr = rand(14, N, T, C).cuda(), rand(15, N, T, C).cuda()
+    lengths = [5, 0, 4]
+    ln = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    r, s_last = plan.forward(x, w, lengths=ln)
+    dx, grads, ds0 = plan.backward(x, w, dr, lengths=ln)
+    torch.cuda.synchronize()
+    w64, none = {k: to64(v) for k, v in w.items()}, np.zeros((N, H, Dk, Dv))
+    wr, ws, kept = block(to64(x), w64, plan.shape, plan.eps, none, lengths)
+    want = block_grads(to64(x), w64, plan.shape, plan.eps, kept, to64(dr), none, none, lengths)
+    got = {"dx": dx, "ds0": ds0, **grads}
+    for name, a, b in [("r", r, wr), ("s_last", s_last, ws)] + [(n, got[n], want[n]) for n in got]:
+        err = np.linalg.norm(to64(a) - b) / np.linalg.norm(b)
+        say(name, err)
+        assert err <= 1e-4, (name, err)
+    assert torch.equal(r[1], x[1]) and (s_last[1] == 0).all()
+
+
 def test_the_oracles_gradients_are_the_losss_differences():
     """Along a random direction of every weight and of x, in 64 bits."""
     N, T, C, H, Dk, Dv = 1, 9, 6, 2, 3, 4
