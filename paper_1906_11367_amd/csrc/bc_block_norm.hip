@@ -325,15 +325,16 @@ constexpr int fwd_blocks(int W) { return W <= 2 ? 2048 : W == 4 ? 1536 : W == 8 
 
 // Waves a SIMD: what the registers of the variant allow without a spill (a reload
 // waits for the loads ahead too).
-constexpr int waves_of(int dt, int W, bool bwd, bool both) {
+constexpr int waves_of(int dt, int W, int NS, bool bwd, bool both) {
   if (W == 16) return 4;
+  if (NS == 2) return 2;
   if (bwd) return dt == kBF16 && !both ? 4 : 2;
   return dt == kBF16 ? (both ? 5 : 6) : 4;
 }
 
 // GATE, PRE: there is a gate; there is a y (or its gradient).
 template <int DT, int W, int NS, bool BWD, bool GATE, bool PRE>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, waves_of(DT, W, BWD, GATE && PRE)) void k_block_norm(NormArgs a) {
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, waves_of(DT, W, NS, BWD, GATE && PRE)) void k_block_norm(NormArgs a) {
   using T = Team<W, NS>;
   __shared__ float lds[T::kFloats];
   const int tid = threadIdx.x;
@@ -380,9 +381,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, waves_of(DT, W, BWD, GATE &&
         for (int e = 0; e < 8; ++e) sum[k][i][e] = 0.0f;
   }
 
-  // a row's inputs are on their way while the row before it is worked on (but for
-  // blocks of 1024 threads, whose 128 registers hold no more)
-  constexpr bool AHEAD = NS == 1 && !(W == 16 && BWD && PRE);
+  // a row's inputs are on their way while the row before it is worked on, where the
+  // registers hold them
+  constexpr bool AHEAD = NS == 1 ? W < 16 || !(BWD && PRE) : W < 16 && (!PRE || (!GATE && DT == kBF16));
   constexpr bool X = PRE || !BWD;   // x is read
   Eight<DT> rz[NS], rg[NS], rx[NS], rdr[NS], rdy[NS];
   auto get = [&](long row0) {
@@ -522,10 +523,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, waves_of(DT, W, BWD, GATE &&
   }
 }
 
-// Blocks of the backward, and shares of the weights' gradients: 2048 waves or more.
+// Blocks of the backward, and shares of the weights' gradients: 2048 waves or more, or
+// one block a CU where it holds no more.
 // With both norms and the weights' gradients, bf16, 65536 rows of 640 (blocks of two
 // waves): 150 us, with 512 blocks 293; 8192 rows of 4096: 98, with 1024 blocks 110.
-constexpr int part_blocks(int W) { return W == 2 ? 1024 : 512; }
+constexpr int part_blocks(int W) { return W == 2 ? 1024 : W == 16 ? 256 : 512; }
 // Rows a block takes at least, past kFewBlocks blocks: a share costs more than a row or
 // two.  600 rows of 4096: 27 us, a block a row 32 to 41; 300 rows of 1024: 12.1, 12.8.
 // Fewer rows follow one another for nothing: 11 rows of 5272 in 11 blocks 21 us, in 3 30.
@@ -594,7 +596,12 @@ hipError_t launch_norm(NormArgs& a, int* blocks, hipStream_t s) {
   if (slots <= 128) return go(k_block_norm<DT, 2, 1, BWD, GATE, PRE>, 128, 1, 2);
   if (slots <= 256) return go(k_block_norm<DT, 4, 1, BWD, GATE, PRE>, 256, 1, 4);
   if (slots <= 512) return go(k_block_norm<DT, 8, 1, BWD, GATE, PRE>, 512, 1, 8);
-  if (slots <= 1024) return go(k_block_norm<DT, 16, 1, BWD, GATE, PRE>, 1024, 1, 16);
+  if (slots <= 1024) {
+    // 8 waves with 256 registers each have room to read ahead: 4096 rows of 8192 bf16,
+    // both norms, 99 us; 16 waves 131
+    if constexpr (BWD) return go(k_block_norm<DT, 8, 2, BWD, GATE, PRE>, 512, 1, 16);
+    else return go(k_block_norm<DT, 16, 1, BWD, GATE, PRE>, 1024, 1, 16);
+  }
   return go(k_block_norm<DT, 16, 2, BWD, GATE, PRE>, 1024, 1, 16);
 }
 
