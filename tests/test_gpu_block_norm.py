@@ -119,6 +119,10 @@ CASES = [
     dict(R=3000, C=20, groups=1, layer=True, x=True), dict(R=1100, C=520, dt="bf16", groups=1, **ALL),
     dict(R=30, C=200, dt="bf16", groups=4, pad=3, **ALL), dict(R=30, C=201, pad=7, layer=True, groups=3, **ALL),
     dict(R=5, C=640, weights=False, groups=2, **ALL), dict(R=5, C=640, r=False, groups=2, dt="bf16", **ALL),
+    # several rows to a block of every kind
+    dict(R=700, C=4200, dt="bf16", groups=1, **ALL), dict(R=600, C=5000, groups=4, layer=True, x=True),
+    dict(R=520, C=6000, groups=20, gate="silu", pre=False), dict(R=600, C=2100, dt="bf16", groups=1, x=True),
+    dict(R=700, C=1300, groups=1, layer=True, x=True),
 ]
 
 
