@@ -159,6 +159,24 @@ def test_against_the_oracle(kw):
     c.check()
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 5, 600])
+@pytest.mark.parametrize("D", [5, 64])
+def test_the_first_gate_of_a_sequence_without_a_state(dt, T, D):
+    """a_0 scales a state of zeros: its gradient is zero, not a rounding error."""
+    c = Case(3, T, 2, D, D, dt, lengths=[T, 1, 0])
+    c.forward()
+    c.backward()
+    assert (c.dgate[:, 0] == 0).all() and (T == 1 or (c.dgate[0, 1] != 0).any())
+    c.check()
+    # the same of a state that is given and is zero; of one that is not, only there
+    c.s0 = torch.zeros((3, 2, D, D), device="cuda")
+    c.s0[0, 1, D - 1, D - 1] = 1.0
+    c.forward()
+    c.backward()
+    assert (c.dgate[1:, 0] == 0).all() and (c.dgate[0, 0, 0] == 0) and c.dgate[0, 0, 1] != 0
+
+
 @pytest.mark.parametrize("dt,D", [("f32", 4), ("bf16", 8)])
 def test_segments_of_many_chunks(dt, D):
     """Heads enough for segments of 2048 tokens, without kept states of all 2113: what is
