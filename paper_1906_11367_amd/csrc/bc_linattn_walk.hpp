@@ -118,20 +118,21 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const char* p, int row
 }
 constexpr uint32_t kNoColumn = 0x80000000u;   // past every row: such offsets stay below 2^32
 
-template <int W> __device__ __forceinline__ Raw<W> buffer_load(__amdgpu_buffer_rsrc_t rs, uint32_t at) {
+// W words at `at`; of 8 the last four only where the row has them (both).
+template <int W> __device__ __forceinline__ Raw<W> buffer_load(__amdgpu_buffer_rsrc_t rs, uint32_t at, bool both = true) {
   if constexpr (W == 2) return __builtin_bit_cast(Raw<2>, __builtin_amdgcn_raw_buffer_load_b64(rs, (int)at, 0, 0));
   else if constexpr (W == 4) return __builtin_bit_cast(Raw<4>, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)at, 0, 0));
   else {
-    const Raw<4> a = buffer_load<4>(rs, at), b = buffer_load<4>(rs, at + 16);
+    const Raw<4> a = buffer_load<4>(rs, at), b = buffer_load<4>(rs, both ? at + 16 : kNoColumn);
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 }
-template <int W> __device__ __forceinline__ void buffer_store(__amdgpu_buffer_rsrc_t rs, uint32_t at, const Raw<W>& v) {
+template <int W> __device__ __forceinline__ void buffer_store(__amdgpu_buffer_rsrc_t rs, uint32_t at, const Raw<W>& v, bool both = true) {
   if constexpr (W == 2) __builtin_amdgcn_raw_buffer_store_b64(v, rs, (int)at, 0, 0);
   else if constexpr (W == 4) __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)at, 0, 0);
   else {
     buffer_store<4>(rs, at, __builtin_shufflevector(v, v, 0, 1, 2, 3));
-    buffer_store<4>(rs, at + 16, __builtin_shufflevector(v, v, 4, 5, 6, 7));
+    buffer_store<4>(rs, both ? at + 16 : kNoColumn, __builtin_shufflevector(v, v, 4, 5, 6, 7));
   }
 }
 
@@ -447,12 +448,13 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
     // the rows that outputs are multiplied with, on their way from here
     constexpr int V = 4 * NT;
     const int col = c0 + V * g, avail = w.V - col;
+    const bool both = DT != kF32 || avail > 4;   // (whole vectors of fp32 are half a lane's columns)
     Raw<scan::kWords<DT, V>> x[DOTS ? IT : 1];
     if constexpr (DOTS) {
 #pragma unroll
       for (int it = 0; it < IT; ++it) {
         const int row = rev ? CH - 1 - it * 16 - m : it * 16 + m;
-        if constexpr (VEC) x[it] = buffer_load<scan::kWords<DT, V>>(rx, avail > 0 ? (uint32_t)((t0 - out_low + row) * xstep + col * kBytes<DT>) : kNoColumn);
+        if constexpr (VEC) x[it] = buffer_load<scan::kWords<DT, V>>(rx, avail > 0 ? (uint32_t)((t0 - out_low + row) * xstep + col * kBytes<DT>) : kNoColumn, both);
         else if (w.V < V) x[it] = scan::load_vec<DT, V>(xp + ((t0 + row) * w.xs.t + col) * kBytes<DT>, t0 + row < hi ? avail : 0);
         else x[it] = scan::load_wide<DT, V>(xp + (max(min(t0 + row, hi - 1), t0) * w.xs.t + min(col, w.V - V)) * kBytes<DT>);
       }
@@ -574,7 +576,7 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
         for (int u = 0; u < V; ++u) o[u] = acc[it][u / 4][u & 3];
         if constexpr (VEC) {
           if (out_bytes == 4)
-            buffer_store<V>(ry, avail > 0 ? (uint32_t)((t0 - out_low + row) * ystep + col * 4) : kNoColumn, scan::rounded<kF32, V>(o));
+            buffer_store<V>(ry, avail > 0 ? (uint32_t)((t0 - out_low + row) * ystep + col * 4) : kNoColumn, scan::rounded<kF32, V>(o), both);
           else
             buffer_store<V / 2>(ry, avail > 0 ? (uint32_t)((t0 - out_low + row) * ystep + col * 2) : kNoColumn, scan::rounded<kBF16, V>(o));
         } else if (t0 + row < e && avail > 0) {

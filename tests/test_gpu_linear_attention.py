@@ -466,3 +466,57 @@ def test_calls_of_one_layout():
         bc.linear_attention_step(q, k, v, g, torch.zeros(N, D, H, D, device="cuda").transpose(1, 2), y)
     with pytest.raises(bc.BoxConvError):
         bc.linear_attention_step(q.cpu(), k, v, g, pool, y)
+
+
+# ---- rows that end inside a lane's columns --------------------------------------
+
+# fp32 rows of 65 to 128 elements that are whole vectors of 4 and not of the 8 columns a lane has
+HALF_ROWS = [dict(N=2, T=70, H=3, Dk=64, Dv=68), dict(N=1, T=90, H=2, Dk=100, Dv=32, start=True),
+             dict(N=2, T=65, H=3, Dk=124, Dv=92, form="log", lengths=[65, 40]), dict(N=1, T=900, H=2, Dk=76, Dv=84, start=True),
+             dict(N=2, T=40, H=6, Dk=108, Dv=116, heads=(2, 3, 1), start=True)]
+
+
+@pytest.mark.parametrize("layout", ["tokens", "heads", "slices"])
+@pytest.mark.parametrize("kw", HALF_ROWS, ids=lambda kw: "-".join(f"{v}" for v in kw.values()).replace(" ", ""))
+def test_rows_that_end_inside_a_lanes_columns(kw, layout):
+    """Every output is the oracle's, and nothing beside a row is written: in `slices` the
+    rows of y, and of the gradients in one buffer, stand between gaps."""
+    say(kw, layout)
+    c = Case(**kw, heads_first=layout == "heads")
+    N, T, H = c.N, c.T, c.H
+    if layout == "slices":
+        parts = [(c.q.shape[2], c.Dk), (c.k.shape[2], c.Dk), (c.v.shape[2], c.Dv), (H, c.Dv)]
+        width = sum(h * (d + 4) for h, d in parts)
+        rows, known = (torch.full((N, T, width), 7.0, device="cuda") for _ in range(2))
+        at = 0
+        for name, (h, d) in zip(("dq", "dk", "dv", "y"), parts):
+            cut = lambda t: t[..., at:at + h * (d + 4)].unflatten(2, (h, d + 4))[..., :d]
+            setattr(c, name, cut(rows))
+            cut(known).fill_(8.0)
+            at += h * (d + 4)
+    c.forward()
+    c.check(("y", "s_last"))
+    c.backward()
+    c.check()
+    if layout == "slices":
+        assert (rows[known == 7.0] == 7.0).all()
+
+
+@pytest.mark.parametrize("layout", ["tokens", "heads"])
+def test_a_neighbouring_row_is_not_looked_at(layout):
+    """Non-finite values of one head, in rows that end inside a lane's columns, leave the others' bits."""
+    names = ("y", "s_last", "dq", "dk", "dv", "dgate", "ds0")
+    cases = [Case(2, 70, 3, 68, 100, start=True, heads_first=layout == "heads") for _ in range(2)]
+    c = cases[1]
+    for t in (c.q, c.k, c.v, c.dy):
+        t[1, :, 1] = float("nan")
+        t[0, 33, 2] = float("inf")
+    for x in cases:
+        x.forward()
+        x.backward()
+    torch.cuda.synchronize()
+    for name in names:
+        a, b = (getattr(x, name).clone() for x in cases)
+        a, b = (t if name in ("s_last", "ds0") else t.transpose(1, 2) for t in (a, b))
+        for n, h in ((0, 0), (0, 1), (1, 0), (1, 2)):
+            assert torch.equal(a[n, h], b[n, h]), (name, n, h)
