@@ -173,9 +173,10 @@ def block_norm(z, gate=None, x=None, w_post=None, res_scale=None, w_pre=None, gr
     out["dres_scale"] = ((d * u).sum(0), (dm * np.abs(u) + np.abs(d) * um).sum(0))
     du, dum = d * s, dm * np.abs(s)
     if gate is not None:
-        slope = sig * (1.0 + gate * (1.0 - sig)) if act == "silu" else sig * (1.0 - sig)
+        rest = 1.0 / (1.0 + np.exp(np.minimum(gate, 700.0)))   # 1 - sig, with its digits
+        slope = sig * (1.0 + gate * rest) if act == "silu" else sig * rest
         # (the slope's own terms: sig, gate sig (1 - sig))
-        slopem = sig * (1.0 + np.abs(gate) * (1.0 - sig)) if act == "silu" else np.abs(slope)
+        slopem = sig * (1.0 + np.abs(gate) * rest) if act == "silu" else np.abs(slope)
         out["dgate"] = (du * p * slope, (dum * np.abs(p) + np.abs(du) * pm) * slopem)
     dp, dpm = du * phi, dum * np.abs(phi)
     if groups:

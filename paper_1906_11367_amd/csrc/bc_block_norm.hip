@@ -59,6 +59,14 @@ template <int DT> __device__ __forceinline__ float sigmoid(float g) {
   const float e = expf(-fabsf(g)), r = __builtin_amdgcn_rcpf(1.0f + e);
   return g >= 0.0f ? r : e * r;
 }
+// The same with its slope e / (1 + e)^2, e = e^-|g|: not s (1 - s), which has no digits
+// left where s is close to 1.
+template <int DT> __device__ __forceinline__ float sigmoid(float g, float& slope) {
+  const float e = DT == kBF16 ? __builtin_amdgcn_exp2f(fabsf(g) * -1.442695041f) : expf(-fabsf(g));
+  const float r = __builtin_amdgcn_rcpf(1.0f + e), er = e * r;
+  slope = er * r;
+  return g >= 0.0f ? r : er;
+}
 
 // Sums over slots, by a team of W waves, or of `size` lanes of one (W = 1), NS
 // slots a lane: slot i * size + lane.
@@ -416,9 +424,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, waves_of(DT, W, NS, BWD, GAT
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if constexpr (GATE) {
-          const float sg = sigmoid<DT>(g[i][e]);
+          float sg, slope;
+          if constexpr (BWD) sg = sigmoid<DT>(g[i][e], slope);
+          else sg = sigmoid<DT>(g[i][e]);
           phi[i][e] = a.sigmoid ? sg : g[i][e] * sg;
-          if constexpr (BWD) g[i][e] = a.sigmoid ? sg * (1.0f - sg) : sg * fmaf(g[i][e], 1.0f - sg, 1.0f);   // the slope
+          if constexpr (BWD) g[i][e] = a.sigmoid ? slope : fmaf(g[i][e], slope, sg);   // phi's slope
         }
         if constexpr (X) r[i][e] = fmaf(GATE ? n[i][e] * phi[i][e] : n[i][e], w[i][e], r[i][e]);
       }

@@ -239,3 +239,19 @@ def test_more_dimensions():
     bc.block_norm_fwd(z, y=y, eps=EPS)
     want = A.block_norm(to64(z).reshape(36, 32), eps=EPS)["y"]
     check("y", y.reshape(36, 32), *want, A.norm_units(32), "f32")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["silu", "sigmoid"])
+def test_gates_far_out_keep_their_slopes(dt, act):
+    """Gates of -30 to 30: the slope of the sigmoid is e^-|g| there, down to 1e-13, and
+    right to its own digits (the logistic function alone rounds to 1 from 17 on)."""
+    R, C = 60, 64
+    c = Case(R, C, dt, groups=1, gate=act, x=True, zero_rows=False)
+    gate = torch.linspace(-30, 30, R * C)[torch.randperm(R * C, generator=torch.Generator().manual_seed(3))].view(R, C).to(DT[dt])
+    c.gate.copy_(gate)
+    c.ref = A.block_norm(to64(c.z), to64(gate), to64(c.x), *(to64(c.w[n]) for n in ("w_post", "res_scale", "w_pre")), 1, False,
+                         act, EPS, True, to64(c.dr), to64(c.dy))
+    c.forward()
+    c.backward()
+    c.check()
