@@ -580,8 +580,10 @@ typedef struct {
  * rounded to its type.  bf16: where the fp32 state or scores meet a bf16 operand
  * on the matrix units they are taken as sums of bf16 parts, two for y (2^-16 of
  * each product), three for the state (2^-24).  gate = -infinity is an exact reset
- * (log a below -10000 is one too); with BC_GATE_LOG a_t > 1 is allowed while
- * states stay inside fp32's range.
+ * (log a below -10000 is one too).  With BC_GATE_LOG a_t > 1 is allowed while
+ * states (and, backward, their gradients) stay below 2^60 and the decays of no
+ * run of up to 32 tokens multiply to more than 2^60; these products are made before they
+ * meet a state, and past fp32's range a state of zeros too gives NaN.
  *
  * q, k, v  : device [N][T][Hq][Dk], [N][T][Hk][Dk], [N][T][Hv][Dv] by their strides.
  * gate     : device [N][T][H] by its strides (its heads gate_strides.head apart);

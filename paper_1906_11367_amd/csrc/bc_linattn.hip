@@ -19,7 +19,7 @@ struct Joint {
   float* entry;
   long entry_nh;           // (segs + 1) cells
   const float* start;      // [nh][cells], or null: zero
-  const float* decay;      // [nh][segs]
+  const Power* decay;      // [nh][segs]
   float* last;             // [nh][cells], or null
   const char* gate;        // rev: last is times the first token's decay
   Str gs;
@@ -34,12 +34,13 @@ __global__ __launch_bounds__(256) void k_join(Joint j) {
   const int blocks = (j.cells + 255) / 256, nh = blockIdx.x / blocks, cell = blockIdx.x % blocks * 256 + threadIdx.x;
   if (cell >= j.cells) return;
   float* p = j.entry + nh * j.entry_nh + cell;
-  const float* dec = j.decay + (long)nh * j.segs;
+  const Power* dec = j.decay + (long)nh * j.segs;
   float s = j.start ? j.start[(long)nh * j.cells + cell] : 0.0f;
   p[j.rev ? (long)j.segs * j.cells : 0] = s;
   auto at = [&](int i) { return (long)(j.rev ? j.segs - 1 - i : i + 1) * j.cells; };
   for (int i0 = 0; i0 < j.segs; i0 += kJointAhead) {
-    float add[kJointAhead], d[kJointAhead];
+    float add[kJointAhead];
+    Power d[kJointAhead];
 #pragma unroll
     for (int u = 0; u < kJointAhead; ++u) {
       const int i = min(i0 + u, j.segs - 1);
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(256) void k_join(Joint j) {
 #pragma unroll
     for (int u = 0; u < kJointAhead; ++u) {
       if (i0 + u < j.segs) {
-        s = fmaf(d[u], s, add[u]);
+        s = scaled(s, d[u], add[u]);
         p[at(i0 + u)] = s;
       }
     }
@@ -316,7 +317,7 @@ Ws ws_of(const bc_attention& a, const Plan& p, bool bwd) {
     return here;
   };
   if (p.segs > 1) {
-    w.decay = take(nh * p.segs * 4);
+    w.decay = take(nh * p.segs * sizeof(Power));
     w.entries = take(nh * (p.segs + 1) * a.Dk * a.Dv * 4);
   }
   if (bwd) {
@@ -407,7 +408,7 @@ hipError_t launch_linear_attention_fwd(const Attention& f, hipStream_t s) {
     w.last = entry + cells;
     w.last_nh = border;
     w.last_seg = cells;
-    w.decay = reinterpret_cast<float*>(wsp + ws.decay);
+    w.decay = reinterpret_cast<Power*>(wsp + ws.decay);
     BC_TRY(launch_walk(w, nullptr, a.dt, s));
     Joint j{};
     j.entry = entry;
@@ -510,7 +511,7 @@ hipError_t launch_linear_attention_bwd(const Attention& f, hipStream_t s) {
     w.last = entry;
     w.last_nh = border;
     w.last_seg = cells;
-    w.decay = reinterpret_cast<float*>(wsp + ws.decay);
+    w.decay = reinterpret_cast<Power*>(wsp + ws.decay);
     if (pairs) {
       BC_TRY(launch_walk(dq, &w, a.dt, s));
     } else {

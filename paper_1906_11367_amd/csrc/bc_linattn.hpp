@@ -7,8 +7,10 @@
 //   y_i = scale (sum_{j <= i} exp(L_i - L_j) (q_i . k_j) v_j + exp(L_i) S^T q_i),
 //   S' = exp(L_end) S + sum_j exp(L_end - L_j) k_j v_j^T,
 // four matrix products with S held in registers from chunk to chunk.  All the
-// exponents are sums of log a, so nothing overflows that the recurrence itself
-// would not (no division by a decay), and a reset (a = 0) is exact.
+// exponents are sums of log a: there is no division by a decay, decays up to one
+// cannot overflow, and a reset (a = 0) is exact.  Decays above one multiply before
+// they meet a state, so the products of a chunk's have to stay inside fp32's range
+// (those of a segment's need not: Power).
 //
 // The gradients are the same walk over other operands.  With R_t the gradient
 // to S_t, R_t = scale q_t dy_t^T + a_{t+1} R_{t+1}:
@@ -62,6 +64,17 @@ __device__ __forceinline__ float exp2_parts(double x) {
   return fmaf(e, (float)(x - (double)hi) * 0.6931472f, e);
 }
 
+// 2^x as two factors that are finite, the first a power of two: s 2^x leaves fp32's
+// range only where the product does.
+struct Power { float a, b; };
+__device__ __forceinline__ Power power_of(double x) {
+  const double c = x < -1000.0 ? -1000.0 : x > 250.0 ? 250.0 : x;   // (a NaN stays one; -1000: zero)
+  const double half = __builtin_rint(c * 0.5);
+  return {__builtin_amdgcn_exp2f((float)half), exp2_parts(c - half)};
+}
+// s 2^x + add
+__device__ __forceinline__ float scaled(float s, const Power& p, float add) { return fmaf(s * p.a, p.b, add); }
+
 // The walk of one block over a segment of one sequence and head: operands are
 // named as in the forward.
 struct Walk {
@@ -83,7 +96,7 @@ struct Walk {
   float* last2;              // the same once more (one segment), entries last2_nh apart
   long last2_nh;
   int last_a0;               // rev: `last` is times the first token's decay
-  float* decay;              // [nh][segs]: the segments' decays, or null
+  Power* decay;              // [nh][segs]: the segments' decays, or null
   char* y;                   // null: states only
   Str ys;
   int y_f32;

@@ -658,7 +658,7 @@ __device__ __forceinline__ void walk(const Walk& w, int block, char* smem_raw) {
       double sum = 0.0;
 #pragma unroll
       for (int u = 0; u < WAVES; ++u) sum += sm.totals[u];
-      w.decay[(long)nh * w.segs + seg] = exp2_parts(sum);
+      w.decay[(long)nh * w.segs + seg] = power_of(sum);
     }
   }
 }

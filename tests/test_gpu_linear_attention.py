@@ -108,8 +108,8 @@ class Case:
         bc.linear_attention_bwd(self.q, self.k, self.v, self.gate, self.states, self.dy, self.dq, self.dk, self.dv,
                                 self.dgate, grad_s_last=self.ds, grad_s0=self.ds0, **self.how(), **kw)
 
-    def check(self, names=("y", "s_last", "dq", "dk", "dv", "dgate", "ds0")):
-        u = A.attention_units(self.T, self.Dk, self.Dv, self.dt)
+    def check(self, names=("y", "s_last", "dq", "dk", "dv", "dgate", "ds0"), extra=0):
+        u = A.attention_units(self.T, self.Dk, self.Dv, self.dt) + extra
         torch.cuda.synchronize()
         for name in names:
             got = getattr(self, name)
@@ -520,3 +520,58 @@ def test_a_neighbouring_row_is_not_looked_at(layout):
         a, b = (t if name in ("s_last", "ds0") else t.transpose(1, 2) for t in (a, b))
         for n, h in ((0, 0), (0, 1), (1, 0), (1, 2)):
             assert torch.equal(a[n, h], b[n, h]), (name, n, h)
+
+
+# ---- decays above one -----------------------------------------------------------
+
+def growing(kind, T, zero_k, zero_dy):
+    """Logarithms of decays [T], those of no run of up to 32 tokens summing to more than 60 log 2;
+    zero_k, zero_dy: tokens whose keys, or output gradients, are zero, so that neither
+    states nor their gradients grow past 2^60."""
+    g = torch.full((T,), -0.1)
+    if kind == "blocks":            # e^40 between two resets: empty states, then ones whose gradient is empty
+        for b in range(0, T - 11, 12):
+            g[b], g[b + 1:b + 11] = -float("inf"), 4.0
+            zero_k[b:b + 6] = True
+            zero_dy[b + 6:b + 12] = True
+    elif kind == "from 1e-30":      # a start state that e^38 brings to 1e-13
+        g[:19] = 2.0
+        zero_k[:18] = True
+        zero_dy[5:] = True
+    elif kind == "segments":        # e^160 in a segment of 128 tokens, over states of zeros
+        g[:1024], g[1024] = 1.25, -float("inf")
+        zero_k[:1024] = True
+        zero_dy[20:1024] = True
+    elif kind == "slowly":          # e^60 over many chunks, from 1e-30
+        g[:] = 0.3
+        zero_k[:T - 30] = True
+        zero_dy[20:] = True
+    else:                           # up and down
+        g = 0.6 * rand(77, T)
+    return g
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("Dk,Dv,heads", [(64, 64, None), (128, 96, (1, 2, 2)), (7, 5, None), (100, 128, (2, 1, 1))])
+@pytest.mark.parametrize("kind,N,T,start", [("blocks", 1, 96, 0.0), ("from 1e-30", 1, 50, 1e-30), ("segments", 8, 2048, 0.0),
+                                            ("slowly", 1, 200, 1e-30), ("random", 1, 130, 1.0)])
+def test_decays_above_one(kind, N, T, start, Dk, Dv, heads, dt):
+    """Outputs and gradients are the recurrence's, also where a segment's decays together
+    pass fp32's range."""
+    say(kind, T, Dk, Dv, dt)
+    if N > 1:
+        Dk, Dv = min(Dk, 8), min(Dv, 8)
+    c = Case(N, T, 2, Dk, Dv, dt, form="log", heads=heads, start=True, gate_f32=True)
+    zero_k, zero_dy = torch.zeros((2, T), dtype=torch.bool)
+    c.gate.copy_(growing(kind, T, zero_k, zero_dy)[None, :, None].expand(N, T, 2))
+    c.k[:, zero_k.cuda()] = 0
+    c.dy[:, zero_dy.cuda()] = 0
+    c.s0 *= start
+    if start != 1.0:
+        c.ds *= 0
+    c.ref = A.attention(*(to64(t) for t in (c.q, c.k, c.v)), to64(c.gate), "log", c.scale, to64(c.s0), None, to64(c.dy),
+                        to64(c.ds))
+    c.forward()
+    c.backward()
+    # a factor 2^x of a score has its exponent to 2^-24 of itself: 60 log 2 units
+    c.check(extra=48)
