@@ -611,7 +611,10 @@ typedef struct {
  *   grad_q_t = scale S_t grad_y_t,  grad_k_t = R_t v_t,  grad_v_t = R_t^T k_t,
  *   d L / d log a_t = a_t <S_{t-1}, R_t>,  grad_s0 = a_0 R_0,
  * and grad_gate_t is d L / d log a_t (BC_GATE_LOG) or (1 - a_t) times that
- * (BC_GATE_LOGIT), zero where a_t is.  A head of q, k or v that several heads read
+ * (BC_GATE_LOGIT), zero where a_t is.  It is formed as the sum of q . grad_q -
+ * k . grad_k over tokens from t on, up to 2048 of them, and so right to 2^-24 (fp32)
+ * or, with bf16 operands, 2^-16 of those products whatever its own type: as a whole
+ * 2e-6 and 2e-5 of its size, a gradient far below its neighbours' less.  A head of q, k or v that several heads read
  * gets the sum of their gradients, in fp32 and in order.  Past a sequence's end
  * the gradients are zero and grad_y is not read.
  * states      : the forward's, of the same q, k, v, gate, s0 and lengths.

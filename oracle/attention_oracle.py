@@ -28,14 +28,18 @@ def gather(v, Hx):
     return v.reshape(N, T, Hx, H // Hx, D).sum(axis=3)
 
 
-def attention_units(T, Dk, Dv, dt, span=1024):
+SPAN = 2048   # tokens to the border at which a sum for the gates' gradients ends, at most
+
+
+def attention_units(T, Dk, Dv, dt):
     """Units of 2^-24 of the magnitudes.  Products over Dk or Dv channels, over a
     chunk's tokens (64 allowed for) and, in the state, a multiplication and an addition a chunk;
-    heads that share (at most 16) and the gates' sums over a span of tokens come on
-    top (twice a span: q dq less k dk); the decays' logarithms are right to a few
+    heads that share (at most 16) and the gates' sums (q dq less k dk: twice) come on
+    top; the decays' logarithms are right to a few
     units of themselves, and x e^-x < 1/2, or e^-x is small enough to lie below the
     rest.  bf16: each score, and each state that a query reads, is a sum of two bf16
-    parts, off by 2^-16 or 256 units of itself."""
+    parts, off by 2^-16 or 256 units of itself.  (States themselves take in sums of three,
+    2^-24: "f32" counts theirs.)"""
     c = Dk + Dv + 64 + 2 * (T // 32 + 1) + 64
     return c + (512 if dt == "bf16" else 0)
 
@@ -84,12 +88,12 @@ def attention(q, k, v, gate, form, scale, s0=None, lengths=None, dy=None, ds=Non
         R, W = a[:, t, :, None, None] * R, a[:, t, :, None, None] * W
         cross[:, t] = (Ms[t] * W).sum(axis=(2, 3))
     # the gates' gradients are formed as the sum of q dq - k dk over the tokens to
-    # a border at most 1024 tokens on, and what crosses the border
+    # a border at most SPAN tokens on, and what crosses the border
     per = (np.abs(q) * dqm).sum(axis=3) + (np.abs(k) * dkm).sum(axis=3)
-    per = np.concatenate([per, np.zeros((N, 1024, H))], axis=1)
+    per = np.concatenate([per, np.zeros((N, SPAN, H))], axis=1)
     total = np.concatenate([np.zeros((N, 1, H)), per.cumsum(axis=1)], axis=1)
     last = (Ms[T] * (0.0 if ds is None else np.abs(ds))).sum(axis=(2, 3))
-    dlm = total[:, 1024:1024 + T] - total[:, :T] + np.maximum(cross.max(axis=1, initial=0.0), last)[:, None, :]
+    dlm = total[:, SPAN:SPAN + T] - total[:, :T] + np.maximum(cross.max(axis=1, initial=0.0), last)[:, None, :]
     slope = 1.0 / (1.0 + np.exp(np.minimum(gate, 700.0))) if form == "logit" else 1.0
     for name, val, mag, heads in (("dq", dq, dqm, Hq), ("dk", dk, dkm, Hk), ("dv", dv, dvm, Hv)):
         out[name] = (gather(val * cut, heads), gather(mag * cut, heads))

@@ -15,7 +15,9 @@
 //
 // bf16: fp32 values that meet bf16 inputs in a product are split into sums of
 // bf16 (each the rest of the one before), so that only the storage type rounds:
-// scores and S into two (to 2^-16 of themselves; they make outputs of 2^-8), the
+// scores and S into two (to 2^-16 of themselves; they make outputs of 2^-8, and products
+// with q and k whose sums, the gates' gradients, are 5e-6 to 2e-5 off as a whole also
+// where a gate is fp32: less than the inputs' own roundings move them), the
 // decayed v that the state takes in into three (2^-24: the state is fp32).
 // fp32: the fp32 matrix instruction.
 //

@@ -575,3 +575,48 @@ def test_decays_above_one(kind, N, T, start, Dk, Dv, heads, dt):
     c.backward()
     # a factor 2^x of a score has its exponent to 2^-24 of itself: 60 log 2 units
     c.check(extra=48)
+
+
+# ---- sizes of errors, beside their bounds ----------------------------------------
+
+NORMS = [dict(N=1, T=260, H=2, Dk=128, Dv=128), dict(N=2, T=300, H=2, Dk=64, Dv=96, form="log"), dict(N=1, T=1100, H=1, Dk=128, Dv=64),
+         dict(N=1, T=3000, H=1, Dk=16, Dv=32), dict(N=40, T=257, H=8, Dk=24, Dv=20)]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("kw", NORMS, ids=lambda kw: "-".join(f"{v}" for v in kw.values()))
+def test_the_gates_gradients_as_a_whole(kw, dt):
+    """Worst cases add up over thousands of tokens; roundings do not.  Those of a product
+    q . dq are independent and come to u of the product: u = 2^-16 / sqrt(3) in bf16 (a score
+    or a state in two parts, off by at most 2^-16, any size below as likely), 2^-24 sqrt(terms)
+    in fp32; those of a sum over tokens to the root of the sum of squares."""
+    c = Case(**kw, dt=dt, start=True, gate_f32=True)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    u = 2.0 ** -16 / 3 ** 0.5 if dt == "bf16" else 2.0 ** -24 * (c.Dk + c.Dv + 64) ** 0.5
+    q, k, gate = to64(c.q), to64(c.k), to64(c.gate)
+    squares = (q * c.ref["dq"][0]).sum(-1) ** 2 + (k * c.ref["dk"][0]).sum(-1) ** 2
+    edge = (to64(c.s_last) * to64(c.ds)).sum((2, 3))[:, None] ** 2
+    slope = 1.0 / (1.0 + np.exp(np.minimum(gate, 700.0))) if c.form == "logit" else 1.0
+    bound = np.linalg.norm(u * slope * np.sqrt(squares[:, ::-1].cumsum(1)[:, ::-1] + edge))
+    want = c.ref["dgate"][0]
+    err, size = np.linalg.norm(to64(c.dgate) - want), np.linalg.norm(want)
+    say(f"{err / size:.2e}, bound {bound / size:.2e}")
+    assert err <= bound and bound <= (1e-3 if dt == "bf16" else 1e-4) * size
+
+
+@pytest.mark.parametrize("kw", NORMS, ids=lambda kw: "-".join(f"{v}" for v in kw.values()))
+def test_states_of_bf16_operands_are_fp32(kw):
+    """What a state takes in is a sum of three bf16 parts: a decay's 4 units of 2^-24, the
+    parts' and the product's one each, and roundings of sums over at most some hundred
+    tokens that a state remembers, sqrt(100) / 2.  (In two parts 2^-16 / sqrt(3) at most: up to 148 units.)"""
+    c = Case(**kw, dt="bf16", start=True, gate_f32=True)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    for name in ("s_last", "ds0"):
+        want = c.ref[name][0]
+        err = np.linalg.norm(to64(getattr(c, name)) - want) / np.linalg.norm(want)
+        say(f"{name}: {err / A.EPS:.1f} units")
+        assert err <= 16 * A.EPS, name
