@@ -165,6 +165,8 @@ class LinearAttentionServer:
     marks an idle row of a batch: it changes no state, and attention gives it
     zeros (its r is x)."""
 
+    _rows = None
+
     def __init__(self, w: dict, H: int, Dk: int, Dv: int, slots: int, Hk: int | None = None,
                  dtype: torch.dtype = torch.bfloat16, eps: float = 1e-6):
         self.shape = _Shape(H, Hk or H, Dk, Dv)
@@ -177,14 +179,20 @@ class LinearAttentionServer:
 
     @property
     def state(self) -> torch.Tensor:
-        """The pool [slots, H, Dk, Dv]: read and written in place, or set (copied)."""
+        """The pool [slots, H, Dk, Dv]: read and written in place, or set (copied).  Setting
+        as many slots leaves it where it is, so that graphs captured before work on it."""
         return self._state
 
     @state.setter
     def state(self, value: torch.Tensor):
-        # a row more, always zero: prefill's idle rows start and end there
-        self._rows = torch.zeros((value.shape[0] + 1, *value.shape[1:]), dtype=torch.float32, device=value.device)
-        self._state = self._rows[:-1]
+        if self._rows is not None and value.shape[1:] != self._rows.shape[1:]:
+            raise ValueError(f"state must be [slots, {', '.join(map(str, self._rows.shape[1:]))}]")
+        if self._rows is None or value.shape[0] + 1 != self._rows.shape[0]:
+            # a row more, always zero: prefill's idle rows start and end there
+            self._rows = torch.zeros((value.shape[0] + 1, *value.shape[1:]), dtype=torch.float32, device=value.device)
+            self._state = self._rows[:-1]
+        elif value.untyped_storage().data_ptr() == self._rows.untyped_storage().data_ptr():
+            value = value.clone()   # the pool's own cells, in another order
         self._state.copy_(value)
 
     @staticmethod

@@ -319,3 +319,25 @@ def test_arguments_that_are_no_tensors_are_refused():
             bc.linear_attention_fwd(t[None], bad, t[None], g[None], t[None])
         with pytest.raises((bc.BoxConvError, RuntimeError)):
             bc.block_norm_fwd(bad, r=t)
+
+
+# ---- the server's pool ---------------------------------------------------------
+
+def test_a_pool_that_is_set_stays_where_it_is():
+    """A graph captured before has its address; prefill's extra row stays behind it."""
+    from paper_1906_11367_amd.attention import LinearAttentionServer
+    server = object.__new__(LinearAttentionServer)
+    server.state = torch.zeros((3, 2, 4, 4))
+    at, new = server.state.data_ptr(), torch.randn(3, 2, 4, 4)
+    for value, want in ((new, new), (new.double(), new), (new[[2, 0, 1]], new[[2, 0, 1]])):
+        server.state = value
+        assert server.state.data_ptr() == at and torch.equal(server.state, want)
+    server.state = server.state.transpose(2, 3)   # a view of itself
+    assert server.state.data_ptr() == at and torch.equal(server.state, new[[2, 0, 1]].transpose(2, 3))
+    server.state = torch.ones(5, 2, 4, 4)         # another number of slots
+    assert server.state.shape == (5, 2, 4, 4) and (server.state == 1).all()
+    assert server._rows.shape[0] == 6 and (server._rows[-1] == 0).all()
+    for bad in (torch.ones(5, 2, 4, 5), torch.ones(3, 2, 4)):
+        with pytest.raises(ValueError, match="state must be"):
+            server.state = bad
+    assert (server.state == 1).all()
