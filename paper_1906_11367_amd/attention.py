@@ -118,12 +118,19 @@ class LinearAttentionPlan:
             bc.bc_cast_bf16(to, out)
         return out
 
+    def _matrices(self, w, what):
+        # (the products see numbers of elements alone)
+        E = self.H * self.Dv
+        bc._need(w["w_in"], (self.C, self.shape.width), (torch.float32, torch.bfloat16), what, "w_in")
+        bc._need(w["w_out"], (E, self.C), (torch.float32, torch.bfloat16), what, "w_out")
+
     def forward(self, x: torch.Tensor, w: dict, s0: torch.Tensor | None = None, lengths: torch.Tensor | None = None):
         """x [N, T, C] of the plan's type; w: w_pre [C], w_in [C, width], w_head
         [H * Dv], w_out [H * Dv, C], w_post [C], res_scale [C], fp32 each
         -> (r [N, T, C], s_last [N, H, Dk, Dv])."""
         s, E = self.shape, self.H * self.Dv
         bc._need(x, (self.N, self.T, self.C), self.t, "LinearAttentionPlan.forward", "x")
+        self._matrices(w, "LinearAttentionPlan.forward")
         bc.block_norm_fwd(x, w_pre=w["w_pre"], y=self.xn, eps=self.eps)
         self._product(bc.BC_MIX_FWD, self.xn, w["w_in"], self.p, self.C, s.width)
         q, k, v, gate, logits = s.parts(self.p)
@@ -140,6 +147,7 @@ class LinearAttentionPlan:
         s, E, g = self.shape, self.H * self.Dv, self.grads
         bc._need(x, (self.N, self.T, self.C), self.t, "LinearAttentionPlan.backward", "x")
         bc._need(grad_r, (self.N, self.T, self.C), self.t, "LinearAttentionPlan.backward", "grad_r")
+        self._matrices(w, "LinearAttentionPlan.backward")
         bc.block_norm_bwd(self.z, x=x, w_post=w["w_post"], res_scale=w["res_scale"], grad_r=grad_r, grad_z=self.dz,
                           grad_x=self.dr, grad_w_post=g["w_post"], grad_res_scale=g["res_scale"], groups=1, eps=self.eps,
                           ws=self.ws)

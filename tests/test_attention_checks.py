@@ -341,3 +341,18 @@ def test_a_pool_that_is_set_stays_where_it_is():
         with pytest.raises(ValueError, match="state must be"):
             server.state = bad
     assert (server.state == 1).all()
+
+
+@built
+@pytest.mark.parametrize("name", ["w_in", "w_out"])
+def test_a_plans_matrices_have_their_shapes(name):
+    """The other way round they have as many elements."""
+    from paper_1906_11367_amd.attention import LinearAttentionPlan
+    plan = LinearAttentionPlan(1, 4, 24, 2, 8, 8, device="cpu")
+    W = plan.shape.width
+    w = {"w_pre": t(24), "w_in": t(24, W), "w_head": t(16), "w_out": t(16, 24), "w_post": t(24), "res_scale": t(24)}
+    w[name] = t(*w[name].shape[::-1])
+    with pytest.raises(bc.BoxConvError, match=f"{name} has shape"):
+        plan.forward(t(1, 4, 24), w)
+    with pytest.raises(bc.BoxConvError, match=f"{name} has shape"):
+        plan.backward(t(1, 4, 24), w, t(1, 4, 24))
