@@ -12,10 +12,12 @@
 // longer ones take a block.  The backward computes the forward's values again (in
 // fp32, none read back rounded) and keeps each lane's share of the weights'
 // gradients over all rows of its block; a second kernel sums the blocks in order.
-// bf16: a norm with a gate of 16 heads of 128, 16384 rows: 43 us (201 MB, 4.7 TB/s),
-// its gradients 74 (335 MB, 4.5); both norms with the residual sum of 8192 rows of
-// 4096: 58 us (268 MB, 4.7 TB/s), the gradients 98 (403 MB, 4.1).  fp32, 777 rows of
+// bf16: a norm with a gate of 16 heads of 128, 16384 rows: 44 us (201 MB, 4.6 TB/s),
+// its gradients 88 (335 MB, 3.8); both norms with the residual sum of 8192 rows of
+// 4096: 61 us (268 MB, 4.4 TB/s), the gradients 104 (403 MB, 3.9).  fp32, 777 rows of
 // 3 x 279: 11 and 18 us, a row's chain of sums.  8 rows: 3.7 us, 7 us with the call.
+// These are medians; single runs of the first two sizes' gradients are a seventh shorter.
+// Where a variant stands beside another below, both ran in turn on one GPU.
 #include <algorithm>
 
 #include "bc_common.hpp"

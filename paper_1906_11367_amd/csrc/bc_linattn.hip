@@ -14,7 +14,7 @@ namespace {
 // place: entry i is border i; forward, entry s + 1 holds segment s's own state, and
 // the states follow from the first border on; backward in time, entry s, from the
 // last.  A thread a cell, its chain's entries read eight at a time.  Bound by memory:
-// 64 heads of 128 x 128, 8 segments, 34 MB in and out in 15 us (4.5 TB/s).
+// 64 heads of 128 x 128, 8 segments, 34 MB in and out in 16 us (4.2 TB/s).
 struct Joint {
   float* entry;
   long entry_nh;           // (segs + 1) cells
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(256) void k_gate_grad(GateGrad a) {
 }
 
 // Gradients of heads that several heads read: the sum over them, in order.
-// part [N * T][H][D] fp32 -> out.  3 x 1531 tokens, 6 heads of 40 and three to one: 4.8 us,
+// part [N * T][H][D] fp32 -> out.  3 x 1531 tokens, 6 heads of 40 and three to one: 5 us,
 // a launch.
 __global__ __launch_bounds__(256) void k_sum_heads(const float* part, char* out, Str os, int f32, int T, int H, int D,
                                                    int share, long count) {
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(256) void k_sum_heads(const float* part, char* out,
 // One token: state' = a state + k v^T, y = scale state'^T q.  A block has V * 2^lc
 // columns of one state; its threads share the rows, kStepRows of each on their way.
 // Bound by the state's bytes, in and out: 128 sequences of 16 heads of 128 x 128, 268 MB
-// in 52 us (5.1 TB/s); four sequences 5 us, and 9 us with the call.
+// in 55 us (4.9 TB/s); four sequences 5 us, and 9 us with the call.
 struct Step {
   const char *q, *k, *v, *gate;
   Str qs, ks, vs, gs;      // t unused

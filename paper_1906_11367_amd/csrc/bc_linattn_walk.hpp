@@ -23,15 +23,18 @@
 //
 // What bounds it: the walk itself, a chunk's steps one after the other with two waves
 // a SIMD (S takes 64 registers of a wave, the chunk on its way 24).  bf16, rows of
-// 128, 64 heads of 4096 tokens in 512 segments: 77 us for outputs (300 MB, 3.9 TB/s;
-// the matrix units are busy 40 % of the time, the vector units 44 %), 42 us for states
-// alone (167 MB, 4.0 TB/s); 8 heads of 65536 tokens, 165 and 83 us.  fp32, 8 heads of
+// 128, 64 heads of 4096 tokens in 512 segments: 79 us for outputs (300 MB, 3.8 TB/s;
+// the matrix units are busy 40 % of the time, the vector units 44 %), 44 us for states
+// alone (167 MB, 3.8 TB/s); 8 heads of 65536 tokens, 172 and 86 us.  fp32, 8 heads of
 // 8192 tokens in 256 segments, rows of 64 and 128: 40 and 21 us (the matrix units 49 %
 // busy, 61 to 65 % where two walks share a launch).  Rows that are not whole vectors (VEC false)
 // cost about a sixth more: in training 64 heads of 4096 with 128 x 122 in place of
 // 128 x 120, 488 us for 420.  Chunks of 64 tokens halve the work on
 // S but leave no registers: 487 us for a training call of the first size, of 32 436.
 // Two places in LDS for a chunk's rows, and so a barrier less, make no difference.
+// No vector register is spilled; of the scalar ones (buffers, strides, bounds) 5 to 265
+// live in lanes of a vector register, and some 40 to 55 of a chunk's 560 to 800
+// instructions fetch and keep them.
 #pragma once
 #include <initializer_list>
 
